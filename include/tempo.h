@@ -219,6 +219,74 @@ TEMPO_API tempo_status tempo_attn_softmax_dropout_bwd_bytemask(const void* dout,
                                             tempo_dtype dt, void* hip_stream);
 
 /*
+ * Rotary positions of the heads of q and k, forward and backward
+ *   theta[b,s,i] = (start + positions[b,s]) freqs[i]   (s for positions[b,s] if there are none), i < R/2,
+ *   c = scale cos theta, n = scale sin theta;   for the pairs (x1, x2) of a head, x[i] and x[i + R/2]
+ *   (HALF) or x[2i] and x[2i + 1] (INTERLEAVED):
+ *     forward   y1 = x1 c - x2 n,  y2 = x2 c + x1 n
+ *     backward  y1 = x1 c + x2 n,  y2 = x2 c - x1 n   (x: the gradients of what the forward wrote)
+ *   Elements R .. D - 1 of a head are copied.
+ *   q, k: element (b, s, head, d) at x[b x_batch + s x_token + head x_head + d], b < B, s < S, d < D (dt), in and out, so that
+ *   heads can be taken out of a projection and put into any order; k may be NULL.  x and y need only the alignment of an element.
+ *   y may be x, with the same strides; elements of y must not overlap otherwise.
+ *   freqs [R/2] in, float64, radians per position; angles are taken in 64 bits, so that far positions keep their place.
+ *   positions in: int32 or int64 (bits 32 or 64), element (b, s) at b batch_stride + s token_stride (strides >= 0; a batch_stride
+ *   of 0 shares them); may be NULL.  A position may be any number, negative ones too.
+ *   INVALID_ARG also: R odd, R < 2, R > D, B S above 2^31 - 1, more than 2^24 elements of q and k together in a token, a negative
+ *   stride, a stride of y that is 0 where there are two elements along it, bits other than 32 and 64.
+ */
+typedef enum { TEMPO_ROTARY_HALF = 0, TEMPO_ROTARY_INTERLEAVED = 1 } tempo_rotary_layout;
+typedef struct {
+  const void* x;
+  void* y;
+  int64_t heads;
+  int64_t x_batch, x_token, x_head, y_batch, y_token, y_head; /* strides in elements */
+} tempo_rotary_heads;
+typedef struct {
+  const void* positions;
+  int bits;
+  int64_t batch_stride, token_stride; /* in elements */
+  int64_t start;
+} tempo_rotary_positions;
+TEMPO_API tempo_status tempo_rotary_fwd(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
+                              const tempo_rotary_positions* positions, int64_t B, int64_t S, int64_t D, int64_t R,
+                              tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream);
+TEMPO_API tempo_status tempo_rotary_bwd(const tempo_rotary_heads* dq, const tempo_rotary_heads* dk, const double* freqs,
+                              const tempo_rotary_positions* positions, int64_t B, int64_t S, int64_t D, int64_t R,
+                              tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream);
+
+/*
+ * Gated feed-forward unit, forward: both projections, the activation and their product
+ *   [g | u] = x w^T + bias,  h = act(g) u;  act: SiLU or GELU (erf, tanh), of sums in float32.
+ *   x [T,H], w [2F,H] (rows of the gate, then of u) in (dt); bias [2F] in (dt), may be NULL;
+ *   gu [T,2F] out (dt): the projections, all that the backward needs of the forward; may be NULL;
+ *   h [T,F] out (dt).
+ *   float32 products are made of bfloat16 ones, of operands taken apart exactly; what is left out is below 2^-21 of |x| |w|.
+ *   An element that is not finite makes NaN of every sum that it takes part in.
+ *   workspace: device memory of at least tempo_glu_fwd_workspace_bytes(T, H, F, dt) bytes, 16-byte aligned (NULL if that is 0).
+ *   UNSUPPORTED also: sizes beyond 2^30 (2F too), or beyond 2^22 tiles of 64 x 64 elements in gu, x or w.
+ */
+typedef enum { TEMPO_GLU_SILU = 0, TEMPO_GLU_GELU_ERF = 1, TEMPO_GLU_GELU_TANH = 2 } tempo_glu_kind;
+TEMPO_API size_t tempo_glu_fwd_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt);
+TEMPO_API tempo_status tempo_glu_fwd(const void* x, const void* w, const void* bias, void* gu, void* h, void* workspace,
+                           size_t workspace_bytes, int64_t T, int64_t H, int64_t F, tempo_glu_kind kind, tempo_dtype dt,
+                           void* hip_stream);
+
+/*
+ * Gated feed-forward unit, backward from the stored projections
+ *   dg = dh u act'(g), du = dh act(g);  dx = [dg | du] w, dw = [dg | du]^T x, dbias = column sums of [dg | du];
+ *   h = act(g) u once more, for the gradient of the product behind the unit: nothing else has to be kept for that.
+ *   dh [T,F], gu [T,2F], x [T,H], w [2F,H] in (dt); dgu [T,2F] out (dt), may alias gu; h [T,F], dx [T,H], dw [2F,H], dbias [2F]
+ *   out (dt), each may be NULL; x is not read without dw, w not without dx (they may be NULL then).
+ *   dx and dw are products of the rounded dgu; dbias adds up what it was before rounding, in a fixed order.
+ *   workspace: at least tempo_glu_bwd_workspace_bytes(T, H, F, dt) bytes, 16-byte aligned.  Else as the forward.
+ */
+TEMPO_API size_t tempo_glu_bwd_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt);
+TEMPO_API tempo_status tempo_glu_bwd(const void* dh, const void* gu, const void* x, const void* w, void* dgu, void* h, void* dx,
+                           void* dw, void* dbias, void* workspace, size_t workspace_bytes, int64_t T, int64_t H, int64_t F,
+                           tempo_glu_kind kind, tempo_dtype dt, void* hip_stream);
+
+/*
  * Mask layout conversion: packed bits <-> one byte per element        [Sec. 3.3 (8-bit masks)]
  *   The paper's implementation keeps the dropout mask as one byte per element; this library
  *   keeps one bit (bit e & 31 of word e >> 5).  These two calls convert between the layouts,

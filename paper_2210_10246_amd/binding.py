@@ -26,9 +26,23 @@ TEMPO_F32, TEMPO_BF16 = 0, 1
 TEMPO_GELU_ERF, TEMPO_GELU_TANH = 0, 1
 _DT = {torch.float32: TEMPO_F32, torch.bfloat16: TEMPO_BF16}
 _KIND = {"erf": TEMPO_GELU_ERF, "tanh": TEMPO_GELU_TANH}
+_LAYOUT = {"half": 0, "interleaved": 1}
+_GLU_KIND = {"silu": 0, "gelu_erf": 1, "gelu_tanh": 2}
 
 _vp, _i64, _u64 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_uint64
 _int, _f32, _sz = ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+
+
+class _RotaryHeads(ctypes.Structure):
+    _fields_ = [("x", _vp), ("y", _vp), ("heads", _i64), ("x_strides", _i64 * 3), ("y_strides", _i64 * 3)]
+
+
+class _RotaryPositions(ctypes.Structure):
+    _fields_ = [("positions", _vp), ("bits", _int), ("strides", _i64 * 2), ("start", _i64)]
+
+
+_rotary_args = [ctypes.POINTER(_RotaryHeads), ctypes.POINTER(_RotaryHeads), _vp, ctypes.POINTER(_RotaryPositions), _i64, _i64,
+                _i64, _i64, _int, _f32, _int, _vp]
 
 _SIGNATURES = {
     "tempo_status_string": (ctypes.c_char_p, [_int]),
@@ -55,6 +69,12 @@ _SIGNATURES = {
                                                        _i64, _f32, _int, _vp]),
     "tempo_attn_softmax_dropout_bwd_regen": (_int, [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64,
                                                     _f32, _u64, _u64, _int, _vp]),
+    "tempo_rotary_fwd": (_int, _rotary_args),
+    "tempo_rotary_bwd": (_int, _rotary_args),
+    "tempo_glu_fwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
+    "tempo_glu_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
+    "tempo_glu_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _sz, _i64, _i64, _i64, _int, _int, _vp]),
+    "tempo_glu_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _i64, _i64, _i64, _int, _int, _vp]),
     "tempo_mask_bits_to_bytes": (_int, [_vp, _vp, _i64, _vp]),
     "tempo_mask_bytes_to_bits": (_int, [_vp, _vp, _i64, _vp]),
 }
@@ -365,6 +385,148 @@ def tempo_attn_softmax_dropout_bwd_regen(dout, probs, dscores, out_recomputed, p
     _check(load().tempo_attn_softmax_dropout_bwd_regen(
         _ptr(dout), _ptr(probs), _ptr(dscores), _ptr(out_recomputed), B, A, Sq, Sk, p, seed,
         offset, dt, _stream(stream)), "tempo_attn_softmax_dropout_bwd_regen")
+
+
+def _same_device(*tensors):
+    """All on the current device: the call goes to its stream."""
+    if not all(t.is_cuda for t in tensors if t is not None):
+        raise ValueError("tensors must be CUDA tensors")
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != current:
+            raise ValueError(f"tensors must be on the current device, cuda:{current}, got {t.device}")
+
+
+def _rotary_heads(name, x, y, like=None):
+    if x is None and y is None:
+        return None, None
+    if x is None or y is None:
+        raise ValueError(f"{name} and {name}_out go together")
+    for n, t in ((name, x), (name + "_out", y)):
+        if t.dim() != 4 or t.shape[-1] < 2 or t.stride(-1) != 1:
+            raise ValueError(f"{n} must be [batch, tokens, heads, elements] with adjacent elements")
+    if y.shape != x.shape:
+        raise ValueError(f"{name}_out must have shape {tuple(x.shape)}, got {tuple(y.shape)}")
+    _want(name + "_out", y, x.dtype)
+    if like is not None:
+        _want(name, x, like.dtype)
+        if x.shape[:2] != like.shape[:2] or x.shape[3] != like.shape[3]:
+            raise ValueError(f"{name} must have the batch, tokens and elements of q, {tuple(like.shape)}, got {tuple(x.shape)}")
+    s = _RotaryHeads(x.data_ptr(), y.data_ptr(), x.shape[2], (_i64 * 3)(*x.stride()[:3]), (_i64 * 3)(*y.stride()[:3]))
+    return s, ctypes.byref(s)
+
+
+def _rotary(where, q, k, freqs, positions, q_out, k_out, layout, scale, start, stream):
+    if stream is None and _native is not None:
+        status = getattr(_native, where)(q, k, freqs, positions, q_out, k_out, layout, scale, start)
+        if status is not None:
+            return _check(status, where)
+    dt = _act_dtype("q", q)
+    _want("freqs", freqs, torch.float64)
+    if layout not in _LAYOUT:
+        raise ValueError(f"layout must be one of {sorted(_LAYOUT)}, got {layout!r}")
+    qs, q_ref = _rotary_heads("q", q, q_out)
+    ks, k_ref = _rotary_heads("k", k, k_out, q)
+    B, S, _, D = q.shape
+    if not 1 <= freqs.numel() <= D // 2:
+        raise ValueError(f"freqs must have 1 to {D // 2} elements, got {freqs.numel()}")
+    at = _RotaryPositions(None, 64, (_i64 * 2)(0, 0), start)
+    if positions is not None:
+        if positions.dtype not in (torch.int32, torch.int64):
+            raise ValueError(f"positions must be int32 or int64, got {positions.dtype}")
+        if positions.shape not in ((S,), (1, S), (B, S)):
+            raise ValueError(f"positions must be [{S}] or [{B}, {S}], got {tuple(positions.shape)}")
+        shared = positions.dim() == 1 or positions.shape[0] == 1
+        at = _RotaryPositions(positions.data_ptr(), 8 * positions.element_size(),
+                              (_i64 * 2)(0 if shared else positions.stride(0), positions.stride(-1)), start)
+    _same_device(q, k, freqs, positions, q_out, k_out)
+    f = _ptr(freqs)
+    _check(getattr(load(), where)(q_ref, k_ref, f, ctypes.byref(at), B, S, D, 2 * freqs.numel(), _LAYOUT[layout], scale, dt,
+                                  _stream(stream)), where)
+
+
+def tempo_rotary_fwd(q, k, freqs, positions, q_out, k_out, layout="half", scale=1.0, start=0, stream=None):
+    """Rotary positions of q and k [batch, tokens, heads, elements], any strides over the first three dimensions; k and k_out
+    may be None, q_out may be q and k_out k.  freqs: float64, for the first 2 freqs.numel() elements of a head.  positions:
+    [tokens] or [batch, tokens], int32 or int64, or None for 0, 1, ...; start is added to them."""
+    _rotary("tempo_rotary_fwd", q, k, freqs, positions, q_out, k_out, layout, scale, start, stream)
+
+
+def tempo_rotary_bwd(dq, dk, freqs, positions, dq_out, dk_out, layout="half", scale=1.0, start=0, stream=None):
+    """The gradients of tempo_rotary_fwd's q and k from those of its outputs; arguments as there."""
+    _rotary("tempo_rotary_bwd", dq, dk, freqs, positions, dq_out, dk_out, layout, scale, start, stream)
+
+
+def tempo_glu_fwd_workspace_bytes(T: int, H: int, F: int, dtype) -> int:
+    return load().tempo_glu_fwd_workspace_bytes(T, H, F, _DT[dtype])
+
+
+def tempo_glu_bwd_workspace_bytes(T: int, H: int, F: int, dtype) -> int:
+    return load().tempo_glu_bwd_workspace_bytes(T, H, F, _DT[dtype])
+
+
+def _glu_sizes(x, w):
+    if w.dim() != 2 or w.shape[0] % 2 != 0:
+        raise ValueError(f"w must be [2 F, H], got {tuple(w.shape)}")
+    F, H = w.shape[0] // 2, w.shape[1]
+    if x.dim() < 1 or x.shape[-1] != H:
+        raise ValueError(f"x must be [..., {H}], got {tuple(x.shape)}")
+    return x.shape[:-1].numel(), H, F
+
+
+def _workspace(workspace, nbytes, device, stream):
+    """The caller's, or memory for the call that is given back to the stream it runs on."""
+    if workspace is not None:
+        return workspace
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _glu_kind(kind):
+    if kind not in _GLU_KIND:
+        raise ValueError(f"kind must be one of {sorted(_GLU_KIND)}, got {kind!r}")
+    return _GLU_KIND[kind]
+
+
+def tempo_glu_fwd(x, w, bias, gu, h, kind="silu", workspace=None, stream=None):
+    """[g | u] = x w^T + bias into gu (None: not kept), act(g) u into h; w [2F, H]: the rows of the gate first.  kind: "silu",
+    "gelu_erf" or "gelu_tanh".  workspace: tempo_glu_fwd_workspace_bytes() bytes, or None: allocated for the call."""
+    if stream is None and _native is not None:
+        status = _native.tempo_glu_fwd(x, w, bias, gu, h, kind, workspace)
+        if status is not None:
+            return _check(status, "tempo_glu_fwd")
+    dt, act = _act_dtype("x", x), _glu_kind(kind)
+    T, H, F = _glu_sizes(x, w)
+    _want("w", w, x.dtype)
+    _want("bias", bias, x.dtype, 2 * F)
+    _want("gu", gu, x.dtype, T * 2 * F)
+    _want("h", h, x.dtype, T * F)
+    pointers = [_ptr(t) for t in (x, w, bias, gu, h)]
+    _same_device(x, w, bias, gu, h, workspace)
+    ws = _workspace(workspace, tempo_glu_fwd_workspace_bytes(T, H, F, x.dtype), x.device, stream)
+    _check(load().tempo_glu_fwd(*pointers, _ptr(ws), ws.numel() * ws.element_size(), T, H, F, act, dt, _stream(stream)),
+           "tempo_glu_fwd")
+
+
+def tempo_glu_bwd(dh, gu, x, w, dgu, h, dx, dw, dbias, kind="silu", workspace=None, stream=None):
+    """From the gradient of h and the kept gu: the gradients of x, w and the bias, and h once more, each of which may be None;
+    dgu, a buffer like gu or gu itself, holds the gradient of gu afterwards."""
+    if stream is None and _native is not None:
+        status = _native.tempo_glu_bwd(dh, gu, x, w, dgu, h, dx, dw, dbias, kind, workspace)
+        if status is not None:
+            return _check(status, "tempo_glu_bwd")
+    dt, act = _act_dtype("gu", gu), _glu_kind(kind)
+    T, H, F = _glu_sizes(x, w)
+    _want("x", x, gu.dtype)
+    _want("w", w, gu.dtype)
+    for name, t, n in (("gu", gu, T * 2 * F), ("dh", dh, T * F), ("dgu", dgu, T * 2 * F), ("h", h, T * F), ("dx", dx, T * H),
+                       ("dw", dw, 2 * F * H), ("dbias", dbias, 2 * F)):
+        _want(name, t, gu.dtype, n)
+    pointers = [_ptr(t) for t in (dh, gu, x, w, dgu, h, dx, dw, dbias)]
+    _same_device(dh, gu, x, w, dgu, h, dx, dw, dbias, workspace)
+    ws = _workspace(workspace, tempo_glu_bwd_workspace_bytes(T, H, F, gu.dtype), gu.device, stream)
+    _check(load().tempo_glu_bwd(*pointers, _ptr(ws), ws.numel() * ws.element_size(), T, H, F, act, dt, _stream(stream)),
+           "tempo_glu_bwd")
 
 
 def tempo_mask_bits_to_bytes(bits, bytes_, n, stream=None):

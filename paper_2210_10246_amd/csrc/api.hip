@@ -339,6 +339,101 @@ tempo_status tempo_attn_softmax_dropout_bwd_regen(const void* dout, const void* 
                                offset, dt, static_cast<hipStream_t>(hip_stream));
 }
 
+static bool rotary_side_ok(const tempo_rotary_heads* h, int64_t B, int64_t S, int64_t D) {
+  const int64_t sizes[] = {B, S, h->heads};
+  const int64_t in[] = {h->x_batch, h->x_token, h->x_head}, out[] = {h->y_batch, h->y_token, h->y_head};
+  int64_t last_in = D, last_out = D;
+  for (int i = 0; i < 3; ++i) {
+    if (in[i] < 0 || out[i] < 0 || !count_ok(sizes[i], in[i]) || !count_ok(sizes[i], out[i])) return false;
+    if (sizes[i] > 1 && out[i] == 0) return false;
+    last_in += sizes[i] * in[i];
+    last_out += sizes[i] * out[i];
+  }
+  return last_in <= kMaxElements && last_out <= kMaxElements;
+}
+static tempo_status rotary(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
+                           const tempo_rotary_positions* at, int64_t B, int64_t S, int64_t D, int64_t R,
+                           tempo_rotary_layout layout, float scale, bool back, tempo_dtype dt, void* hip_stream) {
+  constexpr int64_t most = int64_t{1} << 24;  // elements of a token
+  if (!q || !at || B < 0 || S < 0 || D < 0 || q->heads < 0 || (k && k->heads < 0) || !dtype_ok(dt) ||
+      (layout != TEMPO_ROTARY_HALF && layout != TEMPO_ROTARY_INTERLEAVED))
+    return TEMPO_ERR_INVALID_ARG;
+  if (R < 2 || R % 2 != 0 || R > D || D > most || q->heads > most || (k && k->heads > most) ||
+      (q->heads + (k ? k->heads : 0)) * D > most || !count_ok(B, S) || B * S > INT32_MAX)
+    return TEMPO_ERR_INVALID_ARG;
+  if (!rotary_side_ok(q, B, S, D) || (k && !rotary_side_ok(k, B, S, D))) return TEMPO_ERR_INVALID_ARG;
+  if (at->positions && ((at->bits != 32 && at->bits != 64) || at->batch_stride < 0 || at->token_stride < 0 ||
+                        !count_ok(B, at->batch_stride) || !count_ok(S, at->token_stride)))
+    return TEMPO_ERR_INVALID_ARG;
+  if (k && k->heads == 0) k = nullptr;
+  if (k && q->heads == 0) q = k, k = nullptr;
+  if (B == 0 || S == 0 || q->heads == 0) return TEMPO_OK;
+  if (!q->x || !q->y || !freqs || (k && (!k->x || !k->y))) return TEMPO_ERR_INVALID_ARG;
+  const uintptr_t element = dt == TEMPO_F32 ? 4 : 2;
+  auto aligned = [](const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; };
+  if (!aligned(q->x, element) || !aligned(q->y, element) || (k && (!aligned(k->x, element) || !aligned(k->y, element))) ||
+      !aligned(freqs, 8) || (at->positions && !aligned(at->positions, at->bits / 8)))
+    return TEMPO_ERR_UNSUPPORTED;
+  return launch_rotary(q, k, freqs, at, B, S, D, R, layout, scale, back, dt, static_cast<hipStream_t>(hip_stream));
+}
+
+tempo_status tempo_rotary_fwd(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
+                              const tempo_rotary_positions* positions, int64_t B, int64_t S, int64_t D, int64_t R,
+                              tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream) {
+  return rotary(q, k, freqs, positions, B, S, D, R, layout, scale, false, dt, hip_stream);
+}
+
+tempo_status tempo_rotary_bwd(const tempo_rotary_heads* dq, const tempo_rotary_heads* dk, const double* freqs,
+                              const tempo_rotary_positions* positions, int64_t B, int64_t S, int64_t D, int64_t R,
+                              tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream) {
+  return rotary(dq, dk, freqs, positions, B, S, D, R, layout, scale, true, dt, hip_stream);
+}
+
+static bool glu_ok(int64_t T, int64_t H, int64_t F, tempo_glu_kind kind, tempo_dtype dt) {
+  return T >= 0 && H >= 0 && F >= 0 && dtype_ok(dt) && kind >= TEMPO_GLU_SILU && kind <= TEMPO_GLU_GELU_TANH &&
+         count_ok(T, F, 2) && count_ok(T, H) && count_ok(F, H, 2);
+}
+
+size_t tempo_glu_fwd_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt) {
+  return glu_ok(T, H, F, TEMPO_GLU_SILU, dt) && glu_takes(T, H, F) ? glu_workspace_bytes(T, H, F, dt, false) : 0;
+}
+
+size_t tempo_glu_bwd_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt) {
+  return glu_ok(T, H, F, TEMPO_GLU_SILU, dt) && glu_takes(T, H, F) ? glu_workspace_bytes(T, H, F, dt, true) : 0;
+}
+
+tempo_status tempo_glu_fwd(const void* x, const void* w, const void* bias, void* gu, void* h, void* workspace,
+                           size_t workspace_bytes, int64_t T, int64_t H, int64_t F, tempo_glu_kind kind, tempo_dtype dt,
+                           void* hip_stream) {
+  if (!glu_ok(T, H, F, kind, dt)) return TEMPO_ERR_INVALID_ARG;
+  if (T == 0 || F == 0) return TEMPO_OK;
+  if (!h || (H > 0 && (!x || !w))) return TEMPO_ERR_INVALID_ARG;
+  if (!glu_takes(T, H, F) || !aligned16(x) || !aligned16(w) || !aligned16(bias) || !aligned16(gu) || !aligned16(h) ||
+      !aligned16(workspace))
+    return TEMPO_ERR_UNSUPPORTED;
+  GluCall c{};
+  c.x = x, c.w = w, c.bias = bias, c.gu = gu, c.h = h;
+  c.workspace = workspace, c.workspace_bytes = workspace ? workspace_bytes : 0;
+  c.T = T, c.H = H, c.F = F, c.kind = kind;
+  return launch_glu_fwd(c, dt, static_cast<hipStream_t>(hip_stream));
+}
+
+tempo_status tempo_glu_bwd(const void* dh, const void* gu, const void* x, const void* w, void* dgu, void* h, void* dx,
+                           void* dw, void* dbias, void* workspace, size_t workspace_bytes, int64_t T, int64_t H, int64_t F,
+                           tempo_glu_kind kind, tempo_dtype dt, void* hip_stream) {
+  if (!glu_ok(T, H, F, kind, dt)) return TEMPO_ERR_INVALID_ARG;
+  // Sums of nothing are written too: dw and dbias of no rows, dx of no columns.
+  if (T > 0 && F > 0 && (!dh || !gu || !dgu || (dw && H > 0 && !x) || (dx && H > 0 && !w))) return TEMPO_ERR_INVALID_ARG;
+  if (!glu_takes(T, H, F) || !aligned16(dh) || !aligned16(gu) || !aligned16(x) || !aligned16(w) || !aligned16(dgu) ||
+      !aligned16(h) || !aligned16(dx) || !aligned16(dw) || !aligned16(dbias) || !aligned16(workspace))
+    return TEMPO_ERR_UNSUPPORTED;
+  GluCall c{};
+  c.x = x, c.w = w, c.gu = const_cast<void*>(gu), c.h = h, c.dh = dh, c.dgu = dgu, c.dx = dx, c.dw = dw, c.dbias = dbias;
+  c.workspace = workspace, c.workspace_bytes = workspace ? workspace_bytes : 0;
+  c.T = T, c.H = H, c.F = F, c.kind = kind;
+  return launch_glu_bwd(c, dt, static_cast<hipStream_t>(hip_stream));
+}
+
 tempo_status tempo_mask_bits_to_bytes(const uint32_t* bits, uint8_t* bytes, int64_t n,
                                       void* hip_stream) {
   if (n < 0 || !count_ok(n)) return TEMPO_ERR_INVALID_ARG;

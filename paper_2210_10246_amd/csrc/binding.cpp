@@ -229,6 +229,141 @@ TEMPO_METHOD(attn_softmax_dropout_bwd_bytemask) {  // dout, probs, keep_bytes, d
   });
 }
 
+// ---- rotary positions ------------------------------------------------------------------------------------------------
+// On the current device: its stream takes the call.
+const at::Tensor& here(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda() || !t.has_storage() || t.is_neg() || t.device().index() != c10::hip::current_device()) throw NotPlain{};
+  return t;
+}
+int64_t integer(PyObject* o) {
+  if (!PyLong_CheckExact(o)) throw NotPlain{};
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw NotPlain{};
+  return v;
+}
+tempo_rotary_heads rotary_heads(const at::Tensor& like, PyObject* in, PyObject* out) {
+  const at::Tensor &x = here(in), &y = here(out);
+  if (x.dim() != 4 || x.size(3) < 2 || x.stride(3) != 1 || y.sizes() != x.sizes() || y.stride(3) != 1 ||
+      x.scalar_type() != like.scalar_type() || y.scalar_type() != like.scalar_type() || x.size(0) != like.size(0) ||
+      x.size(1) != like.size(1) || x.size(3) != like.size(3))
+    throw NotPlain{};
+  return {x.data_ptr(), y.data_ptr(), x.size(2), x.stride(0), x.stride(1), x.stride(2), y.stride(0), y.stride(1), y.stride(2)};
+}
+// q, k, freqs, positions, q_out, k_out, layout, scale, start
+PyObject* rotary(PyObject* const* a, Py_ssize_t nargs, decltype(&tempo_rotary_fwd) entry) {
+  return plain_call<9>(nargs, [&] {
+    const at::Tensor &q = here(a[0]), &f = here(a[2]);
+    if (q.dim() != 4 || (q.scalar_type() != at::kFloat && q.scalar_type() != at::kBFloat16)) throw NotPlain{};
+    const int64_t B = q.size(0), S = q.size(1), D = q.size(3), R = 2 * f.numel();
+    const tempo_rotary_heads qh = rotary_heads(q, a[0], a[4]);
+    const bool both = a[1] != Py_None;
+    if (both != (a[5] != Py_None)) throw NotPlain{};
+    const tempo_rotary_heads kh = both ? rotary_heads(q, a[1], a[5]) : tempo_rotary_heads{};
+    if (f.scalar_type() != at::kDouble || !f.is_contiguous() || R < 2 || R > D) throw NotPlain{};
+    tempo_rotary_positions at{nullptr, 64, 0, 0, integer(a[8])};
+    if (a[3] != Py_None) {
+      const at::Tensor& p = here(a[3]);
+      const bool batched = p.dim() == 2;
+      if ((p.scalar_type() != at::kInt && p.scalar_type() != at::kLong) || (p.dim() != 1 && !batched) || p.size(-1) != S ||
+          (batched && p.size(0) != B && p.size(0) != 1))
+        throw NotPlain{};
+      at.positions = p.data_ptr();
+      at.bits = p.scalar_type() == at::kInt ? 32 : 64;
+      at.batch_stride = batched && p.size(0) != 1 ? p.stride(0) : 0;
+      at.token_stride = p.stride(-1);
+    }
+    tempo_rotary_layout layout;
+    if (!PyUnicode_CheckExact(a[6])) throw NotPlain{};
+    if (PyUnicode_CompareWithASCIIString(a[6], "half") == 0) layout = TEMPO_ROTARY_HALF;
+    else if (PyUnicode_CompareWithASCIIString(a[6], "interleaved") == 0) layout = TEMPO_ROTARY_INTERLEAVED;
+    else throw NotPlain{};
+    return [=, freqs = static_cast<const double*>(f.data_ptr()), scale = real(a[7]),
+            dt = q.scalar_type() == at::kFloat ? TEMPO_F32 : TEMPO_BF16, st = stream()] {
+      return entry(&qh, both ? &kh : nullptr, freqs, &at, B, S, D, R, layout, scale, dt, st);
+    };
+  });
+}
+TEMPO_METHOD(rotary_fwd) { return rotary(a, nargs, tempo_rotary_fwd); }
+TEMPO_METHOD(rotary_bwd) { return rotary(a, nargs, tempo_rotary_bwd); }
+
+// ---- the gated unit --------------------------------------------------------------------------------------------------
+struct Glu {
+  int64_t T, H, F;
+  at::ScalarType scalar;
+  tempo_dtype dt;
+  Glu(const at::Tensor& x, const at::Tensor& w) : scalar(x.scalar_type()) {
+    if ((scalar != at::kFloat && scalar != at::kBFloat16) || w.dim() != 2 || w.size(0) % 2 != 0 || x.dim() < 1 ||
+        x.size(-1) != w.size(1))
+      throw NotPlain{};
+    dt = scalar == at::kFloat ? TEMPO_F32 : TEMPO_BF16;
+    F = w.size(0) / 2;
+    H = w.size(1);
+    T = 1;
+    for (int64_t i = 0; i + 1 < x.dim(); ++i) T *= x.size(i);
+  }
+  void* of(PyObject* o, int64_t numel) const {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = here(o);
+    if (t.scalar_type() != scalar || t.numel() != numel || !t.is_contiguous()) throw NotPlain{};
+    return t.data_ptr();
+  }
+};
+tempo_glu_kind glu_kind(PyObject* o) {
+  if (PyUnicode_CheckExact(o)) {
+    if (PyUnicode_CompareWithASCIIString(o, "silu") == 0) return TEMPO_GLU_SILU;
+    if (PyUnicode_CompareWithASCIIString(o, "gelu_erf") == 0) return TEMPO_GLU_GELU_ERF;
+    if (PyUnicode_CompareWithASCIIString(o, "gelu_tanh") == 0) return TEMPO_GLU_GELU_TANH;
+  }
+  throw NotPlain{};
+}
+// The caller's workspace, or one of `bytes` that is given back to the stream's pool behind the call.
+struct Workspace {
+  at::Tensor own;
+  void* p = nullptr;
+  size_t bytes = 0;
+  Workspace(PyObject* o, const at::Tensor& beside, size_t need) {
+    if (o == Py_None) {
+      if (need == 0) return;
+      own = at::empty({static_cast<int64_t>(need)}, beside.options().dtype(at::kByte).requires_grad(false));
+      p = own.data_ptr();
+      bytes = need;
+    } else {
+      const at::Tensor& t = here(o);
+      if (!t.is_contiguous()) throw NotPlain{};
+      p = t.data_ptr();
+      bytes = static_cast<size_t>(t.numel()) * t.element_size();
+    }
+  }
+};
+TEMPO_METHOD(glu_fwd) {  // x, w, bias, gu, h, kind, workspace
+  return plain_call<7>(nargs, [&] {
+    const at::Tensor &x = here(a[0]), &w = here(a[1]);
+    const Glu g(x, w);
+    const int64_t T = g.T, H = g.H, F = g.F;
+    if (a[4] == Py_None) throw NotPlain{};
+    const auto *px = g.of(a[0], T * H), *pw = g.of(a[1], 2 * F * H), *pb = g.of(a[2], 2 * F);
+    auto *gu = g.of(a[3], T * 2 * F), *h = g.of(a[4], T * F);
+    return [=, kind = glu_kind(a[5]), ws = Workspace(a[6], x, tempo_glu_fwd_workspace_bytes(T, H, F, g.dt)), dt = g.dt,
+            st = stream()] { return tempo_glu_fwd(px, pw, pb, gu, h, ws.p, ws.bytes, T, H, F, kind, dt, st); };
+  });
+}
+TEMPO_METHOD(glu_bwd) {  // dh, gu, x, w, dgu, h, dx, dw, dbias, kind, workspace
+  return plain_call<11>(nargs, [&] {
+    const at::Tensor &x = here(a[2]), &w = here(a[3]);
+    const Glu g(x, w);
+    const int64_t T = g.T, H = g.H, F = g.F;
+    if (a[0] == Py_None || a[1] == Py_None || a[4] == Py_None) throw NotPlain{};
+    const auto *dh = g.of(a[0], T * F), *gu = g.of(a[1], T * 2 * F), *px = g.of(a[2], T * H), *pw = g.of(a[3], 2 * F * H);
+    auto *dgu = g.of(a[4], T * 2 * F), *h = g.of(a[5], T * F), *dx = g.of(a[6], T * H), *dw = g.of(a[7], 2 * F * H),
+         *db = g.of(a[8], 2 * F);
+    return [=, kind = glu_kind(a[9]), ws = Workspace(a[10], x, tempo_glu_bwd_workspace_bytes(T, H, F, g.dt)), dt = g.dt,
+            st = stream()] {
+      return tempo_glu_bwd(dh, gu, px, pw, dgu, h, dx, dw, db, ws.p, ws.bytes, T, H, F, kind, dt, st);
+    };
+  });
+}
+
 // ---- the encoder layer of modules.py ---------------------------------------------------------------------------
 // A float32 tensor of these sizes beside x.
 float* beside(const at::Tensor& x, PyObject* o, std::initializer_list<int64_t> sizes) {
@@ -246,12 +381,6 @@ float* input(const at::Tensor& x, tempo_encoder* e) {
   e->seq = x.size(1);
   e->hidden = x.size(2);
   return p;
-}
-int64_t integer(PyObject* o) {
-  if (!PyLong_CheckExact(o)) throw NotPlain{};
-  const long long v = PyLong_AsLongLong(o);
-  if (v == -1 && PyErr_Occurred()) throw NotPlain{};
-  return v;
 }
 // The layer of x with heads, eps1, eps2, p, seed and kind at a[0 .. 5], and its parameters at w.
 tempo_encoder encoder(const at::Tensor& x, PyObject* const* a, PyObject* const* w) {
@@ -493,6 +622,10 @@ PyMethodDef methods[] = {TEMPO_ENTRY(gelu_fwd),
                          TEMPO_ENTRY(attn_softmax_dropout_bwd),
                          TEMPO_ENTRY(attn_softmax_dropout_bwd_regen),
                          TEMPO_ENTRY(attn_softmax_dropout_bwd_bytemask),
+                         TEMPO_ENTRY(rotary_fwd),
+                         TEMPO_ENTRY(rotary_bwd),
+                         TEMPO_ENTRY(glu_fwd),
+                         TEMPO_ENTRY(glu_bwd),
                          TEMPO_ENTRY(encoder_fwd),
                          TEMPO_ENTRY(encoder_bwd),
                          {nullptr, nullptr, 0, nullptr}};

@@ -47,7 +47,7 @@ __device__ __forceinline__ float cubic(const f32x4 c, float z) {
 // Phi 0 or 1).  With w = |x| sqrt(log2(e)/2) the exponential is exp2(-w^2).  x < 0 takes the
 // small value itself, so the left tail keeps its relative accuracy, and the product with x comes
 // last, so the zero at x = 0 is exact.  No table: the kernel needs no LDS.
-__device__ __forceinline__ float gelu_erf_value(float x) {
+__device__ __forceinline__ float gelu_erf_phi(float x) {
   const float w = fabsf(x) * as_f32(TEMPO_GELU_ERFC_W_SCALE);
   const float t = __builtin_amdgcn_rcpf(fmaf(w, as_f32(TEMPO_GELU_ERFC_T_FACTOR), 1.0f));
   const float u = fmaf(t, as_f32(TEMPO_GELU_ERFC_UA), as_f32(TEMPO_GELU_ERFC_UB));
@@ -62,8 +62,10 @@ __device__ __forceinline__ float gelu_erf_value(float x) {
   q = fmaf(q, u, as_f32(TEMPO_GELU_ERFC_Q1));
   q = fmaf(q, u, as_f32(TEMPO_GELU_ERFC_Q0));
   const float half_erfc = t * q * __builtin_amdgcn_exp2f(-(w * w));  // 1/2 erfc(|x| / sqrt 2)
-  const float phi = (x < 0.0f) ? half_erfc : 1.0f - half_erfc;
-  return x * phi;  // NaN stays NaN
+  return (x < 0.0f) ? half_erfc : 1.0f - half_erfc;
+}
+__device__ __forceinline__ float gelu_erf_value(float x) {
+  return x * gelu_erf_phi(x);  // NaN stays NaN
 }
 
 // GELU(x), tanh form written as x * sigmoid(2u): no cancellation on the left tail.

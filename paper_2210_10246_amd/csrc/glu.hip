@@ -1,0 +1,633 @@
+// The gated feed-forward unit:   [g | u] = x W^T + b,   h = act(g) u     (W [2F, H]: the rows of the gate, then those of u)
+// and its backward from what is kept, [g | u]:   dg = dh u act'(g),  du = dh act(g),  h = act(g) u once more,
+//   dx = [dg | du] W,   dW = [dg | du]^T x,   db = column sums of [dg | du].
+//
+// All products are on the matrix cores with bfloat16 operands and float32 sums.  A float32 operand is taken apart into three
+// bfloat16 ones, x = x0 + x1 + x2 exactly, and of the nine products those six are made that count in float32 (the other three
+// are below 2^-21 of |a| |b|).
+#include <algorithm>
+
+#include "gelu_f32.h"
+#include "launch_split.h"
+#include "tempo_host.h"
+
+namespace tempo {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// ---- activations ------------------------------------------------------------------------------------------------------
+struct ActGrad {
+  float value, grad;
+};
+// act(g) and act'(g).  Beside a factor that has long been zero the other one is kept finite.
+template <int KIND>
+__device__ __forceinline__ ActGrad act_grad(float x) {
+  const float xc = fminf(fmaxf(x, -128.0f), 128.0f);
+  if constexpr (KIND == TEMPO_GLU_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x));
+    return {x * s, s * fmaf(xc, 1.0f - s, 1.0f)};
+  } else if constexpr (KIND == TEMPO_GLU_GELU_TANH) {
+    const float k = 0.7978845608028654f, ka = k * 0.044715f;
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-2.0f * 1.4426950408889634f * x * fmaf(x * x, ka, k)));
+    return {x * s, fmaf(2.0f * xc * fmaf(xc * xc, 3.0f * ka, k), s * (1.0f - s), s)};
+  } else {
+    const float w = x * as_f32(TEMPO_GELU_ERFC_W_SCALE);
+    const float density = 0.3989422804014327f * __builtin_amdgcn_exp2f(-(w * w));  // exp(-x^2 / 2) / sqrt(2 pi)
+    const float phi = gelu_erf_phi(x);
+    return {x * phi, fmaf(xc, density, phi)};
+  }
+}
+template <typename F>
+__device__ __forceinline__ void with_kind(int kind, F&& f) {  // uniform
+  if (kind == TEMPO_GLU_SILU) f(std::integral_constant<int, TEMPO_GLU_SILU>{});
+  else if (kind == TEMPO_GLU_GELU_ERF) f(std::integral_constant<int, TEMPO_GLU_GELU_ERF>{});
+  else f(std::integral_constant<int, TEMPO_GLU_GELU_TANH>{});
+}
+__device__ __forceinline__ float act_of(int kind, float x) {
+  float v;
+  with_kind(kind, [&](auto k) { v = act_grad<decltype(k)::value>(x).value; });
+  return v;
+}
+
+// ---- one operand of a product -----------------------------------------------------------------------------------------
+// R rows by BK values of k: from memory to registers a step ahead, then to LDS.  KM: element (row, k) at p[k ld + row],
+// else at p[row ld + k].  LDS holds 16-byte pieces, of a row's k or of a k's rows, in an order in which the lanes of a read
+// meet different banks.
+template <typename T, bool KM, int R, int BK, int THREADS>
+struct Operand {
+  static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int kRun = (KM ? R : BK) / 8;         // pieces side by side
+  static constexpr int kPieces = R * BK / 8 / THREADS;   // of a lane
+  static_assert(kPieces * 8 * THREADS == R * BK && kRun >= 4, "whole pieces per lane");
+  static constexpr int kPlane = R * BK * 2;              // bytes
+  static constexpr int kBytes = kPlanes * kPlane;
+  static constexpr int kWords = sizeof(T) / 2;           // 16-byte words of a piece in memory
+
+  const T* p[kPieces];
+  int64_t step;
+  u32x4 v[kPieces][kWords];
+
+  // row_of: row of the tile -> row in memory, one that exists
+  template <typename F>
+  __device__ __forceinline__ Operand(const void* base, int64_t ld, int row0, int rows, F&& row_of) {
+    step = KM ? BK * ld : BK;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = at % kRun;
+      if constexpr (KM) p[i] = static_cast<const T*>(base) + line * ld + min(row0 + piece * 8, (rows - 1) & ~7);
+      else p[i] = static_cast<const T*>(base) + row_of(line) * ld + piece * 8;
+    }
+  }
+  __device__ __forceinline__ void load(int64_t s) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+#pragma unroll
+      for (int j = 0; j < kWords; ++j)
+        v[i][j] = *reinterpret_cast<const u32x4_any*>(p[i] + s * step + j * (8 / kWords));
+    }
+  }
+  // A step that ends beyond K, or whose pieces of rows may end beyond the tensor: zeros for what does not exist.
+  __device__ __forceinline__ void load_rest(int64_t s, int row0, int rows, int K) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = at % kRun;
+      const int64_t k = s * BK + (KM ? line : piece * 8);
+      const int64_t left = KM ? (k < K ? rows - min(row0 + piece * 8, (rows - 1) & ~7) : 0) : K - k;
+      const T* q = p[i] + s * step;
+#pragma unroll
+      for (int j = 0; j < kWords; ++j) {
+        constexpr int E = 8 / kWords;
+        u32x4 w = {0, 0, 0, 0};
+        if (left >= (j + 1) * E) {
+          w = *reinterpret_cast<const u32x4_any*>(q + j * E);
+        } else if (left > j * E) {
+          uint32_t e[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int n = 0; n < E; ++n) {
+            if (j * E + n < left) {
+              if constexpr (E == 4) e[n] = reinterpret_cast<const uint32_t*>(q)[j * E + n];
+              else e[n / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(q)[j * E + n]) << (16 * (n % 2));
+            }
+          }
+          w = u32x4{e[0], e[1], e[2], e[3]};
+        }
+        v[i][j] = w;
+      }
+    }
+  }
+  __device__ static __forceinline__ int swizzled(int line, int piece) {
+    if constexpr (KM) return piece ^ (2 * (line & 3));
+    else return piece ^ ((kRun >= 8 ? line : line >> 1) & (kRun - 1));
+  }
+  __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = at % kRun;
+      char* to = lds + (line * kRun + swizzled(line, piece)) * 16;
+      if constexpr (kPlanes == 1) {
+        *reinterpret_cast<u32x4*>(to) = v[i][0];
+      } else {
+        u32x4 w[3];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t part[3][2];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const uint32_t x = v[i][j / 2][2 * (j % 2) + n];
+            const float r1 = as_f32(x) - as_f32(x & 0xFFFF0000u);
+            const float r2 = r1 - as_f32(as_u32(r1) & 0xFFFF0000u);
+            part[0][n] = x;
+            part[1][n] = as_u32(r1);
+            part[2][n] = as_u32(r2);
+          }
+#pragma unroll
+          for (int q = 0; q < 3; ++q) w[q][j] = __builtin_amdgcn_perm(part[q][1], part[q][0], 0x07060302u);
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4*>(to + q * kPlane) = w[q];
+      }
+    }
+  }
+  // What a lane gives to a matrix instruction: values k + 8 half .. + 7 of row `row` + lane % 32, half = lane / 32.
+  __device__ static __forceinline__ bf16x8 read(const char* lds, int row, int k) {
+    const int lane = threadIdx.x % kWave, half = lane / 32;
+    if constexpr (!KM) {
+      const int line = row + lane % 32;
+      return *reinterpret_cast<const bf16x8*>(lds + (line * kRun + swizzled(line, k / 8 + half)) * 16);
+    } else {
+      // 16 lanes read 4 values of k of 16 rows, 4 rows each, and get 4 values of k of a row each
+      const int j = lane % 16, r = row + lane % 32 / 16 * 16 + j % 4 * 4, line = k + 8 * half + j / 4;
+      const char* at = lds + (line * kRun + swizzled(line, r / 8)) * 16 + r % 8 * 2;
+      const char* next = lds + ((line + 4) * kRun + swizzled(line + 4, r / 8)) * 16 + r % 8 * 2;
+      union {
+        s16x4 h[2];
+        bf16x8 all;
+      } u;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)next);
+      return u.all;
+    }
+  }
+};
+
+// ---- products ---------------------------------------------------------------------------------------------------------
+// c[m][n] = sum_k a(m, k) b(n, k); GATED: the pairs of columns f and F + f of such a c are g and u.
+struct Product {
+  const void *a, *b;
+  int64_t lda, ldb;
+  int M, N, K;        // N: F if GATED
+  void* c;            // [M, N]
+  float* partial;     // splits > 1: [splits, M, N] ([splits, M, 2F]) sums of k's parts
+  int splits, steps;  // steps of BK values of k in a part
+  const void* bias;   // GATED: [2F] or null
+  void* gu;           // GATED: [M, 2F] or null
+  void* h;            // GATED: [M, F]
+  int kind;
+};
+
+template <int BM_, int BN_, int WM_, int WN_, int BK_>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_;
+  static constexpr int kWavesN = BN / WN, kThreads = kWave * (BM / WM) * kWavesN;
+};
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float (&v)[4], int left) {
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 4) {
+      typedef f32x4 f32x4_any __attribute__((aligned(4)));
+      *reinterpret_cast<f32x4_any*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    } else {
+      typedef u32x2 u32x2_any __attribute__((aligned(2)));
+      *reinterpret_cast<u32x2_any*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < left) Store<T>::store1(p + i, v[i]);
+  }
+}
+
+template <typename T, bool AKM, bool BKM, bool GATED, typename C>
+__global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
+  constexpr int BM = C::BM, BN = C::BN, BK = C::BK, WM = C::WM, WN = C::WN, FM = WM / 32, FN = WN / 32;
+  static_assert(!GATED || (FN % 2 == 0 && !AKM && !BKM), "a wave has g and u of an element");
+  using A = Operand<T, AKM, BM, BK, C::kThreads>;
+  using B = Operand<T, BKM, BN, BK, C::kThreads>;
+  constexpr int kPlanes = A::kPlanes, kBuffer = A::kBytes + B::kBytes;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kBuffer];
+
+  // Neighbouring workgroups go to different XCDs, each with an L2 of its own: every XCD takes a run of tiles, and these go
+  // down 8 rows of tiles before the next column.
+  constexpr int kCols = GATED ? BN / 2 : BN;
+  const int tiles_m = (g.M + BM - 1) / BM, tiles_n = (g.N + kCols - 1) / kCols;
+  const int total = gridDim.x, xcd = blockIdx.x % 8, each = total / 8, more = total % 8;
+  const int tile = xcd * each + min(xcd, more) + static_cast<int>(blockIdx.x) / 8;
+  const int split = tile / (tiles_m * tiles_n), in_split = tile - split * (tiles_m * tiles_n);
+  const int band = in_split / (8 * tiles_n), in_band = in_split - band * (8 * tiles_n), rows = min(8, tiles_m - band * 8);
+  const int m0 = (band * 8 + in_band % rows) * BM, n0 = in_band / rows * kCols;
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int wm = wave / C::kWavesN * WM, wn = wave % C::kWavesN * WN;
+
+  A a(g.a, g.lda, m0, g.M, [&](int r) { return min(m0 + r, g.M - 1); });
+  B b(g.b, g.ldb, n0, g.N, [&](int r) -> int64_t {
+    if constexpr (!GATED) return min(n0 + r, g.N - 1);
+    const int f = min(n0 + r / WN * (WN / 2) + r % (WN / 2), g.N - 1);
+    return r % WN < WN / 2 ? f : int64_t{g.N} + f;
+  });
+  // Steps of BK values of k that are loaded in whole pieces: where rows of a k-major operand are no multiple of a piece,
+  // their last one ends in the next row, so that the last row takes no part.
+  const bool over = (AKM && g.M % 8 != 0) || (BKM && g.N % 8 != 0);
+  const int whole = (over ? g.K - 1 : g.K) / BK;
+  const int first = split * g.steps, last = min(first + g.steps, (g.K + BK - 1) / BK);
+
+  f32x16 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  auto fetch = [&](int s) {
+    if (s < whole) {
+      a.load(s);
+      b.load(s);
+    } else {
+      a.load_rest(s, m0, g.M, g.K);
+      b.load_rest(s, n0, g.N, g.K);
+    }
+  };
+  auto put = [&](int parity) {
+    a.store(lds + parity * kBuffer);
+    b.store(lds + parity * kBuffer + A::kBytes);
+  };
+  if (first < last) {
+    fetch(first);
+    put(0);
+    lds_barrier();
+    for (int s = first; s < last; ++s) {
+      const int parity = (s - first) & 1;
+      if (s + 1 < last) fetch(s + 1);
+      const char* la = lds + parity * kBuffer;
+      const char* lb = la + A::kBytes;
+#pragma unroll
+      for (int k = 0; k < BK; k += 16) {
+        bf16x8 fa[kPlanes][FM], fb[kPlanes][FN];
+#pragma unroll
+        for (int q = 0; q < kPlanes; ++q) {
+#pragma unroll
+          for (int i = 0; i < FM; ++i) fa[q][i] = A::read(la + q * A::kPlane, wm + i * 32, k);
+#pragma unroll
+          for (int j = 0; j < FN; ++j) fb[q][j] = B::read(lb + q * B::kPlane, wn + j * 32, k);
+        }
+        auto multiply = [&](int qa, int qb) {
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[qb][j], fa[qa][i], acc[i][j], 0, 0, 0);
+        };
+        if constexpr (kPlanes == 3) {  // the small ones first
+          multiply(0, 2);
+          multiply(2, 0);
+          multiply(1, 1);
+          multiply(0, 1);
+          multiply(1, 0);
+        }
+        multiply(0, 0);
+      }
+      if (s + 1 < last) put(parity ^ 1);
+      lds_barrier();
+    }
+  }
+
+  // Register r of a lane is element (m = lane % 32, n = 8 (r / 4) + 4 (lane / 32) + r % 4) of a 32 x 32 part.
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int m = m0 + wm + i * 32 + lane % 32;
+    if (m >= g.M) continue;
+#pragma unroll
+    for (int j = 0; j < (GATED ? FN / 2 : FN); ++j) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int in_wave = j * 32 + 8 * q + 4 * (lane / 32);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+        if constexpr (!GATED) {
+          const int n = n0 + wn + in_wave, left = g.N - n;
+          if (left <= 0) continue;
+          if (g.splits > 1) store4(g.partial + (static_cast<int64_t>(split) * g.M + m) * g.N + n, v, left);
+          else store4(static_cast<T*>(g.c) + static_cast<int64_t>(m) * g.N + n, v, left);
+        } else {
+          const int f = n0 + wn / 2 + in_wave, left = g.N - f;
+          if (left <= 0) continue;
+          float u[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) u[e] = acc[i][j + FN / 2][4 * q + e];
+          const int64_t at = static_cast<int64_t>(m) * 2 * g.N + f;
+          if (g.splits > 1) {
+            float* const to = g.partial + static_cast<int64_t>(split) * g.M * 2 * g.N + at;
+            store4(to, v, left);
+            store4(to + g.N, u, left);
+            continue;
+          }
+          if (g.bias) {
+            const T* bias = static_cast<const T*>(g.bias) + f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if (e < left) {
+                v[e] += Store<T>::load1(bias + e);
+                u[e] += Store<T>::load1(bias + g.N + e);
+              }
+            }
+          }
+          if (g.gu) {
+            store4(static_cast<T*>(g.gu) + at, v, left);
+            store4(static_cast<T*>(g.gu) + at + g.N, u, left);
+          }
+          with_kind(g.kind, [&](auto k) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = act_grad<decltype(k)::value>(v[e]).value * u[e];
+          });
+          store4(static_cast<T*>(g.h) + static_cast<int64_t>(m) * g.N + f, v, left);
+        }
+      }
+    }
+  }
+}
+
+// The sums of the parts, in their order.
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void join_kernel(Product g) {
+  const int64_t n = static_cast<int64_t>(g.M) * g.N, e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (e >= n) return;
+  if constexpr (!GATED) {
+    float v = 0.0f;
+    for (int s = 0; s < g.splits; ++s) v += g.partial[s * n + e];
+    Store<T>::store1(static_cast<T*>(g.c) + e, v);
+  } else {
+    const int64_t at = e / g.N * 2 * g.N + e % g.N;
+    float v = 0.0f, u = 0.0f;
+    for (int s = 0; s < g.splits; ++s) {
+      v += g.partial[s * 2 * n + at];
+      u += g.partial[s * 2 * n + at + g.N];
+    }
+    if (g.bias) {
+      const T* bias = static_cast<const T*>(g.bias) + e % g.N;
+      v += Store<T>::load1(bias);
+      u += Store<T>::load1(bias + g.N);
+    }
+    if (g.gu) {
+      Store<T>::store1(static_cast<T*>(g.gu) + at, v);
+      Store<T>::store1(static_cast<T*>(g.gu) + at + g.N, u);
+    }
+    Store<T>::store1(static_cast<T*>(g.h) + e, act_of(g.kind, v) * u);
+  }
+}
+
+// ---- the backward's elementwise part ----------------------------------------------------------------------------------
+struct Gates {
+  const void *dh, *gu;
+  void *dgu, *h;     // h may be null
+  float* sums;       // null, or [chunks, 2F]: column sums of a chunk's rows
+  int64_t rows;
+  int F, kind, chunk;  // chunk: rows of a workgroup
+};
+// A wave takes 64 pieces of 16 bytes of the columns, of `chunk` rows one after the other.
+template <typename T, int KIND>
+__global__ __launch_bounds__(kWave) void gates_kernel(Gates g, int64_t chunk0) {
+  constexpr int V = Store<T>::kVec;
+  const int f = (blockIdx.x * kWave + threadIdx.x) * V, left = g.F - f;
+  if (left <= 0) return;
+  const int64_t c = chunk0 + blockIdx.y, r0 = c * g.chunk, r1 = r0 + g.chunk < g.rows ? r0 + g.chunk : g.rows;
+  float sg[V], su[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) sg[i] = su[i] = 0.0f;
+  for (int64_t r = r0; r < r1; ++r) {
+    const T* dh = static_cast<const T*>(g.dh) + r * g.F + f;
+    const T* gu = static_cast<const T*>(g.gu) + r * 2 * g.F + f;
+    T* dgu = static_cast<T*>(g.dgu) + r * 2 * g.F + f;
+    T* h = g.h ? static_cast<T*>(g.h) + r * g.F + f : nullptr;
+    float d[V], x[V], u[V];
+    if (left >= V) {
+      Store<T>::unpack(ldg_stream_any(dh), d);
+      Store<T>::unpack(*reinterpret_cast<const u32x4_any*>(gu), x);
+      Store<T>::unpack(*reinterpret_cast<const u32x4_any*>(gu + g.F), u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        d[i] = i < left ? Store<T>::load1(dh + i) : 0.0f;
+        x[i] = i < left ? Store<T>::load1(gu + i) : 0.0f;
+        u[i] = i < left ? Store<T>::load1(gu + g.F + i) : 0.0f;
+      }
+    }
+    float dg[V], du[V], y[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const ActGrad a = act_grad<KIND>(x[i]);
+      y[i] = a.value * u[i];
+      dg[i] = d[i] * u[i] * a.grad;
+      du[i] = d[i] * a.value;
+      sg[i] += dg[i];
+      su[i] += du[i];
+    }
+    if (left >= V) {
+      *reinterpret_cast<u32x4_any*>(dgu) = Store<T>::pack(dg);
+      *reinterpret_cast<u32x4_any*>(dgu + g.F) = Store<T>::pack(du);
+      if (h) stg_stream_any(h, Store<T>::pack(y));
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (i >= left) break;
+        Store<T>::store1(dgu + i, dg[i]);
+        Store<T>::store1(dgu + g.F + i, du[i]);
+        if (h) Store<T>::store1(h + i, y[i]);
+      }
+    }
+  }
+  if (g.sums) {
+    float* to = g.sums + c * 2 * g.F + f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (i >= left) break;
+      to[i] = sg[i];
+      to[g.F + i] = su[i];
+    }
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(kWave) void bias_kernel(const float* sums, T* dbias, int64_t chunks, int n) {
+  const int e = blockIdx.x * kWave + threadIdx.x;
+  if (e >= n) return;
+  float v = 0.0f;
+  for (int64_t c = 0; c < chunks; ++c) v += sums[c * n + e];
+  Store<T>::store1(dbias + e, v);
+}
+
+// ---- plans ------------------------------------------------------------------------------------------------------------
+enum class Size { kLarge, kMiddle, kSmall };
+template <typename T>
+struct Tiles;
+template <>
+struct Tiles<bf16_t> {
+  using Large = Tile<256, 256, 128, 64, 64>;
+  using Middle = Tile<128, 128, 64, 64, 64>;
+  using Small = Tile<64, 64, 32, 64, 64>;
+};
+template <>
+struct Tiles<float> {
+  using Large = Tile<128, 128, 64, 64, 32>;
+  using Middle = Tile<128, 128, 64, 64, 32>;
+  using Small = Tile<64, 64, 32, 64, 32>;
+};
+
+struct Plan {
+  Size size;
+  int splits, steps;
+  int64_t tiles;
+};
+Plan plan_for(int64_t M, int64_t N, int64_t K, tempo_dtype dt) {  // N: columns of all rows of b
+  const int64_t cus = compute_units();
+  auto count = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  const int bk = dt == TEMPO_F32 ? 32 : 64;
+  Plan p{};
+  int64_t tiles;
+  if (dt == TEMPO_BF16 && count(256, 256) >= cus) p.size = Size::kLarge, tiles = count(256, 256);
+  else if (count(128, 128) >= cus) p.size = Size::kMiddle, tiles = count(128, 128);
+  else p.size = Size::kSmall, tiles = count(64, 64);
+  const int64_t steps = std::max<int64_t>(1, (K + bk - 1) / bk);
+  int64_t splits = tiles >= cus || tiles == 0 ? 1 : std::max<int64_t>(1, std::min(2 * cus / tiles, steps / 4));
+  p.steps = static_cast<int>((steps + splits - 1) / splits);
+  p.splits = static_cast<int>((steps + p.steps - 1) / p.steps);
+  p.tiles = tiles * p.splits;
+  return p;
+}
+size_t partial_bytes(const Plan& p, int64_t M, int64_t N) {
+  return p.splits > 1 ? static_cast<size_t>(p.splits) * M * N * sizeof(float) : 0;
+}
+
+template <typename T, bool AKM, bool BKM, bool GATED>
+tempo_status launch_product(Product g, const Plan& p, hipStream_t st) {
+  g.splits = p.splits;
+  g.steps = p.steps;
+  auto go = [&](auto tile) {
+    using C = decltype(tile);
+    hipLaunchKernelGGL((product_kernel<T, AKM, BKM, GATED, C>), dim3(static_cast<unsigned>(p.tiles)), dim3(C::kThreads), 0, st, g);
+    return launch_status();
+  };
+  if (p.tiles == 0) return TEMPO_OK;
+  tempo_status status;
+  if (p.size == Size::kLarge) status = go(typename Tiles<T>::Large{});
+  else if (p.size == Size::kMiddle) status = go(typename Tiles<T>::Middle{});
+  else status = go(typename Tiles<T>::Small{});
+  if (status != TEMPO_OK || p.splits == 1) return status;
+  const int64_t n = int64_t{g.M} * g.N;
+  hipLaunchKernelGGL((join_kernel<T, GATED>), dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, g);
+  return launch_status();
+}
+
+constexpr int kChunk = 32;  // rows whose column sums a wave makes
+int64_t chunks_of(int64_t T) { return (T + kChunk - 1) / kChunk; }
+
+template <typename T>
+tempo_status forward(const GluCall& c, const Plan& p, hipStream_t st) {
+  Product g{};
+  g.a = c.x;
+  g.b = c.w;
+  g.lda = g.ldb = c.H;
+  g.M = static_cast<int>(c.T);
+  g.N = static_cast<int>(c.F);
+  g.K = static_cast<int>(c.H);
+  g.partial = static_cast<float*>(c.workspace);
+  g.bias = c.bias;
+  g.gu = c.gu;
+  g.h = c.h;
+  g.kind = c.kind;
+  return launch_product<T, false, false, true>(g, p, st);
+}
+
+template <typename T>
+tempo_status backward(const GluCall& c, const Plan& px, const Plan& pw, hipStream_t st) {
+  constexpr int V = Store<T>::kVec;
+  Gates e{c.dh, c.gu, c.dgu, c.h, c.dbias ? static_cast<float*>(c.workspace) : nullptr, c.T, static_cast<int>(c.F), c.kind, kChunk};
+  const int64_t chunks = chunks_of(c.T);
+  const unsigned across = static_cast<unsigned>((c.F + V * kWave - 1) / (V * kWave));
+  auto gates = [&](auto kernel) {
+    return split_launch(chunks, std::min<int64_t>(65535, most_groups(chunks, kWave * across)), [&](uint32_t first, uint32_t n) {
+      hipLaunchKernelGGL(kernel, dim3(across, n), dim3(kWave), 0, st, e, int64_t{first});
+      return launch_status() == TEMPO_OK;
+    });
+  };
+  if (chunks > 0 && across > 0 &&
+      !(c.kind == TEMPO_GLU_SILU ? gates(gates_kernel<T, TEMPO_GLU_SILU>)
+        : c.kind == TEMPO_GLU_GELU_ERF ? gates(gates_kernel<T, TEMPO_GLU_GELU_ERF>)
+                                       : gates(gates_kernel<T, TEMPO_GLU_GELU_TANH>)))
+    return TEMPO_ERR_LAUNCH;
+  tempo_status status = TEMPO_OK;
+  if (c.dbias && c.F > 0) {
+    const int n = static_cast<int>(2 * c.F);
+    hipLaunchKernelGGL((bias_kernel<T>), dim3((n + kWave - 1) / kWave), dim3(kWave), 0, st, e.sums, static_cast<T*>(c.dbias), chunks, n);
+    status = launch_status();
+  }
+  Product g{};
+  g.a = c.dgu;
+  g.lda = 2 * c.F;
+  g.ldb = c.H;
+  g.N = static_cast<int>(c.H);
+  g.partial = static_cast<float*>(c.workspace);
+  if (status == TEMPO_OK && c.dx) {
+    g.b = c.w;
+    g.M = static_cast<int>(c.T);
+    g.K = static_cast<int>(2 * c.F);
+    g.c = c.dx;
+    status = launch_product<T, false, true, false>(g, px, st);
+  }
+  if (status == TEMPO_OK && c.dw) {
+    g.b = c.x;
+    g.M = static_cast<int>(2 * c.F);
+    g.K = static_cast<int>(c.T);
+    g.c = c.dw;
+    status = launch_product<T, true, true, false>(g, pw, st);
+  }
+  return status;
+}
+
+}  // namespace
+
+bool glu_takes(int64_t T, int64_t H, int64_t F) {
+  const int64_t most = int64_t{1} << 30;  // of what is counted in 32 bits
+  if (T > most || H > most || F > most / 2) return false;
+  // tiles of 64 x 64 elements, up to 512 lanes a tile, in one launch
+  auto tiles = [](int64_t M, int64_t N) { return ((M + 63) / 64) * ((N + 63) / 64); };
+  return tiles(T, 2 * F) < most / 256 && tiles(T, H) < most / 256 && tiles(2 * F, H) < most / 256;
+}
+
+size_t glu_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt, bool back) {
+  if (!back) return partial_bytes(plan_for(T, 2 * F, H, dt), T, 2 * F);
+  return std::max({partial_bytes(plan_for(T, H, 2 * F, dt), T, H), partial_bytes(plan_for(2 * F, H, T, dt), 2 * F, H),
+                   static_cast<size_t>(chunks_of(T)) * 2 * F * sizeof(float)});
+}
+
+tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
+  const Plan p = plan_for(c.T, 2 * c.F, c.H, dt);
+  if (partial_bytes(p, c.T, 2 * c.F) > c.workspace_bytes) return TEMPO_ERR_WORKSPACE;
+  return dt == TEMPO_F32 ? forward<float>(c, p, st) : forward<bf16_t>(c, p, st);
+}
+
+tempo_status launch_glu_bwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
+  const Plan px = plan_for(c.T, c.H, 2 * c.F, dt), pw = plan_for(2 * c.F, c.H, c.T, dt);
+  if ((c.dx && partial_bytes(px, c.T, c.H) > c.workspace_bytes) || (c.dw && partial_bytes(pw, 2 * c.F, c.H) > c.workspace_bytes) ||
+      (c.dbias && static_cast<size_t>(chunks_of(c.T)) * 2 * c.F * sizeof(float) > c.workspace_bytes))
+    return TEMPO_ERR_WORKSPACE;
+  return dt == TEMPO_F32 ? backward<float>(c, px, pw, st) : backward<bf16_t>(c, px, pw, st);
+}
+
+}  // namespace tempo

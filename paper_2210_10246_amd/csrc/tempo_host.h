@@ -69,6 +69,25 @@ tempo_status launch_attn_bwd_regen(const void* dout, const void* probs, void* ds
                                    void* out_re, int64_t B, int64_t A, int64_t Sq, int64_t Sk,
                                    float p, uint64_t seed, uint64_t offset, tempo_dtype dt,
                                    hipStream_t st);
+// back: the other way round.
+tempo_status launch_rotary(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
+                           const tempo_rotary_positions* at, int64_t B, int64_t S, int64_t D, int64_t R,
+                           tempo_rotary_layout layout, float scale, bool back, tempo_dtype dt, hipStream_t st);
+// What the two entry points of the gated unit take; each looks at its own.
+struct GluCall {
+  const void *x, *w, *bias;
+  void *gu, *h;
+  const void* dh;
+  void *dgu, *dx, *dw, *dbias;
+  void* workspace;
+  size_t workspace_bytes;
+  int64_t T, H, F;
+  tempo_glu_kind kind;
+};
+bool glu_takes(int64_t T, int64_t H, int64_t F);
+size_t glu_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt, bool back);
+tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st);
+tempo_status launch_glu_bwd(const GluCall& c, tempo_dtype dt, hipStream_t st);
 tempo_status launch_mask_bits_to_bytes(const uint32_t* bits, uint8_t* bytes, int64_t n,
                                        hipStream_t st);
 tempo_status launch_mask_bytes_to_bits(const uint8_t* bytes, uint32_t* bits, int64_t n,
