@@ -190,6 +190,21 @@ struct Product {
   int kind;
 };
 
+// The order of a part's instructions: N groups, in each the matrix instructions, LDS reads, LDS writes and loads that are
+// its share.
+template <int MFMA, int READS, int WRITES, int LOADS, int N, int I = 0>
+__device__ __forceinline__ void spread() {
+  if constexpr (I < N) {
+    constexpr int m = MFMA * (I + 1) / N - MFMA * I / N, r = READS * (I + 1) / N - READS * I / N,
+                  w = WRITES * (I + 1) / N - WRITES * I / N, l = LOADS * (I + 1) / N - LOADS * I / N;
+    if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+    if constexpr (m > 0) __builtin_amdgcn_sched_group_barrier(0x008, m, 0);
+    if constexpr (w > 0) __builtin_amdgcn_sched_group_barrier(0x200, w, 0);
+    if constexpr (l > 0) __builtin_amdgcn_sched_group_barrier(0x020, l, 0);
+    spread<MFMA, READS, WRITES, LOADS, N, I + 1>();
+  }
+}
+
 template <int BM_, int BN_, int WM_, int WN_, int BK_>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_;
@@ -220,7 +235,8 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
   using A = Operand<T, AKM, BM, BK, C::kThreads>;
   using B = Operand<T, BKM, BN, BK, C::kThreads>;
   constexpr int kPlanes = A::kPlanes, kBuffer = A::kBytes + B::kBytes;
-  __shared__ __attribute__((aligned(16))) char lds[2 * kBuffer];
+  // Two objects, so that writes to one are known not to be what is read from the other.
+  __shared__ __attribute__((aligned(16))) char even[kBuffer], odd[kBuffer];
 
   // Neighbouring workgroups go to different XCDs, each with an L2 of its own: every XCD takes a run of tiles, and these go
   // down 8 rows of tiles before the next column.
@@ -245,7 +261,7 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
   // their last one ends in the next row, so that the last row takes no part.
   const bool over = (AKM && g.M % 8 != 0) || (BKM && g.N % 8 != 0);
   const int whole = (over ? g.K - 1 : g.K) / BK;
-  const int first = split * g.steps, last = min(first + g.steps, (g.K + BK - 1) / BK);
+  const int first = split * g.steps, end = first + g.steps, last = min(end, whole);
 
   f32x16 acc[FM][FN];
 #pragma unroll
@@ -255,56 +271,95 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-  auto fetch = [&](int s) {
-    if (s < whole) {
-      a.load(s);
-      b.load(s);
-    } else {
-      a.load_rest(s, m0, g.M, g.K);
-      b.load_rest(s, n0, g.N, g.K);
+  constexpr int kParts = BK / 16;  // of a step, between which operands are read from LDS
+  static_assert(kParts % 2 == 0, "parities below");
+  bf16x8 fa[2][kPlanes][FM], fb[2][kPlanes][FN];
+  auto put = [&](char* lds) {
+    a.store(lds);
+    b.store(lds + A::kBytes);
+  };
+  auto get = [&](int to, const char* la, int part) {
+    const char* lb = la + A::kBytes;
+#pragma unroll
+    for (int q = 0; q < kPlanes; ++q) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[to][q][i] = A::read(la + q * A::kPlane, wm + i * 32, part * 16);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[to][q][j] = B::read(lb + q * B::kPlane, wn + j * 32, part * 16);
     }
   };
-  auto put = [&](int parity) {
-    a.store(lds + parity * kBuffer);
-    b.store(lds + parity * kBuffer + A::kBytes);
+  auto multiply = [&](int from) {
+    auto planes = [&](int qa, int qb) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][qb][j], fa[from][qa][i], acc[i][j], 0, 0, 0);
+    };
+    if constexpr (kPlanes == 3) {  // the small ones first
+      planes(0, 2);
+      planes(2, 0);
+      planes(1, 1);
+      planes(0, 1);
+      planes(1, 0);
+    }
+    planes(0, 0);
   };
-  if (first < last) {
-    fetch(first);
-    put(0);
-    lds_barrier();
-    for (int s = first; s < last; ++s) {
-      const int parity = (s - first) & 1;
-      if (s + 1 < last) fetch(s + 1);
-      const char* la = lds + parity * kBuffer;
-      const char* lb = la + A::kBytes;
-#pragma unroll
-      for (int k = 0; k < BK; k += 16) {
-        bf16x8 fa[kPlanes][FM], fb[kPlanes][FN];
-#pragma unroll
-        for (int q = 0; q < kPlanes; ++q) {
-#pragma unroll
-          for (int i = 0; i < FM; ++i) fa[q][i] = A::read(la + q * A::kPlane, wm + i * 32, k);
-#pragma unroll
-          for (int j = 0; j < FN; ++j) fb[q][j] = B::read(lb + q * B::kPlane, wn + j * 32, k);
-        }
-        auto multiply = [&](int qa, int qb) {
-#pragma unroll
-          for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[qb][j], fa[qa][i], acc[i][j], 0, 0, 0);
-        };
-        if constexpr (kPlanes == 3) {  // the small ones first
-          multiply(0, 2);
-          multiply(2, 0);
-          multiply(1, 1);
-          multiply(0, 1);
-          multiply(1, 0);
-        }
-        multiply(0, 0);
-      }
-      if (s + 1 < last) put(parity ^ 1);
+  if (whole * BK < g.K && end > whole && first <= whole) {  // the rest, in steps of its own
+    for (int s = whole; s < end && s * int64_t{BK} < g.K; ++s) {
+      a.load_rest(s, m0, g.M, g.K);
+      b.load_rest(s, n0, g.N, g.K);
+      put(even);
       lds_barrier();
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+        get(0, even, part);
+        multiply(0);
+      }
+      lds_barrier();
+    }
+  }
+  // While the matrix cores work on a part, the operands of the next one come from LDS; step s + 1 is written there in the
+  // first part of s, and s + 2 is on its way from memory.  The one barrier of a step stands before its last part, whose
+  // operands all waves have read by then.  No branch in here: beyond the last step that one is fetched again.
+  if (first < last) {
+    auto fetch = [&](int s) {
+      s = min(s, last - 1);
+      a.load(s);
+      b.load(s);
+    };
+    fetch(first);
+    put(even);
+    fetch(first + 1);
+    lds_barrier();
+    get(0, even, 0);
+    constexpr int kPutB = kParts > 2 ? 1 : 0, kLoadB = kParts > 2 ? 2 : 1;
+    auto step = [&](int s, const char* from, char* to) {
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+        if (part == kParts - 1) {
+          lds_barrier();
+          get(0, to, 0);
+        } else {
+          get((part + 1) & 1, from, part + 1);
+        }
+        if (part == 0) a.store(to);
+        if (part == kPutB) b.store(to + A::kBytes);
+        if (part == kPutB) a.load(min(s + 2, last - 1));
+        if (part == kLoadB) b.load(min(s + 2, last - 1));
+        multiply(part & 1);
+        constexpr int kMfma = FM * FN * (kPlanes == 3 ? 6 : 1), kReads = kPlanes * (FM * (AKM ? 2 : 1) + FN * (BKM ? 2 : 1));
+        if (part == 0) spread<kMfma, kReads, kPlanes * A::kPieces, 0, kReads>();
+        else if (part == 1) spread<kMfma, kReads, kPlanes * B::kPieces, A::kWords * A::kPieces, kReads>();
+        else if (part == 2) spread<kMfma, kReads, 0, B::kWords * B::kPieces, kReads>();
+        else spread<kMfma, kReads, 0, 0, kReads>();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    for (int s = first; s < last; s += 2) {
+      step(s, even, odd);
+      if (s + 1 == last) break;
+      step(s + 1, odd, even);
     }
   }
 
@@ -478,7 +533,7 @@ template <typename T>
 struct Tiles;
 template <>
 struct Tiles<bf16_t> {
-  using Large = Tile<256, 256, 128, 64, 64>;
+  using Large = Tile<256, 256, 128, 128, 64>;
   using Middle = Tile<128, 128, 64, 64, 64>;
   using Small = Tile<64, 64, 32, 64, 64>;
 };
