@@ -42,6 +42,12 @@ __device__ __forceinline__ ActGrad act_grad(float x) {
     return {x * phi, fmaf(xc, density, phi)};
   }
 }
+// act(g) where no branch is wanted: SiLU and the tanh form of GELU are g sigmoid(g (c0 + c1 g^2)).
+template <bool ERF>
+__device__ __forceinline__ float act_value(float x, float c0, float c1) {
+  if constexpr (ERF) return gelu_erf_value(x);
+  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * fmaf(c1 * x, x, c0)));  // -log2(e) is part of c0 and c1
+}
 template <typename F>
 __device__ __forceinline__ void with_kind(int kind, F&& f) {  // uniform
   if (kind == TEMPO_GLU_SILU) f(std::integral_constant<int, TEMPO_GLU_SILU>{});
@@ -121,8 +127,9 @@ struct Operand {
     }
   }
   __device__ static __forceinline__ int swizzled(int line, int piece) {
-    if constexpr (KM) return piece ^ (2 * (line & 3));
-    else return piece ^ ((kRun >= 8 ? line : line >> 1) & (kRun - 1));
+    // 64 banks are 16 pieces: 16 lanes that read a piece each of 16 rows, or 32 that read 8 bytes each of 4 rows of k.
+    if constexpr (KM) return piece ^ (kRun >= 16 ? 4 * (line & 3) : 4 * (line / 2 & 1));
+    else return piece ^ (line / (16 / kRun) & (kRun - 1));
   }
   __device__ __forceinline__ void store(char* lds) const {
 #pragma unroll
@@ -188,21 +195,29 @@ struct Product {
   void* gu;           // GATED: [M, 2F] or null
   void* h;            // GATED: [M, F]
   int kind;
+  float c0, c1;       // of act_value()
 };
+enum Epilogue { kPlain, kSigmoid, kErf };  // kPlain: not GATED
 
-// The order of a part's instructions: N groups, in each the matrix instructions, LDS reads, LDS writes and loads that are
-// its share.
+// The order of a part's instructions: in N groups, each with its share of the matrix instructions and of what else there is.
 template <int MFMA, int READS, int WRITES, int LOADS, int N, int I = 0>
-__device__ __forceinline__ void spread() {
+__device__ __forceinline__ void groups() {
   if constexpr (I < N) {
     constexpr int m = MFMA * (I + 1) / N - MFMA * I / N, r = READS * (I + 1) / N - READS * I / N,
                   w = WRITES * (I + 1) / N - WRITES * I / N, l = LOADS * (I + 1) / N - LOADS * I / N;
     if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
-    if constexpr (m > 0) __builtin_amdgcn_sched_group_barrier(0x008, m, 0);
     if constexpr (w > 0) __builtin_amdgcn_sched_group_barrier(0x200, w, 0);
     if constexpr (l > 0) __builtin_amdgcn_sched_group_barrier(0x020, l, 0);
-    spread<MFMA, READS, WRITES, LOADS, N, I + 1>();
+    if constexpr (m > 0) __builtin_amdgcn_sched_group_barrier(0x008, m, 0);
+    groups<MFMA, READS, WRITES, LOADS, N, I + 1>();
   }
+}
+// The reads, which the next part begins with, in the first half: they are on their way for the second half's matrix instructions.
+template <int MFMA, int READS, int WRITES, int LOADS>
+__device__ __forceinline__ void spread() {
+  constexpr int kFirst = (MFMA + 1) / 2, kSecond = MFMA - kFirst;
+  groups<kFirst, READS, 0, 0, kFirst>();
+  groups<kSecond, 0, WRITES, LOADS, kSecond>();
 }
 
 template <int BM_, int BN_, int WM_, int WN_, int BK_>
@@ -211,25 +226,48 @@ struct Tile {
   static constexpr int kWavesN = BN / WN, kThreads = kWave * (BM / WM) * kWavesN;
 };
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, const float (&v)[4], int left) {
-  if (left >= 4) {
-    if constexpr (sizeof(T) == 4) {
-      typedef f32x4 f32x4_any __attribute__((aligned(4)));
-      *reinterpret_cast<f32x4_any*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    } else {
-      typedef u32x2 u32x2_any __attribute__((aligned(2)));
-      *reinterpret_cast<u32x2_any*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-    }
-  } else {
+// 32 rows by J x 32 columns of a wave's sums to memory, through LDS of its own, so that lanes side by side store pieces side
+// by side: 4 elements of a lane, in 32 rows at once, took [16384, 4096] x 2 x 11008 2877 us where this takes XXX.
+// value(j, q): registers 4q .. 4q + 3 of part j, elements (m = lane % 32, n = 32 j + 8 q + 4 (lane / 32) ..) of the block;
+// rows, cols: how many exist.
+template <typename U, int J, typename F>
+__device__ __forceinline__ void store_rows(char* lds, U* out, int64_t ld, int rows, int cols, F&& value) {
+  constexpr int kRow = J * 32 * sizeof(U), kPitch = kRow + 16, E = 16 / sizeof(U), kLanes = kRow / 16, kOnce = kWave / kLanes;
+  const int lane = threadIdx.x % kWave;
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (i < left) Store<T>::store1(p + i, v[i]);
+  for (int j = 0; j < J; ++j) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      char* to = lds + lane % 32 * kPitch + (j * 32 + 8 * q + 4 * (lane / 32)) * sizeof(U);
+      const f32x4 v = value(j, q);
+      if constexpr (sizeof(U) == 4) *reinterpret_cast<f32x4*>(to) = v;
+      else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    }
   }
+  wave_lds_fence();
+  const int col = lane % kLanes * E, left = cols - col;
+#pragma unroll
+  for (int i = 0; i < 32; i += kOnce) {
+    const int row = i + lane / kLanes;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * kPitch + col * sizeof(U));
+    if (row >= rows || left <= 0) continue;
+    U* to = out + row * ld + col;
+    if (left >= E) {
+      *reinterpret_cast<u32x4_any*>(to) = w;
+    } else {
+      float v[E];
+      Store<U>::unpack(w, v);
+#pragma unroll
+      for (int e = 0; e < E - 1; ++e)
+        if (e < left) Store<U>::store1(to + e, v[e]);
+    }
+  }
+  wave_lds_fence();
 }
 
-template <typename T, bool AKM, bool BKM, bool GATED, typename C>
+template <typename T, bool AKM, bool BKM, Epilogue END, typename C>
 __global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
+  constexpr bool GATED = END != kPlain;
   constexpr int BM = C::BM, BN = C::BN, BK = C::BK, WM = C::WM, WN = C::WN, FM = WM / 32, FN = WN / 32;
   static_assert(!GATED || (FN % 2 == 0 && !AKM && !BKM), "a wave has g and u of an element");
   using A = Operand<T, AKM, BM, BK, C::kThreads>;
@@ -349,10 +387,10 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
         if (part == kLoadB) b.load(min(s + 2, last - 1));
         multiply(part & 1);
         constexpr int kMfma = FM * FN * (kPlanes == 3 ? 6 : 1), kReads = kPlanes * (FM * (AKM ? 2 : 1) + FN * (BKM ? 2 : 1));
-        if (part == 0) spread<kMfma, kReads, kPlanes * A::kPieces, 0, kReads>();
-        else if (part == 1) spread<kMfma, kReads, kPlanes * B::kPieces, A::kWords * A::kPieces, kReads>();
-        else if (part == 2) spread<kMfma, kReads, 0, B::kWords * B::kPieces, kReads>();
-        else spread<kMfma, kReads, 0, 0, kReads>();
+        if (part == 0) spread<kMfma, kReads, kPlanes * A::kPieces, 0>();
+        else if (part == 1) spread<kMfma, kReads, kPlanes * B::kPieces, A::kWords * A::kPieces>();
+        else if (part == 2) spread<kMfma, kReads, 0, B::kWords * B::kPieces>();
+        else spread<kMfma, kReads, 0, 0>();
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -363,57 +401,57 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
     }
   }
 
-  // Register r of a lane is element (m = lane % 32, n = 8 (r / 4) + 4 (lane / 32) + r % 4) of a 32 x 32 part.
+  // The bias of the tile's gates, then of the rest, behind the waves' rooms.
+  constexpr int kWaves = C::kThreads / kWave, kRoom = 32 * (WN * 4 + 16);
+  static_assert(kWaves % 2 == 0 && kWaves / 2 * kRoom + (GATED ? BN * 4 : 0) <= kBuffer, "a wave's rows");
+  char* const room = (wave < kWaves / 2 ? even : odd) + wave % (kWaves / 2) * kRoom;
+  float* const bias = reinterpret_cast<float*>(odd + kBuffer) - BN;
+  lds_barrier();
+  if constexpr (GATED) {
+    for (int i = threadIdx.x; i < BN; i += C::kThreads) {
+      const int f = min(n0 + i % (BN / 2), g.N - 1) + i / (BN / 2) * g.N;
+      bias[i] = g.bias && g.splits == 1 ? Store<T>::load1(static_cast<const T*>(g.bias) + f) : 0.0f;
+    }
+    lds_barrier();
+  }
+  auto part = [&](const f32x16& v, int q) { return f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]}; };
+  const int m_first = m0 + wm;
+  if constexpr (!GATED) {
+    const int n = n0 + wn;
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int m = m0 + wm + i * 32 + lane % 32;
-    if (m >= g.M) continue;
+    for (int i = 0; i < FM; ++i) {
+      const int m = m_first + i * 32;
+      auto value = [&](int j, int q) { return part(acc[i][j], q); };
+      if (g.splits > 1)
+        store_rows<float, FN>(room, g.partial + (static_cast<int64_t>(split) * g.M + m) * g.N + n, g.N, g.M - m, g.N - n, value);
+      else
+        store_rows<T, FN>(room, static_cast<T*>(g.c) + static_cast<int64_t>(m) * g.N + n, g.N, g.M - m, g.N - n, value);
+    }
+  } else {
+    constexpr int J = FN / 2;
+    const int f = n0 + wn / 2, left = g.N - f;
+    const int64_t ld = 2 * static_cast<int64_t>(g.N);
+    const float* const own = bias + wn / 2 + 4 * (lane / 32);
 #pragma unroll
-    for (int j = 0; j < (GATED ? FN / 2 : FN); ++j) {
+    for (int i = 0; i < FM; ++i) {
+      const int m = m_first + i * 32;
+      auto gate = [&](int j, int q) { return part(acc[i][j], q) + *reinterpret_cast<const f32x4*>(own + j * 32 + 8 * q); };
+      auto up = [&](int j, int q) { return part(acc[i][j + J], q) + *reinterpret_cast<const f32x4*>(own + BN / 2 + j * 32 + 8 * q); };
+      auto sums = [&](auto* to) {
+        using U = std::remove_pointer_t<decltype(to)>;
+        store_rows<U, J>(room, to + m * ld + f, ld, g.M - m, left, gate);
+        store_rows<U, J>(room, to + m * ld + f + g.N, ld, g.M - m, left, up);
+      };
+      if (g.splits > 1) {
+        sums(g.partial + static_cast<int64_t>(split) * g.M * ld);
+      } else {
+        if (g.gu) sums(static_cast<T*>(g.gu));
+        store_rows<T, J>(room, static_cast<T*>(g.h) + static_cast<int64_t>(m) * g.N + f, g.N, g.M - m, left, [&](int j, int q) {
+          f32x4 v = gate(j, q);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int in_wave = j * 32 + 8 * q + 4 * (lane / 32);
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
-        if constexpr (!GATED) {
-          const int n = n0 + wn + in_wave, left = g.N - n;
-          if (left <= 0) continue;
-          if (g.splits > 1) store4(g.partial + (static_cast<int64_t>(split) * g.M + m) * g.N + n, v, left);
-          else store4(static_cast<T*>(g.c) + static_cast<int64_t>(m) * g.N + n, v, left);
-        } else {
-          const int f = n0 + wn / 2 + in_wave, left = g.N - f;
-          if (left <= 0) continue;
-          float u[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) u[e] = acc[i][j + FN / 2][4 * q + e];
-          const int64_t at = static_cast<int64_t>(m) * 2 * g.N + f;
-          if (g.splits > 1) {
-            float* const to = g.partial + static_cast<int64_t>(split) * g.M * 2 * g.N + at;
-            store4(to, v, left);
-            store4(to + g.N, u, left);
-            continue;
-          }
-          if (g.bias) {
-            const T* bias = static_cast<const T*>(g.bias) + f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (e < left) {
-                v[e] += Store<T>::load1(bias + e);
-                u[e] += Store<T>::load1(bias + g.N + e);
-              }
-            }
-          }
-          if (g.gu) {
-            store4(static_cast<T*>(g.gu) + at, v, left);
-            store4(static_cast<T*>(g.gu) + at + g.N, u, left);
-          }
-          with_kind(g.kind, [&](auto k) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = act_grad<decltype(k)::value>(v[e]).value * u[e];
-          });
-          store4(static_cast<T*>(g.h) + static_cast<int64_t>(m) * g.N + f, v, left);
-        }
+          for (int e = 0; e < 4; ++e) v[e] = act_value<END == kErf>(v[e], g.c0, g.c1);
+          return v * up(j, q);
+        });
       }
     }
   }
@@ -569,13 +607,13 @@ size_t partial_bytes(const Plan& p, int64_t M, int64_t N) {
   return p.splits > 1 ? static_cast<size_t>(p.splits) * M * N * sizeof(float) : 0;
 }
 
-template <typename T, bool AKM, bool BKM, bool GATED>
+template <typename T, bool AKM, bool BKM, Epilogue END>
 tempo_status launch_product(Product g, const Plan& p, hipStream_t st) {
   g.splits = p.splits;
   g.steps = p.steps;
   auto go = [&](auto tile) {
     using C = decltype(tile);
-    hipLaunchKernelGGL((product_kernel<T, AKM, BKM, GATED, C>), dim3(static_cast<unsigned>(p.tiles)), dim3(C::kThreads), 0, st, g);
+    hipLaunchKernelGGL((product_kernel<T, AKM, BKM, END, C>), dim3(static_cast<unsigned>(p.tiles)), dim3(C::kThreads), 0, st, g);
     return launch_status();
   };
   if (p.tiles == 0) return TEMPO_OK;
@@ -585,7 +623,7 @@ tempo_status launch_product(Product g, const Plan& p, hipStream_t st) {
   else status = go(typename Tiles<T>::Small{});
   if (status != TEMPO_OK || p.splits == 1) return status;
   const int64_t n = int64_t{g.M} * g.N;
-  hipLaunchKernelGGL((join_kernel<T, GATED>), dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, g);
+  hipLaunchKernelGGL((join_kernel<T, END != kPlain>), dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, g);
   return launch_status();
 }
 
@@ -606,7 +644,11 @@ tempo_status forward(const GluCall& c, const Plan& p, hipStream_t st) {
   g.gu = c.gu;
   g.h = c.h;
   g.kind = c.kind;
-  return launch_product<T, false, false, true>(g, p, st);
+  constexpr float log2e = 1.4426950408889634f, k = 0.7978845608028654f;
+  if (c.kind == TEMPO_GLU_GELU_ERF) return launch_product<T, false, false, kErf>(g, p, st);
+  g.c0 = c.kind == TEMPO_GLU_SILU ? -log2e : -2.0f * log2e * k;
+  g.c1 = c.kind == TEMPO_GLU_SILU ? 0.0f : -2.0f * log2e * k * 0.044715f;
+  return launch_product<T, false, false, kSigmoid>(g, p, st);
 }
 
 template <typename T>
@@ -643,14 +685,14 @@ tempo_status backward(const GluCall& c, const Plan& px, const Plan& pw, hipStrea
     g.M = static_cast<int>(c.T);
     g.K = static_cast<int>(2 * c.F);
     g.c = c.dx;
-    status = launch_product<T, false, true, false>(g, px, st);
+    status = launch_product<T, false, true, kPlain>(g, px, st);
   }
   if (status == TEMPO_OK && c.dw) {
     g.b = c.x;
     g.M = static_cast<int>(2 * c.F);
     g.K = static_cast<int>(c.T);
     g.c = c.dw;
-    status = launch_product<T, true, true, false>(g, pw, st);
+    status = launch_product<T, true, true, kPlain>(g, pw, st);
   }
   return status;
 }
