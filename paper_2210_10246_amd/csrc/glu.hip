@@ -6,6 +6,7 @@
 // bfloat16 ones, x = x0 + x1 + x2 exactly, and of the nine products those six are made that count in float32 (the other three
 // are below 2^-21 of |a| |b|).
 #include <algorithm>
+#include <utility>
 
 #include "gelu_f32.h"
 #include "launch_split.h"
@@ -15,7 +16,6 @@ namespace tempo {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -60,48 +60,97 @@ __device__ __forceinline__ float act_of(int kind, float x) {
   return v;
 }
 
+template <int... I, typename F>
+__device__ __forceinline__ void for_each(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+template <int... I, typename F>
+__device__ __forceinline__ bool for_each_while(std::integer_sequence<int, I...>, F&& f) {
+  return (f(std::integral_constant<int, I>{}) && ...);
+}
+
 // ---- one operand of a product -----------------------------------------------------------------------------------------
-// R rows by BK values of k: from memory to registers a step ahead, then to LDS.  KM: element (row, k) at p[k ld + row],
-// else at p[row ld + k].  LDS holds 16-byte pieces, of a row's k or of a k's rows, in an order in which the lanes of a read
-// meet different banks.
+// R rows by BK values of k in LDS.  KM: element (row, k) at p[k ld + row], else at p[row ld + k].  LDS holds 16-byte pieces,
+// of a row's k or of a k's rows, in an order in which the lanes of a read meet different banks.
 template <typename T, bool KM, int R, int BK, int THREADS>
 struct Operand {
+  static constexpr bool kKMajor = KM;
   static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
   static constexpr int kRun = (KM ? R : BK) / 8;         // pieces side by side
   static constexpr int kPieces = R * BK / 8 / THREADS;   // of a lane
-  static_assert(kPieces * 8 * THREADS == R * BK && kRun >= 4, "whole pieces per lane");
+  static_assert(kPieces * 8 * THREADS == R * BK && (KM ? kRun >= 8 : kRun == 4 || kRun == 8), "whole pieces per lane");
   static constexpr int kPlane = R * BK * 2;              // bytes
   static constexpr int kBytes = kPlanes * kPlane;
   static constexpr int kWords = sizeof(T) / 2;           // 16-byte words of a piece in memory
 
+  // 64 banks are 16 pieces.  Row by row, 16 lanes at a time read one each, in rows 0 - 3 and 12 - 15 the one and in 4 - 11 the
+  // other of two neighbours, then the other way round; by k, 32 lanes read 8 bytes each of 4 rows and of 4 eight rows on.
+  __device__ static __forceinline__ int swizzled(int line, int piece) {
+    if constexpr (!KM && kRun == 4) return piece ^ (line / 4 & 1) * 2 ^ (line / 8 & 1) * 3;
+    else if constexpr (!KM) return piece ^ (line / 2 & 7);
+    else if constexpr (kRun >= 16) return piece ^ 2 * ((line & 3) + 4 * (line / 8 & 1));
+    else return piece ^ 2 * ((line / 2 & 1) + 2 * (line / 8 & 1));
+  }
+  // What a lane gives to a matrix instruction: values k + 8 (lane / 16) .. + 7 of row `row` + lane % 16.
+  __device__ static __forceinline__ bf16x8 read(const char* lds, int row, int k) {
+    const int lane = threadIdx.x % kWave;
+    if constexpr (!KM) {
+      const int line = row + lane % 16;
+      return *reinterpret_cast<const bf16x8*>(lds + (line * kRun + swizzled(line, k / 8 + lane / 16)) * 16);
+    } else {
+      // 16 lanes read 4 values of k of 16 rows, 4 rows each, and get 4 values of k of a row each
+      const int j = lane % 16, r = row + j % 4 * 4, line = k + 8 * (lane / 16) + j / 4;
+      const char* at = lds + (line * kRun + swizzled(line, r / 8)) * 16 + r % 8 * 2;
+      union {
+        s16x4 h[2];
+        bf16x8 all;
+      } u;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * kRun * 16));
+      return u.all;
+    }
+  }
+
+  // From memory: piece i of a lane is the one at place (i THREADS + lane) of the LDS image.
   const T* p[kPieces];
   int64_t step;
-  u32x4 v[kPieces][kWords];
-
   // row_of: row of the tile -> row in memory, one that exists
   template <typename F>
   __device__ __forceinline__ Operand(const void* base, int64_t ld, int row0, int rows, F&& row_of) {
     step = KM ? BK * ld : BK;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = at % kRun;
+      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = swizzled(line, at % kRun);
       if constexpr (KM) p[i] = static_cast<const T*>(base) + line * ld + min(row0 + piece * 8, (rows - 1) & ~7);
       else p[i] = static_cast<const T*>(base) + row_of(line) * ld + piece * 8;
     }
   }
-  __device__ __forceinline__ void load(int64_t s) {
+  // Straight to LDS, piece i of every lane: bfloat16 at addresses that are multiples of 16 bytes.  In assembly because the
+  // compiler waits for all such loads before any read of LDS; whoever calls this waits for them (landed()).  It has no output.
+  __device__ __forceinline__ void load_lds(int i, int64_t s, char* lds) const {
+    static_assert(sizeof(T) == 2, "as it is in memory");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds)) +
+                        (i * THREADS + wave * kWave) * 16;
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p[i] + s * step), "s"(to) : "m0", "memory");
+  }
+  // By way of registers.
+  struct Staged {
+    u32x4 v[kPieces][kWords];
+  };
+  __device__ __forceinline__ void load(int64_t s, Staged& to) const {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
 #pragma unroll
-      for (int j = 0; j < kWords; ++j)
-        v[i][j] = *reinterpret_cast<const u32x4_any*>(p[i] + s * step + j * (8 / kWords));
+      for (int j = 0; j < kWords; ++j) to.v[i][j] = *reinterpret_cast<const u32x4_any*>(p[i] + s * step + j * (8 / kWords));
     }
   }
   // A step that ends beyond K, or whose pieces of rows may end beyond the tensor: zeros for what does not exist.
-  __device__ __forceinline__ void load_rest(int64_t s, int row0, int rows, int K) {
+  __device__ __forceinline__ void load_rest(int64_t s, int row0, int rows, int K, Staged& to) const {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = at % kRun;
+      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = swizzled(line, at % kRun);
       const int64_t k = s * BK + (KM ? line : piece * 8);
       const int64_t left = KM ? (k < K ? rows - min(row0 + piece * 8, (rows - 1) & ~7) : 0) : K - k;
       const T* q = p[i] + s * step;
@@ -122,22 +171,16 @@ struct Operand {
           }
           w = u32x4{e[0], e[1], e[2], e[3]};
         }
-        v[i][j] = w;
+        to.v[i][j] = w;
       }
     }
   }
-  __device__ static __forceinline__ int swizzled(int line, int piece) {
-    // 64 banks are 16 pieces: 16 lanes that read a piece each of 16 rows, or 32 that read 8 bytes each of 4 rows of k.
-    if constexpr (KM) return piece ^ (kRun >= 16 ? 4 * (line & 3) : 4 * (line / 2 & 1));
-    else return piece ^ (line / (16 / kRun) & (kRun - 1));
-  }
-  __device__ __forceinline__ void store(char* lds) const {
+  __device__ static __forceinline__ void store(const Staged& from, char* lds) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = at % kRun;
-      char* to = lds + (line * kRun + swizzled(line, piece)) * 16;
+      char* to = lds + (i * THREADS + static_cast<int>(threadIdx.x)) * 16;
       if constexpr (kPlanes == 1) {
-        *reinterpret_cast<u32x4*>(to) = v[i][0];
+        *reinterpret_cast<u32x4*>(to) = from.v[i][0];
       } else {
         u32x4 w[3];
 #pragma unroll
@@ -145,7 +188,7 @@ struct Operand {
           uint32_t part[3][2];
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            const uint32_t x = v[i][j / 2][2 * (j % 2) + n];
+            const uint32_t x = from.v[i][j / 2][2 * (j % 2) + n];
             const float r1 = as_f32(x) - as_f32(x & 0xFFFF0000u);
             const float r2 = r1 - as_f32(as_u32(r1) & 0xFFFF0000u);
             part[0][n] = x;
@@ -160,44 +203,92 @@ struct Operand {
       }
     }
   }
-  // What a lane gives to a matrix instruction: values k + 8 half .. + 7 of row `row` + lane % 32, half = lane / 32.
-  __device__ static __forceinline__ bf16x8 read(const char* lds, int row, int k) {
-    const int lane = threadIdx.x % kWave, half = lane / 32;
-    if constexpr (!KM) {
-      const int line = row + lane % 32;
-      return *reinterpret_cast<const bf16x8*>(lds + (line * kRun + swizzled(line, k / 8 + half)) * 16);
-    } else {
-      // 16 lanes read 4 values of k of 16 rows, 4 rows each, and get 4 values of k of a row each
-      const int j = lane % 16, r = row + lane % 32 / 16 * 16 + j % 4 * 4, line = k + 8 * half + j / 4;
-      const char* at = lds + (line * kRun + swizzled(line, r / 8)) * 16 + r % 8 * 2;
-      const char* next = lds + ((line + 4) * kRun + swizzled(line + 4, r / 8)) * 16 + r % 8 * 2;
-      union {
-        s16x4 h[2];
-        bf16x8 all;
-      } u;
-      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)next);
-      return u.all;
-    }
-  }
 };
 
 // ---- products ---------------------------------------------------------------------------------------------------------
-// c[m][n] = sum_k a(m, k) b(n, k); GATED: the pairs of columns f and F + f of such a c are g and u.
+// c[m][n] = sum_k a(m, k) b(n, k); gated: the pairs of columns f and F + f of such a c are g and u.
 struct Product {
   const void *a, *b;
   int64_t lda, ldb;
-  int M, N, K;        // N: F if GATED
+  int M, N, K;        // N: F if gated
   void* c;            // [M, N]
   float* partial;     // splits > 1: [splits, M, N] ([splits, M, 2F]) sums of k's parts
   int splits, steps;  // steps of BK values of k in a part
-  const void* bias;   // GATED: [2F] or null
-  void* gu;           // GATED: [M, 2F] or null
-  void* h;            // GATED: [M, F]
+  const void* bias;   // gated: [2F] or null
+  void* gu;           // gated: [M, 2F] or null
+  void* h;            // gated: [M, F]
   int kind;
   float c0, c1;       // of act_value()
 };
-enum Epilogue { kPlain, kSigmoid, kErf };  // kPlain: not GATED
+enum Epilogue { kPlain, kSigmoid, kErf };  // kPlain: not gated
+
+// A workgroup owns BM x BN elements (gated: the g and u of BM x BN / 2), a wave WM x WN of them.
+template <int BM_, int BN_, int WM_, int WN_, int BK_>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, FM = WM / 16, FN = WN / 16;
+  static constexpr int kWavesN = BN / WN, kWaves = BM / WM * kWavesN, kThreads = kWave * kWaves;
+};
+
+// Where the workgroup's tile is.  Neighbouring workgroups go to different XCDs, each with an L2 of its own: every XCD takes a
+// run of tiles, and these go down 8 rows of tiles before the next column.
+template <typename C, bool GATED>
+struct Place {
+  static constexpr int kCols = GATED ? C::BN / 2 : C::BN;
+  int split, m0, n0, wm, wn, wave;
+  __device__ __forceinline__ explicit Place(const Product& g) {
+    const int tiles_m = (g.M + C::BM - 1) / C::BM, tiles_n = (g.N + kCols - 1) / kCols;
+    const int total = gridDim.x, xcd = blockIdx.x % 8, each = total / 8, more = total % 8;
+    const int tile = xcd * each + min(xcd, more) + static_cast<int>(blockIdx.x) / 8;
+    split = tile / (tiles_m * tiles_n);
+    const int in_split = tile - split * (tiles_m * tiles_n);
+    const int band = in_split / (8 * tiles_n), in_band = in_split - band * (8 * tiles_n), rows = min(8, tiles_m - band * 8);
+    m0 = (band * 8 + in_band % rows) * C::BM;
+    n0 = in_band / rows * kCols;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    wm = wave / C::kWavesN * C::WM;
+    wn = wave % C::kWavesN * C::WN;
+  }
+  // Rows of a tile's operands that exist; a wave's WN rows of b are those of g, then those of u, of WN / 2 columns of h.
+  __device__ __forceinline__ int64_t a_row(const Product& g, int r) const { return min(m0 + r, g.M - 1); }
+  __device__ __forceinline__ int64_t b_row(const Product& g, int r) const {
+    if constexpr (!GATED) return min(n0 + r, g.N - 1);
+    const int f = min(n0 + r / C::WN * (C::WN / 2) + r % (C::WN / 2), g.N - 1);
+    return r % C::WN < C::WN / 2 ? f : int64_t{g.N} + f;
+  }
+};
+
+// The operands of a wave for 32 values of k, and their product.
+template <int PLANES, typename C>
+struct Fragments {
+  bf16x8 a[PLANES][C::FM], b[PLANES][C::FN];
+  template <typename A, typename B>
+  __device__ __forceinline__ void read(const char* la, const char* lb, int wm, int wn, int k) {
+#pragma unroll
+    for (int q = 0; q < PLANES; ++q) {
+#pragma unroll
+      for (int i = 0; i < C::FM; ++i) a[q][i] = A::read(la + q * A::kPlane, wm + i * 16, k);
+#pragma unroll
+      for (int j = 0; j < C::FN; ++j) b[q][j] = B::read(lb + q * B::kPlane, wn + j * 16, k);
+    }
+  }
+  __device__ __forceinline__ void multiply(f32x4 (&acc)[C::FM][C::FN]) const {
+    auto planes = [&](int qa, int qb) {
+#pragma unroll
+      for (int i = 0; i < C::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::FN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[qb][j], a[qa][i], acc[i][j], 0, 0, 0);
+    };
+    if constexpr (PLANES == 3) {  // the small ones first
+      planes(0, 2);
+      planes(2, 0);
+      planes(1, 1);
+      planes(0, 1);
+      planes(1, 0);
+    }
+    planes(0, 0);
+  }
+};
 
 // The order of a part's instructions: in N groups, each with its share of the matrix instructions and of what else there is.
 template <int MFMA, int READS, int WRITES, int LOADS, int N, int I = 0>
@@ -216,30 +307,25 @@ __device__ __forceinline__ void groups() {
 template <int MFMA, int READS, int WRITES, int LOADS>
 __device__ __forceinline__ void spread() {
   constexpr int kFirst = (MFMA + 1) / 2, kSecond = MFMA - kFirst;
-  groups<kFirst, READS, 0, 0, kFirst>();
-  groups<kSecond, 0, WRITES, LOADS, kSecond>();
+  groups<kFirst, READS, 0, 0, (kFirst < 16 ? kFirst : 16)>();
+  groups<kSecond, 0, WRITES, LOADS, (kSecond < 16 ? kSecond : 16)>();
 }
 
-template <int BM_, int BN_, int WM_, int WN_, int BK_>
-struct Tile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_;
-  static constexpr int kWavesN = BN / WN, kThreads = kWave * (BM / WM) * kWavesN;
-};
-
-// 32 rows by J x 32 columns of a wave's sums to memory, through LDS of its own, so that lanes side by side store pieces side
-// by side: 4 elements of a lane, in 32 rows at once, took [16384, 4096] x 2 x 11008 2877 us where this takes XXX.
-// value(j, q): registers 4q .. 4q + 3 of part j, elements (m = lane % 32, n = 32 j + 8 q + 4 (lane / 32) ..) of the block;
-// rows, cols: how many exist.
-template <typename U, int J, typename F>
+// Blocks of 16 rows, of the N that a wave has, which fit into `bytes` of LDS in rows of `row` bytes and 16 more.
+constexpr int blocks_at_once(int N, int row, int bytes) { return 16 * N * (row + 16) <= bytes ? N : blocks_at_once(N / 2, row, bytes); }
+// 16 BLOCKS rows by J x 16 columns of a wave's sums to memory, through LDS of its own, so that lanes side by side store pieces
+// side by side.  value(i, j): elements (m = 16 i + lane % 16, n = 16 j + 4 (lane / 16) ..) of them; rows, cols: how many exist.
+template <typename U, int BLOCKS, int J, typename F>
 __device__ __forceinline__ void store_rows(char* lds, U* out, int64_t ld, int rows, int cols, F&& value) {
-  constexpr int kRow = J * 32 * sizeof(U), kPitch = kRow + 16, E = 16 / sizeof(U), kLanes = kRow / 16, kOnce = kWave / kLanes;
+  constexpr int kRow = J * 16 * sizeof(U), kPitch = kRow + 16, E = 16 / sizeof(U), kLanes = kRow / 16, kOnce = kWave / kLanes;
+  static_assert(16 % kOnce == 0, "whole rows");
   const int lane = threadIdx.x % kWave;
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
+  for (int i = 0; i < BLOCKS; ++i) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      char* to = lds + lane % 32 * kPitch + (j * 32 + 8 * q + 4 * (lane / 32)) * sizeof(U);
-      const f32x4 v = value(j, q);
+    for (int j = 0; j < J; ++j) {
+      char* to = lds + (16 * i + lane % 16) * kPitch + (j * 16 + 4 * (lane / 16)) * sizeof(U);
+      const f32x4 v = value(i, j);
       if constexpr (sizeof(U) == 4) *reinterpret_cast<f32x4*>(to) = v;
       else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     }
@@ -247,7 +333,7 @@ __device__ __forceinline__ void store_rows(char* lds, U* out, int64_t ld, int ro
   wave_lds_fence();
   const int col = lane % kLanes * E, left = cols - col;
 #pragma unroll
-  for (int i = 0; i < 32; i += kOnce) {
+  for (int i = 0; i < 16 * BLOCKS; i += kOnce) {
     const int row = i + lane / kLanes;
     const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * kPitch + col * sizeof(U));
     if (row >= rows || left <= 0) continue;
@@ -265,196 +351,237 @@ __device__ __forceinline__ void store_rows(char* lds, U* out, int64_t ld, int ro
   wave_lds_fence();
 }
 
+// A wave's sums to memory.  room: its LDS, ROOM bytes; bias: LDS for the workgroup's BN values.  All waves call it, when LDS is
+// free.
+template <typename T, Epilogue END, typename C, int ROOM, typename P>
+__device__ __forceinline__ void finish(const Product& g, const P& at, const f32x4 (&acc)[C::FM][C::FN], char* room, float* bias) {
+  constexpr int FM = C::FM, FN = C::FN, BN = C::BN;
+  const int lane = threadIdx.x % kWave, m = at.m0 + at.wm;
+  if constexpr (END == kPlain) {
+    const int n = at.n0 + at.wn;
+    auto sums = [&](auto* to) {
+      using U = std::remove_pointer_t<decltype(to)>;
+      constexpr int kOnce = blocks_at_once(FM, FN * 16 * sizeof(U), ROOM);
+#pragma unroll
+      for (int i0 = 0; i0 < FM; i0 += kOnce)
+        store_rows<U, kOnce, FN>(room, to + static_cast<int64_t>(m + 16 * i0) * g.N + n, g.N, g.M - m - 16 * i0, g.N - n,
+                                 [&](int i, int j) { return acc[i0 + i][j]; });
+    };
+    if (g.splits > 1) sums(g.partial + static_cast<int64_t>(at.split) * g.M * g.N);
+    else sums(static_cast<T*>(g.c));
+  } else {
+    for (int i = threadIdx.x; i < BN; i += C::kThreads) {
+      const int f = min(at.n0 + i % (BN / 2), g.N - 1) + i / (BN / 2) * g.N;
+      bias[i] = g.bias && g.splits == 1 ? Store<T>::load1(static_cast<const T*>(g.bias) + f) : 0.0f;
+    }
+    lds_barrier();
+    constexpr int J = FN / 2;
+    const int f = at.n0 + at.wn / 2;
+    const float* const own = bias + at.wn / 2 + 4 * (lane / 16);
+    auto gate = [&](int i, int j) { return acc[i][j] + *reinterpret_cast<const f32x4*>(own + j * 16); };
+    auto up = [&](int i, int j) { return acc[i][j + J] + *reinterpret_cast<const f32x4*>(own + BN / 2 + j * 16); };
+    auto rows = [&](auto* to, int64_t ld, auto&& value) {
+      using U = std::remove_pointer_t<decltype(to)>;
+      constexpr int kOnce = blocks_at_once(FM, J * 16 * sizeof(U), ROOM);
+#pragma unroll
+      for (int i0 = 0; i0 < FM; i0 += kOnce)
+        store_rows<U, kOnce, J>(room, to + (m + 16 * i0) * ld + f, ld, g.M - m - 16 * i0, g.N - f,
+                                [&](int i, int j) { return value(i0 + i, j); });
+    };
+    auto sums = [&](auto* to) {
+      rows(to, 2 * static_cast<int64_t>(g.N), gate);
+      rows(to + g.N, 2 * static_cast<int64_t>(g.N), up);
+    };
+    if (g.splits > 1) {
+      sums(g.partial + static_cast<int64_t>(at.split) * g.M * 2 * g.N);
+    } else {
+      if (g.gu) sums(static_cast<T*>(g.gu));
+      rows(static_cast<T*>(g.h), g.N, [&](int i, int j) {
+        f32x4 v = gate(i, j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = act_value<END == kErf>(v[e], g.c0, g.c1);
+        return v * up(i, j);
+      });
+    }
+  }
+}
+
+template <typename C>
+__device__ __forceinline__ void clear(f32x4 (&acc)[C::FM][C::FN]) {
+#pragma unroll
+  for (int i = 0; i < C::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < C::FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+// The steps from `whole` on, one after the other, through one buffer.
+template <typename A, typename B, typename C, typename P>
+__device__ __forceinline__ void rest_of_k(const Product& g, const P& at, const A& a, const B& b, int whole, int end, char* lds,
+                                          f32x4 (&acc)[C::FM][C::FN]) {
+  for (int s = whole; s < end && s * int64_t{C::BK} < g.K; ++s) {
+    typename A::Staged va;
+    typename B::Staged vb;
+    a.load_rest(s, at.m0, g.M, g.K, va);
+    b.load_rest(s, at.n0, g.N, g.K, vb);
+    A::store(va, lds);
+    B::store(vb, lds + A::kBytes);
+    lds_barrier();
+#pragma unroll
+    for (int k = 0; k < C::BK; k += 32) {
+      Fragments<A::kPlanes, C> f;
+      f.template read<A, B>(lds, lds + A::kBytes, at.wm, at.wn, k);
+      f.multiply(acc);
+    }
+    lds_barrier();
+  }
+}
+
+// Any type, size and address: operands by way of registers, two buffers in LDS.  While the matrix cores work on 32 values of
+// k, the operands of the next ones come from LDS; behind the one barrier of a step, when all waves have read what it held,
+// a buffer gets the step after the next, and the one behind that is on its way from memory.
 template <typename T, bool AKM, bool BKM, Epilogue END, typename C>
 __global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
-  constexpr bool GATED = END != kPlain;
-  constexpr int BM = C::BM, BN = C::BN, BK = C::BK, WM = C::WM, WN = C::WN, FM = WM / 32, FN = WN / 32;
-  static_assert(!GATED || (FN % 2 == 0 && !AKM && !BKM), "a wave has g and u of an element");
-  using A = Operand<T, AKM, BM, BK, C::kThreads>;
-  using B = Operand<T, BKM, BN, BK, C::kThreads>;
-  constexpr int kPlanes = A::kPlanes, kBuffer = A::kBytes + B::kBytes;
+  using A = Operand<T, AKM, C::BM, C::BK, C::kThreads>;
+  using B = Operand<T, BKM, C::BN, C::BK, C::kThreads>;
+  constexpr int kPlanes = A::kPlanes, kBuffer = A::kBytes + B::kBytes, kParts = C::BK / 32;
   // Two objects, so that writes to one are known not to be what is read from the other.
   __shared__ __attribute__((aligned(16))) char even[kBuffer], odd[kBuffer];
-
-  // Neighbouring workgroups go to different XCDs, each with an L2 of its own: every XCD takes a run of tiles, and these go
-  // down 8 rows of tiles before the next column.
-  constexpr int kCols = GATED ? BN / 2 : BN;
-  const int tiles_m = (g.M + BM - 1) / BM, tiles_n = (g.N + kCols - 1) / kCols;
-  const int total = gridDim.x, xcd = blockIdx.x % 8, each = total / 8, more = total % 8;
-  const int tile = xcd * each + min(xcd, more) + static_cast<int>(blockIdx.x) / 8;
-  const int split = tile / (tiles_m * tiles_n), in_split = tile - split * (tiles_m * tiles_n);
-  const int band = in_split / (8 * tiles_n), in_band = in_split - band * (8 * tiles_n), rows = min(8, tiles_m - band * 8);
-  const int m0 = (band * 8 + in_band % rows) * BM, n0 = in_band / rows * kCols;
-
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int wm = wave / C::kWavesN * WM, wn = wave % C::kWavesN * WN;
-
-  A a(g.a, g.lda, m0, g.M, [&](int r) { return min(m0 + r, g.M - 1); });
-  B b(g.b, g.ldb, n0, g.N, [&](int r) -> int64_t {
-    if constexpr (!GATED) return min(n0 + r, g.N - 1);
-    const int f = min(n0 + r / WN * (WN / 2) + r % (WN / 2), g.N - 1);
-    return r % WN < WN / 2 ? f : int64_t{g.N} + f;
-  });
+  const Place<C, END != kPlain> at(g);
+  const A a(g.a, g.lda, at.m0, g.M, [&](int r) { return at.a_row(g, r); });
+  const B b(g.b, g.ldb, at.n0, g.N, [&](int r) { return at.b_row(g, r); });
   // Steps of BK values of k that are loaded in whole pieces: where rows of a k-major operand are no multiple of a piece,
   // their last one ends in the next row, so that the last row takes no part.
   const bool over = (AKM && g.M % 8 != 0) || (BKM && g.N % 8 != 0);
-  const int whole = (over ? g.K - 1 : g.K) / BK;
-  const int first = split * g.steps, end = first + g.steps, last = min(end, whole);
-
-  f32x16 acc[FM][FN];
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-
-  constexpr int kParts = BK / 16;  // of a step, between which operands are read from LDS
-  static_assert(kParts % 2 == 0, "parities below");
-  bf16x8 fa[2][kPlanes][FM], fb[2][kPlanes][FN];
-  auto put = [&](char* lds) {
-    a.store(lds);
-    b.store(lds + A::kBytes);
-  };
-  auto get = [&](int to, const char* la, int part) {
-    const char* lb = la + A::kBytes;
-#pragma unroll
-    for (int q = 0; q < kPlanes; ++q) {
-#pragma unroll
-      for (int i = 0; i < FM; ++i) fa[to][q][i] = A::read(la + q * A::kPlane, wm + i * 32, part * 16);
-#pragma unroll
-      for (int j = 0; j < FN; ++j) fb[to][q][j] = B::read(lb + q * B::kPlane, wn + j * 32, part * 16);
-    }
-  };
-  auto multiply = [&](int from) {
-    auto planes = [&](int qa, int qb) {
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][qb][j], fa[from][qa][i], acc[i][j], 0, 0, 0);
-    };
-    if constexpr (kPlanes == 3) {  // the small ones first
-      planes(0, 2);
-      planes(2, 0);
-      planes(1, 1);
-      planes(0, 1);
-      planes(1, 0);
-    }
-    planes(0, 0);
-  };
-  if (whole * BK < g.K && end > whole && first <= whole) {  // the rest, in steps of its own
-    for (int s = whole; s < end && s * int64_t{BK} < g.K; ++s) {
-      a.load_rest(s, m0, g.M, g.K);
-      b.load_rest(s, n0, g.N, g.K);
-      put(even);
-      lds_barrier();
-#pragma unroll
-      for (int part = 0; part < kParts; ++part) {
-        get(0, even, part);
-        multiply(0);
-      }
-      lds_barrier();
-    }
-  }
-  // While the matrix cores work on a part, the operands of the next one come from LDS; step s + 1 is written there in the
-  // first part of s, and s + 2 is on its way from memory.  The one barrier of a step stands before its last part, whose
-  // operands all waves have read by then.  No branch in here: beyond the last step that one is fetched again.
+  const int whole = (over ? g.K - 1 : g.K) / C::BK;
+  const int first = at.split * g.steps, end = first + g.steps, last = min(end, whole);
+  f32x4 acc[C::FM][C::FN];
+  clear<C>(acc);
+  if (end > whole) rest_of_k<A, B, C>(g, at, a, b, max(whole, first), end, even, acc);
   if (first < last) {
+    typename A::Staged va;
+    typename B::Staged vb;
+    Fragments<kPlanes, C> f[2];
+    // No branch around the loads: behind one, the compiler waits for all that are under way.  Beyond the last step they
+    // fetch that one again.
     auto fetch = [&](int s) {
-      s = min(s, last - 1);
-      a.load(s);
-      b.load(s);
+      a.load(min(s, last - 1), va);
+      b.load(min(s, last - 1), vb);
+    };
+    auto put = [&](char* lds) {
+      A::store(va, lds);
+      B::store(vb, lds + A::kBytes);
     };
     fetch(first);
     put(even);
     fetch(first + 1);
+    put(odd);
+    fetch(first + 2);
     lds_barrier();
-    get(0, even, 0);
-    constexpr int kPutB = kParts > 2 ? 1 : 0, kLoadB = kParts > 2 ? 2 : 1;
-    auto step = [&](int s, const char* from, char* to) {
+    f[0].template read<A, B>(even, even + A::kBytes, at.wm, at.wn, 0);
+    auto step = [&](int s, char* from, char* to, int parity) {
 #pragma unroll
       for (int part = 0; part < kParts; ++part) {
+        const int now = (parity * kParts + part) & 1;
+        constexpr int kMfma = C::FM * C::FN * (kPlanes == 3 ? 6 : 1);
+        constexpr int kReads = kPlanes * (C::FM * (AKM ? 2 : 1) + C::FN * (BKM ? 2 : 1));
         if (part == kParts - 1) {
           lds_barrier();
-          get(0, to, 0);
+          f[now ^ 1].template read<A, B>(to, to + A::kBytes, at.wm, at.wn, 0);
+          put(from);
+          fetch(s + 3);
+          f[now].multiply(acc);
+          spread<kMfma, kReads, kPlanes*(A::kPieces + B::kPieces), A::kWords * A::kPieces + B::kWords * B::kPieces>();
         } else {
-          get((part + 1) & 1, from, part + 1);
+          f[now ^ 1].template read<A, B>(from, from + A::kBytes, at.wm, at.wn, (part + 1) * 32);
+          f[now].multiply(acc);
+          spread<kMfma, kReads, 0, 0>();
         }
-        if (part == 0) a.store(to);
-        if (part == kPutB) b.store(to + A::kBytes);
-        if (part == kPutB) a.load(min(s + 2, last - 1));
-        if (part == kLoadB) b.load(min(s + 2, last - 1));
-        multiply(part & 1);
-        constexpr int kMfma = FM * FN * (kPlanes == 3 ? 6 : 1), kReads = kPlanes * (FM * (AKM ? 2 : 1) + FN * (BKM ? 2 : 1));
-        if (part == 0) spread<kMfma, kReads, kPlanes * A::kPieces, 0>();
-        else if (part == 1) spread<kMfma, kReads, kPlanes * B::kPieces, A::kWords * A::kPieces>();
-        else if (part == 2) spread<kMfma, kReads, 0, B::kWords * B::kPieces>();
-        else spread<kMfma, kReads, 0, 0>();
         __builtin_amdgcn_sched_barrier(0);
       }
     };
     for (int s = first; s < last; s += 2) {
-      step(s, even, odd);
+      step(s, even, odd, 0);
       if (s + 1 == last) break;
-      step(s + 1, odd, even);
-    }
-  }
-
-  // The bias of the tile's gates, then of the rest, behind the waves' rooms.
-  constexpr int kWaves = C::kThreads / kWave, kRoom = 32 * (WN * 4 + 16);
-  static_assert(kWaves % 2 == 0 && kWaves / 2 * kRoom + (GATED ? BN * 4 : 0) <= kBuffer, "a wave's rows");
-  char* const room = (wave < kWaves / 2 ? even : odd) + wave % (kWaves / 2) * kRoom;
-  float* const bias = reinterpret_cast<float*>(odd + kBuffer) - BN;
-  lds_barrier();
-  if constexpr (GATED) {
-    for (int i = threadIdx.x; i < BN; i += C::kThreads) {
-      const int f = min(n0 + i % (BN / 2), g.N - 1) + i / (BN / 2) * g.N;
-      bias[i] = g.bias && g.splits == 1 ? Store<T>::load1(static_cast<const T*>(g.bias) + f) : 0.0f;
+      step(s + 1, odd, even, 1);
     }
     lds_barrier();
   }
-  auto part = [&](const f32x16& v, int q) { return f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]}; };
-  const int m_first = m0 + wm;
-  if constexpr (!GATED) {
-    const int n = n0 + wn;
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = m_first + i * 32;
-      auto value = [&](int j, int q) { return part(acc[i][j], q); };
-      if (g.splits > 1)
-        store_rows<float, FN>(room, g.partial + (static_cast<int64_t>(split) * g.M + m) * g.N + n, g.N, g.M - m, g.N - n, value);
-      else
-        store_rows<T, FN>(room, static_cast<T*>(g.c) + static_cast<int64_t>(m) * g.N + n, g.N, g.M - m, g.N - n, value);
-    }
-  } else {
-    constexpr int J = FN / 2;
-    const int f = n0 + wn / 2, left = g.N - f;
-    const int64_t ld = 2 * static_cast<int64_t>(g.N);
-    const float* const own = bias + wn / 2 + 4 * (lane / 32);
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = m_first + i * 32;
-      auto gate = [&](int j, int q) { return part(acc[i][j], q) + *reinterpret_cast<const f32x4*>(own + j * 32 + 8 * q); };
-      auto up = [&](int j, int q) { return part(acc[i][j + J], q) + *reinterpret_cast<const f32x4*>(own + BN / 2 + j * 32 + 8 * q); };
-      auto sums = [&](auto* to) {
-        using U = std::remove_pointer_t<decltype(to)>;
-        store_rows<U, J>(room, to + m * ld + f, ld, g.M - m, left, gate);
-        store_rows<U, J>(room, to + m * ld + f + g.N, ld, g.M - m, left, up);
-      };
-      if (g.splits > 1) {
-        sums(g.partial + static_cast<int64_t>(split) * g.M * ld);
-      } else {
-        if (g.gu) sums(static_cast<T*>(g.gu));
-        store_rows<T, J>(room, static_cast<T*>(g.h) + static_cast<int64_t>(m) * g.N + f, g.N, g.M - m, left, [&](int j, int q) {
-          f32x4 v = gate(j, q);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = act_value<END == kErf>(v[e], g.c0, g.c1);
-          return v * up(j, q);
+  constexpr int kRoom = (kBuffer - C::BN * 4) / ((C::kWaves + 1) / 2) & ~15;
+  finish<T, END, C, kRoom>(g, at, acc, (at.wave % 2 == 0 ? even : odd) + at.wave / 2 * kRoom,
+                           reinterpret_cast<float*>(odd + kBuffer) - C::BN);
+}
+
+// Waits until all but the last N loads of the wave have come (and for nothing else).
+template <int N>
+__device__ __forceinline__ void landed() {
+  static_assert(N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xF70);
+}
+// bfloat16 whose rows begin at multiples of 16 bytes: memory to LDS without registers, BUFS - 1 steps ahead.
+template <bool AKM, bool BKM, Epilogue END, typename C, int BUFS, int PER_CU>
+__global__ __launch_bounds__(C::kThreads, PER_CU * C::kWaves / 4) void aligned_product_kernel(Product g) {
+  using A = Operand<bf16_t, AKM, C::BM, C::BK, C::kThreads>;
+  using B = Operand<bf16_t, BKM, C::BN, C::BK, C::kThreads>;
+  static_assert(C::BK == 32, "a step is one instruction's values of k");
+  constexpr int kBuffer = A::kBytes + B::kBytes, kLoads = A::kPieces + B::kPieces;
+  __shared__ __attribute__((aligned(16))) char lds[BUFS * kBuffer];
+  const Place<C, END != kPlain> at(g);
+  const A a(g.a, g.lda, at.m0, g.M, [&](int r) { return at.a_row(g, r); });
+  const B b(g.b, g.ldb, at.n0, g.N, [&](int r) { return at.b_row(g, r); });
+  const int whole = g.K / C::BK, first = at.split * g.steps, end = first + g.steps, last = min(end, whole);
+  f32x4 acc[C::FM][C::FN];
+  clear<C>(acc);
+  if (end > whole) rest_of_k<A, B, C>(g, at, a, b, max(whole, first), end, lds, acc);
+  if (first < last) {
+    Fragments<1, C> f[2];
+    auto load = [&](int i, int s, int buffer) {  // piece i of step s, beyond the last one that one's again
+      char* const to = lds + buffer * kBuffer;
+      if (i < A::kPieces) a.load_lds(i, min(s, last - 1), to);
+      else b.load_lds(i - A::kPieces, min(s, last - 1), to + A::kBytes);
+    };
+    auto read = [&](int i, int to, int buffer) {  // operand i of a wave
+      const char* const from = lds + buffer * kBuffer;
+      if (i < C::FN) f[to].b[0][i] = B::read(from + A::kBytes, at.wn + i * 16, 0);
+      else f[to].a[0][i - C::FN] = A::read(from, at.wm + (i - C::FN) * 16, 0);
+    };
+    // Buffer s % BUFS has been read when all waves have come to the barrier of step s + 1; what step s loads goes to that of
+    // s - 1.  The next step's operands are read in the first half of the matrix instructions, to have come by the end.
+    auto step = [&](int s, auto turn) {
+      constexpr int kMfma = C::FM * C::FN, kHalf = kMfma / 2, kReads = C::FM + C::FN, buffer = turn % BUFS, now = turn & 1;
+      landed<(BUFS - 3) * kLoads>();
+      lds_barrier();
+      for_each(std::make_integer_sequence<int, kMfma>{}, [&](auto count) {
+        constexpr int n = decltype(count)::value, i = n / C::FN, j = n % C::FN;
+        for_each(std::make_integer_sequence<int, kReads>{}, [&](auto r) {
+          if constexpr (r * kHalf / kReads == n) read(r, now ^ 1, (buffer + 1) % BUFS);
         });
-      }
+        for_each(std::make_integer_sequence<int, kLoads>{}, [&](auto l) {
+          if constexpr ((2 * l + 1) * kMfma / (2 * kLoads) == n) load(l, s + BUFS - 1, (buffer + BUFS - 1) % BUFS);
+        });
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[now].b[0][j], f[now].a[0][i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+#pragma unroll
+    for (int s = 0; s < BUFS - 1; ++s)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) load(i, first + s, s);
+    landed<(BUFS - 2) * kLoads>();
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < C::FM + C::FN; ++i) read(i, 0, 0);
+    constexpr int kTurns = BUFS % 2 == 0 ? BUFS : 2 * BUFS;  // buffers and operands' registers come round
+    for (int s = first; s < last; s += kTurns) {
+      const bool all = for_each_while(std::make_integer_sequence<int, kTurns>{}, [&](auto turn) {
+        step(s + turn, turn);
+        return s + turn + 1 < last;
+      });
+      if (!all) break;
     }
+    landed<0>();
+    lds_barrier();
   }
+  constexpr int kRoom = (BUFS * kBuffer - C::BN * 4) / C::kWaves & ~15;
+  finish<bf16_t, END, C, kRoom>(g, at, acc, lds + at.wave * kRoom, reinterpret_cast<float*>(lds + BUFS * kBuffer) - C::BN);
 }
 
 // The sums of the parts, in their order.
@@ -566,43 +693,48 @@ __global__ __launch_bounds__(kWave) void bias_kernel(const float* sums, T* dbias
 }
 
 // ---- plans ------------------------------------------------------------------------------------------------------------
-enum class Size { kLarge, kMiddle, kSmall };
+// Register path: what has any type or address.  Aligned path: bfloat16 in rows of whole 16-byte pieces.
 template <typename T>
-struct Tiles;
-template <>
-struct Tiles<bf16_t> {
-  using Large = Tile<256, 256, 128, 128, 64>;
-  using Middle = Tile<128, 128, 64, 64, 64>;
-  using Small = Tile<64, 64, 32, 64, 64>;
-};
-template <>
-struct Tiles<float> {
-  using Large = Tile<128, 128, 64, 64, 32>;
-  using Middle = Tile<128, 128, 64, 64, 32>;
-  using Small = Tile<64, 64, 32, 64, 32>;
-};
+using Middle = Tile<128, 128, 64, 64, sizeof(T) == 4 ? 32 : 64>;
+template <typename T>
+using Small = Tile<64, 64, 32, 64, sizeof(T) == 4 ? 32 : 64>;
+using AlignedLarge = Tile<256, 256, 128, 128, 32>;
+using AlignedTall = Tile<256, 128, 128, 64, 32>;
+using AlignedMiddle = Tile<128, 128, 64, 64, 32>;
+using AlignedSmall = Tile<64, 64, 32, 64, 32>;
 
+enum class Size { kLarge, kTall, kMiddle, kMiddle3, kSmall };
 struct Plan {
+  bool aligned;
   Size size;
   int splits, steps;
   int64_t tiles;
 };
-Plan plan_for(int64_t M, int64_t N, int64_t K, tempo_dtype dt) {  // N: columns of all rows of b
+Plan plan_for(int64_t M, int64_t N, int64_t K, tempo_dtype dt, bool aligned) {  // N: columns of all rows of b
   const int64_t cus = compute_units();
   auto count = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  const int bk = dt == TEMPO_F32 ? 32 : 64;
   Plan p{};
+  p.aligned = aligned && dt == TEMPO_BF16;
   int64_t tiles;
-  if (dt == TEMPO_BF16 && count(256, 256) >= cus) p.size = Size::kLarge, tiles = count(256, 256);
+  if (p.aligned && count(256, 256) >= cus) p.size = Size::kLarge, tiles = count(256, 256);
   else if (count(128, 128) >= cus) p.size = Size::kMiddle, tiles = count(128, 128);
   else p.size = Size::kSmall, tiles = count(64, 64);
+  if (const char* e = p.aligned ? getenv("GLUSIZE") : nullptr) {
+    p.size = static_cast<Size>(atoi(e));
+    tiles = p.size == Size::kLarge ? count(256, 256) : p.size == Size::kTall ? count(256, 128) : p.size == Size::kSmall ? count(64, 64) : count(128, 128);
+  }
+  const int bk = p.aligned || dt == TEMPO_F32 ? 32 : 64;
   const int64_t steps = std::max<int64_t>(1, (K + bk - 1) / bk);
-  int64_t splits = tiles >= cus || tiles == 0 ? 1 : std::max<int64_t>(1, std::min(2 * cus / tiles, steps / 4));
+  int64_t splits = tiles >= cus || tiles == 0 ? 1 : std::max<int64_t>(1, std::min(2 * cus / tiles, steps * bk / 256));
   p.steps = static_cast<int>((steps + splits - 1) / splits);
   p.splits = static_cast<int>((steps + p.steps - 1) / p.steps);
   p.tiles = tiles * p.splits;
   return p;
 }
+// The three products.  Rows of x and w have H elements, of [g | u] 2F.
+Plan forward_plan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) { return plan_for(T, 2 * F, H, dt, H % 8 == 0); }
+Plan dx_plan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) { return plan_for(T, H, 2 * F, dt, H % 8 == 0 && F % 4 == 0); }
+Plan dw_plan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) { return plan_for(2 * F, H, T, dt, H % 8 == 0 && F % 4 == 0); }
 size_t partial_bytes(const Plan& p, int64_t M, int64_t N) {
   return p.splits > 1 ? static_cast<size_t>(p.splits) * M * N * sizeof(float) : 0;
 }
@@ -611,16 +743,22 @@ template <typename T, bool AKM, bool BKM, Epilogue END>
 tempo_status launch_product(Product g, const Plan& p, hipStream_t st) {
   g.splits = p.splits;
   g.steps = p.steps;
-  auto go = [&](auto tile) {
-    using C = decltype(tile);
-    hipLaunchKernelGGL((product_kernel<T, AKM, BKM, END, C>), dim3(static_cast<unsigned>(p.tiles)), dim3(C::kThreads), 0, st, g);
+  if (p.tiles == 0) return TEMPO_OK;
+  auto go = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(p.tiles)), dim3(threads), 0, st, g);
     return launch_status();
   };
-  if (p.tiles == 0) return TEMPO_OK;
-  tempo_status status;
-  if (p.size == Size::kLarge) status = go(typename Tiles<T>::Large{});
-  else if (p.size == Size::kMiddle) status = go(typename Tiles<T>::Middle{});
-  else status = go(typename Tiles<T>::Small{});
+  tempo_status status = TEMPO_ERR_UNSUPPORTED;
+  if (!p.aligned) {
+    if (p.size == Size::kMiddle) status = go(product_kernel<T, AKM, BKM, END, Middle<T>>, Middle<T>::kThreads);
+    else status = go(product_kernel<T, AKM, BKM, END, Small<T>>, Small<T>::kThreads);
+  } else if constexpr (sizeof(T) == 2) {
+    if (p.size == Size::kLarge) status = go(aligned_product_kernel<AKM, BKM, END, AlignedLarge, 4, 1>, AlignedLarge::kThreads);
+    else if (p.size == Size::kTall) status = go(aligned_product_kernel<AKM, BKM, END, AlignedTall, 3, 2>, AlignedTall::kThreads);
+    else if (p.size == Size::kMiddle) status = go(aligned_product_kernel<AKM, BKM, END, AlignedMiddle, 4, 2>, AlignedMiddle::kThreads);
+    else if (p.size == Size::kMiddle3) status = go(aligned_product_kernel<AKM, BKM, END, AlignedMiddle, 3, 3>, AlignedMiddle::kThreads);
+    else status = go(aligned_product_kernel<AKM, BKM, END, AlignedSmall, 4, 4>, AlignedSmall::kThreads);
+  }
   if (status != TEMPO_OK || p.splits == 1) return status;
   const int64_t n = int64_t{g.M} * g.N;
   hipLaunchKernelGGL((join_kernel<T, END != kPlain>), dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, g);
@@ -708,19 +846,19 @@ bool glu_takes(int64_t T, int64_t H, int64_t F) {
 }
 
 size_t glu_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt, bool back) {
-  if (!back) return partial_bytes(plan_for(T, 2 * F, H, dt), T, 2 * F);
-  return std::max({partial_bytes(plan_for(T, H, 2 * F, dt), T, H), partial_bytes(plan_for(2 * F, H, T, dt), 2 * F, H),
+  if (!back) return partial_bytes(forward_plan(T, H, F, dt), T, 2 * F);
+  return std::max({partial_bytes(dx_plan(T, H, F, dt), T, H), partial_bytes(dw_plan(T, H, F, dt), 2 * F, H),
                    static_cast<size_t>(chunks_of(T)) * 2 * F * sizeof(float)});
 }
 
 tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
-  const Plan p = plan_for(c.T, 2 * c.F, c.H, dt);
+  const Plan p = forward_plan(c.T, c.H, c.F, dt);
   if (partial_bytes(p, c.T, 2 * c.F) > c.workspace_bytes) return TEMPO_ERR_WORKSPACE;
   return dt == TEMPO_F32 ? forward<float>(c, p, st) : forward<bf16_t>(c, p, st);
 }
 
 tempo_status launch_glu_bwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
-  const Plan px = plan_for(c.T, c.H, 2 * c.F, dt), pw = plan_for(2 * c.F, c.H, c.T, dt);
+  const Plan px = dx_plan(c.T, c.H, c.F, dt), pw = dw_plan(c.T, c.H, c.F, dt);
   if ((c.dx && partial_bytes(px, c.T, c.H) > c.workspace_bytes) || (c.dw && partial_bytes(pw, 2 * c.F, c.H) > c.workspace_bytes) ||
       (c.dbias && static_cast<size_t>(chunks_of(c.T)) * 2 * c.F * sizeof(float) > c.workspace_bytes))
     return TEMPO_ERR_WORKSPACE;
