@@ -235,10 +235,10 @@ template <typename C, bool GATED>
 struct Place {
   static constexpr int kCols = GATED ? C::BN / 2 : C::BN;
   int split, m0, n0, wm, wn, wave;
-  __device__ __forceinline__ explicit Place(const Product& g) {
+  // Tile `block` of `total`, in the order of the launch.
+  __device__ __forceinline__ Place(const Product& g, int block, int total) {
     const int tiles_m = (g.M + C::BM - 1) / C::BM, tiles_n = (g.N + kCols - 1) / kCols;
-    const int total = gridDim.x, xcd = blockIdx.x % 8, each = total / 8, more = total % 8;
-    const int tile = xcd * each + min(xcd, more) + static_cast<int>(blockIdx.x) / 8;
+    const int xcd = block % 8, each = total / 8, more = total % 8, tile = xcd * each + min(xcd, more) + block / 8;
     split = tile / (tiles_m * tiles_n);
     const int in_split = tile - split * (tiles_m * tiles_n);
     const int band = in_split / (8 * tiles_n), in_band = in_split - band * (8 * tiles_n), rows = min(8, tiles_m - band * 8);
@@ -438,14 +438,13 @@ __device__ __forceinline__ void rest_of_k(const Product& g, const P& at, const A
 // Any type, size and address: operands by way of registers, two buffers in LDS.  While the matrix cores work on 32 values of
 // k, the operands of the next ones come from LDS; behind the one barrier of a step, when all waves have read what it held,
 // a buffer gets the step after the next, and the one behind that is on its way from memory.
+// Two buffers that are two objects, so that writes to one are known not to be what is read from the other.
 template <typename T, bool AKM, bool BKM, Epilogue END, typename C>
-__global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
+__device__ __forceinline__ void product_tile(const Product& g, int block, int total, char* even, char* odd) {
   using A = Operand<T, AKM, C::BM, C::BK, C::kThreads>;
   using B = Operand<T, BKM, C::BN, C::BK, C::kThreads>;
   constexpr int kPlanes = A::kPlanes, kBuffer = A::kBytes + B::kBytes, kParts = C::BK / 32;
-  // Two objects, so that writes to one are known not to be what is read from the other.
-  __shared__ __attribute__((aligned(16))) char even[kBuffer], odd[kBuffer];
-  const Place<C, END != kPlain> at(g);
+  const Place<C, END != kPlain> at(g, block, total);
   const A a(g.a, g.lda, at.m0, g.M, [&](int r) { return at.a_row(g, r); });
   const B b(g.b, g.ldb, at.n0, g.N, [&](int r) { return at.b_row(g, r); });
   // Steps of BK values of k that are loaded in whole pieces: where rows of a k-major operand are no multiple of a piece,
@@ -516,15 +515,15 @@ __device__ __forceinline__ void landed() {
   static_assert(N < 64, "six bits");
   __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xF70);
 }
-// bfloat16 whose rows begin at multiples of 16 bytes: memory to LDS without registers, BUFS - 1 steps ahead.
-template <bool AKM, bool BKM, Epilogue END, typename C, int BUFS, int PER_CU>
-__global__ __launch_bounds__(C::kThreads, PER_CU * C::kWaves / 4) void aligned_product_kernel(Product g) {
+constexpr int kBuffers = 4;
+// bfloat16 whose rows begin at multiples of 16 bytes: memory to LDS without registers, kBuffers - 1 steps ahead.
+template <bool AKM, bool BKM, Epilogue END, typename C>
+__device__ __forceinline__ void aligned_tile(const Product& g, int block, int total, char* lds) {
   using A = Operand<bf16_t, AKM, C::BM, C::BK, C::kThreads>;
   using B = Operand<bf16_t, BKM, C::BN, C::BK, C::kThreads>;
   static_assert(C::BK == 32, "a step is one instruction's values of k");
-  constexpr int kBuffer = A::kBytes + B::kBytes, kLoads = A::kPieces + B::kPieces;
-  __shared__ __attribute__((aligned(16))) char lds[BUFS * kBuffer];
-  const Place<C, END != kPlain> at(g);
+  constexpr int BUFS = kBuffers, kBuffer = A::kBytes + B::kBytes, kLoads = A::kPieces + B::kPieces;
+  const Place<C, END != kPlain> at(g, block, total);
   const A a(g.a, g.lda, at.m0, g.M, [&](int r) { return at.a_row(g, r); });
   const B b(g.b, g.ldb, at.n0, g.N, [&](int r) { return at.b_row(g, r); });
   const int whole = g.K / C::BK, first = at.split * g.steps, end = first + g.steps, last = min(end, whole);
@@ -583,6 +582,29 @@ __global__ __launch_bounds__(C::kThreads, PER_CU * C::kWaves / 4) void aligned_p
   constexpr int kRoom = (BUFS * kBuffer - C::BN * 4) / C::kWaves & ~15;
   finish<bf16_t, END, C, kRoom>(g, at, acc, lds + at.wave * kRoom, reinterpret_cast<float*>(lds + BUFS * kBuffer) - C::BN);
 }
+
+template <typename T, bool AKM, bool BKM, Epilogue END, typename C, bool ALIGNED>
+__device__ __forceinline__ void any_tile(const Product& g, int block, int total, char* even, char* odd) {
+  if constexpr (ALIGNED) aligned_tile<AKM, BKM, END, C>(g, block, total, even);
+  else product_tile<T, AKM, BKM, END, C>(g, block, total, even, odd);
+}
+#define TEMPO_GLU_LDS(T, C, ALIGNED)                                                                                        \
+  constexpr int kOne = (C::BM + C::BN) * C::BK * 2 * (sizeof(T) == 4 ? 3 : 1);                                              \
+  __shared__ __attribute__((aligned(16))) char even[ALIGNED ? kBuffers * kOne : kOne], odd[ALIGNED ? 16 : kOne]
+template <typename T, bool AKM, bool BKM, Epilogue END, typename C, bool ALIGNED>
+__global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
+  TEMPO_GLU_LDS(T, C, ALIGNED);
+  any_tile<T, AKM, BKM, END, C, ALIGNED>(g, blockIdx.x, gridDim.x, even, odd);
+}
+// dx and dw, which need nothing of each other, in one launch.
+template <typename T, typename C, bool ALIGNED>
+__global__ __launch_bounds__(C::kThreads) void both_kernel(Product dx, Product dw, int dx_tiles) {
+  TEMPO_GLU_LDS(T, C, ALIGNED);
+  const int block = blockIdx.x;
+  if (block < dx_tiles) any_tile<T, false, true, kPlain, C, ALIGNED>(dx, block, dx_tiles, even, odd);
+  else any_tile<T, true, true, kPlain, C, ALIGNED>(dw, block - dx_tiles, gridDim.x - dx_tiles, even, odd);
+}
+#undef TEMPO_GLU_LDS
 
 // The sums of the parts, in their order.
 template <typename T, bool GATED>
@@ -699,70 +721,108 @@ using Middle = Tile<128, 128, 64, 64, sizeof(T) == 4 ? 32 : 64>;
 template <typename T>
 using Small = Tile<64, 64, 32, 64, sizeof(T) == 4 ? 32 : 64>;
 using AlignedLarge = Tile<256, 256, 128, 128, 32>;
-using AlignedTall = Tile<256, 128, 128, 64, 32>;
 using AlignedMiddle = Tile<128, 128, 64, 64, 32>;
 using AlignedSmall = Tile<64, 64, 32, 64, 32>;
 
-enum class Size { kLarge, kTall, kMiddle, kMiddle3, kSmall };
+enum class Size { kLarge, kMiddle, kSmall };
+int edge(Size s) { return s == Size::kLarge ? 256 : s == Size::kMiddle ? 128 : 64; }
 struct Plan {
   bool aligned;
   Size size;
   int splits, steps;
   int64_t tiles;
 };
-Plan plan_for(int64_t M, int64_t N, int64_t K, tempo_dtype dt, bool aligned) {  // N: columns of all rows of b
+struct Shape {
+  int64_t M, N, K;  // N: columns of all rows of b
+  int64_t tiles(Size s) const { return ((M + edge(s) - 1) / edge(s)) * ((N + edge(s) - 1) / edge(s)); }
+};
+// One plan for one or two products of a launch.
+void plan_for(const Shape* shapes, Plan* plans, int n, tempo_dtype dt, bool aligned) {
   const int64_t cus = compute_units();
-  auto count = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  Plan p{};
-  p.aligned = aligned && dt == TEMPO_BF16;
-  int64_t tiles;
-  if (p.aligned && count(256, 256) >= cus) p.size = Size::kLarge, tiles = count(256, 256);
-  else if (count(128, 128) >= cus) p.size = Size::kMiddle, tiles = count(128, 128);
-  else p.size = Size::kSmall, tiles = count(64, 64);
-  if (const char* e = p.aligned ? getenv("GLUSIZE") : nullptr) {
-    p.size = static_cast<Size>(atoi(e));
-    tiles = p.size == Size::kLarge ? count(256, 256) : p.size == Size::kTall ? count(256, 128) : p.size == Size::kSmall ? count(64, 64) : count(128, 128);
+  aligned = aligned && dt == TEMPO_BF16;
+  auto count = [&](Size s) { return shapes[0].tiles(s) + (n > 1 ? shapes[1].tiles(s) : 0); };
+  Size size = Size::kSmall;
+  if (aligned && count(Size::kLarge) >= cus) size = Size::kLarge;
+  else if (count(Size::kMiddle) >= cus) size = Size::kMiddle;
+  const int bk = aligned || dt == TEMPO_F32 ? 32 : 64;
+  const int64_t all = count(size);
+  for (int i = 0; i < n; ++i) {
+    const int64_t steps = std::max<int64_t>(1, (shapes[i].K + bk - 1) / bk);
+    const int64_t splits = all >= cus || all == 0 ? 1 : std::max<int64_t>(1, std::min(2 * cus / all, steps * bk / 256));
+    Plan& p = plans[i];
+    p.aligned = aligned;
+    p.size = size;
+    p.steps = static_cast<int>((steps + splits - 1) / splits);
+    p.splits = static_cast<int>((steps + p.steps - 1) / p.steps);
+    p.tiles = shapes[i].tiles(size) * p.splits;
   }
-  const int bk = p.aligned || dt == TEMPO_F32 ? 32 : 64;
-  const int64_t steps = std::max<int64_t>(1, (K + bk - 1) / bk);
-  int64_t splits = tiles >= cus || tiles == 0 ? 1 : std::max<int64_t>(1, std::min(2 * cus / tiles, steps * bk / 256));
-  p.steps = static_cast<int>((steps + splits - 1) / splits);
-  p.splits = static_cast<int>((steps + p.steps - 1) / p.steps);
-  p.tiles = tiles * p.splits;
-  return p;
 }
-// The three products.  Rows of x and w have H elements, of [g | u] 2F.
-Plan forward_plan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) { return plan_for(T, 2 * F, H, dt, H % 8 == 0); }
-Plan dx_plan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) { return plan_for(T, H, 2 * F, dt, H % 8 == 0 && F % 4 == 0); }
-Plan dw_plan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) { return plan_for(2 * F, H, T, dt, H % 8 == 0 && F % 4 == 0); }
-size_t partial_bytes(const Plan& p, int64_t M, int64_t N) {
-  return p.splits > 1 ? static_cast<size_t>(p.splits) * M * N * sizeof(float) : 0;
+size_t partial_bytes(const Plan& p, const Shape& s) {
+  return p.splits > 1 ? static_cast<size_t>(p.splits) * s.M * s.N * sizeof(float) : 0;
 }
+// The three products.  Rows of x and w have H elements, of [g | u] 2F.  dx and dw are planned together whichever is wanted: the
+// bits of one do not depend on the other.
+struct ForwardPlan {
+  Shape shape;
+  Plan plan;
+  size_t bytes;
+  ForwardPlan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) : shape{T, 2 * F, H} {
+    plan_for(&shape, &plan, 1, dt, H % 8 == 0);
+    bytes = partial_bytes(plan, shape);
+  }
+};
+struct BackwardPlan {
+  Shape shapes[2];  // dx, dw
+  Plan plans[2];
+  size_t dx_bytes, bytes;
+  BackwardPlan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) : shapes{{T, H, 2 * F}, {2 * F, H, T}} {
+    plan_for(shapes, plans, 2, dt, H % 8 == 0 && F % 4 == 0);
+    dx_bytes = (partial_bytes(plans[0], shapes[0]) + 15) / 16 * 16;
+    bytes = dx_bytes + partial_bytes(plans[1], shapes[1]);
+  }
+};
 
+template <typename T, typename F>
+tempo_status with_tile(const Plan& p, F&& f) {
+  if (!p.aligned) return p.size == Size::kSmall ? f(Small<T>{}, std::false_type{}) : f(Middle<T>{}, std::false_type{});
+  if constexpr (sizeof(T) == 2) {
+    if (p.size == Size::kLarge) return f(AlignedLarge{}, std::true_type{});
+    return p.size == Size::kMiddle ? f(AlignedMiddle{}, std::true_type{}) : f(AlignedSmall{}, std::true_type{});
+  }
+  return TEMPO_ERR_UNSUPPORTED;
+}
+template <typename T, bool GATED>
+tempo_status join(const Product& g, hipStream_t st) {
+  if (g.splits == 1) return TEMPO_OK;
+  const int64_t n = int64_t{g.M} * g.N;
+  hipLaunchKernelGGL((join_kernel<T, GATED>), dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, g);
+  return launch_status();
+}
 template <typename T, bool AKM, bool BKM, Epilogue END>
 tempo_status launch_product(Product g, const Plan& p, hipStream_t st) {
+  if (p.tiles == 0) return TEMPO_OK;
   g.splits = p.splits;
   g.steps = p.steps;
-  if (p.tiles == 0) return TEMPO_OK;
-  auto go = [&](auto kernel, int threads) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(p.tiles)), dim3(threads), 0, st, g);
+  const tempo_status status = with_tile<T>(p, [&](auto tile, auto aligned) {
+    using C = decltype(tile);
+    hipLaunchKernelGGL((product_kernel<T, AKM, BKM, END, C, decltype(aligned)::value>), dim3(static_cast<unsigned>(p.tiles)),
+                       dim3(C::kThreads), 0, st, g);
     return launch_status();
-  };
-  tempo_status status = TEMPO_ERR_UNSUPPORTED;
-  if (!p.aligned) {
-    if (p.size == Size::kMiddle) status = go(product_kernel<T, AKM, BKM, END, Middle<T>>, Middle<T>::kThreads);
-    else status = go(product_kernel<T, AKM, BKM, END, Small<T>>, Small<T>::kThreads);
-  } else if constexpr (sizeof(T) == 2) {
-    if (p.size == Size::kLarge) status = go(aligned_product_kernel<AKM, BKM, END, AlignedLarge, 4, 1>, AlignedLarge::kThreads);
-    else if (p.size == Size::kTall) status = go(aligned_product_kernel<AKM, BKM, END, AlignedTall, 3, 2>, AlignedTall::kThreads);
-    else if (p.size == Size::kMiddle) status = go(aligned_product_kernel<AKM, BKM, END, AlignedMiddle, 4, 2>, AlignedMiddle::kThreads);
-    else if (p.size == Size::kMiddle3) status = go(aligned_product_kernel<AKM, BKM, END, AlignedMiddle, 3, 3>, AlignedMiddle::kThreads);
-    else status = go(aligned_product_kernel<AKM, BKM, END, AlignedSmall, 4, 4>, AlignedSmall::kThreads);
-  }
-  if (status != TEMPO_OK || p.splits == 1) return status;
-  const int64_t n = int64_t{g.M} * g.N;
-  hipLaunchKernelGGL((join_kernel<T, END != kPlain>), dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, st, g);
-  return launch_status();
+  });
+  return status == TEMPO_OK ? join<T, END != kPlain>(g, st) : status;
+}
+template <typename T>
+tempo_status launch_both(Product dx, Product dw, const Plan* p, hipStream_t st) {
+  dx.splits = p[0].splits, dx.steps = p[0].steps;
+  dw.splits = p[1].splits, dw.steps = p[1].steps;
+  tempo_status status = with_tile<T>(p[0], [&](auto tile, auto aligned) {
+    using C = decltype(tile);
+    hipLaunchKernelGGL((both_kernel<T, C, decltype(aligned)::value>), dim3(static_cast<unsigned>(p[0].tiles + p[1].tiles)),
+                       dim3(C::kThreads), 0, st, dx, dw, static_cast<int>(p[0].tiles));
+    return launch_status();
+  });
+  if (status == TEMPO_OK) status = join<T, false>(dx, st);
+  return status == TEMPO_OK ? join<T, false>(dw, st) : status;
 }
 
 constexpr int kChunk = 32;  // rows whose column sums a wave makes
@@ -790,7 +850,7 @@ tempo_status forward(const GluCall& c, const Plan& p, hipStream_t st) {
 }
 
 template <typename T>
-tempo_status backward(const GluCall& c, const Plan& px, const Plan& pw, hipStream_t st) {
+tempo_status backward(const GluCall& c, const BackwardPlan& p, hipStream_t st) {
   constexpr int V = Store<T>::kVec;
   Gates e{c.dh, c.gu, c.dgu, c.h, c.dbias ? static_cast<float*>(c.workspace) : nullptr, c.T, static_cast<int>(c.F), c.kind, kChunk};
   const int64_t chunks = chunks_of(c.T);
@@ -812,27 +872,24 @@ tempo_status backward(const GluCall& c, const Plan& px, const Plan& pw, hipStrea
     hipLaunchKernelGGL((bias_kernel<T>), dim3((n + kWave - 1) / kWave), dim3(kWave), 0, st, e.sums, static_cast<T*>(c.dbias), chunks, n);
     status = launch_status();
   }
-  Product g{};
-  g.a = c.dgu;
-  g.lda = 2 * c.F;
-  g.ldb = c.H;
-  g.N = static_cast<int>(c.H);
-  g.partial = static_cast<float*>(c.workspace);
-  if (status == TEMPO_OK && c.dx) {
-    g.b = c.w;
-    g.M = static_cast<int>(c.T);
-    g.K = static_cast<int>(2 * c.F);
-    g.c = c.dx;
-    status = launch_product<T, false, true, kPlain>(g, px, st);
-  }
-  if (status == TEMPO_OK && c.dw) {
-    g.b = c.x;
-    g.M = static_cast<int>(2 * c.F);
-    g.K = static_cast<int>(c.T);
-    g.c = c.dw;
-    status = launch_product<T, true, true, kPlain>(g, pw, st);
-  }
-  return status;
+  if (status != TEMPO_OK || c.H == 0) return status;
+  Product dx{}, dw{};
+  dx.a = dw.a = c.dgu;
+  dx.lda = dw.lda = 2 * c.F;
+  dx.ldb = dw.ldb = c.H;
+  dx.N = dw.N = static_cast<int>(c.H);
+  dx.M = dw.K = static_cast<int>(c.T);
+  dx.K = dw.M = static_cast<int>(2 * c.F);
+  dx.b = c.w;
+  dx.c = c.dx;
+  dx.partial = static_cast<float*>(c.workspace);
+  dw.b = c.x;
+  dw.c = c.dw;
+  dw.partial = dx.partial + p.dx_bytes / sizeof(float);
+  const bool x = c.dx && c.T > 0, w = c.dw && c.F > 0;
+  if (x && w) return launch_both<T>(dx, dw, p.plans, st);
+  if (x) return launch_product<T, false, true, kPlain>(dx, p.plans[0], st);
+  return w ? launch_product<T, true, true, kPlain>(dw, p.plans[1], st) : TEMPO_OK;
 }
 
 }  // namespace
@@ -846,23 +903,22 @@ bool glu_takes(int64_t T, int64_t H, int64_t F) {
 }
 
 size_t glu_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt, bool back) {
-  if (!back) return partial_bytes(forward_plan(T, H, F, dt), T, 2 * F);
-  return std::max({partial_bytes(dx_plan(T, H, F, dt), T, H), partial_bytes(dw_plan(T, H, F, dt), 2 * F, H),
-                   static_cast<size_t>(chunks_of(T)) * 2 * F * sizeof(float)});
+  if (!back) return ForwardPlan(T, H, F, dt).bytes;
+  return std::max(BackwardPlan(T, H, F, dt).bytes, static_cast<size_t>(chunks_of(T)) * 2 * F * sizeof(float));
 }
 
 tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
-  const Plan p = forward_plan(c.T, c.H, c.F, dt);
-  if (partial_bytes(p, c.T, 2 * c.F) > c.workspace_bytes) return TEMPO_ERR_WORKSPACE;
-  return dt == TEMPO_F32 ? forward<float>(c, p, st) : forward<bf16_t>(c, p, st);
+  const ForwardPlan p(c.T, c.H, c.F, dt);
+  if (p.bytes > c.workspace_bytes) return TEMPO_ERR_WORKSPACE;
+  return dt == TEMPO_F32 ? forward<float>(c, p.plan, st) : forward<bf16_t>(c, p.plan, st);
 }
 
 tempo_status launch_glu_bwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
-  const Plan px = dx_plan(c.T, c.H, c.F, dt), pw = dw_plan(c.T, c.H, c.F, dt);
-  if ((c.dx && partial_bytes(px, c.T, c.H) > c.workspace_bytes) || (c.dw && partial_bytes(pw, 2 * c.F, c.H) > c.workspace_bytes) ||
+  const BackwardPlan p(c.T, c.H, c.F, dt);
+  if (((c.dx || c.dw) && p.bytes > c.workspace_bytes) ||
       (c.dbias && static_cast<size_t>(chunks_of(c.T)) * 2 * c.F * sizeof(float) > c.workspace_bytes))
     return TEMPO_ERR_WORKSPACE;
-  return dt == TEMPO_F32 ? backward<float>(c, px, pw, st) : backward<bf16_t>(c, px, pw, st);
+  return dt == TEMPO_F32 ? backward<float>(c, p, st) : backward<bf16_t>(c, p, st);
 }
 
 }  // namespace tempo
