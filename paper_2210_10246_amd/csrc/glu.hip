@@ -6,6 +6,7 @@
 // bfloat16 ones, x = x0 + x1 + x2 exactly, and of the nine products those six are made that count in float32 (the other three
 // are below 2^-21 of |a| |b|).
 #include <algorithm>
+#include <cmath>
 #include <utility>
 
 #include "gelu_f32.h"
@@ -705,13 +706,23 @@ __global__ __launch_bounds__(kWave) void gates_kernel(Gates g, int64_t chunk0) {
     }
   }
 }
+// The chunks' sums of 64 columns, a quarter of the chunks a wave, then the quarters.
 template <typename T>
-__global__ __launch_bounds__(kWave) void bias_kernel(const float* sums, T* dbias, int64_t chunks, int n) {
-  const int e = blockIdx.x * kWave + threadIdx.x;
-  if (e >= n) return;
+__global__ __launch_bounds__(4 * kWave) void bias_kernel(const float* sums, T* dbias, int64_t chunks, int n) {
+  __shared__ float quarters[4 * kWave];
+  const int e = blockIdx.x * kWave + threadIdx.x % kWave, quarter = threadIdx.x / kWave;
+  const int64_t each = (chunks + 3) / 4, first = quarter * each, last = first + each < chunks ? first + each : chunks;
   float v = 0.0f;
-  for (int64_t c = 0; c < chunks; ++c) v += sums[c * n + e];
-  Store<T>::store1(dbias + e, v);
+  if (e < n) {
+#pragma unroll 8
+    for (int64_t c = first; c < last; ++c) v += sums[c * n + e];
+  }
+  quarters[threadIdx.x] = v;
+  lds_barrier();
+  if (quarter == 0 && e < n) {
+    const float* q = quarters + threadIdx.x;
+    Store<T>::store1(dbias + e, (q[0] + q[kWave]) + (q[2 * kWave] + q[3 * kWave]));
+  }
 }
 
 // ---- plans ------------------------------------------------------------------------------------------------------------
@@ -736,25 +747,60 @@ struct Shape {
   int64_t M, N, K;  // N: columns of all rows of b
   int64_t tiles(Size s) const { return ((M + edge(s) - 1) / edge(s)) * ((N + edge(s) - 1) / edge(s)); }
 };
-// One plan for one or two products of a launch.
+// What a tile takes, in us: `step` for 32 values of k and `tile` for its beginning and end, times the tiles of a compute unit,
+// and `wait` more for every 32 values of k of the longest one, alone or not.  Measured, us of [T, H] x 2F with tiles of 256 /
+// 128 / 64, bfloat16 in whole pieces: 16384 x 4096 x 11008 2390 / 3535 / 6490, 2048 x 1024 x 4096 41 / 49 / 71, 1024 x 1024 x 4096
+// 35 / 26 / 39, 128 x 1024 x 4096 - / 11.0 / 8.0, 1000 x 128 x 8192 23.1 / 18.3 / 23.1; by way of registers, 128 / 64: 1021 x 1001 x
+// 2729 36 / 48, 300 x 513 x 1031 15 / 10; float32 4096 x 2048 x 5504 936 / -, 1024 x 1024 x 4096 112 / 130, 512 x 512 x 1024 22 / 18.
+struct Pace {
+  double step, tile, wait;
+  bool one;  // workgroup of a compute unit: tiles count in whole rounds
+};
+Pace pace(Size size, tempo_dtype dt, bool aligned) {
+  if (dt == TEMPO_F32) return size == Size::kSmall ? Pace{0.45, 1.5, 0.45, false} : Pace{1.36, 6.0, 0.0, true};
+  if (!aligned) return size == Size::kSmall ? Pace{0.2, 1.5, 0.15, false} : Pace{0.5, 5.0, 0.1, false};
+  if (size == Size::kLarge) return {0.8, 12.0, 0.0, true};
+  return size == Size::kMiddle ? Pace{0.225, 5.0, 0.1, false} : Pace{0.13, 1.0, 0.07, false};
+}
+// One plan for one or two products of a launch: the sizes of tiles, and in how many parts of k each is made where otherwise a
+// few long tiles would be waited for ([32, 8192] x [8192, 1024] beside [8192, 32] x [32, 1024]: 92 us, 47 with 6 parts of the first).
 void plan_for(const Shape* shapes, Plan* plans, int n, tempo_dtype dt, bool aligned) {
-  const int64_t cus = compute_units();
+  const double cus = compute_units();
   aligned = aligned && dt == TEMPO_BF16;
-  auto count = [&](Size s) { return shapes[0].tiles(s) + (n > 1 ? shapes[1].tiles(s) : 0); };
-  Size size = Size::kSmall;
-  if (aligned && count(Size::kLarge) >= cus) size = Size::kLarge;
-  else if (count(Size::kMiddle) >= cus) size = Size::kMiddle;
   const int bk = aligned || dt == TEMPO_F32 ? 32 : 64;
-  const int64_t all = count(size);
-  for (int i = 0; i < n; ++i) {
-    const int64_t steps = std::max<int64_t>(1, (shapes[i].K + bk - 1) / bk);
-    const int64_t splits = all >= cus || all == 0 ? 1 : std::max<int64_t>(1, std::min(2 * cus / all, steps * bk / 256));
-    Plan& p = plans[i];
-    p.aligned = aligned;
-    p.size = size;
-    p.steps = static_cast<int>((steps + splits - 1) / splits);
-    p.splits = static_cast<int>((steps + p.steps - 1) / p.steps);
-    p.tiles = shapes[i].tiles(size) * p.splits;
+  double least = 0.0;
+  for (int way = 0; way < 6; ++way) {
+    const Size size = way / 2 == 0 ? Size::kMiddle : way / 2 == 1 ? Size::kSmall : Size::kLarge;
+    if (size == Size::kLarge && !aligned) break;
+    const Pace at = pace(size, dt, aligned);
+    Plan made[2];
+    double tiles = 0.0, work = 0.0, longest = 0.0, join = 0.0;  // work, longest: in 32 values of k
+    for (int i = 0; i < n; ++i) {
+      tiles += shapes[i].tiles(size);
+      work += shapes[i].tiles(size) * (shapes[i].K / 32.0);
+    }
+    const double share = std::max({work / cus, tiles / cus * at.tile / at.step, 8.0});
+    tiles = 0.0;
+    for (int i = 0; i < n; ++i) {
+      const int64_t steps = std::max<int64_t>(1, (shapes[i].K + bk - 1) / bk);
+      int64_t splits = way % 2 == 0 ? 1 : std::min<int64_t>(16, std::max<int64_t>(1, static_cast<int64_t>(shapes[i].K / 32.0 / share)));
+      Plan& p = made[i];
+      p.aligned = aligned;
+      p.size = size;
+      p.steps = static_cast<int>((steps + splits - 1) / splits);
+      p.splits = static_cast<int>((steps + p.steps - 1) / p.steps);
+      p.tiles = shapes[i].tiles(size) * p.splits;
+      tiles += p.tiles;
+      longest = std::max(longest, p.steps * bk / 32.0);
+      if (p.splits > 1) join += 3.0 + 8e-6 * p.splits * shapes[i].M * shapes[i].N / 4.0;  // a launch, and bytes at 4 TB/s
+    }
+    double here = std::max(work / cus, longest);
+    if (at.one && tiles > cus) here = std::max(here, work / tiles * std::ceil(tiles / cus));
+    const double cost = here * at.step + longest * at.wait + at.tile * std::max(1.0, at.one ? std::ceil(tiles / cus) : tiles / cus) + join;
+    if (way == 0 || cost < least) {
+      least = cost;
+      for (int i = 0; i < n; ++i) plans[i] = made[i];
+    }
   }
 }
 size_t partial_bytes(const Plan& p, const Shape& s) {
@@ -825,8 +871,16 @@ tempo_status launch_both(Product dx, Product dw, const Plan* p, hipStream_t st) 
   return status == TEMPO_OK ? join<T, false>(dw, st) : status;
 }
 
-constexpr int kChunk = 32;  // rows whose column sums a wave makes
-int64_t chunks_of(int64_t T) { return (T + kChunk - 1) / kChunk; }
+// Rows that a wave of the backward's elementwise part takes: 32, fewer where they would make less than 16 waves per compute unit,
+// and not fewer than 4, so that the column sums of a wave's rows are few beside the rows.
+int chunk_of(int64_t T, int64_t F, tempo_dtype dt) {
+  const int64_t across = (F + (dt == TEMPO_F32 ? 4 : 8) * kWave - 1) / ((dt == TEMPO_F32 ? 4 : 8) * kWave);
+  return static_cast<int>(std::min<int64_t>(32, std::max<int64_t>(4, T * across / (16 * int64_t{compute_units()}))));
+}
+size_t sums_bytes(int64_t T, int64_t F, tempo_dtype dt) {
+  const int chunk = chunk_of(T, F, dt);
+  return static_cast<size_t>((T + chunk - 1) / chunk) * 2 * F * sizeof(float);
+}
 
 template <typename T>
 tempo_status forward(const GluCall& c, const Plan& p, hipStream_t st) {
@@ -852,8 +906,9 @@ tempo_status forward(const GluCall& c, const Plan& p, hipStream_t st) {
 template <typename T>
 tempo_status backward(const GluCall& c, const BackwardPlan& p, hipStream_t st) {
   constexpr int V = Store<T>::kVec;
-  Gates e{c.dh, c.gu, c.dgu, c.h, c.dbias ? static_cast<float*>(c.workspace) : nullptr, c.T, static_cast<int>(c.F), c.kind, kChunk};
-  const int64_t chunks = chunks_of(c.T);
+  Gates e{c.dh, c.gu, c.dgu, c.h, c.dbias ? static_cast<float*>(c.workspace) : nullptr, c.T, static_cast<int>(c.F), c.kind,
+          chunk_of(c.T, c.F, sizeof(T) == 4 ? TEMPO_F32 : TEMPO_BF16)};
+  const int64_t chunks = (c.T + e.chunk - 1) / e.chunk;
   const unsigned across = static_cast<unsigned>((c.F + V * kWave - 1) / (V * kWave));
   auto gates = [&](auto kernel) {
     return split_launch(chunks, std::min<int64_t>(65535, most_groups(chunks, kWave * across)), [&](uint32_t first, uint32_t n) {
@@ -869,7 +924,7 @@ tempo_status backward(const GluCall& c, const BackwardPlan& p, hipStream_t st) {
   tempo_status status = TEMPO_OK;
   if (c.dbias && c.F > 0) {
     const int n = static_cast<int>(2 * c.F);
-    hipLaunchKernelGGL((bias_kernel<T>), dim3((n + kWave - 1) / kWave), dim3(kWave), 0, st, e.sums, static_cast<T*>(c.dbias), chunks, n);
+    hipLaunchKernelGGL((bias_kernel<T>), dim3((n + kWave - 1) / kWave), dim3(4 * kWave), 0, st, e.sums, static_cast<T*>(c.dbias), chunks, n);
     status = launch_status();
   }
   if (status != TEMPO_OK || c.H == 0) return status;
@@ -904,7 +959,7 @@ bool glu_takes(int64_t T, int64_t H, int64_t F) {
 
 size_t glu_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt, bool back) {
   if (!back) return ForwardPlan(T, H, F, dt).bytes;
-  return std::max(BackwardPlan(T, H, F, dt).bytes, static_cast<size_t>(chunks_of(T)) * 2 * F * sizeof(float));
+  return std::max(BackwardPlan(T, H, F, dt).bytes, sums_bytes(T, F, dt));
 }
 
 tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
@@ -916,7 +971,7 @@ tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
 tempo_status launch_glu_bwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
   const BackwardPlan p(c.T, c.H, c.F, dt);
   if (((c.dx || c.dw) && p.bytes > c.workspace_bytes) ||
-      (c.dbias && static_cast<size_t>(chunks_of(c.T)) * 2 * c.F * sizeof(float) > c.workspace_bytes))
+      (c.dbias && sums_bytes(c.T, c.F, dt) > c.workspace_bytes))
     return TEMPO_ERR_WORKSPACE;
   return dt == TEMPO_F32 ? backward<float>(c, p, st) : backward<bf16_t>(c, p, st);
 }
