@@ -79,8 +79,9 @@ struct Operand {
   static constexpr bool kKMajor = KM;
   static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
   static constexpr int kRun = (KM ? R : BK) / 8;         // pieces side by side
-  static constexpr int kPieces = R * BK / 8 / THREADS;   // of a lane
-  static_assert(kPieces * 8 * THREADS == R * BK && (KM ? kRun >= 8 : kRun == 4 || kRun == 8), "whole pieces per lane");
+  static constexpr int kAll = R * BK / 8, kPieces = kAll < THREADS ? 1 : kAll / THREADS;  // of all lanes, and of a lane
+  static_assert((kAll % THREADS == 0 || (THREADS % kAll == 0 && kAll % kWave == 0)) && (KM ? kRun >= 8 : kRun == 4 || kRun == 8),
+                "whole pieces per lane");
   static constexpr int kPlane = R * BK * 2;              // bytes
   static constexpr int kBytes = kPlanes * kPlane;
   static constexpr int kWords = sizeof(T) / 2;           // 16-byte words of a piece in memory
@@ -113,7 +114,9 @@ struct Operand {
     }
   }
 
-  // From memory: piece i of a lane is the one at place (i THREADS + lane) of the LDS image.
+  // From memory: piece i of a lane is the one at this place of the LDS image; where there are fewer pieces than lanes, several
+  // lanes do the same.
+  __device__ static __forceinline__ int place(int i) { return (i * THREADS + static_cast<int>(threadIdx.x)) % kAll; }
   const T* p[kPieces];
   int64_t step;
   // row_of: row of the tile -> row in memory, one that exists
@@ -122,7 +125,7 @@ struct Operand {
     step = KM ? BK * ld : BK;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = swizzled(line, at % kRun);
+      const int at = place(i), line = at / kRun, piece = swizzled(line, at % kRun);
       if constexpr (KM) p[i] = static_cast<const T*>(base) + line * ld + min(row0 + piece * 8, (rows - 1) & ~7);
       else p[i] = static_cast<const T*>(base) + row_of(line) * ld + piece * 8;
     }
@@ -133,7 +136,7 @@ struct Operand {
     static_assert(sizeof(T) == 2, "as it is in memory");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds)) +
-                        (i * THREADS + wave * kWave) * 16;
+                        (i * THREADS + wave * kWave) % kAll * 16;
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p[i] + s * step), "s"(to) : "m0", "memory");
   }
   // By way of registers.
@@ -151,7 +154,7 @@ struct Operand {
   __device__ __forceinline__ void load_rest(int64_t s, int row0, int rows, int K, Staged& to) const {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = i * THREADS + static_cast<int>(threadIdx.x), line = at / kRun, piece = swizzled(line, at % kRun);
+      const int at = place(i), line = at / kRun, piece = swizzled(line, at % kRun);
       const int64_t k = s * BK + (KM ? line : piece * 8);
       const int64_t left = KM ? (k < K ? rows - min(row0 + piece * 8, (rows - 1) & ~7) : 0) : K - k;
       const T* q = p[i] + s * step;
@@ -179,7 +182,7 @@ struct Operand {
   __device__ static __forceinline__ void store(const Staged& from, char* lds) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      char* to = lds + (i * THREADS + static_cast<int>(threadIdx.x)) * 16;
+      char* to = lds + place(i) * 16;
       if constexpr (kPlanes == 1) {
         *reinterpret_cast<u32x4*>(to) = from.v[i][0];
       } else {
@@ -224,9 +227,9 @@ struct Product {
 enum Epilogue { kPlain, kSigmoid, kErf };  // kPlain: not gated
 
 // A workgroup owns BM x BN elements (gated: the g and u of BM x BN / 2), a wave WM x WN of them.
-template <int BM_, int BN_, int WM_, int WN_, int BK_>
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int BUFS_ = 2>
 struct Tile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, FM = WM / 16, FN = WN / 16;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, BUFS = BUFS_, FM = WM / 16, FN = WN / 16;
   static constexpr int kWavesN = BN / WN, kWaves = BM / WM * kWavesN, kThreads = kWave * kWaves;
 };
 
@@ -319,7 +322,6 @@ constexpr int blocks_at_once(int N, int row, int bytes) { return 16 * N * (row +
 template <typename U, int BLOCKS, int J, typename F>
 __device__ __forceinline__ void store_rows(char* lds, U* out, int64_t ld, int rows, int cols, F&& value) {
   constexpr int kRow = J * 16 * sizeof(U), kPitch = kRow + 16, E = 16 / sizeof(U), kLanes = kRow / 16, kOnce = kWave / kLanes;
-  static_assert(16 % kOnce == 0, "whole rows");
   const int lane = threadIdx.x % kWave;
 #pragma unroll
   for (int i = 0; i < BLOCKS; ++i) {
@@ -336,8 +338,8 @@ __device__ __forceinline__ void store_rows(char* lds, U* out, int64_t ld, int ro
 #pragma unroll
   for (int i = 0; i < 16 * BLOCKS; i += kOnce) {
     const int row = i + lane / kLanes;
+    if (row >= min(rows, 16 * BLOCKS) || left <= 0) continue;
     const u32x4 w = *reinterpret_cast<const u32x4*>(lds + row * kPitch + col * sizeof(U));
-    if (row >= rows || left <= 0) continue;
     U* to = out + row * ld + col;
     if (left >= E) {
       *reinterpret_cast<u32x4_any*>(to) = w;
@@ -516,14 +518,12 @@ __device__ __forceinline__ void landed() {
   static_assert(N < 64, "six bits");
   __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xF70);
 }
-constexpr int kBuffers = 4;
-// bfloat16 whose rows begin at multiples of 16 bytes: memory to LDS without registers, kBuffers - 1 steps ahead.
+// bfloat16 whose rows begin at multiples of 16 bytes: memory to LDS without registers, BUFS - 1 steps ahead.
 template <bool AKM, bool BKM, Epilogue END, typename C>
 __device__ __forceinline__ void aligned_tile(const Product& g, int block, int total, char* lds) {
   using A = Operand<bf16_t, AKM, C::BM, C::BK, C::kThreads>;
   using B = Operand<bf16_t, BKM, C::BN, C::BK, C::kThreads>;
-  static_assert(C::BK == 32, "a step is one instruction's values of k");
-  constexpr int BUFS = kBuffers, kBuffer = A::kBytes + B::kBytes, kLoads = A::kPieces + B::kPieces;
+  constexpr int BUFS = C::BUFS, kParts = C::BK / 32, kBuffer = A::kBytes + B::kBytes, kLoads = A::kPieces + B::kPieces;
   const Place<C, END != kPlain> at(g, block, total);
   const A a(g.a, g.lda, at.m0, g.M, [&](int r) { return at.a_row(g, r); });
   const B b(g.b, g.ldb, at.n0, g.N, [&](int r) { return at.b_row(g, r); });
@@ -538,24 +538,27 @@ __device__ __forceinline__ void aligned_tile(const Product& g, int block, int to
       if (i < A::kPieces) a.load_lds(i, min(s, last - 1), to);
       else b.load_lds(i - A::kPieces, min(s, last - 1), to + A::kBytes);
     };
-    auto read = [&](int i, int to, int buffer) {  // operand i of a wave
+    auto read = [&](int i, int to, int buffer, int k) {  // operand i of a wave
       const char* const from = lds + buffer * kBuffer;
-      if (i < C::FN) f[to].b[0][i] = B::read(from + A::kBytes, at.wn + i * 16, 0);
-      else f[to].a[0][i - C::FN] = A::read(from, at.wm + (i - C::FN) * 16, 0);
+      if (i < C::FN) f[to].b[0][i] = B::read(from + A::kBytes, at.wn + i * 16, k);
+      else f[to].a[0][i - C::FN] = A::read(from, at.wm + (i - C::FN) * 16, k);
     };
     // Buffer s % BUFS has been read when all waves have come to the barrier of step s + 1; what step s loads goes to that of
     // s - 1.  The next step's operands are read in the first half of the matrix instructions, to have come by the end.
     auto step = [&](int s, auto turn) {
-      constexpr int kMfma = C::FM * C::FN, kHalf = kMfma / 2, kReads = C::FM + C::FN, buffer = turn % BUFS, now = turn & 1;
+      constexpr int kMfma = C::FM * C::FN, kHalf = (kMfma + 1) / 2, kReads = C::FM + C::FN, buffer = turn % BUFS;
       landed<(BUFS - 3) * kLoads>();
       lds_barrier();
-      for_each(std::make_integer_sequence<int, kMfma>{}, [&](auto count) {
-        constexpr int n = decltype(count)::value, i = n / C::FN, j = n % C::FN;
+      for_each(std::make_integer_sequence<int, kParts * kMfma>{}, [&](auto count) {
+        constexpr int part = count / kMfma, n = count % kMfma, i = n / C::FN, j = n % C::FN, now = (turn * kParts + part) & 1;
         for_each(std::make_integer_sequence<int, kReads>{}, [&](auto r) {
-          if constexpr (r * kHalf / kReads == n) read(r, now ^ 1, (buffer + 1) % BUFS);
+          if constexpr (r * kHalf / kReads == n) {
+            if constexpr (part + 1 < kParts) read(r, now ^ 1, buffer, (part + 1) * 32);
+            else read(r, now ^ 1, (buffer + 1) % BUFS, 0);
+          }
         });
         for_each(std::make_integer_sequence<int, kLoads>{}, [&](auto l) {
-          if constexpr ((2 * l + 1) * kMfma / (2 * kLoads) == n) load(l, s + BUFS - 1, (buffer + BUFS - 1) % BUFS);
+          if constexpr ((2 * l + 1) * kParts * kMfma / (2 * kLoads) == count) load(l, s + BUFS - 1, (buffer + BUFS - 1) % BUFS);
         });
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[now].b[0][j], f[now].a[0][i], acc[i][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -568,8 +571,8 @@ __device__ __forceinline__ void aligned_tile(const Product& g, int block, int to
     landed<(BUFS - 2) * kLoads>();
     lds_barrier();
 #pragma unroll
-    for (int i = 0; i < C::FM + C::FN; ++i) read(i, 0, 0);
-    constexpr int kTurns = BUFS % 2 == 0 ? BUFS : 2 * BUFS;  // buffers and operands' registers come round
+    for (int i = 0; i < C::FM + C::FN; ++i) read(i, 0, 0, 0);
+    constexpr int kTurns = BUFS * kParts % 2 == 0 ? BUFS : 2 * BUFS;  // buffers and operands' registers come round
     for (int s = first; s < last; s += kTurns) {
       const bool all = for_each_while(std::make_integer_sequence<int, kTurns>{}, [&](auto turn) {
         step(s + turn, turn);
@@ -591,7 +594,7 @@ __device__ __forceinline__ void any_tile(const Product& g, int block, int total,
 }
 #define TEMPO_GLU_LDS(T, C, ALIGNED)                                                                                        \
   constexpr int kOne = (C::BM + C::BN) * C::BK * 2 * (sizeof(T) == 4 ? 3 : 1);                                              \
-  __shared__ __attribute__((aligned(16))) char even[ALIGNED ? kBuffers * kOne : kOne], odd[ALIGNED ? 16 : kOne]
+  __shared__ __attribute__((aligned(16))) char even[ALIGNED ? C::BUFS * kOne : kOne], odd[ALIGNED ? 16 : kOne]
 template <typename T, bool AKM, bool BKM, Epilogue END, typename C, bool ALIGNED>
 __global__ __launch_bounds__(C::kThreads) void product_kernel(Product g) {
   TEMPO_GLU_LDS(T, C, ALIGNED);
@@ -731,11 +734,14 @@ template <typename T>
 using Middle = Tile<128, 128, 64, 64, sizeof(T) == 4 ? 32 : 64>;
 template <typename T>
 using Small = Tile<64, 64, 32, 64, sizeof(T) == 4 ? 32 : 64>;
-using AlignedLarge = Tile<256, 256, 128, 128, 32>;
-using AlignedMiddle = Tile<128, 128, 64, 64, 32>;
-using AlignedSmall = Tile<64, 64, 32, 64, 32>;
+using AlignedLarge = Tile<256, 256, 128, 128, 32, 4>;
+using AlignedMiddle = Tile<128, 128, 64, 64, 32, 4>;
+using AlignedSmall = Tile<64, 64, 32, 64, 32, 4>;
+using AlignedFewest = Tile<16, 64, 16, 32, 64, 8>;
+using AlignedFew = Tile<64, 64, 64, 32, 64, 5>;
+using AlignedFewWide = Tile<64, 128, 64, 32, 64, 6>;
 
-enum class Size { kLarge, kMiddle, kSmall };
+enum class Size { kLarge, kMiddle, kSmall, kFewest, kFew, kFewWide };  // the last three: forward only
 int edge(Size s) { return s == Size::kLarge ? 256 : s == Size::kMiddle ? 128 : 64; }
 struct Plan {
   bool aligned;
@@ -814,6 +820,17 @@ struct ForwardPlan {
   size_t bytes;
   ForwardPlan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) : shape{T, 2 * F, H} {
     plan_for(&shape, &plan, 1, dt, H % 8 == 0);
+    // Up to 64 rows read W once, nothing else counts: whole lines of W's rows at a time, as much on its way as LDS holds, few rows
+    // of x beside them.  us, 64 x 64 tiles of above / this: 48 x 4096 x 11008 57 / 41 (64 columns at a time 44), 1 x 4096 x 11008 52 /
+    // 38, 48 x 1024 x 4096 13.2 / 8.4 (128 columns 10.5), 1 x 1024 x 4096 13.0 / 6.1.  Where W has few columns of many values of k,
+    // parts of k are worth more.
+    if (plan.aligned && T <= AlignedFew::BM && (F >= 2048 || H <= 1024)) {
+      plan.size = T <= AlignedFewest::BM ? Size::kFewest : 2 * F >= 80 * int64_t{compute_units()} ? Size::kFewWide : Size::kFew;
+      const int columns = plan.size == Size::kFewWide ? AlignedFewWide::BN : AlignedFew::BN;
+      plan.splits = 1;
+      plan.steps = static_cast<int>((H + AlignedFew::BK - 1) / AlignedFew::BK);
+      plan.tiles = (2 * F + columns - 1) / columns;
+    }
     bytes = partial_bytes(plan, shape);
   }
 };
@@ -828,10 +845,15 @@ struct BackwardPlan {
   }
 };
 
-template <typename T, typename F>
+template <typename T, bool GATED, typename F>
 tempo_status with_tile(const Plan& p, F&& f) {
   if (!p.aligned) return p.size == Size::kSmall ? f(Small<T>{}, std::false_type{}) : f(Middle<T>{}, std::false_type{});
   if constexpr (sizeof(T) == 2) {
+    if constexpr (GATED) {
+      if (p.size == Size::kFewest) return f(AlignedFewest{}, std::true_type{});
+      if (p.size == Size::kFew) return f(AlignedFew{}, std::true_type{});
+      if (p.size == Size::kFewWide) return f(AlignedFewWide{}, std::true_type{});
+    }
     if (p.size == Size::kLarge) return f(AlignedLarge{}, std::true_type{});
     return p.size == Size::kMiddle ? f(AlignedMiddle{}, std::true_type{}) : f(AlignedSmall{}, std::true_type{});
   }
@@ -849,7 +871,7 @@ tempo_status launch_product(Product g, const Plan& p, hipStream_t st) {
   if (p.tiles == 0) return TEMPO_OK;
   g.splits = p.splits;
   g.steps = p.steps;
-  const tempo_status status = with_tile<T>(p, [&](auto tile, auto aligned) {
+  const tempo_status status = with_tile<T, END != kPlain>(p, [&](auto tile, auto aligned) {
     using C = decltype(tile);
     hipLaunchKernelGGL((product_kernel<T, AKM, BKM, END, C, decltype(aligned)::value>), dim3(static_cast<unsigned>(p.tiles)),
                        dim3(C::kThreads), 0, st, g);
@@ -861,7 +883,7 @@ template <typename T>
 tempo_status launch_both(Product dx, Product dw, const Plan* p, hipStream_t st) {
   dx.splits = p[0].splits, dx.steps = p[0].steps;
   dw.splits = p[1].splits, dw.steps = p[1].steps;
-  tempo_status status = with_tile<T>(p[0], [&](auto tile, auto aligned) {
+  tempo_status status = with_tile<T, false>(p[0], [&](auto tile, auto aligned) {
     using C = decltype(tile);
     hipLaunchKernelGGL((both_kernel<T, C, decltype(aligned)::value>), dim3(static_cast<unsigned>(p[0].tiles + p[1].tiles)),
                        dim3(C::kThreads), 0, st, dx, dw, static_cast<int>(p[0].tiles));

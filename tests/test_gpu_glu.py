@@ -128,6 +128,17 @@ def test_sizes_of_every_tile(T, H, F, bias, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 48, 63, 64, 65])
+@pytest.mark.parametrize("H,F", [(64, 40), (72, 516), (520, 2048), (1000, 2052), (96, 10300), (1024, 31), (1001, 2050)])
+def test_few_rows(T, H, F, dtype):
+    x, w, b = inputs(T, H, F, dtype)
+    (gu, e1), (h, e2) = guarded(T, 2 * F, dtype=dtype), guarded(T, F, dtype=dtype)
+    B.tempo_glu_fwd(x, w, b, gu, h, "gelu_tanh")
+    check_forward(x, w, b, gu, h, "gelu_tanh", dtype)
+    assert bool((e1 == 777).all() and (e2 == 777).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,H,F", [(0, 16, 8), (5, 0, 8), (5, 16, 0), (0, 0, 0)])
 def test_sums_of_nothing(T, H, F, dtype):
     x, w, b = inputs(T, H, F, dtype)
