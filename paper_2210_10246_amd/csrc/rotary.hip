@@ -6,6 +6,9 @@
 // Bound by the bytes of q and k, read once and written once.  Angles are made where they are used: in 64 bits, which this
 // chip multiplies at the rate of 32, so that a position of any size keeps its place within the turn; no table is read, kept or
 // bounded by a longest sequence.
+#include <algorithm>
+#include <type_traits>
+
 #include "launch_split.h"
 #include "tempo_device.h"
 #include "tempo_host.h"
@@ -14,7 +17,10 @@ namespace tempo {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kHeadsPerLane = 4;  // heads that share the angles of a lane
+// Heads that share the angles of a lane, each in two pieces (half) or one: 128 bytes of a lane on their way.  One where that
+// leaves the chip short of waves: 64 tokens of 32 + 8 heads of 128 bfloat16 5.4 us with 4, 4.7 with 1; 3063 tokens of 12 heads of 83
+// float32, neighbours in pairs, 14.5 with 8, 10.4 with 1.
+constexpr int heads_per_lane(bool half) { return half ? 4 : 8; }
 
 // cos and sin of a turn in 64 bits.  The quarter is taken off in 64 bits, what is left, at most an eighth of a turn, goes
 // through the Taylor polynomials of sin and cos (next terms below 2e-9 and 2e-10).
@@ -49,40 +55,78 @@ struct Rotary {
   int R2, D;
   float scale;
   int rot_units, units;  // pieces of a head: rotated, and all
-  int groups;            // lanes that share the heads of a piece
-  int lanes;             // units * groups: lanes of a token
-  int tokens_per_block;  // > 1: whole tokens
-  uint32_t first;        // token of the first workgroup
+  uint32_t units_per_block, tokens_per_block;  // one of both is 1, or all units and several tokens
+  uint32_t groups, per_tokens;                 // of heads; workgroups of the same tokens
+  uint32_t first;                              // workgroup of the call that is the launch's first
+  bool in_place;
 };
 
-// A lane owns one piece of a token's heads group, group + groups, ...: V pairs (half) or V / 2 (interleaved), or V elements
-// behind the rotated ones; V elements are 16 bytes.  The last piece of each kind may have fewer.
-template <typename T, bool HALF, bool BACK>
+// A lane owns one piece of HEADS heads of a token: V pairs (half) or V / 2 (interleaved), or V elements
+// behind the rotated ones; V elements are 16 bytes.
+// STREAM: what is written will not be in a cache when it is read.
+template <typename T, bool HALF, bool BACK, int HEADS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r) {
   constexpr int V = Store<T>::kVec, kPairs = HALF ? V : V / 2;
-  uint32_t token, lane;
-  if (r.tokens_per_block > 1) {
-    const uint32_t in_block = threadIdx.x / static_cast<uint32_t>(r.lanes);
-    if (in_block >= static_cast<uint32_t>(r.tokens_per_block)) return;
-    token = r.first + blockIdx.x * r.tokens_per_block + in_block;
-    lane = threadIdx.x - in_block * r.lanes;
-  } else {
-    token = r.first + blockIdx.x;
-    lane = blockIdx.y * kThreads + threadIdx.x;
-    if (lane >= static_cast<uint32_t>(r.lanes)) return;
+  // Workgroups of the same tokens follow one another; each takes heads side by side of tokens side by side, whichever of the
+  // two is the nearer in memory.
+  uint32_t block = blockIdx.x;
+  if constexpr (STREAM) {  // a run of them on each XCD: 65536 tokens of 40 heads of 128 bfloat16 262 / 242 us
+    const uint32_t each = gridDim.x / 8;
+    if (block < each * 8) block = block % 8 * each + block / 8;
   }
-  if (token >= r.tokens) return;
-  const uint32_t group = lane / static_cast<uint32_t>(r.units);
-  const int unit = static_cast<int>(lane - group * r.units);
+  block += r.first;
+  const uint32_t tokens = block / r.per_tokens, part = block - tokens * r.per_tokens;
+  const uint32_t unit_block = part / r.groups, group = part - unit_block * r.groups;
+  const uint32_t in_block = threadIdx.x / r.units_per_block, token = tokens * r.tokens_per_block + in_block;
+  const int unit = static_cast<int>(unit_block * kThreads + threadIdx.x - in_block * r.units_per_block);
+  if (in_block >= r.tokens_per_block || token >= r.tokens || unit >= r.units) return;
   const uint32_t b = token / r.seq, s = token - b * r.seq;
   const int64_t q_in = b * r.q.x_batch + s * r.q.x_token, q_to = b * r.q.y_batch + s * r.q.y_token;
   const int64_t k_in = b * r.k.x_batch + s * r.k.x_token, k_to = b * r.k.y_batch + s * r.k.y_token;
   const bool turns = unit < r.rot_units;
-  const int first = (turns ? unit : unit - r.rot_units) * (turns ? kPairs : V);  // pair, or element behind the rotated ones
-  const int count = min(turns ? kPairs : V, (turns ? r.R2 : r.D - 2 * r.R2) - first);
-  const bool whole = count == (turns ? kPairs : V);
+  // Of the pairs, or of the elements behind the rotated ones: the first of the piece, and how many it has.  Out of place a last
+  // piece that is not whole ends where it does but begins earlier, and makes what the one before makes too; in place that could
+  // have been written already.
+  const int full = turns ? kPairs : V, all = turns ? r.R2 : r.D - 2 * r.R2, in_order = (turns ? unit : unit - r.rot_units) * full;
+  const int first = r.in_place || all < full ? in_order : min(in_order, all - full), count = min(full, all - first);
+  const int elements = turns && !HALF ? 2 * count : count;  // of a piece
   const int at = turns ? (HALF ? first : 2 * first) : 2 * r.R2 + first, other = at + r.R2;  // elements; other: HALF only
+  auto in = [&](int h) {
+    return h < r.q_heads ? static_cast<const T*>(r.q.x) + q_in + h * r.q.x_head
+                         : static_cast<const T*>(r.k.x) + k_in + (h - r.q_heads) * r.k.x_head;
+  };
+  auto out = [&](int h) {
+    return h < r.q_heads ? static_cast<T*>(r.q.y) + q_to + h * r.q.y_head
+                         : static_cast<T*>(r.k.y) + k_to + (h - r.q_heads) * r.k.y_head;
+  };
+  auto load = [&](const T* p) {
+    if (elements == V) return ldg_stream_any(p);
+    float e[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) e[j] = j < elements ? Store<T>::load1(p + j) : 0.0f;
+    return Store<T>::pack(e);
+  };
+  auto store = [&](T* p, u32x4 w) {
+    if (elements == V) {
+      if constexpr (STREAM) stg_stream_any(p, w);
+      else *reinterpret_cast<u32x4_any*>(p) = w;
+      return;
+    }
+    float e[V];
+    Store<T>::unpack(w, e);
+#pragma unroll
+    for (int j = 0; j < V - 1; ++j)
+      if (j < elements) Store<T>::store1(p + j, e[j]);
+  };
 
+  // All heads are on their way while the angles are made.
+  u32x4 w1[HEADS], w2[HEADS];
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i) {
+    const T* x = in(min(static_cast<int>(group) * HEADS + i, r.heads - 1));
+    w1[i] = load(x + at);
+    if (HALF && turns) w2[i] = load(x + other);
+  }
   float c[kPairs], sn[kPairs];
   if (turns) {
     const int64_t p = b * r.pos_batch + s * r.pos_token;
@@ -98,68 +142,33 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r) {
       if (BACK) sn[i] = -sn[i];
     }
   }
-  auto in = [&](int h) {
-    return h < r.q_heads ? static_cast<const T*>(r.q.x) + q_in + h * r.q.x_head
-                         : static_cast<const T*>(r.k.x) + k_in + (h - r.q_heads) * r.k.x_head;
-  };
-  auto out = [&](int h) {
-    return h < r.q_heads ? static_cast<T*>(r.q.y) + q_to + h * r.q.y_head
-                         : static_cast<T*>(r.k.y) + k_to + (h - r.q_heads) * r.k.y_head;
-  };
-  if (whole) {
-    u32x4 w1[kHeadsPerLane], w2[kHeadsPerLane];
 #pragma unroll
-    for (int i = 0; i < kHeadsPerLane; ++i) {
-      const int h = min(static_cast<int>(group) + i * r.groups, r.heads - 1);
-      const T* x = in(h);
-      w1[i] = ldg_stream_any(x + at);
-      if (HALF && turns) w2[i] = ldg_stream_any(x + other);
-    }
-#pragma unroll
-    for (int i = 0; i < kHeadsPerLane; ++i) {
-      const int h = static_cast<int>(group) + i * r.groups;
-      if (h >= r.heads) break;
-      T* y = out(h);
-      if (!turns) {
-        stg_stream_any(y + at, w1[i]);
-        continue;
-      }
-      float x1[V], x2[V], y1[V], y2[V];
-      Store<T>::unpack(w1[i], x1);
-      if constexpr (HALF) {
-        Store<T>::unpack(w2[i], x2);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          y1[j] = fmaf(x1[j], c[j], -(x2[j] * sn[j]));
-          y2[j] = fmaf(x2[j], c[j], x1[j] * sn[j]);
-        }
-        stg_stream_any(y + other, Store<T>::pack(y2));
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; j += 2) {
-          y1[j] = fmaf(x1[j], c[j / 2], -(x1[j + 1] * sn[j / 2]));
-          y1[j + 1] = fmaf(x1[j + 1], c[j / 2], x1[j] * sn[j / 2]);
-        }
-      }
-      stg_stream_any(y + at, Store<T>::pack(y1));
-    }
-    return;
-  }
-  for (int h = static_cast<int>(group); h < r.heads; h += r.groups) {
-    const T* x = in(h);
+  for (int i = 0; i < HEADS; ++i) {
+    const int h = static_cast<int>(group) * HEADS + i;
+    if (h >= r.heads) break;
     T* y = out(h);
     if (!turns) {
-      for (int j = 0; j < count; ++j) y[at + j] = x[at + j];
+      store(y + at, w1[i]);
       continue;
     }
+    float x1[V], x2[V], y1[V], y2[V];
+    Store<T>::unpack(w1[i], x1);
+    if constexpr (HALF) {
+      Store<T>::unpack(w2[i], x2);
 #pragma unroll
-    for (int j = 0; j < kPairs; ++j) {
-      if (j >= count) break;
-      const int e1 = HALF ? at + j : at + 2 * j, e2 = HALF ? other + j : at + 2 * j + 1;
-      const float a = Store<T>::load1(x + e1), d = Store<T>::load1(x + e2);
-      Store<T>::store1(y + e1, fmaf(a, c[j], -(d * sn[j])));
-      Store<T>::store1(y + e2, fmaf(d, c[j], a * sn[j]));
+      for (int j = 0; j < V; ++j) {
+        y1[j] = fmaf(x1[j], c[j], -(x2[j] * sn[j]));
+        y2[j] = fmaf(x2[j], c[j], x1[j] * sn[j]);
+      }
+      store(y + other, Store<T>::pack(y2));
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; j += 2) {
+        y1[j] = fmaf(x1[j], c[j / 2], -(x1[j + 1] * sn[j / 2]));
+        y1[j + 1] = fmaf(x1[j + 1], c[j / 2], x1[j] * sn[j / 2]);
+      }
     }
+    store(y + at, Store<T>::pack(y1));
   }
 }
 
@@ -194,30 +203,38 @@ tempo_status launch_rotary(const tempo_rotary_heads* q, const tempo_rotary_heads
   r.rot_units = (r.R2 + pairs - 1) / pairs;
   // Elements behind the rotated ones are there already where the call is in place.
   const bool in_place = q->x == q->y && (!k || k->x == k->y);
+  r.in_place = q->x == q->y || (k && k->x == k->y);
   r.units = r.rot_units + (in_place ? 0 : (r.D - 2 * r.R2 + V - 1) / V);
-  r.groups = (r.heads + kHeadsPerLane - 1) / kHeadsPerLane;
-  r.lanes = r.units * r.groups;
-  r.tokens_per_block = r.lanes < kThreads ? kThreads / r.lanes : 1;
-  if (r.tokens_per_block == 1 && r.lanes < kThreads) r.tokens_per_block = 1;
-  const int64_t blocks = (int64_t{r.tokens} + r.tokens_per_block - 1) / r.tokens_per_block;
-  const int per_token = (r.lanes + kThreads - 1) / kThreads;
+  const int64_t pieces = int64_t{r.tokens} * r.units * r.heads;
+  const bool few = pieces < int64_t{compute_units()} * (half ? 4 : 16) * kWave * heads_per_lane(half);
+  const int per_lane = few ? 1 : heads_per_lane(half);
+  r.groups = (r.heads + per_lane - 1) / per_lane;
+  r.units_per_block = std::min(r.units, kThreads);
+  r.tokens_per_block = std::min(kThreads / r.units_per_block, r.tokens);
+  r.per_tokens = r.groups * ((r.units + kThreads - 1) / kThreads);
+  const int threads = (r.units_per_block * r.tokens_per_block + kWave - 1) / kWave * kWave;
+  const int64_t blocks = (int64_t{r.tokens} + r.tokens_per_block - 1) / r.tokens_per_block * r.per_tokens;
+  // What is written stays in the 256 MiB of cache where it is a part of that: 16 x 512 x 32 heads of 64 bfloat16 (34 MB) 17.3 / 15.4 us
+  // streamed / not, 4 x 2048 x 32 of 64 float32 (67 MB) 26.7 / 29.5, 65536 x 40 of 128 bfloat16 (671 MB) 254 / 268.
+  const bool stream = pieces * (half ? 32 : 16) > (int64_t{48} << 20);
   auto go = [&](auto kernel) {
-    const bool ok = split_launch(blocks, most_groups(blocks, kThreads * per_token), [&](uint32_t from, uint32_t count) {
-      r.first = from * r.tokens_per_block;
-      hipLaunchKernelGGL(kernel, dim3(count, per_token), dim3(kThreads), 0, st, r);
+    const bool ok = split_launch(blocks, most_groups(blocks, threads), [&](uint32_t first, uint32_t count) {
+      r.first = first;
+      hipLaunchKernelGGL(kernel, dim3(count), dim3(threads), 0, st, r);
       return launch_status() == TEMPO_OK;
     });
     return ok ? TEMPO_OK : TEMPO_ERR_LAUNCH;
   };
-  auto by_way = [&](auto f32, auto f32_back, auto bf16, auto bf16_back) {
-    if (dt == TEMPO_F32) return back ? go(f32_back) : go(f32);
-    return back ? go(bf16_back) : go(bf16);
+  auto by_way = [&](auto type, auto halves) {
+    using T = decltype(type);
+    constexpr bool HALF = decltype(halves)::value;
+    constexpr int HEADS = heads_per_lane(HALF);
+    if (few) return back ? go(rotary_kernel<T, HALF, true, 1, false>) : go(rotary_kernel<T, HALF, false, 1, false>);
+    if (stream) return back ? go(rotary_kernel<T, HALF, true, HEADS, true>) : go(rotary_kernel<T, HALF, false, HEADS, true>);
+    return back ? go(rotary_kernel<T, HALF, true, HEADS, false>) : go(rotary_kernel<T, HALF, false, HEADS, false>);
   };
-  if (half)
-    return by_way(rotary_kernel<float, true, false>, rotary_kernel<float, true, true>, rotary_kernel<bf16_t, true, false>,
-                  rotary_kernel<bf16_t, true, true>);
-  return by_way(rotary_kernel<float, false, false>, rotary_kernel<float, false, true>, rotary_kernel<bf16_t, false, false>,
-                rotary_kernel<bf16_t, false, true>);
+  if (half) return dt == TEMPO_F32 ? by_way(float{}, std::true_type{}) : by_way(bf16_t{}, std::true_type{});
+  return dt == TEMPO_F32 ? by_way(float{}, std::false_type{}) : by_way(bf16_t{}, std::false_type{});
 }
 
 }  // namespace tempo
