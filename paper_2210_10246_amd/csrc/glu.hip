@@ -733,10 +733,10 @@ __global__ __launch_bounds__(4 * kWave) void bias_kernel(const float* sums, T* d
 template <typename T>
 using Middle = Tile<128, 128, 64, 64, sizeof(T) == 4 ? 32 : 64>;
 template <typename T>
-using Small = Tile<64, 64, 32, 64, sizeof(T) == 4 ? 32 : 64>;
+using Small = Tile<64, 64, 32, 32, sizeof(T) == 4 ? 32 : 64>;
 using AlignedLarge = Tile<256, 256, 128, 128, 32, 4>;
 using AlignedMiddle = Tile<128, 128, 64, 64, 32, 4>;
-using AlignedSmall = Tile<64, 64, 32, 64, 32, 4>;
+using AlignedSmall = Tile<64, 64, 32, 32, 64, 4>;
 using AlignedFewest = Tile<16, 64, 16, 32, 64, 8>;
 using AlignedFew = Tile<64, 64, 64, 32, 64, 5>;
 using AlignedFewWide = Tile<64, 128, 64, 32, 64, 6>;
@@ -756,29 +756,29 @@ struct Shape {
 // What a tile takes, in us: `step` for 32 values of k and `tile` for its beginning and end, times the tiles of a compute unit,
 // and `wait` more for every 32 values of k of the longest one, alone or not.  Measured, us of [T, H] x 2F with tiles of 256 /
 // 128 / 64, bfloat16 in whole pieces: 16384 x 4096 x 11008 2390 / 3535 / 6490, 2048 x 1024 x 4096 41 / 49 / 71, 1024 x 1024 x 4096
-// 35 / 26 / 39, 128 x 1024 x 4096 - / 11.0 / 8.0, 1000 x 128 x 8192 23.1 / 18.3 / 23.1; by way of registers, 128 / 64: 1021 x 1001 x
-// 2729 36 / 48, 300 x 513 x 1031 15 / 10; float32 4096 x 2048 x 5504 936 / -, 1024 x 1024 x 4096 112 / 130, 512 x 512 x 1024 22 / 18.
+// 35 / 26 / 39, 128 x 1024 x 4096 - / 11.0 / 6.5, 1000 x 128 x 8192 23.1 / 18.3 / 23.1; by way of registers, 128 / 64: 1021 x 1001 x
+// 2729 36 / 48, 300 x 513 x 1031 15 / 8; float32 4096 x 2048 x 5504 936 / -, 1024 x 1024 x 4096 112 / 130, 512 x 512 x 1024 22 / 11.
 struct Pace {
   double step, tile, wait;
   bool one;  // workgroup of a compute unit: tiles count in whole rounds
 };
 Pace pace(Size size, tempo_dtype dt, bool aligned) {
-  if (dt == TEMPO_F32) return size == Size::kSmall ? Pace{0.45, 1.5, 0.45, false} : Pace{1.36, 6.0, 0.0, true};
-  if (!aligned) return size == Size::kSmall ? Pace{0.2, 1.5, 0.15, false} : Pace{0.5, 5.0, 0.1, false};
+  if (dt == TEMPO_F32) return size == Size::kSmall ? Pace{0.4, 1.5, 0.2, false} : Pace{1.36, 6.0, 0.0, true};
+  if (!aligned) return size == Size::kSmall ? Pace{0.17, 1.5, 0.12, false} : Pace{0.5, 5.0, 0.1, false};
   if (size == Size::kLarge) return {0.8, 12.0, 0.0, true};
-  return size == Size::kMiddle ? Pace{0.225, 5.0, 0.1, false} : Pace{0.13, 1.0, 0.07, false};
+  return size == Size::kMiddle ? Pace{0.225, 5.0, 0.1, false} : Pace{0.11, 1.0, 0.06, false};
 }
 // One plan for one or two products of a launch: the sizes of tiles, and in how many parts of k each is made where otherwise a
 // few long tiles would be waited for ([32, 8192] x [8192, 1024] beside [8192, 32] x [32, 1024]: 92 us, 47 with 6 parts of the first).
 void plan_for(const Shape* shapes, Plan* plans, int n, tempo_dtype dt, bool aligned) {
   const double cus = compute_units();
   aligned = aligned && dt == TEMPO_BF16;
-  const int bk = aligned || dt == TEMPO_F32 ? 32 : 64;
   double least = 0.0;
   for (int way = 0; way < 6; ++way) {
     const Size size = way / 2 == 0 ? Size::kMiddle : way / 2 == 1 ? Size::kSmall : Size::kLarge;
     if (size == Size::kLarge && !aligned) break;
     const Pace at = pace(size, dt, aligned);
+    const int bk = dt == TEMPO_F32 || (aligned && size != Size::kSmall) ? 32 : 64;
     Plan made[2];
     double tiles = 0.0, work = 0.0, longest = 0.0, join = 0.0;  // work, longest: in 32 values of k
     for (int i = 0; i < n; ++i) {
