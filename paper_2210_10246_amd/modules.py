@@ -7,14 +7,20 @@ Only what is stashed for backward differs from the stock layers:
   TempoAttentionCore softmax -> dropout -> (. @ V) keeping the softmax output P and a 1-bit
                      mask; the dropout output is a transient in forward and is recomputed by
                      the backward kernel for the gradient of V (Sec. 3.3).
-  TempoEncoderLayer  an encoder layer of the three: in float32 one native call each way on HIP
-                     kernels alone where nothing else can see its parts, else those parts
-Every arithmetic step of the three layers runs in the HIP kernels; the matrix products around
+  RotaryPositions    turns the heads of q and k by their positions; keeps nothing but those
+  TempoGatedFFN      a gated feed-forward block keeping its input and the two projections; their
+                     activated product, which the second Linear would keep, is made once more by
+                     the backward kernel
+  TempoEncoderLayer  an encoder layer of the first three: in float32 one native call each way on HIP
+                     kernels alone where nothing else can see its parts, else those parts; with
+                     rotary positions or a gated feed-forward block in it on request
+Every arithmetic step of these layers runs in the HIP kernels; the matrix products around
 them, where the layer is made of its parts, are ordinary library GEMMs (torch.matmul, nn.Linear).
 """
 from __future__ import annotations
 
 import math
+from typing import Optional, Tuple
 
 import torch
 import torch.nn.functional as F
@@ -187,6 +193,156 @@ class TempoAttentionCore(nn.Module):
                                       self.store_mask, None)
 
 
+def rotary_frequencies(dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                       trained: int = 0, turns: Tuple[float, float] = (1.0, 32.0)):
+    """The dim / 2 frequencies base^(-2 i / dim) of rotary positions in float64, radians per position, and what q and k are
+    scaled by.  scaling, for contexts `factor` times as long as the trained one:
+      "linear"  positions are factor times closer;
+      "base"    the base grows by factor^(dim / (dim - 2)): the slowest frequency is divided by factor, the fastest left;
+      "parts"   frequencies that make fewer than turns[0] turns in the `trained` positions are divided by factor, those that
+                make more than turns[1] are left, with a linear ramp between; q and k are scaled by 0.1 ln(factor) + 1."""
+    if dim < 2 or dim % 2:
+        raise ValueError(f"dim must be even and positive, got {dim}")
+    if not (base > 0 and factor >= 1.0):
+        raise ValueError(f"base must be positive and factor at least 1, got {base} and {factor}")
+    if scaling == "base":
+        if dim == 2:
+            raise ValueError("scaling the base needs more than one frequency")
+        base *= factor ** (dim / (dim - 2))
+    f = base ** (-torch.arange(0, dim, 2, dtype=torch.float64) / dim)
+    if scaling in (None, "base"):
+        return f, 1.0
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling != "parts":
+        raise ValueError(f'scaling must be None, "linear", "base" or "parts", got {scaling!r}')
+    if trained < 1 or not turns[0] < turns[1]:
+        raise ValueError(f"trained must be positive and turns ascending, got {trained} and {turns}")
+    left = ((trained * f / (2 * math.pi) - turns[0]) / (turns[1] - turns[0])).clamp(0.0, 1.0)
+    return f * (left + (1.0 - left) / factor), 0.1 * math.log(factor) + 1.0
+
+
+class _RotaryFn(torch.autograd.Function):
+    """q and k [B, S, heads, D], either of which may be None, to tensors that lie by head.  Linear: the gradient is the turn the
+    other way, which is differentiable in turn."""
+
+    @staticmethod
+    def forward(ctx, q, k, freqs, positions, start, layout, scale, back):
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(freqs, positions)
+        ctx.setting = start, layout, scale, back
+        sides = [None if t is None else t if t.stride(-1) == 1 else t.contiguous() for t in (q, k)]
+        out = [None if t is None else t.new_empty(t.shape[0], t.shape[2], t.shape[1], t.shape[3]).transpose(1, 2) for t in sides]
+        call = B.tempo_rotary_bwd if back else B.tempo_rotary_fwd
+        first, second = (0, 1) if q is not None else (1, 0)
+        call(sides[first], sides[second], freqs, positions, out[first], out[second], layout, scale, start)
+        return tuple(out)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        start, layout, scale, back = ctx.setting
+        freqs, positions = ctx.saved_tensors
+        dq, dk = (g if n else None for g, n in zip((dq, dk), ctx.needs_input_grad))
+        if dq is not None or dk is not None:
+            dq, dk = _RotaryFn.apply(dq, dk, freqs, positions, start, layout, scale, not back)
+        return dq, dk, None, None, None, None, None, None
+
+
+class RotaryPositions(nn.Module):
+    """Rotary positions of q and k [B, heads, S, D], of any strides, whose numbers of heads may differ; k may be None.  positions:
+    [S] or [B, S], int32 or int64 (0, 1, ... if None); start is added to them.  Turns the first `dim` elements of a head; layout:
+    "half" pairs element i with i + dim / 2, "interleaved" 2 i with 2 i + 1.  The other arguments are rotary_frequencies()'s."""
+
+    def __init__(self, dim: int, base: float = 10000.0, layout: str = "half", scaling: Optional[str] = None, factor: float = 1.0,
+                 trained: int = 0, turns: Tuple[float, float] = (1.0, 32.0)):
+        super().__init__()
+        if layout not in ("half", "interleaved"):
+            raise ValueError(f'layout must be "half" or "interleaved", got {layout!r}')
+        freqs, self.scale = rotary_frequencies(dim, base, scaling, factor, trained, turns)
+        self.layout = layout
+        self.register_buffer("freqs", freqs, persistent=False)
+
+    def _apply(self, fn, recurse=True):
+        # a cast of the model follows the device and leaves the frequencies in float64
+        freqs = self.freqs
+        super()._apply(fn, recurse)
+        if self.freqs.dtype != torch.float64:
+            self.freqs = freqs.to(device=self.freqs.device)
+        return self
+
+    def forward(self, q, k=None, positions=None, start: int = 0):
+        k_in = None if k is None else k.transpose(1, 2)
+        q, k = _RotaryFn.apply(q.transpose(1, 2), k_in, self.freqs, positions, start, self.layout, self.scale, False)
+        return q.transpose(1, 2), None if k is None else k.transpose(1, 2)
+
+
+def _aligned(t):
+    """t as the kernels take it: contiguous, from a multiple of 16 bytes on."""
+    if t is None:
+        return None
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
+class _GatedFFNFn(torch.autograd.Function):
+    """y = (act(g) u) wd^T + bd, [g | u] = x w^T + b: keeps x and [g | u]."""
+
+    @staticmethod
+    def forward(ctx, x, w, b, wd, bd, kind, keep):
+        x, w, b = _aligned(x), _aligned(w), _aligned(b)
+        ffn = w.shape[0] // 2
+        h = x.new_empty(*x.shape[:-1], ffn)      # transient: made once more by the backward
+        gu = x.new_empty(*x.shape[:-1], 2 * ffn) if keep else None
+        B.tempo_glu_fwd(x, w, b, gu, h, kind)
+        ctx.kind = kind
+        if keep:
+            ctx.save_for_backward(x, w, wd, gu)
+        return F.linear(h, wd, bd)
+
+    @staticmethod
+    def backward(ctx, dy):
+        if torch.is_grad_enabled():      # the kernels' gradients would be constants to a second derivative
+            raise RuntimeError("TempoGatedFFN has no second derivative: its gradients cannot be taken with create_graph=True")
+        x, w, wd, gu = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        rows = dy.reshape(-1, dy.shape[-1])
+        inner = need[0] or need[1] or need[2]
+        h = gu.new_empty(rows.shape[0], wd.shape[1]) if need[3] else None
+        dx = torch.empty_like(x) if need[0] else None
+        dw = torch.empty_like(w) if need[1] else None
+        db = w.new_empty(w.shape[0]) if need[2] else None
+        if inner or need[3]:
+            dh = torch.matmul(rows, wd) if inner else gu.new_zeros(rows.shape[0], wd.shape[1])
+            B.tempo_glu_bwd(_aligned(dh), gu, x, w, torch.empty_like(gu), h, dx, dw, db, ctx.kind)
+        dwd = torch.matmul(rows.t(), h) if need[3] else None
+        return dx, dw, db, dwd, rows.sum(0) if need[4] else None, None, None
+
+
+class TempoGatedFFN(nn.Module):
+    """A gated feed-forward block, y = (act(g) u) down^T with [g | u] = x gate_up^T: the rows of the gate come first.  kind: "silu",
+    "gelu_erf" or "gelu_tanh".  Its weights are its own parameters, drawn as nn.Linear draws them.  No second derivative."""
+
+    def __init__(self, hidden: int, ffn: int, kind: str = "silu", bias: bool = False, dtype=torch.float32):
+        super().__init__()
+        if kind not in ("silu", "gelu_erf", "gelu_tanh"):
+            raise ValueError(f'kind must be "silu", "gelu_erf" or "gelu_tanh", got {kind!r}')
+        self.kind = kind
+        for name, rows, columns in (("gate_up", 2 * ffn, hidden), ("down", hidden, ffn)):
+            w = nn.Parameter(torch.empty(rows, columns, dtype=dtype))
+            nn.init.kaiming_uniform_(w, a=math.sqrt(5))
+            b = nn.Parameter(torch.empty(rows, dtype=dtype).uniform_(-columns ** -0.5, columns ** -0.5)) if bias else None
+            self.register_parameter(name + "_weight", w)
+            self.register_parameter(name + "_bias", b)
+
+    def forward(self, x):
+        args = [x, self.gate_up_weight, self.gate_up_bias, self.down_weight, self.down_bias]
+        if torch.is_autocast_enabled("cuda"):    # as a Linear would take them
+            args = [None if t is None else t.to(torch.get_autocast_dtype("cuda")) for t in args]
+        keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in args)
+        with torch.autocast("cuda", enabled=False):
+            return _GatedFFNFn.apply(*args, self.kind, keep)
+
+
 class _EncoderLayerFn(torch.autograd.Function):
     """The whole layer, whose forward has been made (_native.tempo_encoder_fwd): keeps what the layer's parts keep for the
     inputs that require a gradient.  The backward is one native call too."""
@@ -309,33 +465,46 @@ def _attention(qkv, shape, heads, core):
 
 class TempoEncoderLayer(nn.Module):
     """A post-LN BERT encoder layer built from the three memory-reduced layers (Fig. 1 of the
-    paper); hidden-state dropouts are left out (they are not part of the method)."""
+    paper); hidden-state dropouts are left out (they are not part of the method).  rotary: a RotaryPositions that q and k go
+    through; gated: the kind of a TempoGatedFFN in the place of the two feed-forward layers and GELU."""
 
     def __init__(self, hidden: int, heads: int, ffn: int, p_attn: float = 0.1, eps: float = 1e-12,
-                 dtype=torch.float32):
+                 dtype=torch.float32, rotary: Optional[RotaryPositions] = None, gated: Optional[str] = None):
         super().__init__()
         self.heads = heads
         self.qkv = nn.Linear(hidden, 3 * hidden, dtype=dtype)
         self.proj = nn.Linear(hidden, hidden, dtype=dtype)
-        self.fc1 = nn.Linear(hidden, ffn, dtype=dtype)
-        self.fc2 = nn.Linear(ffn, hidden, dtype=dtype)
+        if gated is None:
+            self.fc1 = nn.Linear(hidden, ffn, dtype=dtype)
+            self.fc2 = nn.Linear(ffn, hidden, dtype=dtype)
+        else:
+            self.ffn = TempoGatedFFN(hidden, ffn, gated, True, dtype)
         self.ln1 = InplaceLayerNorm(hidden, eps)
         self.ln2 = InplaceLayerNorm(hidden, eps)
-        self.act = InplaceGELU()
+        if gated is None:
+            self.act = InplaceGELU()
         self.core = TempoAttentionCore(p_attn)
+        if rotary is not None:
+            self.rotary = rotary
 
-    def forward(self, x, key_len=None):
-        out = self._as_one(x, key_len)
+    def forward(self, x, key_len=None, positions=None):
+        rotary = self._modules.get("rotary")
+        if positions is not None and rotary is None:
+            raise ValueError("positions are those of rotary, which this layer has none of")
+        out = self._as_one(x, key_len) if rotary is None else None
         if out is not None:
             return out
 
         def core(q, k, v):
+            if rotary is not None:
+                q, k = rotary(q, k, positions)
             scores = torch.matmul(q, k.transpose(-1, -2)) * (1.0 / math.sqrt(q.shape[-1]))
             return self.core(scores, v, key_len)
         Bn, S, H = x.shape
         ctxt = _attention(self.qkv(x), (Bn, S, H), self.heads, core)
         x = self.ln1(x + self.proj(ctxt))
-        return self.ln2(x + self.fc2(self.act(self.fc1(x))))
+        ffn = self._modules.get("ffn")
+        return self.ln2(x + (self.fc2(self.act(self.fc1(x))) if ffn is None else ffn(x)))
 
     def _as_one(self, x, key_len):
         """The layer as one native call each way, or None where something may see or change its parts: hooks, other
