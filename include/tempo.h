@@ -228,12 +228,13 @@ TEMPO_API tempo_status tempo_attn_softmax_dropout_bwd_bytemask(const void* dout,
  *   Elements R .. D - 1 of a head are copied.
  *   q, k: element (b, s, head, d) at x[b x_batch + s x_token + head x_head + d], b < B, s < S, d < D (dt), in and out, so that
  *   heads can be taken out of a projection and put into any order; k may be NULL.  x and y need only the alignment of an element.
- *   y may be x, with the same strides; elements of y must not overlap otherwise.
+ *   y may be x, with the same strides; otherwise no element of a y is that of another, of an x, freqs or positions.
  *   freqs [R/2] in, float64, radians per position; angles are taken in 64 bits, so that far positions keep their place.
  *   positions in: int32 or int64 (bits 32 or 64), element (b, s) at b batch_stride + s token_stride (strides >= 0; a batch_stride
- *   of 0 shares them); may be NULL.  A position may be any number, negative ones too.
+ *   of 0 shares them); may be NULL.  A position may be negative; start + positions[b,s] lies within 2^53.
  *   INVALID_ARG also: R odd, R < 2, R > D, B S above 2^31 - 1, more than 2^24 elements of q and k together in a token, a negative
- *   stride, a stride of y that is 0 where there are two elements along it, bits other than 32 and 64.
+ *   stride, a stride of y that is 0 where there are two elements along it, y == x with other strides, bits other than 32 and 64, a
+ *   start beyond 2^53.
  */
 typedef enum { TEMPO_ROTARY_HALF = 0, TEMPO_ROTARY_INTERLEAVED = 1 } tempo_rotary_layout;
 typedef struct {
@@ -261,8 +262,9 @@ TEMPO_API tempo_status tempo_rotary_bwd(const tempo_rotary_heads* dq, const temp
  *   x [T,H], w [2F,H] (rows of the gate, then of u) in (dt); bias [2F] in (dt), may be NULL;
  *   gu [T,2F] out (dt): the projections, all that the backward needs of the forward; may be NULL;
  *   h [T,F] out (dt).
- *   float32 products are made of bfloat16 ones, of operands taken apart exactly; what is left out is below 2^-21 of |x| |w|.
- *   An element that is not finite makes NaN of every sum that it takes part in.
+ *   float32 products are made of bfloat16 ones, of operands that are taken apart into three; what is left out is below 2^-21 of
+ *   |x| |w|, where no part of an element falls below 2^-126.  A float32 element that is not finite makes NaN of every sum that it
+ *   takes part in, a bfloat16 one what its products make.
  *   workspace: device memory of at least tempo_glu_fwd_workspace_bytes(T, H, F, dt) bytes, 16-byte aligned (NULL if that is 0).
  *   UNSUPPORTED also: sizes beyond 2^30 (2F too), or beyond 2^22 tiles of 64 x 64 elements in gu, x or w.
  */

@@ -430,6 +430,8 @@ def _rotary(where, q, k, freqs, positions, q_out, k_out, layout, scale, start, s
     B, S, _, D = q.shape
     if not 1 <= freqs.numel() <= D // 2:
         raise ValueError(f"freqs must have 1 to {D // 2} elements, got {freqs.numel()}")
+    if abs(start) > 2 ** 53:
+        raise ValueError(f"start must lie within 2^53, got {start}")
     at = _RotaryPositions(None, 64, (_i64 * 2)(0, 0), start)
     if positions is not None:
         if positions.dtype not in (torch.int32, torch.int64):

@@ -345,7 +345,7 @@ static bool rotary_side_ok(const tempo_rotary_heads* h, int64_t B, int64_t S, in
   int64_t last_in = D, last_out = D;
   for (int i = 0; i < 3; ++i) {
     if (in[i] < 0 || out[i] < 0 || !count_ok(sizes[i], in[i]) || !count_ok(sizes[i], out[i])) return false;
-    if (sizes[i] > 1 && out[i] == 0) return false;
+    if (sizes[i] > 1 && (out[i] == 0 || (h->x == h->y && in[i] != out[i]))) return false;
     last_in += sizes[i] * in[i];
     last_out += sizes[i] * out[i];
   }
@@ -362,6 +362,7 @@ static tempo_status rotary(const tempo_rotary_heads* q, const tempo_rotary_heads
       (q->heads + (k ? k->heads : 0)) * D > most || !count_ok(B, S) || B * S > INT32_MAX)
     return TEMPO_ERR_INVALID_ARG;
   if (!rotary_side_ok(q, B, S, D) || (k && !rotary_side_ok(k, B, S, D))) return TEMPO_ERR_INVALID_ARG;
+  if (at->start < -(int64_t{1} << 53) || at->start > int64_t{1} << 53) return TEMPO_ERR_INVALID_ARG;
   if (at->positions && ((at->bits != 32 && at->bits != 64) || at->batch_stride < 0 || at->token_stride < 0 ||
                         !count_ok(B, at->batch_stride) || !count_ok(S, at->token_stride)))
     return TEMPO_ERR_INVALID_ARG;

@@ -3,8 +3,13 @@
 //   dx = [dg | du] W,   dW = [dg | du]^T x,   db = column sums of [dg | du].
 //
 // All products are on the matrix cores with bfloat16 operands and float32 sums.  A float32 operand is taken apart into three
-// bfloat16 ones, x = x0 + x1 + x2 exactly, and of the nine products those six are made that count in float32 (the other three
-// are below 2^-21 of |a| |b|).
+// bfloat16 ones, x = x0 + x1 + x2 exactly (each takes the first 8 bits of what is left), and of the nine products those six are
+// made that count in float32; the other three are below 2^-21 of |a| |b|.  Six products at the rate of bfloat16 are a quarter
+// of its rate, half as fast again as the float32 matrix instructions: 1350 TFLOP/s and 154 for the library's, 8192^3.
+//
+// The products' bound is the power of the matrix cores (the clock falls from 2.4 to 1.7 GHz) and, beside it, what comes from the
+// L2s; LDS is read without bank conflicts and takes a quarter of the time.  [16384, 4096] x 2 x 11008 bfloat16: forward 2.44 ms, 1210
+// TFLOP/s with 1.1 GB written (2.30 ms without [g | u]; the library's plain product of that size 2.12), dx 2.17, dw 2.21 ms.
 #include <algorithm>
 #include <cmath>
 #include <utility>
@@ -316,7 +321,9 @@ __device__ __forceinline__ void spread() {
 }
 
 // Blocks of 16 rows, of the N that a wave has, which fit into `bytes` of LDS in rows of `row` bytes and 16 more.
-constexpr int blocks_at_once(int N, int row, int bytes) { return 16 * N * (row + 16) <= bytes ? N : blocks_at_once(N / 2, row, bytes); }
+constexpr int blocks_at_once(int N, int row, int bytes) {
+  return N <= 1 || 16 * N * (row + 16) <= bytes ? N : blocks_at_once(N / 2, row, bytes);
+}
 // 16 BLOCKS rows by J x 16 columns of a wave's sums to memory, through LDS of its own, so that lanes side by side store pieces
 // side by side.  value(i, j): elements (m = 16 i + lane % 16, n = 16 j + 4 (lane / 16) ..) of them; rows, cols: how many exist.
 template <typename U, int BLOCKS, int J, typename F>
@@ -365,6 +372,7 @@ __device__ __forceinline__ void finish(const Product& g, const P& at, const f32x
     auto sums = [&](auto* to) {
       using U = std::remove_pointer_t<decltype(to)>;
       constexpr int kOnce = blocks_at_once(FM, FN * 16 * sizeof(U), ROOM);
+      static_assert(16 * kOnce * (FN * 16 * sizeof(U) + 16) <= ROOM, "a block's rows");
 #pragma unroll
       for (int i0 = 0; i0 < FM; i0 += kOnce)
         store_rows<U, kOnce, FN>(room, to + static_cast<int64_t>(m + 16 * i0) * g.N + n, g.N, g.M - m - 16 * i0, g.N - n,
@@ -386,6 +394,7 @@ __device__ __forceinline__ void finish(const Product& g, const P& at, const f32x
     auto rows = [&](auto* to, int64_t ld, auto&& value) {
       using U = std::remove_pointer_t<decltype(to)>;
       constexpr int kOnce = blocks_at_once(FM, J * 16 * sizeof(U), ROOM);
+      static_assert(16 * kOnce * (J * 16 * sizeof(U) + 16) <= ROOM, "a block's rows");
 #pragma unroll
       for (int i0 = 0; i0 < FM; i0 += kOnce)
         store_rows<U, kOnce, J>(room, to + (m + 16 * i0) * ld + f, ld, g.M - m - 16 * i0, g.N - f,

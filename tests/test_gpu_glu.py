@@ -270,3 +270,18 @@ def test_replays_streams_and_workspaces(dtype):
     if need > 16:
         with pytest.raises(B.TempoError, match="workspace"):
             step(*other, ws=mine[:16])
+
+
+def test_more_than_2_32_elements():
+    """[g | u] and h beyond 2^32 elements; the last rows, and every row's sum over the tiles, against float64."""
+    T, H, F = 70001, 32, 32768
+    x, w, _ = inputs(T, H, F, "bf16", False)
+    gu, h = torch.empty(T, 2 * F, device="cuda", dtype=torch.bfloat16), torch.empty(T, F, device="cuda", dtype=torch.bfloat16)
+    B.tempo_glu_fwd(x, w, None, gu, h)
+    rows = torch.tensor([0, 32767, 32768, 65535, 65536, T - 2, T - 1], device="cuda")
+    check_forward(x[rows], w, None, gu[rows], h[rows], "silu", "bf16")
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    B.tempo_glu_bwd(h, gu, x, w, gu, None, dx, dw, None)      # dgu in gu's place, h as its gradient
+    near(dx[rows], *sums(gu[rows].double(), w.double().t(), "bf16"))
+    columns = torch.tensor([0, F - 1, F, 2 * F - 1], device="cuda")
+    near(dw[columns], *sums(gu[:, columns].double().t(), x.double().t(), "bf16"))

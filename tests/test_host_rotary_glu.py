@@ -37,6 +37,8 @@ def test_rotary_arguments_are_checked_before_any_launch(way):
         dict(q=heads(x_strides=(1 << 50, 16, 8)), at=ok), dict(q=heads(), k=heads(y_strides=(64, 16, 0)), at=ok),
         dict(q=heads(), at=positions(32, bits=16)), dict(q=heads(), at=positions(32, strides=(-1, 1))),
         dict(q=heads(), at=positions(32, strides=(0, -1))), dict(q=heads(), at=positions(32, strides=(1 << 50, 1))),
+        dict(q=heads(y_strides=(64, 8, 16)), at=ok), dict(q=heads(), at=positions(start=2 ** 53 + 1)),
+        dict(q=heads(), at=positions(start=-2 ** 53 - 1)),
         dict(q=heads(x=None), at=ok), dict(q=heads(y=None), at=ok), dict(q=heads(), k=heads(x=None), at=ok), dict(q=heads(), at=ok, freqs=None),
     ]
     for args in refused:
@@ -104,6 +106,9 @@ def test_binding_refuses_what_the_rotary_call_would_misread():
     refused("freqs must be torch.float64", freqs=f.float())
     refused("layout", layout="quarter")
     refused("CUDA")
+    for start in (2 ** 53 + 1, -2 ** 70):
+        with pytest.raises(ValueError, match="start"):
+            B.tempo_rotary_fwd(q, None, f, None, q, None, "half", 1.0, start)
     refused("q must be", q=q[0])
     refused("q must be", q=q.transpose(2, 3))
     refused("q_out must be", q_out=q[..., ::2])
