@@ -648,21 +648,46 @@ __global__ __launch_bounds__(256) void join_kernel(Product g) {
   }
 }
 
+// Rows of `columns` bfloat16 elements, those of `first`, then those of `second`, copied to rows of `pieces` 16-byte pieces, zeros
+// behind them.
+__global__ __launch_bounds__(256) void pad_kernel(const bf16_t* first, uint32_t first_rows, const bf16_t* second, uint32_t rows,
+                                                  int columns, uint32_t pieces, u32x4* to) {
+  const uint32_t at = blockIdx.x * 256 + threadIdx.x, row = at / pieces, column = (at - row * pieces) * 8;
+  if (row >= rows) return;
+  const bf16_t* from = (row < first_rows ? first + static_cast<int64_t>(row) * columns
+                                         : second + static_cast<int64_t>(row - first_rows) * columns) + column;
+  const int left = columns - static_cast<int>(column);
+  u32x4 w;
+  if (left >= 8) {
+    w = *reinterpret_cast<const u32x4_any*>(from);
+  } else {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? Store<bf16_t>::load1(from + e) : 0.0f;
+    w = Store<bf16_t>::pack(v);
+  }
+  to[at] = w;
+}
+
 // ---- the backward's elementwise part ----------------------------------------------------------------------------------
 struct Gates {
   const void *dh, *gu;
   void *dgu, *h;     // h may be null
-  float* sums;       // null, or [chunks, 2F]: column sums of a chunk's rows
+  float* sums;       // null, or [groups, 2F]: column sums of a workgroup's rows
   int64_t rows;
-  int F, kind, chunk;  // chunk: rows of a workgroup
+  int F, kind, chunk;  // chunk: rows of a wave
+  void* pad;           // null, or dgu once more, in rows of pad_ld elements
+  int64_t pad_ld;
 };
-// A wave takes 64 pieces of 16 bytes of the columns, of `chunk` rows one after the other.
+// A wave takes 64 pieces of 16 bytes of the columns, of `chunk` rows one after the other, the four of a workgroup those of
+// neighbouring rows, whose sums they add up.
+constexpr int kGateWaves = 4;
 template <typename T, int KIND>
-__global__ __launch_bounds__(kWave) void gates_kernel(Gates g, int64_t chunk0) {
+__global__ __launch_bounds__(kGateWaves* kWave) void gates_kernel(Gates g, int64_t group0) {
   constexpr int V = Store<T>::kVec;
-  const int f = (blockIdx.x * kWave + threadIdx.x) * V, left = g.F - f;
-  if (left <= 0) return;
-  const int64_t c = chunk0 + blockIdx.y, r0 = c * g.chunk, r1 = r0 + g.chunk < g.rows ? r0 + g.chunk : g.rows;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, f = (blockIdx.x * kWave + lane) * V, left = g.F - f;
+  const int64_t group = group0 + blockIdx.y, r0 = (group * kGateWaves + wave) * g.chunk;
+  const int64_t r1 = left <= 0 ? r0 : r0 + g.chunk < g.rows ? r0 + g.chunk : g.rows;
   float sg[V], su[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) sg[i] = su[i] = 0.0f;
@@ -694,10 +719,16 @@ __global__ __launch_bounds__(kWave) void gates_kernel(Gates g, int64_t chunk0) {
       sg[i] += dg[i];
       su[i] += du[i];
     }
+    T* pad = g.pad ? static_cast<T*>(g.pad) + r * g.pad_ld + f : nullptr;
     if (left >= V) {
-      *reinterpret_cast<u32x4_any*>(dgu) = Store<T>::pack(dg);
-      *reinterpret_cast<u32x4_any*>(dgu + g.F) = Store<T>::pack(du);
+      const u32x4 wg = Store<T>::pack(dg), wu = Store<T>::pack(du);
+      *reinterpret_cast<u32x4_any*>(dgu) = wg;
+      *reinterpret_cast<u32x4_any*>(dgu + g.F) = wu;
       if (h) stg_stream_any(h, Store<T>::pack(y));
+      if (pad) {
+        *reinterpret_cast<u32x4_any*>(pad) = wg;
+        *reinterpret_cast<u32x4_any*>(pad + g.F) = wu;
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -705,25 +736,36 @@ __global__ __launch_bounds__(kWave) void gates_kernel(Gates g, int64_t chunk0) {
         Store<T>::store1(dgu + i, dg[i]);
         Store<T>::store1(dgu + g.F + i, du[i]);
         if (h) Store<T>::store1(h + i, y[i]);
+        if (pad) {
+          Store<T>::store1(pad + i, dg[i]);
+          Store<T>::store1(pad + g.F + i, du[i]);
+        }
       }
     }
   }
-  if (g.sums) {
-    float* to = g.sums + c * 2 * g.F + f;
+  if (g.sums) {  // uniform
+    __shared__ float of_waves[kGateWaves][2 * V][kWave];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      if (i >= left) break;
-      to[i] = sg[i];
-      to[g.F + i] = su[i];
+      of_waves[wave][i][lane] = sg[i];
+      of_waves[wave][V + i][lane] = su[i];
+    }
+    lds_barrier();
+    float* const to = g.sums + group * 2 * g.F + f;
+#pragma unroll
+    for (int n = 0; n < 2 * V / kGateWaves; ++n) {
+      const int i = wave * (2 * V / kGateWaves) + n, column = i % V;
+      const float v = (of_waves[0][i][lane] + of_waves[1][i][lane]) + (of_waves[2][i][lane] + of_waves[3][i][lane]);
+      if (column < left) to[i / V * g.F + column] = v;
     }
   }
 }
-// The chunks' sums of 64 columns, a quarter of the chunks a wave, then the quarters.
+// The groups' sums of 64 columns, a quarter of the groups a wave, then the quarters.
 template <typename T>
-__global__ __launch_bounds__(4 * kWave) void bias_kernel(const float* sums, T* dbias, int64_t chunks, int n) {
+__global__ __launch_bounds__(4 * kWave) void bias_kernel(const float* sums, T* dbias, int64_t groups, int n) {
   __shared__ float quarters[4 * kWave];
   const int e = blockIdx.x * kWave + threadIdx.x % kWave, quarter = threadIdx.x / kWave;
-  const int64_t each = (chunks + 3) / 4, first = quarter * each, last = first + each < chunks ? first + each : chunks;
+  const int64_t each = (groups + 3) / 4, first = quarter * each, last = first + each < groups ? first + each : groups;
   float v = 0.0f;
   if (e < n) {
 #pragma unroll 8
@@ -773,13 +815,13 @@ struct Pace {
 };
 Pace pace(Size size, tempo_dtype dt, bool aligned) {
   if (dt == TEMPO_F32) return size == Size::kSmall ? Pace{0.4, 1.5, 0.2, false} : Pace{1.36, 6.0, 0.0, true};
-  if (!aligned) return size == Size::kSmall ? Pace{0.17, 1.5, 0.12, false} : Pace{0.5, 5.0, 0.1, false};
+  if (!aligned) return size == Size::kSmall ? Pace{0.17, 1.5, 0.12, false} : Pace{0.4, 5.0, 0.1, false};
   if (size == Size::kLarge) return {0.8, 12.0, 0.0, true};
   return size == Size::kMiddle ? Pace{0.225, 5.0, 0.1, false} : Pace{0.11, 1.0, 0.06, false};
 }
 // One plan for one or two products of a launch: the sizes of tiles, and in how many parts of k each is made where otherwise a
 // few long tiles would be waited for ([32, 8192] x [8192, 1024] beside [8192, 32] x [32, 1024]: 92 us, 47 with 6 parts of the first).
-void plan_for(const Shape* shapes, Plan* plans, int n, tempo_dtype dt, bool aligned) {
+double plan_for(const Shape* shapes, Plan* plans, int n, tempo_dtype dt, bool aligned) {
   const double cus = compute_units();
   aligned = aligned && dt == TEMPO_BF16;
   double least = 0.0;
@@ -798,7 +840,7 @@ void plan_for(const Shape* shapes, Plan* plans, int n, tempo_dtype dt, bool alig
     tiles = 0.0;
     for (int i = 0; i < n; ++i) {
       const int64_t steps = std::max<int64_t>(1, (shapes[i].K + bk - 1) / bk);
-      int64_t splits = way % 2 == 0 ? 1 : std::min<int64_t>(16, std::max<int64_t>(1, static_cast<int64_t>(shapes[i].K / 32.0 / share)));
+      int64_t splits = way % 2 == 0 ? 1 : std::min<int64_t>(16, std::max<int64_t>(1, static_cast<int64_t>(shapes[i].K / 32.0 / share + 0.5)));
       Plan& p = made[i];
       p.aligned = aligned;
       p.size = size;
@@ -817,7 +859,19 @@ void plan_for(const Shape* shapes, Plan* plans, int n, tempo_dtype dt, bool alig
       for (int i = 0; i < n; ++i) plans[i] = made[i];
     }
   }
+  return least;
 }
+// bfloat16 rows that do not all begin at multiples of 16 bytes: whether a copy with rows that do, of `bytes`, is worth what the
+// products then save; plans is what is the cheaper.  us with copies / without: [8192, 1023] x 2 x 4095 forward 206 / 297, backward 383 /
+// 494, [1021, 1001] x 2 x 2729 40 / 36 and 82 / 76, [513, 4095] x 2 x 11007 forward 237 / 178.
+bool plan_padded(const Shape* shapes, Plan* plans, int n, double bytes) {
+  Plan other[2];
+  const double as_is = plan_for(shapes, plans, n, TEMPO_BF16, false), padded = plan_for(shapes, other, n, TEMPO_BF16, true);
+  if (1.25 * (padded + 10.0 + bytes / 2.5e6) >= as_is) return false;
+  for (int i = 0; i < n; ++i) plans[i] = other[i];
+  return true;
+}
+int64_t whole_pieces(int64_t elements) { return (elements + 7) / 8 * 8; }
 size_t partial_bytes(const Plan& p, const Shape& s) {
   return p.splits > 1 ? static_cast<size_t>(p.splits) * s.M * s.N * sizeof(float) : 0;
 }
@@ -826,31 +880,46 @@ size_t partial_bytes(const Plan& p, const Shape& s) {
 struct ForwardPlan {
   Shape shape;
   Plan plan;
-  size_t bytes;
+  bool padded = false;  // x and w copied to rows of H_pad elements
+  int64_t H_pad;
+  size_t x_at, bytes;   // of the copies in the workspace; all of it
   ForwardPlan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) : shape{T, 2 * F, H} {
-    plan_for(&shape, &plan, 1, dt, H % 8 == 0);
+    H_pad = whole_pieces(H);
+    const size_t copies = static_cast<size_t>(T + 2 * F) * H_pad * 2;
+    if (dt == TEMPO_BF16 && H_pad != H) padded = plan_padded(&shape, &plan, 1, 2.0 * copies);
+    else plan_for(&shape, &plan, 1, dt, true);
     // Up to 64 rows read W once, nothing else counts: whole lines of W's rows at a time, as much on its way as LDS holds, few rows
     // of x beside them.  us, 64 x 64 tiles of above / this: 48 x 4096 x 11008 57 / 41 (64 columns at a time 44), 1 x 4096 x 11008 52 /
     // 38, 48 x 1024 x 4096 13.2 / 8.4 (128 columns 10.5), 1 x 1024 x 4096 13.0 / 6.1.  Where W has few columns of many values of k,
     // parts of k are worth more.
-    if (plan.aligned && T <= AlignedFew::BM && (F >= 2048 || H <= 1024)) {
+    if (plan.aligned && !padded && T <= AlignedFew::BM && (F >= 2048 || H <= 1024)) {
       plan.size = T <= AlignedFewest::BM ? Size::kFewest : 2 * F >= 80 * int64_t{compute_units()} ? Size::kFewWide : Size::kFew;
       const int columns = plan.size == Size::kFewWide ? AlignedFewWide::BN : AlignedFew::BN;
       plan.splits = 1;
       plan.steps = static_cast<int>((H + AlignedFew::BK - 1) / AlignedFew::BK);
       plan.tiles = (2 * F + columns - 1) / columns;
     }
-    bytes = partial_bytes(plan, shape);
+    x_at = (partial_bytes(plan, shape) + 15) / 16 * 16;
+    bytes = x_at + (padded ? copies : 0);
   }
 };
 struct BackwardPlan {
   Shape shapes[2];  // dx, dw
   Plan plans[2];
-  size_t dx_bytes, bytes;
+  bool padded = false;  // x and w copied to rows of H_pad elements if those are more than H, dgu to rows of F2_pad if more than 2F
+  int64_t H_pad, F2_pad;
+  size_t dx_bytes, dgu_at, x_at, bytes;
   BackwardPlan(int64_t T, int64_t H, int64_t F, tempo_dtype dt) : shapes{{T, H, 2 * F}, {2 * F, H, T}} {
-    plan_for(shapes, plans, 2, dt, H % 8 == 0 && F % 4 == 0);
+    H_pad = whole_pieces(H);
+    F2_pad = whole_pieces(2 * F);
+    const size_t dgu_bytes = F2_pad != 2 * F ? static_cast<size_t>(T) * F2_pad * 2 : 0;
+    const size_t copies = H_pad != H ? static_cast<size_t>(T + 2 * F) * H_pad * 2 : 0;
+    if (dt == TEMPO_BF16 && dgu_bytes + copies > 0) padded = plan_padded(shapes, plans, 2, dgu_bytes + 2.0 * copies);
+    else plan_for(shapes, plans, 2, dt, true);
     dx_bytes = (partial_bytes(plans[0], shapes[0]) + 15) / 16 * 16;
-    bytes = dx_bytes + partial_bytes(plans[1], shapes[1]);
+    dgu_at = (dx_bytes + partial_bytes(plans[1], shapes[1]) + 15) / 16 * 16;
+    x_at = dgu_at + (padded ? dgu_bytes : 0);
+    bytes = x_at + (padded ? copies : 0);
   }
 };
 
@@ -903,18 +972,28 @@ tempo_status launch_both(Product dx, Product dw, const Plan* p, hipStream_t st) 
 }
 
 // Rows that a wave of the backward's elementwise part takes: 32, fewer where they would make less than 16 waves per compute unit,
-// and not fewer than 4, so that the column sums of a wave's rows are few beside the rows.
+// and not fewer than 4, so that the column sums of a workgroup's rows are few beside the rows.
 int chunk_of(int64_t T, int64_t F, tempo_dtype dt) {
   const int64_t across = (F + (dt == TEMPO_F32 ? 4 : 8) * kWave - 1) / ((dt == TEMPO_F32 ? 4 : 8) * kWave);
   return static_cast<int>(std::min<int64_t>(32, std::max<int64_t>(4, T * across / (16 * int64_t{compute_units()}))));
 }
+int64_t groups_of(int64_t T, int chunk) { return (T + kGateWaves * chunk - 1) / (kGateWaves * chunk); }
 size_t sums_bytes(int64_t T, int64_t F, tempo_dtype dt) {
-  const int chunk = chunk_of(T, F, dt);
-  return static_cast<size_t>((T + chunk - 1) / chunk) * 2 * F * sizeof(float);
+  return static_cast<size_t>(groups_of(T, chunk_of(T, F, dt))) * 2 * F * sizeof(float);
 }
 
+// The rows of first, then those of second; either may have none.
+tempo_status pad(const void* first, int64_t first_rows, const void* second, int64_t second_rows, int64_t columns, int64_t ld, void* to,
+                 hipStream_t st) {
+  const int64_t rows = first_rows + second_rows, pieces = ld / 8;
+  if (rows == 0) return TEMPO_OK;
+  hipLaunchKernelGGL(pad_kernel, dim3(static_cast<unsigned>((rows * pieces + 255) / 256)), dim3(256), 0, st,
+                     static_cast<const bf16_t*>(first), static_cast<uint32_t>(first_rows), static_cast<const bf16_t*>(second),
+                     static_cast<uint32_t>(rows), static_cast<int>(columns), static_cast<uint32_t>(pieces), static_cast<u32x4*>(to));
+  return launch_status();
+}
 template <typename T>
-tempo_status forward(const GluCall& c, const Plan& p, hipStream_t st) {
+tempo_status forward(const GluCall& c, const ForwardPlan& p, hipStream_t st) {
   Product g{};
   g.a = c.x;
   g.b = c.w;
@@ -927,11 +1006,19 @@ tempo_status forward(const GluCall& c, const Plan& p, hipStream_t st) {
   g.gu = c.gu;
   g.h = c.h;
   g.kind = c.kind;
+  if (p.padded) {
+    char* const to = static_cast<char*>(c.workspace) + p.x_at;
+    const tempo_status status = pad(c.x, c.T, c.w, 2 * c.F, c.H, p.H_pad, to, st);
+    if (status != TEMPO_OK) return status;
+    g.a = to;
+    g.b = to + c.T * p.H_pad * 2;
+    g.lda = g.ldb = p.H_pad;
+  }
   constexpr float log2e = 1.4426950408889634f, k = 0.7978845608028654f;
-  if (c.kind == TEMPO_GLU_GELU_ERF) return launch_product<T, false, false, kErf>(g, p, st);
+  if (c.kind == TEMPO_GLU_GELU_ERF) return launch_product<T, false, false, kErf>(g, p.plan, st);
   g.c0 = c.kind == TEMPO_GLU_SILU ? -log2e : -2.0f * log2e * k;
   g.c1 = c.kind == TEMPO_GLU_SILU ? 0.0f : -2.0f * log2e * k * 0.044715f;
-  return launch_product<T, false, false, kSigmoid>(g, p, st);
+  return launch_product<T, false, false, kSigmoid>(g, p.plan, st);
 }
 
 template <typename T>
@@ -939,15 +1026,23 @@ tempo_status backward(const GluCall& c, const BackwardPlan& p, hipStream_t st) {
   constexpr int V = Store<T>::kVec;
   Gates e{c.dh, c.gu, c.dgu, c.h, c.dbias ? static_cast<float*>(c.workspace) : nullptr, c.T, static_cast<int>(c.F), c.kind,
           chunk_of(c.T, c.F, sizeof(T) == 4 ? TEMPO_F32 : TEMPO_BF16)};
-  const int64_t chunks = (c.T + e.chunk - 1) / e.chunk;
+  const int64_t row_groups = groups_of(c.T, e.chunk);
+  char* const workspace = static_cast<char*>(c.workspace);
+  const bool copied = p.padded && p.F2_pad != 2 * c.F && (c.dx || c.dw);
+  if (copied) {
+    e.pad = workspace + p.dgu_at;
+    e.pad_ld = p.F2_pad;
+    if (c.dbias) e.sums = reinterpret_cast<float*>(workspace + p.bytes);  // else where the products' parts will be
+  }
   const unsigned across = static_cast<unsigned>((c.F + V * kWave - 1) / (V * kWave));
   auto gates = [&](auto kernel) {
-    return split_launch(chunks, std::min<int64_t>(65535, most_groups(chunks, kWave * across)), [&](uint32_t first, uint32_t n) {
-      hipLaunchKernelGGL(kernel, dim3(across, n), dim3(kWave), 0, st, e, int64_t{first});
+    constexpr int kThreads = kGateWaves * kWave;
+    return split_launch(row_groups, std::min<int64_t>(65535, most_groups(row_groups, kThreads * across)), [&](uint32_t first, uint32_t n) {
+      hipLaunchKernelGGL(kernel, dim3(across, n), dim3(kThreads), 0, st, e, int64_t{first});
       return launch_status() == TEMPO_OK;
     });
   };
-  if (chunks > 0 && across > 0 &&
+  if (row_groups > 0 && across > 0 &&
       !(c.kind == TEMPO_GLU_SILU ? gates(gates_kernel<T, TEMPO_GLU_SILU>)
         : c.kind == TEMPO_GLU_GELU_ERF ? gates(gates_kernel<T, TEMPO_GLU_GELU_ERF>)
                                        : gates(gates_kernel<T, TEMPO_GLU_GELU_TANH>)))
@@ -955,7 +1050,7 @@ tempo_status backward(const GluCall& c, const BackwardPlan& p, hipStream_t st) {
   tempo_status status = TEMPO_OK;
   if (c.dbias && c.F > 0) {
     const int n = static_cast<int>(2 * c.F);
-    hipLaunchKernelGGL((bias_kernel<T>), dim3((n + kWave - 1) / kWave), dim3(4 * kWave), 0, st, e.sums, static_cast<T*>(c.dbias), chunks, n);
+    hipLaunchKernelGGL((bias_kernel<T>), dim3((n + kWave - 1) / kWave), dim3(4 * kWave), 0, st, e.sums, static_cast<T*>(c.dbias), row_groups, n);
     status = launch_status();
   }
   if (status != TEMPO_OK || c.H == 0) return status;
@@ -973,6 +1068,18 @@ tempo_status backward(const GluCall& c, const BackwardPlan& p, hipStream_t st) {
   dw.c = c.dw;
   dw.partial = dx.partial + p.dx_bytes / sizeof(float);
   const bool x = c.dx && c.T > 0, w = c.dw && c.F > 0;
+  if (copied) {
+    dx.a = dw.a = e.pad;
+    dx.lda = dw.lda = p.F2_pad;
+  }
+  if (p.padded && p.H_pad != c.H) {
+    char* const to = workspace + p.x_at;
+    status = pad(c.x, w ? c.T : 0, c.w, x ? 2 * c.F : 0, c.H, p.H_pad, to, st);
+    if (status != TEMPO_OK) return status;
+    dw.b = to;
+    dx.b = to + (w ? c.T : 0) * p.H_pad * 2;
+    dx.ldb = dw.ldb = p.H_pad;
+  }
   if (x && w) return launch_both<T>(dx, dw, p.plans, st);
   if (x) return launch_product<T, false, true, kPlain>(dx, p.plans[0], st);
   return w ? launch_product<T, true, true, kPlain>(dw, p.plans[1], st) : TEMPO_OK;
@@ -990,20 +1097,20 @@ bool glu_takes(int64_t T, int64_t H, int64_t F) {
 
 size_t glu_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt, bool back) {
   if (!back) return ForwardPlan(T, H, F, dt).bytes;
-  return std::max(BackwardPlan(T, H, F, dt).bytes, sums_bytes(T, F, dt));
+  const BackwardPlan p(T, H, F, dt);
+  return p.padded ? p.bytes + sums_bytes(T, F, dt) : std::max(p.bytes, sums_bytes(T, F, dt));
 }
 
 tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
   const ForwardPlan p(c.T, c.H, c.F, dt);
   if (p.bytes > c.workspace_bytes) return TEMPO_ERR_WORKSPACE;
-  return dt == TEMPO_F32 ? forward<float>(c, p.plan, st) : forward<bf16_t>(c, p.plan, st);
+  return dt == TEMPO_F32 ? forward<float>(c, p, st) : forward<bf16_t>(c, p, st);
 }
 
 tempo_status launch_glu_bwd(const GluCall& c, tempo_dtype dt, hipStream_t st) {
   const BackwardPlan p(c.T, c.H, c.F, dt);
-  if (((c.dx || c.dw) && p.bytes > c.workspace_bytes) ||
-      (c.dbias && sums_bytes(c.T, c.F, dt) > c.workspace_bytes))
-    return TEMPO_ERR_WORKSPACE;
+  const size_t products = c.dx || c.dw ? p.bytes : 0, sums = c.dbias ? sums_bytes(c.T, c.F, dt) : 0;
+  if ((p.padded ? products + sums : std::max(products, sums)) > c.workspace_bytes) return TEMPO_ERR_WORKSPACE;
   return dt == TEMPO_F32 ? backward<float>(c, p, st) : backward<bf16_t>(c, p, st);
 }
 
