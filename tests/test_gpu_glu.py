@@ -122,7 +122,8 @@ def test_sizes_both_ways(T, H, F, dtype, kind, bias):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,H,F,bias", [(4096, 128, 2048, False), (4099, 72, 2050, True), (2048, 2048, 1024, False),
-                                        (2050, 1031, 1029, True), (512, 4096, 1024, True), (40, 512, 8192, True)])
+                                        (2050, 1031, 1029, True), (512, 4096, 1024, True), (40, 512, 8192, True),
+                                        (8200, 1031, 4099, True), (8200, 1024, 4099, False), (8200, 1031, 4100, False)])
 def test_sizes_of_every_tile(T, H, F, bias, dtype):
     both_ways(T, H, F, dtype, "silu", bias)
 
