@@ -265,7 +265,8 @@ TEMPO_API tempo_status tempo_rotary_bwd(const tempo_rotary_heads* dq, const temp
  *   float32 products are made of bfloat16 ones, of operands that are taken apart into three; what is left out is below 2^-21 of
  *   |x| |w|, where no part of an element falls below 2^-126.  A float32 element that is not finite makes NaN of every sum that it
  *   takes part in, a bfloat16 one what its products make.
- *   workspace: device memory of at least tempo_glu_fwd_workspace_bytes(T, H, F, dt) bytes, 16-byte aligned (NULL if that is 0).
+ *   workspace: device memory of at least tempo_glu_fwd_workspace_bytes(T, H, F, dt) bytes, 16-byte aligned (NULL if that is 0); calls
+ *   that may run at the same time need one each.
  *   UNSUPPORTED also: sizes beyond 2^30 (2F too), or beyond 2^22 tiles of 64 x 64 elements in gu, x or w.
  */
 typedef enum { TEMPO_GLU_SILU = 0, TEMPO_GLU_GELU_ERF = 1, TEMPO_GLU_GELU_TANH = 2 } tempo_glu_kind;
