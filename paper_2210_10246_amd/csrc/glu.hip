@@ -48,11 +48,13 @@ __device__ __forceinline__ ActGrad act_grad(float x) {
     return {x * phi, fmaf(xc, density, phi)};
   }
 }
-// act(g) where no branch is wanted: SiLU and the tanh form of GELU are g sigmoid(g (c0 + c1 g^2)).
+// act(g) where no branch is wanted: SiLU and the tanh form of GELU are g sigmoid(g (c0 + c1 g^2)).  g^2 is that of at most 128, where
+// the sigmoid has long been 0 or 1: c1 is 0 for SiLU, and 0 times an infinite square would be NaN.
 template <bool ERF>
 __device__ __forceinline__ float act_value(float x, float c0, float c1) {
   if constexpr (ERF) return gelu_erf_value(x);
-  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * fmaf(c1 * x, x, c0)));  // -log2(e) is part of c0 and c1
+  const float xc = fminf(fmaxf(x, -128.0f), 128.0f);
+  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * fmaf(c1 * xc, xc, c0)));  // -log2(e) is part of c0 and c1
 }
 template <typename F>
 __device__ __forceinline__ void with_kind(int kind, F&& f) {  // uniform
