@@ -15,6 +15,7 @@
 #include <utility>
 
 #include "gelu_f32.h"
+#include "glu_plan.h"
 #include "launch_split.h"
 #include "tempo_host.h"
 
@@ -461,10 +462,7 @@ __device__ __forceinline__ void product_tile(const Product& g, int block, int to
   const Place<C, END != kPlain> at(g, block, total);
   const A a(g.a, g.lda, at.m0, g.M, [&](int r) { return at.a_row(g, r); });
   const B b(g.b, g.ldb, at.n0, g.N, [&](int r) { return at.b_row(g, r); });
-  // Steps of BK values of k that are loaded in whole pieces: where rows of a k-major operand are no multiple of a piece,
-  // their last one ends in the next row, so that the last row takes no part.
-  const bool over = (AKM && g.M % 8 != 0) || (BKM && g.N % 8 != 0);
-  const int whole = (over ? g.K - 1 : g.K) / C::BK;
+  const int whole = whole_steps(g.K, C::BK, AKM ? g.M : 0, BKM ? g.N : 0);
   const int first = at.split * g.steps, end = first + g.steps, last = min(end, whole);
   f32x4 acc[C::FM][C::FN];
   clear<C>(acc);
