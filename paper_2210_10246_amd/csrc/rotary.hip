@@ -3,8 +3,8 @@
 // for the pairs (x1, x2) = (x[i], x[i + R/2]) or (x[2i], x[2i + 1]); elements from R on are copied.  The backward turns the
 // other way: the transposed map.
 //
-// Bound by the bytes of q and k, read once and written once.  Angles are made where they are used: in 64 bits, which this
-// chip multiplies at the rate of 32, so that a position of any size keeps its place within the turn; no table is read, kept or
+// Bound by the bytes of q and k, read once and written once.  Angles are made where they are used: in two numbers of 64 bits, which
+// this chip multiplies at the rate of 32, so that a position of any size keeps its place within the turn; no table is read, kept or
 // bounded by a longest sequence.
 #include <algorithm>
 #include <type_traits>
@@ -22,10 +22,16 @@ constexpr int kThreads = 256;
 // float32, neighbours in pairs, 14.5 with 8, 10.4 with 1.
 constexpr int heads_per_lane(bool half) { return half ? 4 : 8; }
 
-// cos and sin of a turn in 64 bits.  The quarter is taken off in 64 bits, what is left, at most an eighth of a turn, goes
-// through the Taylor polynomials of sin and cos (next terms below 2e-9 and 2e-10).
-__device__ __forceinline__ void cos_sin(double turns, float scale, float* c, float* s) {
-  const double part = turns - rint(turns);
+// cos and sin of position f radians.  f / 2 pi and its product with the position are taken in two numbers of 64 bits, the second what
+// the first one's rounding left out, so that less the whole turns they are good to 2^-50 at any position of 53 bits (in one number each
+// the angle was off by 1.6e-4 at 2^40).  The quarter is taken off in 64 bits, what is left, at most an eighth of a turn, goes through
+// the Taylor polynomials of sin and cos (next terms below 2e-9 and 2e-10).
+__device__ __forceinline__ void cos_sin(double position, double f, float scale, float* c, float* s) {
+#pragma clang fp contract(off)  // turns less its whole ones has to be that of the rounded product
+  constexpr double inv = 0.15915494309189535, inv_rest = -9.839338337591243e-18;  // 1 / 2 pi
+  const double t = f * inv, t_rest = fma(f, inv_rest, fma(f, inv, -t));
+  const double turns = position * t, rest = fma(position, t_rest, fma(position, t, -turns));
+  const double part = (turns - rint(turns)) + rest;
   const double quarters = part * 4.0;
   const double q = rint(quarters);
   const float a = static_cast<float>((quarters - q) * 1.5707963267948966);
@@ -33,7 +39,7 @@ __device__ __forceinline__ void cos_sin(double turns, float scale, float* c, flo
   float sn = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), 0.0f);
   sn = fmaf(a, sn, a);
   float cs = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.0f);
-  const int n = static_cast<int>(q);  // -2 .. 2
+  const int n = static_cast<int>(q);  // its last two bits count
   const float c0 = n & 1 ? sn : cs, s0 = n & 1 ? cs : sn;
   *c = scale * ((n + 1) & 2 ? -c0 : c0);
   *s = scale * (n & 2 ? -s0 : s0);
@@ -138,7 +144,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r) {
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
       const double f = r.freqs[first + min(i, count - 1)];
-      cos_sin(pos * (f * 0.15915494309189535), r.scale, &c[i], &sn[i]);
+      cos_sin(pos, f, r.scale, &c[i], &sn[i]);
       if (BACK) sn[i] = -sn[i];
     }
   }
