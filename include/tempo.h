@@ -229,8 +229,8 @@ TEMPO_API tempo_status tempo_attn_softmax_dropout_bwd_bytemask(const void* dout,
  *   q, k: element (b, s, head, d) at x[b x_batch + s x_token + head x_head + d], b < B, s < S, d < D (dt), in and out, so that
  *   heads can be taken out of a projection and put into any order; k may be NULL.  x and y need only the alignment of an element.
  *   y may be x, with the same strides; otherwise no element of a y is that of another, of an x, freqs or positions.
- *   freqs [R/2] in, float64, radians per position; an angle is good to 2^-47 less its whole turns, and c and n to 2^-22 of scale, at any
- *   position.
+ *   freqs [R/2] in, float64, radians per position; an angle below 2^80 is good to 2^-47 less its whole turns, and c and n to 2^-22 of scale,
+ *   at any position.
  *   positions in: int32 or int64 (bits 32 or 64), element (b, s) at b batch_stride + s token_stride (strides >= 0; a batch_stride
  *   of 0 shares them); may be NULL.  A position may be negative; start + positions[b,s] lies within 2^53.
  *   INVALID_ARG also: R odd, R < 2, R > D, B S above 2^31 - 1, more than 2^24 elements of q and k together in a token, a negative
