@@ -108,6 +108,15 @@ inline int64_t whole_pieces(int64_t elements) { return (elements + 7) / 8 * 8; }
 inline size_t partial_bytes(const Plan& p, const Shape& s) {
   return p.splits > 1 ? static_cast<size_t>(p.splits) * s.M * s.N * sizeof(float) : 0;
 }
+// Whether a forward of up to 64 rows is made on the tiles for few rows, in whose workgroups all of k follows on: that takes a time of
+// its own however few columns W has, and the tiles above can be made in parts of k, which all compute units read.  us, those / these, on either
+// side of where this changes over: 8 x 4096 x 2048 13.0 / 14.2, 1 x 4096 x 4096 20.1 / 15.4; 16 x 8192 x 2048 21.0 / 26.7, 4096 columns each 34.7
+// / 32.6; 24 x 8192 x 2048 21 / 38, 24 x 4096 x 4096 20.4 / 22.3, 5504 columns each 29.0 / 24.7; 64 x 1024 x 512 6.8 / 7.2, 2048 columns
+// each 8.7 / 8.4.  A step of 64 values of k is then not waited for where there are few: 64 x 512 x 2048 4.9 / 5.4, 64 x 768 x 2500 7.6 / 7.5.
+inline bool few_pay(int64_t T, int64_t H, int64_t F) {
+  const double steps = (H + kFewStep - 1) / kFewStep, here = 2.0 + (T <= kFewestRows ? 0.2 : 0.3) * steps;
+  return (T <= kFewestRows || H > 512) && here < 5.0 + 4.0 * F * H / 4.5e6;  // W at 4.5 TB/s
+}
 // The three products.  Rows of x and w have H elements, of [g | u] 2F.  dx and dw are planned together whichever is wanted: the
 // bits of one do not depend on the other.
 struct ForwardPlan {
@@ -122,11 +131,12 @@ struct ForwardPlan {
     if (dt == TEMPO_BF16 && H_pad != H) padded = plan_padded(&shape, &plan, 1, 2.0 * copies, cus);
     else plan_for(&shape, &plan, 1, dt, true, cus);
     // Up to 64 rows read W once, nothing else counts: whole lines of W's rows at a time, as much on its way as LDS holds, few rows
-    // of x beside them.  us, 64 x 64 tiles of above / this: 48 x 4096 x 11008 57 / 41 (64 columns at a time 44), 1 x 4096 x 11008 52 /
-    // 38, 48 x 1024 x 4096 13.2 / 8.4 (128 columns 10.5), 1 x 1024 x 4096 13.0 / 6.1.  Where W has few columns of many values of k,
-    // parts of k are worth more.
-    if (plan.aligned && !padded && T <= kFewRows && (F >= 2048 || H <= 1024)) {
-      plan.size = T <= kFewestRows ? Size::kFewest : 2 * F >= 80 * int64_t{cus} ? Size::kFewWide : Size::kFew;
+    // of x beside them.  us, 64 x 64 tiles of above / this: 64 x 4096 x 11008 46 / 43 (64 columns at a time 46), 24 x 8192 x 5504 60 / 45,
+    // 16 x 4096 x 5504 29 / 20, 1 x 1024 x 4096 8.8 / 6.1, 1 x 1536 x 512 6.9 / 6.5.
+    if (plan.aligned && !padded && T <= kFewRows && few_pay(T, H, F)) {
+      // More columns at a time once 64 would make more workgroups than there are compute units: 24 x 1024 x 8192 (256 of 64 columns)
+      // 8.9 us with 64, 10.3 with 128; 48 x 4096 x 9600 (300) 42.0 and 39.3, 64 x 1024 x 11008 13.8 and 12.5, 48 x 4096 x 20480 90 and 86.
+      plan.size = T <= kFewestRows ? Size::kFewest : 2 * F > 64 * int64_t{cus} ? Size::kFewWide : Size::kFew;
       plan.splits = 1;
       plan.steps = static_cast<int>((H + kFewStep - 1) / kFewStep);
       plan.tiles = (2 * F + few_columns(plan.size) - 1) / few_columns(plan.size);

@@ -63,3 +63,12 @@ def test_parts_and_workspaces_of_any_size(program, cus):
     for f32 in (0, 1):
         lines = program("plan", f32, cus, *(n for s in sizes for n in s)).splitlines()
         assert len(lines) == len(sizes) and all(line.endswith("| fits") for line in lines)
+
+
+@pytest.mark.parametrize("T,H,F,forward", [
+    (24, 8192, 2048, "A64+"), (24, 8192, 5504, "few 64"), (64, 512, 2048, "A64"), (64, 776, 2500, "few 64"), (16, 8192, 2048, "A64+"),
+    (16, 8192, 4096, "few 16"), (1, 1024, 4096, "few 16"), (64, 1024, 8192, "few 64"), (64, 4096, 9600, "few 128"),
+    (65, 1024, 8192, "A64"), (8, 4096, 64, "A64+")])
+def test_which_forward_few_rows_take(program, T, H, F, forward):
+    """The faster one on either side of where it changes over, by the times in csrc/glu_plan.h."""
+    assert program("plan", 0, 256, T, H, F).split(" | ")[0] == forward
