@@ -17,9 +17,8 @@ namespace tempo {
 namespace {
 
 constexpr int kThreads = 256;
-// Heads that share the angles of a lane, each in two pieces (half) or one: 128 bytes of a lane on their way.  One where that
-// leaves the chip short of waves: 64 tokens of 32 + 8 heads of 128 bfloat16 5.4 us with 4, 4.7 with 1; 3063 tokens of 12 heads of 83
-// float32, neighbours in pairs, 14.5 with 8, 10.4 with 1.
+// Heads that share the angles of a lane, each in two pieces (half) or one: 128 bytes of a lane on their way.  One each where that leaves
+// the chip short of waves and the angles, made for every head then, are few.
 constexpr int heads_per_lane(bool half) { return half ? 4 : 8; }
 
 // cos and sin of position f radians.  f / 2 pi and its product with the position are taken in two numbers of 64 bits, the second what
@@ -212,7 +211,10 @@ tempo_status launch_rotary(const tempo_rotary_heads* q, const tempo_rotary_heads
   r.in_place = q->x == q->y || (k && k->x == k->y);
   r.units = r.rot_units + (in_place ? 0 : (r.D - 2 * r.R2 + V - 1) / V);
   const int64_t pieces = int64_t{r.tokens} * r.units * r.heads;
-  const bool few = pieces < int64_t{compute_units()} * (half ? 4 : 16) * kWave * heads_per_lane(half);
+  // us with one / several heads a lane, at 1, 2 and 4 Mi angles: half, float32, 40 heads of 128 5.9 / 7.9, 9.4 / 10.1 and 15.6 / 14.0,
+  // bfloat16 5.6 / 6.1, 7.8 / 7.6 and 12.5 / 10.4; neighbours, float32 6.4 / 7.1, 10.5 / 9.7 and 17.5 / 13.6, bfloat16 (2, 4 and 8 Mi)
+  // 7.6 / 7.5, 12.7 / 10.3 and 21.7 / 14.2; 12 heads of 83, 38 turned, neighbours, float32 (1 and 2 Mi) 7.2 / 8.1 and 11.8 / 10.6.
+  const bool few = pieces * pairs < int64_t{compute_units()} * 8192;
   const int per_lane = few ? 1 : heads_per_lane(half);
   r.groups = (r.heads + per_lane - 1) / per_lane;
   r.units_per_block = std::min(r.units, kThreads);

@@ -25,7 +25,7 @@ def tokens_for(streamed, heads, D, half, layout, dtype):
     """The fewest tokens [3, S] of several heads a lane, below and above the streaming limit, in workgroups that are no multiple of 8.
     In place there may be fewer pieces: of several heads a lane there too."""
     cus = torch.cuda.get_device_properties(0).multi_processor_count
-    several = cus * (4 if layout == "half" else 16) * 64 * (4 if layout == "half" else 8)
+    several = cus * 8192 // ((4 if dtype == "f32" else 8) // (1 if layout == "half" else 2))
     stream = (48 << 20) // (32 if layout == "half" else 16)
     S = 1
     while True:
