@@ -222,9 +222,20 @@ tempo_status launch_rotary(const tempo_rotary_heads* q, const tempo_rotary_heads
   r.per_tokens = r.groups * ((r.units + kThreads - 1) / kThreads);
   const int threads = (r.units_per_block * r.tokens_per_block + kWave - 1) / kWave * kWave;
   const int64_t blocks = (int64_t{r.tokens} + r.tokens_per_block - 1) / r.tokens_per_block * r.per_tokens;
-  // What is written stays in the 256 MiB of cache where it is a part of that: 16 x 512 x 32 heads of 64 bfloat16 (34 MB) 17.3 / 15.4 us
-  // streamed / not, 4 x 2048 x 32 of 64 float32 (67 MB) 26.7 / 29.5, 65536 x 40 of 128 bfloat16 (671 MB) 254 / 268.
-  const bool stream = pieces * (half ? 32 : 16) > (int64_t{48} << 20);
+  // What is written stays in the 256 MiB of cache where it is a part of that, and where lanes side by side do not write the whole of
+  // each line at once.  us not streamed / streamed, 65536 tokens of 32 heads, bfloat16: halves, heads of 128 206 / 193, of 256 434 / 385,
+  // of 128 in rows of 192 from 64 bytes on 292 / 260, of 128 in rows of 136 344 / 426, of 96 (halves of 96 bytes) 177 / 270, of 64 121 / 152,
+  // half of a head of 128 turned 201 / 220; neighbours, heads of 128 221 / 192, in rows of 136 344 / 318, of 80 144 / 143, of 83 (95325
+  // tokens of 12) 115 / 131.  4 x 2048 x 32 of 64 float32 (67 MB) 29.5 / 26.7.
+  auto in_rows_of = [&](int64_t bytes, const Side& t, int64_t heads) {
+    auto whole = [&](int64_t elements) { return elements * (16 / V) % bytes == 0; };
+    return reinterpret_cast<uintptr_t>(t.y) % bytes == 0 && (B == 1 || whole(t.y_batch)) && (S == 1 || whole(t.y_token)) &&
+           (heads == 1 || whole(t.y_head));
+  };
+  const int64_t row = half ? 64 : 16, run = half ? 128 : 16;
+  const bool lines = (half ? r.R2 : R) * (16 / V) % run == 0 && in_rows_of(row, r.q, r.q_heads) &&
+                     (!k || in_rows_of(row, r.k, k->heads));
+  const bool stream = lines && pieces * (half ? 32 : 16) > (int64_t{48} << 20);
   auto go = [&](auto kernel) {
     const bool ok = split_launch(blocks, most_groups(blocks, threads), [&](uint32_t first, uint32_t count) {
       r.first = first;

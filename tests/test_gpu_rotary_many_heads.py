@@ -1,7 +1,8 @@
 """Rotary positions of as many tokens as make a lane take several heads, below and above the size from which what is written is not
 kept in a cache: heads that are no multiple of a lane's, lanes whose heads are of q and of k, workgroups that are no multiple of 8.
 
-The limits of csrc/rotary.hip are restated here, so that each case is where it is meant to be; tolerance: test_gpu_rotary's."""
+The limits of csrc/rotary.hip are restated here, so that each case is where it is meant to be (what is written is not kept in a cache at
+heads of 128 and 160, of neighbours at 64 and of 64 in float32 too); tolerance: test_gpu_rotary's."""
 import pytest
 import torch
 
@@ -40,7 +41,8 @@ def tokens_for(streamed, heads, D, half, layout, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("streamed", [False, True])
-@pytest.mark.parametrize("A,K,D,half", [(9, 4, 83, 33), (9, 4, 64, 32), (5, 2, 40, 19), (11, 0, 18, 9)])
+@pytest.mark.parametrize("A,K,D,half", [(9, 4, 83, 33), (9, 4, 64, 32), (5, 2, 40, 19), (11, 0, 18, 9), (9, 4, 128, 64),
+                                         (5, 2, 160, 64)])
 def test_several_heads_a_lane(A, K, D, half, streamed, layout, dtype):
     S = tokens_for(streamed, A + K, D, half, layout, dtype)
     freqs = freqs_of(half)
