@@ -4,8 +4,8 @@
 //
 // All products are on the matrix cores with bfloat16 operands and float32 sums.  A float32 operand is taken apart into three
 // bfloat16 ones, x = x0 + x1 + x2 exactly (each takes the first 8 bits of what is left), and of the nine products those six are
-// made that count in float32; the other three are below 2^-21 of |a| |b|.  Six products at the rate of bfloat16 are a quarter
-// of its rate, half as fast again as the float32 matrix instructions: 1350 TFLOP/s and 154 for the library's, 8192^3.
+// made that count in float32; the other three are below 2^-21 of |a| |b|.  Six products at the rate of bfloat16 are a sixth
+// of its rate, half as fast again as the float32 matrix instructions: 1350 / 6 TFLOP/s and 154 for the library's, 8192^3.
 //
 // The products' bound is the power of the matrix cores (the clock falls from 2.4 to 1.7 GHz) and, beside it, what comes from the
 // L2s; LDS is read without bank conflicts and takes a quarter of the time.  [16384, 4096] x 2 x 11008 bfloat16: forward 2.44 ms, 1210
@@ -30,7 +30,9 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 struct ActGrad {
   float value, grad;
 };
-// act(g) and act'(g).  Beside a factor that has long been zero the other one is kept finite.
+// act(g) and act'(g).  Beside a factor that has long been zero the other one is kept finite.  The argument of exp2 is rounded in 32 bits
+// as g itself was: a sigmoid far on the left is off by up to |g| 2^-23 of itself (1e-5 at -80, where it is 2e-35), no more than by a last
+// bit of g.
 template <int KIND>
 __device__ __forceinline__ ActGrad act_grad(float x) {
   const float xc = fminf(fmaxf(x, -128.0f), 128.0f);
@@ -138,7 +140,8 @@ struct Operand {
     }
   }
   // Straight to LDS, piece i of every lane: bfloat16 at addresses that are multiples of 16 bytes.  In assembly because the
-  // compiler waits for all such loads before any read of LDS; whoever calls this waits for them (landed()).  It has no output.
+  // compiler waits for all such loads before any read of LDS; whoever calls this waits for them (landed()).  It has no output,
+  // and nothing else here uses m0.
   __device__ __forceinline__ void load_lds(int i, int64_t s, char* lds) const {
     static_assert(sizeof(T) == 2, "as it is in memory");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -669,6 +672,9 @@ __global__ __launch_bounds__(256) void pad_kernel(const bf16_t* first, uint32_t 
 }
 
 // ---- the backward's elementwise part ----------------------------------------------------------------------------------
+// dg and du are rounded to the storage type before dx and dw: one operand of a matrix instruction each, as an autograd that keeps its
+// tensors in that type has them.  In two bfloat16 parts they would count in float32, at twice the products: of [8192, 1024] x 2 x 4096 dx and dw are
+// off by 2.34e-3 of their norm, by 1.66e-3 (their own rounding alone) with dgu in float32.  dbias is summed before the rounding.
 struct Gates {
   const void *dh, *gu;
   void *dgu, *h;     // h may be null
@@ -964,7 +970,8 @@ tempo_status backward(const GluCall& c, const BackwardPlan& p, hipStream_t st) {
 bool glu_takes(int64_t T, int64_t H, int64_t F) {
   const int64_t most = int64_t{1} << 30;  // of what is counted in 32 bits
   if (T > most || H > most || F > most / 2) return false;
-  // tiles of 64 x 64 elements, up to 512 lanes a tile, in one launch
+  // Two products of tiles of 64 x 64 elements, 256 lanes each, make 2^31 of the 2^32 lanes that a launch may have; parts of k are made
+  // of few tiles.
   auto tiles = [](int64_t M, int64_t N) { return ((M + 63) / 64) * ((N + 63) / 64); };
   return tiles(T, 2 * F) < most / 256 && tiles(T, H) < most / 256 && tiles(2 * F, H) < most / 256;
 }
