@@ -291,6 +291,49 @@ TEMPO_API tempo_status tempo_glu_bwd(const void* dh, const void* gu, const void*
                            tempo_glu_kind kind, tempo_dtype dt, void* hip_stream);
 
 /*
+ * Attention with a sliding window and first tokens that stay visible, forward and backward, without a matrix of scores in memory
+ *   Query i of sequence b stands at position P = query_start[b] + i (Sk - Sq + i if query_start is NULL) and sees the keys j <= P,
+ *   j < key_len[b] (Sk if NULL) with j > P - window or j < sinks.
+ *     s_ij = scale q_i . k_j,  lse_i = ln sum_j exp s_ij,  out_i = sum_j exp(s_ij - lse_i) v_j;   a query that sees no key: out 0, lse -inf
+ *     delta_i = dout_i . out_i,  ds_ij = exp(s_ij - lse_i) (dout_i . v_j - delta_i),
+ *     dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i exp(s_ij - lse_i) dout_i
+ *   Query head h reads key head h / (heads / kv_heads), whose gradients are sums over the heads that read it.
+ *   q, out, dout, dq [B, Sq, heads, D], k, v, dk, dv [B, Sk, kv_heads, D] (dt): element (b, s, head, d) at p[b batch + s token + head head_stride + d],
+ *   with any strides >= 0; they need only the alignment of an element.  out, dq, dk and dv overlap nothing.
+ *   lse [B, heads, Sq] (f32) out of the forward, where it may be NULL, and in to the backward.
+ *   key_len, query_start [B] int32 in, device, may be NULL; key_len is taken as 0 below 0 and as Sk above it, query_start may be negative.
+ *   Keys that none of 128 neighbouring rows sees (a row: a query of one of the heads that share a key head) are not looked at, whatever they hold; an element of k, v, q or dout that is not finite
+ *   makes NaN of the sums that it takes part in, and may of those of the rows and keys beside it that do not see it.  dk and dv of keys that no query sees are 0.
+ *   bfloat16: the weights exp(s - max) and ds are rounded to bfloat16 for the second product, sums are in float32.  Sums are made in a
+ *   fixed order: the same call gives the same bits.
+ *   workspace: device memory of at least tempo_window_attn_fwd/bwd_workspace_bytes() bytes, 16-byte aligned (NULL if that is 0); calls that
+ *   may run at the same time need one each.
+ *   INVALID_ARG also: kv_heads < 1 (with heads > 0), heads no multiple of it, D < 1, window < 1, sinks < 0, a scale that is not positive
+ *   and finite, a negative stride, a stride of an output that is 0 where there are two elements along it.
+ *   UNSUPPORTED also: D > 256; more than 2^31 - 129 rows of a key head (Sq heads / kv_heads) or 2^32 queries of all heads; more than 2^23 tiles of 128 rows,
+ *   or 2^22 of 128 keys, in all.
+ */
+typedef struct {
+  const void* p; /* written through if it is an output */
+  int64_t batch, token, head; /* strides in elements */
+} tempo_attn_heads;
+TEMPO_API size_t tempo_window_attn_fwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D,
+                                             int64_t window, int64_t sinks);
+TEMPO_API tempo_status tempo_window_attn_fwd(const tempo_attn_heads* q, const tempo_attn_heads* k, const tempo_attn_heads* v,
+                                   const tempo_attn_heads* out, float* lse, const int32_t* key_len, const int32_t* query_start,
+                                   void* workspace, size_t workspace_bytes, int64_t B, int64_t Sq, int64_t Sk, int64_t heads,
+                                   int64_t kv_heads, int64_t D, int64_t window, int64_t sinks, float scale, tempo_dtype dt,
+                                   void* hip_stream);
+TEMPO_API size_t tempo_window_attn_bwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D,
+                                             int64_t window, int64_t sinks);
+TEMPO_API tempo_status tempo_window_attn_bwd(const tempo_attn_heads* dout, const tempo_attn_heads* q, const tempo_attn_heads* k,
+                                   const tempo_attn_heads* v, const tempo_attn_heads* out, const float* lse, const tempo_attn_heads* dq,
+                                   const tempo_attn_heads* dk, const tempo_attn_heads* dv, const int32_t* key_len,
+                                   const int32_t* query_start, void* workspace, size_t workspace_bytes, int64_t B, int64_t Sq,
+                                   int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D, int64_t window, int64_t sinks, float scale,
+                                   tempo_dtype dt, void* hip_stream);
+
+/*
  * Mask layout conversion: packed bits <-> one byte per element        [Sec. 3.3 (8-bit masks)]
  *   The paper's implementation keeps the dropout mask as one byte per element; this library
  *   keeps one bit (bit e & 31 of word e >> 5).  These two calls convert between the layouts,

@@ -41,6 +41,11 @@ class _RotaryPositions(ctypes.Structure):
     _fields_ = [("positions", _vp), ("bits", _int), ("strides", _i64 * 2), ("start", _i64)]
 
 
+class _AttnHeads(ctypes.Structure):
+    _fields_ = [("p", _vp), ("strides", _i64 * 3)]
+
+
+_heads = ctypes.POINTER(_AttnHeads)
 _rotary_args = [ctypes.POINTER(_RotaryHeads), ctypes.POINTER(_RotaryHeads), _vp, ctypes.POINTER(_RotaryPositions), _i64, _i64,
                 _i64, _i64, _int, _f32, _int, _vp]
 
@@ -75,6 +80,10 @@ _SIGNATURES = {
     "tempo_glu_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
     "tempo_glu_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _sz, _i64, _i64, _i64, _int, _int, _vp]),
     "tempo_glu_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _i64, _i64, _i64, _int, _int, _vp]),
+    "tempo_window_attn_fwd_workspace_bytes": (_sz, [_i64] * 8),
+    "tempo_window_attn_bwd_workspace_bytes": (_sz, [_i64] * 8),
+    "tempo_window_attn_fwd": (_int, [_heads] * 4 + [_vp] * 4 + [_sz] + [_i64] * 8 + [_f32, _int, _vp]),
+    "tempo_window_attn_bwd": (_int, [_heads] * 5 + [_vp] + [_heads] * 3 + [_vp] * 3 + [_sz] + [_i64] * 8 + [_f32, _int, _vp]),
     "tempo_mask_bits_to_bytes": (_int, [_vp, _vp, _i64, _vp]),
     "tempo_mask_bytes_to_bits": (_int, [_vp, _vp, _i64, _vp]),
 }
@@ -529,6 +538,78 @@ def tempo_glu_bwd(dh, gu, x, w, dgu, h, dx, dw, dbias, kind="silu", workspace=No
     ws = _workspace(workspace, tempo_glu_bwd_workspace_bytes(T, H, F, gu.dtype), gu.device, stream)
     _check(load().tempo_glu_bwd(*pointers, _ptr(ws), ws.numel() * ws.element_size(), T, H, F, act, dt, _stream(stream)),
            "tempo_glu_bwd")
+
+
+def tempo_window_attn_fwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks) -> int:
+    return load().tempo_window_attn_fwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks)
+
+
+def tempo_window_attn_bwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks) -> int:
+    return load().tempo_window_attn_bwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks)
+
+
+def _window_attn(where, like_q, like_k, lse, window, sinks, scale, key_len, query_start, workspace, stream):
+    """The checks of both ways; like_q, like_k: (name, tensor) of q's and of k's shape, of which the first are q and k."""
+    q, k = like_q[0][1], like_k[0][1]
+    dt = _act_dtype("q", q)
+    for (name, t), first in [(x, q) for x in like_q] + [(x, k) for x in like_k]:
+        if t.dim() != 4 or (t.shape[-1] != 1 and t.stride(-1) != 1):
+            raise ValueError(f"{name} must be [batch, tokens, heads, elements] with adjacent elements")
+        _want(name, t, q.dtype)
+        if t.shape != first.shape:
+            raise ValueError(f"{name} must have shape {tuple(first.shape)}, got {tuple(t.shape)}")
+    B, Sq, heads, D = q.shape
+    Sk, kv_heads = k.shape[1:3]
+    if k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"k must have the batch and elements of q, {tuple(q.shape)}, got {tuple(k.shape)}")
+    if heads > 0 and (kv_heads < 1 or heads % kv_heads != 0):
+        raise ValueError(f"the heads of q must be a multiple of those of k, got {heads} and {kv_heads}")
+    if not 1 <= window < 2 ** 63 or not 0 <= sinks < 2 ** 63:
+        raise ValueError(f"window must be at least 1 and sinks at least 0, got {window} and {sinks}")
+    scale = D ** -0.5 if scale is None and D > 0 else scale
+    if not 0.0 < scale <= torch.finfo(torch.float32).max:
+        raise ValueError(f"scale must be positive and finite, got {scale}")
+    _want("lse", lse, torch.float32, B * heads * Sq)
+    _want("key_len", key_len, torch.int32, B)
+    _want("query_start", query_start, torch.int32, B)
+    tensors = [t for _, t in like_q + like_k]
+    pointers = [_ptr(t) for t in (lse, key_len, query_start)]
+    _same_device(*tensors, lse, key_len, query_start, workspace)
+    structs = {n: _AttnHeads(t.data_ptr(), (_i64 * 3)(*t.stride()[:3])) for n, t in like_q + like_k}
+    sizes = B, Sq, Sk, heads, kv_heads, D, window, sinks
+    ws = _workspace(workspace, getattr(load(), where + "_workspace_bytes")(*sizes), q.device, stream)
+    return structs, pointers, [_ptr(ws), ws.numel() * ws.element_size(), *sizes, scale, dt, _stream(stream)]
+
+
+def tempo_window_attn_fwd(q, k, v, out, lse, window, sinks=0, scale=None, key_len=None, query_start=None, workspace=None, stream=None):
+    """Attention of q [batch, queries, heads, elements] over k and v [batch, keys, kv_heads, elements], any strides over the first three
+    dimensions, into out, which is like q.  A query at position P sees the keys up to P that are among the last `window` or the first
+    `sinks`; positions begin at query_start[b] (default: so that the last query stands at the last key), keys from key_len[b] on do not
+    exist.  lse [batch, heads, queries] float32 (None: not kept): for the backward.  scale: elements^-0.5 if None.  workspace:
+    tempo_window_attn_fwd_workspace_bytes() bytes, or None: allocated for the call."""
+    if stream is None and _native is not None:
+        status = _native.tempo_window_attn_fwd(q, k, v, out, lse, window, sinks, scale, key_len, query_start, workspace)
+        if status is not None:
+            return _check(status, "tempo_window_attn_fwd")
+    s, (lse_p, len_p, start_p), rest = _window_attn("tempo_window_attn_fwd", [("q", q), ("out", out)], [("k", k), ("v", v)], lse, window,
+                                                    sinks, scale, key_len, query_start, workspace, stream)
+    _check(load().tempo_window_attn_fwd(s["q"], s["k"], s["v"], s["out"], lse_p, len_p, start_p, *rest), "tempo_window_attn_fwd")
+
+
+def tempo_window_attn_bwd(dout, q, k, v, out, lse, dq, dk, dv, window, sinks=0, scale=None, key_len=None, query_start=None,
+                          workspace=None, stream=None):
+    """The gradients of q, k and v from that of out and what the forward kept; arguments as there."""
+    if stream is None and _native is not None:
+        status = _native.tempo_window_attn_bwd(dout, q, k, v, out, lse, dq, dk, dv, window, sinks, scale, key_len, query_start, workspace)
+        if status is not None:
+            return _check(status, "tempo_window_attn_bwd")
+    if lse is None:
+        raise ValueError("lse, which the forward keeps, is needed")
+    s, (lse_p, len_p, start_p), rest = _window_attn(
+        "tempo_window_attn_bwd", [("q", q), ("out", out), ("dout", dout), ("dq", dq)], [("k", k), ("v", v), ("dk", dk), ("dv", dv)],
+        lse, window, sinks, scale, key_len, query_start, workspace, stream)
+    _check(load().tempo_window_attn_bwd(s["dout"], s["q"], s["k"], s["v"], s["out"], lse_p, s["dq"], s["dk"], s["dv"], len_p, start_p,
+                                        *rest), "tempo_window_attn_bwd")
 
 
 def tempo_mask_bits_to_bytes(bits, bytes_, n, stream=None):

@@ -435,6 +435,105 @@ tempo_status tempo_glu_bwd(const void* dh, const void* gu, const void* x, const 
   return launch_glu_bwd(c, dt, static_cast<hipStream_t>(hip_stream));
 }
 
+static bool window_attn_ok(const WindowCall& c) {
+  return c.B >= 0 && c.Sq >= 0 && c.Sk >= 0 && c.heads >= 0 && c.kv_heads >= 0 && c.D >= 1 && c.window >= 1 && c.sinks >= 0 &&
+         (c.heads == 0 || (c.kv_heads >= 1 && c.heads % c.kv_heads == 0)) && c.Sq <= INT32_MAX && c.Sk <= INT32_MAX &&
+         count_ok(c.B, c.Sq, c.heads, c.D) && count_ok(c.B, c.Sk, c.kv_heads, c.D) && count_ok(c.B, c.heads) &&
+         c.B * c.heads <= INT32_MAX;
+}
+// A [batch, tokens, heads, elements] whose elements lie within what a tensor may have, those of an output apart.
+static bool attn_heads_ok(const tempo_attn_heads* h, int64_t B, int64_t S, int64_t heads, int64_t D, bool out) {
+  if (!h) return false;
+  const int64_t sizes[] = {B, S, heads}, strides[] = {h->batch, h->token, h->head};
+  int64_t last = D;
+  for (int i = 0; i < 3; ++i) {
+    if (strides[i] < 0 || !count_ok(sizes[i], strides[i]) || (out && sizes[i] > 1 && strides[i] == 0)) return false;
+    last += sizes[i] * strides[i];
+  }
+  return last <= kMaxElements;
+}
+static WindowCall window_sizes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D, int64_t window,
+                               int64_t sinks) {
+  constexpr int64_t most = INT32_MAX;  // beyond any position
+  WindowCall c{};
+  c.B = B, c.Sq = Sq, c.Sk = Sk, c.heads = heads, c.kv_heads = kv_heads, c.D = D;
+  c.window = window < most ? window : most;
+  c.sinks = sinks < most ? sinks : most;
+  return c;
+}
+static size_t window_attn_bytes(const WindowCall& c, bool back) {
+  return window_attn_ok(c) && c.B > 0 && c.heads > 0 && window_attn_takes(c) ? window_attn_workspace_bytes(c, back) : 0;
+}
+
+size_t tempo_window_attn_fwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D,
+                                             int64_t window, int64_t sinks) {
+  const WindowCall c = window_sizes(B, Sq, Sk, heads, kv_heads, D, window, sinks);
+  return window_attn_bytes(c, false);
+}
+
+size_t tempo_window_attn_bwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D,
+                                             int64_t window, int64_t sinks) {
+  const WindowCall c = window_sizes(B, Sq, Sk, heads, kv_heads, D, window, sinks);
+  return window_attn_bytes(c, true);
+}
+
+static bool scale_ok(float scale) { return scale > 0.0f && scale <= 3.402823466e+38f; }  // false for NaN
+static bool aligned_to(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+tempo_status tempo_window_attn_fwd(const tempo_attn_heads* q, const tempo_attn_heads* k, const tempo_attn_heads* v,
+                                   const tempo_attn_heads* out, float* lse, const int32_t* key_len, const int32_t* query_start,
+                                   void* workspace, size_t workspace_bytes, int64_t B, int64_t Sq, int64_t Sk, int64_t heads,
+                                   int64_t kv_heads, int64_t D, int64_t window, int64_t sinks, float scale, tempo_dtype dt,
+                                   void* hip_stream) {
+  WindowCall c = window_sizes(B, Sq, Sk, heads, kv_heads, D, window, sinks);
+  if (!window_attn_ok(c) || !dtype_ok(dt) || !scale_ok(scale) || !attn_heads_ok(q, B, Sq, heads, D, false) ||
+      !attn_heads_ok(k, B, Sk, kv_heads, D, false) || !attn_heads_ok(v, B, Sk, kv_heads, D, false) ||
+      !attn_heads_ok(out, B, Sq, heads, D, true))
+    return TEMPO_ERR_INVALID_ARG;
+  if (B == 0 || Sq == 0 || heads == 0) return TEMPO_OK;
+  if (!q->p || !out->p || (Sk > 0 && (!k->p || !v->p))) return TEMPO_ERR_INVALID_ARG;
+  const uintptr_t element = dt == TEMPO_F32 ? 4 : 2;
+  for (const tempo_attn_heads* h : {q, k, v, out})
+    if (!aligned_to(h->p, element)) return TEMPO_ERR_UNSUPPORTED;
+  if (!window_attn_takes(c) || !aligned_to(lse, 4) || !aligned_to(key_len, 4) || !aligned_to(query_start, 4) || !aligned16(workspace))
+    return TEMPO_ERR_UNSUPPORTED;
+  c.q = q, c.k = k, c.v = v, c.out = out, c.lse = lse, c.key_len = key_len, c.query_start = query_start;
+  c.workspace = workspace, c.workspace_bytes = workspace ? workspace_bytes : 0;
+  c.scale = scale;
+  return launch_window_attn_fwd(c, dt, static_cast<hipStream_t>(hip_stream));
+}
+
+tempo_status tempo_window_attn_bwd(const tempo_attn_heads* dout, const tempo_attn_heads* q, const tempo_attn_heads* k,
+                                   const tempo_attn_heads* v, const tempo_attn_heads* out, const float* lse, const tempo_attn_heads* dq,
+                                   const tempo_attn_heads* dk, const tempo_attn_heads* dv, const int32_t* key_len,
+                                   const int32_t* query_start, void* workspace, size_t workspace_bytes, int64_t B, int64_t Sq,
+                                   int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D, int64_t window, int64_t sinks, float scale,
+                                   tempo_dtype dt, void* hip_stream) {
+  WindowCall c = window_sizes(B, Sq, Sk, heads, kv_heads, D, window, sinks);
+  if (!window_attn_ok(c) || !dtype_ok(dt) || !scale_ok(scale)) return TEMPO_ERR_INVALID_ARG;
+  for (const tempo_attn_heads* h : {q, out, dout})
+    if (!attn_heads_ok(h, B, Sq, heads, D, false)) return TEMPO_ERR_INVALID_ARG;
+  for (const tempo_attn_heads* h : {k, v})
+    if (!attn_heads_ok(h, B, Sk, kv_heads, D, false)) return TEMPO_ERR_INVALID_ARG;
+  if (!attn_heads_ok(dq, B, Sq, heads, D, true) || !attn_heads_ok(dk, B, Sk, kv_heads, D, true) ||
+      !attn_heads_ok(dv, B, Sk, kv_heads, D, true))
+    return TEMPO_ERR_INVALID_ARG;
+  if (B == 0 || heads == 0 || (Sq == 0 && Sk == 0)) return TEMPO_OK;
+  // Gradients of no queries are written too: zeros.
+  if (Sq > 0 && (!q->p || !out->p || !dout->p || !dq->p || !lse)) return TEMPO_ERR_INVALID_ARG;
+  if (Sk > 0 && (!k->p || !v->p || !dk->p || !dv->p)) return TEMPO_ERR_INVALID_ARG;
+  const uintptr_t element = dt == TEMPO_F32 ? 4 : 2;
+  for (const tempo_attn_heads* h : {q, k, v, out, dout, dq, dk, dv})
+    if (!aligned_to(h->p, element)) return TEMPO_ERR_UNSUPPORTED;
+  if (!window_attn_takes(c) || !aligned_to(lse, 4) || !aligned_to(key_len, 4) || !aligned_to(query_start, 4) || !aligned16(workspace))
+    return TEMPO_ERR_UNSUPPORTED;
+  c.q = q, c.k = k, c.v = v, c.out = out, c.dout = dout, c.dq = dq, c.dk = dk, c.dv = dv;
+  c.lse = const_cast<float*>(lse), c.key_len = key_len, c.query_start = query_start;
+  c.workspace = workspace, c.workspace_bytes = workspace ? workspace_bytes : 0;
+  c.scale = scale;
+  return launch_window_attn_bwd(c, dt, static_cast<hipStream_t>(hip_stream));
+}
+
 tempo_status tempo_mask_bits_to_bytes(const uint32_t* bits, uint8_t* bytes, int64_t n,
                                       void* hip_stream) {
   if (n < 0 || !count_ok(n)) return TEMPO_ERR_INVALID_ARG;

@@ -8,6 +8,7 @@
 // is no float or int.  Nothing has happened then, and binding.py goes through its own checks, which
 // raise what they always raised.
 #include <Python.h>
+#include <cmath>
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -364,6 +365,69 @@ TEMPO_METHOD(glu_bwd) {  // dh, gu, x, w, dgu, h, dx, dw, dbias, kind, workspace
   });
 }
 
+// ---- window attention --------------------------------------------------------------------------------------------------
+// A [batch, tokens, heads, elements] of the sizes and type of `like`.
+tempo_attn_heads attn_heads(PyObject* o, const at::Tensor& like) {
+  const at::Tensor& t = here(o);
+  if (t.dim() != 4 || t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type() || (t.size(3) != 1 && t.stride(3) != 1))
+    throw NotPlain{};
+  return {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+}
+struct Window {
+  int64_t B, Sq, Sk, heads, kv_heads, D, window, sinks;
+  float scale;
+  tempo_dtype dt;
+  Window(const at::Tensor& q, const at::Tensor& k, PyObject* w, PyObject* s, PyObject* by) : window(integer(w)), sinks(integer(s)) {
+    if ((q.scalar_type() != at::kFloat && q.scalar_type() != at::kBFloat16) || q.dim() != 4 || k.dim() != 4 ||
+        k.scalar_type() != q.scalar_type() || k.size(0) != q.size(0) || k.size(3) != q.size(3))
+      throw NotPlain{};
+    dt = q.scalar_type() == at::kFloat ? TEMPO_F32 : TEMPO_BF16;
+    B = q.size(0), Sq = q.size(1), heads = q.size(2), D = q.size(3);
+    Sk = k.size(1), kv_heads = k.size(2);
+    if (D < 1 || window < 1 || sinks < 0 || (heads > 0 && (kv_heads < 1 || heads % kv_heads != 0))) throw NotPlain{};
+    scale = by == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(D))) : real(by);
+    if (!(scale > 0.0f) || !std::isfinite(scale)) throw NotPlain{};
+  }
+};
+template <typename T>
+T* small_or_none(PyObject* o, at::ScalarType type, int64_t numel) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = here(o);
+  if (t.scalar_type() != type || t.numel() != numel || !t.is_contiguous()) throw NotPlain{};
+  return static_cast<T*>(t.data_ptr());
+}
+TEMPO_METHOD(window_attn_fwd) {  // q, k, v, out, lse, window, sinks, scale, key_len, query_start, workspace
+  return plain_call<11>(nargs, [&] {
+    const at::Tensor &tq = here(a[0]), &tk = here(a[1]);
+    const Window w(tq, tk, a[5], a[6], a[7]);
+    const tempo_attn_heads q = attn_heads(a[0], tq), k = attn_heads(a[1], tk), v = attn_heads(a[2], tk), out = attn_heads(a[3], tq);
+    float* lse = small_or_none<float>(a[4], at::kFloat, w.B * w.heads * w.Sq);
+    const auto *len = small_or_none<int32_t>(a[8], at::kInt, w.B), *start = small_or_none<int32_t>(a[9], at::kInt, w.B);
+    return [=, ws = Workspace(a[10], tq, tempo_window_attn_fwd_workspace_bytes(w.B, w.Sq, w.Sk, w.heads, w.kv_heads, w.D, w.window, w.sinks)),
+            st = stream()] {
+      return tempo_window_attn_fwd(&q, &k, &v, &out, lse, len, start, ws.p, ws.bytes, w.B, w.Sq, w.Sk, w.heads, w.kv_heads, w.D, w.window,
+                                   w.sinks, w.scale, w.dt, st);
+    };
+  });
+}
+// dout, q, k, v, out, lse, dq, dk, dv, window, sinks, scale, key_len, query_start, workspace
+TEMPO_METHOD(window_attn_bwd) {
+  return plain_call<15>(nargs, [&] {
+    const at::Tensor &tq = here(a[1]), &tk = here(a[2]);
+    const Window w(tq, tk, a[9], a[10], a[11]);
+    const tempo_attn_heads dout = attn_heads(a[0], tq), q = attn_heads(a[1], tq), k = attn_heads(a[2], tk), v = attn_heads(a[3], tk),
+                           out = attn_heads(a[4], tq), dq = attn_heads(a[6], tq), dk = attn_heads(a[7], tk), dv = attn_heads(a[8], tk);
+    if (a[5] == Py_None) throw NotPlain{};
+    const float* lse = small_or_none<float>(a[5], at::kFloat, w.B * w.heads * w.Sq);
+    const auto *len = small_or_none<int32_t>(a[12], at::kInt, w.B), *start = small_or_none<int32_t>(a[13], at::kInt, w.B);
+    return [=, ws = Workspace(a[14], tq, tempo_window_attn_bwd_workspace_bytes(w.B, w.Sq, w.Sk, w.heads, w.kv_heads, w.D, w.window, w.sinks)),
+            st = stream()] {
+      return tempo_window_attn_bwd(&dout, &q, &k, &v, &out, lse, &dq, &dk, &dv, len, start, ws.p, ws.bytes, w.B, w.Sq, w.Sk, w.heads,
+                                   w.kv_heads, w.D, w.window, w.sinks, w.scale, w.dt, st);
+    };
+  });
+}
+
 // ---- the encoder layer of modules.py ---------------------------------------------------------------------------
 // A float32 tensor of these sizes beside x.
 float* beside(const at::Tensor& x, PyObject* o, std::initializer_list<int64_t> sizes) {
@@ -626,6 +690,8 @@ PyMethodDef methods[] = {TEMPO_ENTRY(gelu_fwd),
                          TEMPO_ENTRY(rotary_bwd),
                          TEMPO_ENTRY(glu_fwd),
                          TEMPO_ENTRY(glu_bwd),
+                         TEMPO_ENTRY(window_attn_fwd),
+                         TEMPO_ENTRY(window_attn_bwd),
                          TEMPO_ENTRY(encoder_fwd),
                          TEMPO_ENTRY(encoder_bwd),
                          {nullptr, nullptr, 0, nullptr}};

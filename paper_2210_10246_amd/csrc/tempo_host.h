@@ -88,6 +88,20 @@ bool glu_takes(int64_t T, int64_t H, int64_t F);
 size_t glu_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt, bool back);
 tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st);
 tempo_status launch_glu_bwd(const GluCall& c, tempo_dtype dt, hipStream_t st);
+// What the two entry points of window attention take; each looks at its own.
+struct WindowCall {
+  const tempo_attn_heads *q, *k, *v, *out, *dout, *dq, *dk, *dv;
+  float* lse;
+  const int32_t *key_len, *query_start;
+  void* workspace;
+  size_t workspace_bytes;
+  int64_t B, Sq, Sk, heads, kv_heads, D, window, sinks;
+  float scale;
+};
+bool window_attn_takes(const WindowCall& c);
+size_t window_attn_workspace_bytes(const WindowCall& c, bool back);
+tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStream_t st);
+tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStream_t st);
 tempo_status launch_mask_bits_to_bytes(const uint32_t* bits, uint8_t* bytes, int64_t n,
                                        hipStream_t st);
 tempo_status launch_mask_bytes_to_bits(const uint8_t* bytes, uint32_t* bits, int64_t n,

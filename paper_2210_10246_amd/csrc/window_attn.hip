@@ -1,0 +1,809 @@
+// Attention with a sliding window and first tokens that stay visible, forward and backward, without a matrix of scores in memory:
+//   s_ij = scale q_i . k_j of the keys that row i sees,  lse_i = ln sum_j exp s_ij,  p_ij = exp(s_ij - lse_i),  out_i = sum_j p_ij v_j;
+//   delta_i = dout_i . out_i,  ds_ij = p_ij (dout_i . v_j - delta_i) scale,
+//   dq_i = sum_j ds_ij k_j,  dk_j = sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i.
+// Row i of a sequence stands at position P = query_start + i and sees the keys j <= P, j < key_len with j > P - window or j < sinks.
+//
+// The query heads that share a key head are rows of one problem: row r is query r / group of head r % group of them, so that a key is
+// read once for all of them, in a call for a single token too, and the gradients of a shared head are one sum.
+//
+// All products are on the matrix cores, 32 x 32 at a time, and made so that what a lane gets of one is what it has to give to the next:
+// of S^T = K Q^T lane n holds 16 keys of row n % 32, which is how a matrix instruction takes P^T for O^T = V^T P^T, whatever the
+// order of the keys, so long as the other operand has the same one.  Maximum, sum and what rescales the output are then one number a
+// lane.  The backward is made twice from S, once by rows (dq) and once by keys (dk, dv): 14 D operations a pair and not 10, but each
+// gradient is summed in one place in a fixed order, without atomics.
+#include <algorithm>
+#include <type_traits>
+
+#include "launch_split.h"
+#include "tempo_device.h"
+#include "tempo_host.h"
+
+namespace tempo {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kRows = 32 * kWaves;  // rows (or keys, in the backward by keys) of a workgroup, 32 of a wave
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kMinusInf = -__builtin_inff();
+
+struct Heads {
+  const void* p;
+  int64_t batch, token, head;  // elements
+};
+struct Attn {
+  Heads q, k, v, out, dout, dq, dk, dv;
+  float *lse, *delta;  // [B, heads, Sq]
+  const int32_t *key_len, *query_start;
+  int Sq, Sk, heads, kv_heads, group, rows, D;  // rows: Sq * group
+  FastDiv by_group;
+  int window, sinks;
+  float scale, c;  // c: scale log2(e)
+  int tiles, splits;
+  float *partial, *partial_lse;  // splits > 1: [splits, B kv_heads, rows, D] and [splits, B kv_heads, rows], of base 2
+};
+
+// Which keys the queries of a sequence see.
+struct Sight {
+  int64_t start;
+  int keys, window, sinks;
+  __device__ __forceinline__ Sight(const Attn& a, int b) : window(a.window) {
+    keys = a.key_len ? min(max(a.key_len[b], 0), a.Sk) : a.Sk;
+    start = a.query_start ? a.query_start[b] : int64_t{a.Sk} - a.Sq;
+    sinks = min(a.sinks, keys);
+  }
+  // keys [begin, end) and those below min(sinks, end)
+  __device__ __forceinline__ int end(int i) const {
+    const int64_t e = start + i + 1;
+    return e <= 0 ? 0 : e < keys ? static_cast<int>(e) : keys;
+  }
+  __device__ __forceinline__ int begin(int i) const {
+    const int64_t e = start + i + 1 - window;
+    return e <= 0 ? 0 : e < INT32_MAX ? static_cast<int>(e) : INT32_MAX;
+  }
+};
+
+// ---- matrices in LDS ----------------------------------------------------------------------------------------------------
+// Rows of DP elements in pieces of 16 bytes.  A matrix instruction takes 32 rows by two pieces (lane n: row n % 32, piece 2 s + n / 32)
+// or, transposed, 32 columns by the rows that a lane's sums of the other product lie in (4 (n / 32) + 0 .. 3 of each eight).
+// Pieces are stored in another order in each row so that the lanes of a read meet different banks.
+template <typename T, int DP>
+struct Rows {
+  static constexpr int V = Store<T>::kVec, P = DP / V, kPitch = P * 16, kSteps = P / 2;
+  static_assert(P >= 8, "");
+  __device__ static __forceinline__ int swizzle(int row) {
+    if constexpr (sizeof(T) == 4) return (row >> 2 & 1) << 3 | (row & 3) | (row >> 3 & 1) << 2;
+    else if constexpr (P == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    else return (row & 3) << 2 | (row >> 2 & 3);
+  }
+  __device__ static __forceinline__ u32x4 rows(const char* lds, int row0, int step) {
+    const int lane = threadIdx.x % kWave, row = row0 + lane % 32, piece = 2 * step + lane / 32;
+    return *reinterpret_cast<const u32x4*>(lds + row * kPitch + ((piece ^ swizzle(row)) << 4));
+  }
+};
+
+// 32 x 32 sums += 32 rows x two pieces of each operand.
+template <typename T>
+__device__ __forceinline__ f32x16 multiply(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(as_f32(a[e]), as_f32(b[e]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// The 16 sums of a lane as operands of the next product.  bfloat16: rounded, as its other operand is; the sums that they go into
+// are over hundreds of them.
+template <typename T>
+struct Weights;
+template <>
+struct Weights<bf16_t> {
+  u32x4 w[2];
+  __device__ __forceinline__ explicit Weights(const f32x16& p) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i / 4][i % 4] = pack_bf16(p[2 * i], p[2 * i + 1]);
+  }
+};
+template <>
+struct Weights<float> {
+  f32x16 w;
+  __device__ __forceinline__ explicit Weights(const f32x16& p) : w(p) {}
+};
+
+// sums[columns 32 block .. + 31] += transposed 32 rows of LDS x weights
+template <typename T, int DP>
+__device__ __forceinline__ f32x16 multiply_columns(const char* lds, int row0, int block, const Weights<T>& w, f32x16 c) {
+  using R = Rows<T, DP>;
+  const int lane = threadIdx.x % kWave;
+  if constexpr (sizeof(T) == 2) {
+    // 16 lanes read 4 rows of 16 columns, 4 columns each, and get 4 rows of a column each
+    const int j = lane % 16, line = row0 + 4 * (lane / 32) + j / 4, piece = block * 4 + (lane / 16 & 1) * 2 + (j % 4) / 2;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      union {
+        s16x4 h[2];
+        bf16x8 all;
+      } a;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int r = line + 16 * u + 8 * n;
+        a.h[n] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + r * R::kPitch + ((piece ^ R::swizzle(r)) << 4) + (j & 1) * 8));
+      }
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.all, __builtin_bit_cast(bf16x8, w.w[u]), c, 0, 0, 0);
+    }
+  } else {
+    const int column = block * 32 + lane % 32;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = row0 + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
+      const float a = *reinterpret_cast<const float*>(lds + r * R::kPitch + ((column / 4 ^ R::swizzle(r)) << 4) + column % 4 * 4);
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[i], c, 0, 0, 0);
+    }
+  }
+  return c;
+}
+
+// Piece `piece` of a row of D elements at any address; zeros behind its end.
+template <typename T>
+__device__ __forceinline__ u32x4 load_of_row(const T* row, int piece, int D) {
+  constexpr int V = Store<T>::kVec;
+  const int left = D - piece * V;
+  if (left >= V) return *reinterpret_cast<const u32x4_any*>(row + piece * V);
+  float e[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) e[j] = j < left ? Store<T>::load1(row + piece * V + j) : 0.0f;
+  return Store<T>::pack(e);
+}
+
+// N rows of a matrix on their way to LDS by way of registers.
+template <typename T, int DP, int N>
+struct Staged {
+  using R = Rows<T, DP>;
+  static constexpr int kPieces = N * R::P / kThreads;
+  static_assert(N * R::P % kThreads == 0, "whole pieces a lane");
+  u32x4 v[kPieces];
+  // row_at: row -> its elements, or null for zeros
+  template <typename F>
+  __device__ __forceinline__ void load(int D, F&& row_at) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = i * kThreads + static_cast<int>(threadIdx.x), row = at / R::P, piece = at % R::P ^ R::swizzle(row);
+      const T* p = row_at(row);
+      v[i] = p ? load_of_row<T>(p, piece, D) : u32x4{0, 0, 0, 0};
+    }
+  }
+  __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) *reinterpret_cast<u32x4*>(lds + (i * kThreads + static_cast<int>(threadIdx.x)) * 16) = v[i];
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ const T* at(const Heads& h, int b, int token, int head) {
+  return static_cast<const T*>(h.p) + b * h.batch + token * h.token + head * h.head;
+}
+
+// A lane's sums of column block `block` to a row of D elements: 8 (i / 4) + 4 (lane / 32) + i % 4 are four neighbours each.
+template <typename T>
+__device__ __forceinline__ void store_sums(T* row, int D, int block, const f32x16& s, float by) {
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int d = block * 32 + 8 * n + 4 * (lane / 32), left = D - d;
+    const float v[4] = {s[4 * n] * by, s[4 * n + 1] * by, s[4 * n + 2] * by, s[4 * n + 3] * by};
+    if (left >= 4) {
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_any*>(row + d) = f32x4{v[0], v[1], v[2], v[3]};
+      else *reinterpret_cast<u32x2_any*>(row + d) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < left) Store<T>::store1(row + d + e, v[e]);
+    }
+  }
+}
+__device__ __forceinline__ f32x16 zeros() { return f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}; }
+
+// Neighbouring workgroups go to different XCDs, each with an L2 of its own: every XCD takes a run of them.
+__device__ __forceinline__ int in_order(int block, int total) {
+  const int xcd = block % 8, each = total / 8, more = total % 8;
+  return xcd * each + min(xcd, more) + block / 8;
+}
+
+// The key tiles that the rows of a workgroup see: those of the first keys, then those of the window.
+struct KeyTiles {
+  int of_sinks, first, count;
+  int low, high;  // of the window; keys from high on are seen by none
+  __device__ __forceinline__ KeyTiles(const Sight& s, int i0, int i1, int keys) {
+    low = s.begin(i0);
+    high = s.end(i1);
+    of_sinks = (min(s.sinks, high) + keys - 1) / keys;
+    first = max(low / keys, of_sinks);
+    count = of_sinks + max((high + keys - 1) / keys - first, 0);
+  }
+  __device__ __forceinline__ int key(int n, int keys) const { return (n < of_sinks ? n : first + n - of_sinks) * keys; }
+};
+
+// What a wave's 32 rows see of keys [j0, j0 + n).
+struct WaveRows {
+  int r0, row, i, g;        // the wave's first row, the lane's, its query and head
+  bool any;                 // rows that exist
+  int begin, end;           // of the lane
+  int first_begin, last_begin, first_end, last_end;
+  __device__ __forceinline__ WaveRows(const Attn& a, const Sight& s, int r0_) : r0(r0_), any(r0_ < a.rows) {
+    const int lane = threadIdx.x % kWave, last = a.rows - 1;
+    row = min(r0 + lane % 32, last);
+    i = a.by_group.divide(row);
+    g = row - i * a.group;
+    begin = s.begin(i);
+    end = s.end(i);
+    const int i0 = a.by_group.divide(min(r0, last)), i1 = a.by_group.divide(min(r0 + 31, last));
+    first_begin = s.begin(i0), last_begin = s.begin(i1), first_end = s.end(i0), last_end = s.end(i1);
+  }
+  __device__ __forceinline__ bool none(const Sight& s, int j0, int n) const {
+    return j0 >= last_end || (j0 + n <= first_begin && j0 >= s.sinks);
+  }
+  __device__ __forceinline__ bool all(const Sight& s, int j0, int n) const {
+    return j0 + n <= first_end && (j0 >= last_begin || j0 + n <= s.sinks);
+  }
+  __device__ __forceinline__ bool sees(const Sight& s, int j) const { return j < end && (j >= begin || j < s.sinks); }
+};
+__device__ __forceinline__ int key_of(int i) { return 8 * (i / 4) + 4 * (static_cast<int>(threadIdx.x) % kWave / 32) + i % 4; }
+
+// ---- forward ------------------------------------------------------------------------------------------------------------
+template <typename T, int DP, int BK>
+__global__ __launch_bounds__(kThreads) void forward_kernel(Attn a) {
+  using R = Rows<T, DP>;
+  constexpr int kBytes = BK * R::kPitch, kBlocks = BK / 32, kColumns = DP / 32;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][kBytes];
+  const int job = in_order(blockIdx.x, gridDim.x), split = job % a.splits, tile = job / a.splits % a.tiles;
+  const int bk = job / a.splits / a.tiles, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
+  const Sight s(a, b);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int first_row = tile * kRows, last_row = min(first_row + kRows, a.rows) - 1;
+  const KeyTiles keys(s, a.by_group.divide(first_row), a.by_group.divide(last_row), BK);
+  const int each = (keys.count + a.splits - 1) / a.splits, n0 = split * each, n1 = min(n0 + each, keys.count);
+  const WaveRows w(a, s, first_row + wave * 32);
+  u32x4 q[R::kSteps];
+  {
+    const T* row = at<T>(a.q, b, w.i, kv * a.group + w.g);
+#pragma unroll
+    for (int p = 0; p < R::kSteps; ++p) q[p] = load_of_row<T>(row, 2 * p + threadIdx.x % kWave / 32, a.D);
+  }
+  f32x16 acc[kColumns];
+#pragma unroll
+  for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
+  float m = kMinusInf, sum = 0.0f;  // maximum, of base 2, and the lane's part of the sum
+  Staged<T, DP, BK> ks, vs;
+  auto fetch = [&](int n) {
+    const int j0 = keys.key(n, BK);
+    auto there = [&](int r) { return j0 + r < keys.high && (j0 + r >= keys.low || j0 + r < s.sinks); };
+    ks.load(a.D, [&](int r) { return there(r) ? at<T>(a.k, b, j0 + r, kv) : nullptr; });
+    vs.load(a.D, [&](int r) { return there(r) ? at<T>(a.v, b, j0 + r, kv) : nullptr; });
+  };
+  if (n0 < n1) {
+    fetch(n0);
+    ks.store(lds[0][0]);
+    vs.store(lds[0][1]);
+    lds_barrier();
+  }
+  for (int n = n0; n < n1; ++n) {
+    const int j0 = keys.key(n, BK), now = (n - n0) & 1;
+    if (n + 1 < n1) fetch(n + 1);
+    if (w.any && !w.none(s, j0, BK)) {
+      f32x16 p[kBlocks];
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb) {
+        p[kb] = zeros();
+#pragma unroll
+        for (int t = 0; t < R::kSteps; ++t) p[kb] = multiply<T>(R::rows(lds[now][0], kb * 32, t), q[t], p[kb]);
+      }
+      if (!w.all(s, j0, BK)) {
+#pragma unroll
+        for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p[kb][i] = w.sees(s, j0 + kb * 32 + key_of(i)) ? p[kb][i] : kMinusInf;
+      }
+      float top = p[0][0];
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, p[kb][i]);
+      top = a.c * across_rows<32>(top, [](float x, float y) { return fmaxf(x, y); });
+      // What the exponentials are relative to follows the maximum only where they would pass 2^8: nothing is lost below that.
+      if (__any(top > m + 8.0f)) {
+        const float next = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (next == kMinusInf ? 0.0f : next));
+        m = next;
+        sum *= by;
+#pragma unroll
+        for (int d = 0; d < kColumns; ++d) acc[d] *= by;
+      }
+      const float from = m == kMinusInf ? 0.0f : m;
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          p[kb][i] = __builtin_amdgcn_exp2f(fmaf(p[kb][i], a.c, -from));
+          sum += p[kb][i];
+        }
+        const Weights<T> weights(p[kb]);
+#pragma unroll
+        for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(lds[now][1], kb * 32, d, weights, acc[d]);
+      }
+    }
+    if (n + 1 < n1) {
+      ks.store(lds[now ^ 1][0]);
+      vs.store(lds[now ^ 1][1]);
+    }
+    lds_barrier();
+  }
+  if (w.r0 + static_cast<int>(threadIdx.x) % 32 >= a.rows) return;
+  sum = across_rows<32>(sum, [](float x, float y) { return x + y; });
+  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float lse = sum == 0.0f ? kMinusInf : m + __builtin_amdgcn_logf(sum);
+  const bool first_half = threadIdx.x % kWave < 32;
+  if (a.splits > 1) {
+    const int64_t at_row = (static_cast<int64_t>(split) * (gridDim.x / (a.splits * a.tiles)) + bk) * a.rows + w.row;
+    if (first_half) a.partial_lse[at_row] = lse;
+#pragma unroll
+    for (int d = 0; d < kColumns; ++d) store_sums(a.partial + at_row * a.D, a.D, d, acc[d], by);
+  } else {
+    const int head = kv * a.group + w.g;
+    if (a.lse && first_half) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + w.i] = lse * kLn2;
+    T* const row = const_cast<T*>(at<T>(a.out, b, w.i, head));
+#pragma unroll
+    for (int d = 0; d < kColumns; ++d) store_sums(row, a.D, d, acc[d], by);
+  }
+}
+
+// The parts of a row, each weighted by its sum of exponentials: a wave a row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void join_kernel(Attn a, int64_t all) {
+  const int64_t at_row = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.x / kWave;
+  if (at_row >= all) return;
+  const int lane = threadIdx.x % kWave;
+  float top = kMinusInf;
+  for (int p = 0; p < a.splits; ++p) top = fmaxf(top, a.partial_lse[p * all + at_row]);
+  const float from = top == kMinusInf ? 0.0f : top;
+  float sum = 0.0f, out[4] = {0, 0, 0, 0};
+  for (int p = 0; p < a.splits; ++p) {
+    const float by = __builtin_amdgcn_exp2f(a.partial_lse[p * all + at_row] - from);
+    sum += by;
+    const float* o = a.partial + (p * all + at_row) * a.D;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (lane + e * kWave < a.D) out[e] = fmaf(by, o[lane + e * kWave], out[e]);
+  }
+  const int bk = static_cast<int>(at_row / a.rows), row = static_cast<int>(at_row - static_cast<int64_t>(bk) * a.rows);
+  const int b = bk / a.kv_heads, i = a.by_group.divide(row), head = (bk - b * a.kv_heads) * a.group + row - i * a.group;
+  if (a.lse && lane == 0)
+    a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + i] = sum == 0.0f ? kMinusInf : (from + __builtin_amdgcn_logf(sum)) * kLn2;
+  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+  T* const to = const_cast<T*>(at<T>(a.out, b, i, head));
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (lane + e * kWave < a.D) Store<T>::store1(to + lane + e * kWave, out[e] * by);
+}
+
+// ---- backward by rows: delta and dq ---------------------------------------------------------------------------------------
+template <typename T, int DP, int BK>
+__global__ __launch_bounds__(kThreads) void rows_kernel(Attn a) {
+  using R = Rows<T, DP>;
+  constexpr int kBytes = BK * R::kPitch, kBlocks = BK / 32, kColumns = DP / 32;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][kBytes];
+  const int job = in_order(blockIdx.x, gridDim.x), tile = job % a.tiles;
+  const int bk = job / a.tiles, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
+  const Sight s(a, b);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int first_row = tile * kRows, last_row = min(first_row + kRows, a.rows) - 1;
+  const KeyTiles keys(s, a.by_group.divide(first_row), a.by_group.divide(last_row), BK);
+  const WaveRows w(a, s, first_row + wave * 32);
+  const int head = kv * a.group + w.g, half = threadIdx.x % kWave / 32;
+  const int64_t stat = (static_cast<int64_t>(b) * a.heads + head) * a.Sq + w.i;
+  u32x4 q[R::kSteps], dout[R::kSteps];
+  float delta = 0.0f;
+  {
+    const T *qr = at<T>(a.q, b, w.i, head), *dr = at<T>(a.dout, b, w.i, head), *orow = at<T>(a.out, b, w.i, head);
+#pragma unroll
+    for (int p = 0; p < R::kSteps; ++p) {
+      q[p] = load_of_row<T>(qr, 2 * p + half, a.D);
+      dout[p] = load_of_row<T>(dr, 2 * p + half, a.D);
+      float x[R::V], y[R::V];
+      Store<T>::unpack(dout[p], x);
+      Store<T>::unpack(load_of_row<T>(orow, 2 * p + half, a.D), y);
+#pragma unroll
+      for (int e = 0; e < R::V; ++e) delta = fmaf(x[e], y[e], delta);
+    }
+    delta = across_rows<32>(delta, [](float x, float y) { return x + y; });
+  }
+  const bool exists = w.r0 + static_cast<int>(threadIdx.x) % 32 < a.rows;
+  if (exists && half == 0) a.delta[stat] = delta;
+  const float lse = a.lse[stat] * kLog2e;
+  f32x16 acc[kColumns];
+#pragma unroll
+  for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
+  Staged<T, DP, BK> ks, vs;
+  auto fetch = [&](int n) {
+    const int j0 = keys.key(n, BK);
+    auto there = [&](int r) { return j0 + r < keys.high && (j0 + r >= keys.low || j0 + r < s.sinks); };
+    ks.load(a.D, [&](int r) { return there(r) ? at<T>(a.k, b, j0 + r, kv) : nullptr; });
+    vs.load(a.D, [&](int r) { return there(r) ? at<T>(a.v, b, j0 + r, kv) : nullptr; });
+  };
+  if (keys.count > 0) {
+    fetch(0);
+    ks.store(lds[0][0]);
+    vs.store(lds[0][1]);
+    lds_barrier();
+  }
+  for (int n = 0; n < keys.count; ++n) {
+    const int j0 = keys.key(n, BK), now = n & 1;
+    if (n + 1 < keys.count) fetch(n + 1);
+    if (w.any && !w.none(s, j0, BK)) {
+      const bool all = w.all(s, j0, BK);
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb) {
+        f32x16 p = zeros(), dp = zeros();
+#pragma unroll
+        for (int t = 0; t < R::kSteps; ++t) {
+          p = multiply<T>(R::rows(lds[now][0], kb * 32, t), q[t], p);
+          dp = multiply<T>(R::rows(lds[now][1], kb * 32, t), dout[t], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float ds = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - delta);
+          p[i] = all || w.sees(s, j0 + kb * 32 + key_of(i)) ? ds : 0.0f;
+        }
+        const Weights<T> weights(p);
+#pragma unroll
+        for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(lds[now][0], kb * 32, d, weights, acc[d]);
+      }
+    }
+    if (n + 1 < keys.count) {
+      ks.store(lds[now ^ 1][0]);
+      vs.store(lds[now ^ 1][1]);
+    }
+    lds_barrier();
+  }
+  if (!exists) return;
+  T* const to = const_cast<T*>(at<T>(a.dq, b, w.i, head));
+#pragma unroll
+  for (int d = 0; d < kColumns; ++d) store_sums(to, a.D, d, acc[d], a.scale);
+}
+
+// ---- backward by keys: dk and dv ------------------------------------------------------------------------------------------
+// The rows that see a tile of keys are those of its window, or all behind it where one of its keys is one of the first.  A tile's rows
+// may be taken in several parts, whose sums are joined in their order.
+struct KeyJobs {
+  int tiles, sink_tiles;            // of kRows keys; the first sink_tiles have first keys
+  int parts, sink_parts;            // of a tile's rows
+  int part_rows, sink_part_rows;
+  int64_t sink_jobs;
+  float *partial, *sink_partial;    // [job][2][kRows][D], where there is more than one part
+};
+enum Wanted { kBoth, kOnlyV, kOnlyK };
+
+template <typename T, int DP, Wanted WANTED>
+__global__ __launch_bounds__(kThreads) void keys_kernel(Attn a, KeyJobs jobs) {
+  using R = Rows<T, DP>;
+  constexpr int BQ = sizeof(T) == 2 && DP == 64 ? 64 : 32, kBytes = BQ * R::kPitch, kColumns = DP / 32;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][kBytes];
+  __shared__ __attribute__((aligned(16))) float stats[2][2][BQ];  // lse of base 2, delta
+  __shared__ __attribute__((aligned(16))) int sight[2][2][BQ];    // begin, end
+  int64_t job = blockIdx.x;
+  const bool of_sinks = job < jobs.sink_jobs;
+  if (!of_sinks) job -= jobs.sink_jobs;
+  const int parts = of_sinks ? jobs.sink_parts : jobs.parts, part_rows = of_sinks ? jobs.sink_part_rows : jobs.part_rows;
+  const int tiles = of_sinks ? jobs.sink_tiles : jobs.tiles - jobs.sink_tiles;
+  if (!of_sinks) job = in_order(static_cast<int>(job), static_cast<int>(gridDim.x - jobs.sink_jobs));
+  const int part = static_cast<int>(job % parts), tile = static_cast<int>(job / parts % tiles) + (of_sinks ? 0 : jobs.sink_tiles);
+  const int bk = static_cast<int>(job / parts / tiles), b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
+  const Sight s(a, b);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
+  const int key0 = tile * kRows, wave_key = key0 + wave * 32, key = wave_key + lane % 32;
+  // rows [r, end) of this part
+  int r_first, r_end;
+  {
+    const int64_t i0 = key0 - s.start, last = min(key0 + kRows, s.keys) - 1;
+    const int64_t i1 = key0 < s.sinks ? int64_t{a.Sq} : last + s.window - s.start;
+    const int64_t from = (i0 > 0 ? i0 : 0) * a.group, to = (i1 < a.Sq ? i1 : int64_t{a.Sq}) * a.group;
+    const int64_t first = from + static_cast<int64_t>(part) * part_rows, end = first + part_rows < to ? first + part_rows : to;
+    const bool none = key0 >= s.keys || first >= end;
+    r_first = none ? 0 : static_cast<int>(first);
+    r_end = none ? 0 : static_cast<int>(end);
+  }
+  u32x4 k[R::kSteps], v[R::kSteps];
+  {
+    const int there = min(key, a.Sk - 1);
+    const T *kr = at<T>(a.k, b, there, kv), *vr = at<T>(a.v, b, there, kv);
+#pragma unroll
+    for (int p = 0; p < R::kSteps; ++p) {
+      k[p] = load_of_row<T>(kr, 2 * p + half, a.D);
+      if (WANTED != kOnlyV) v[p] = load_of_row<T>(vr, 2 * p + half, a.D);
+    }
+  }
+  constexpr bool kK = WANTED != kOnlyV, kV = WANTED != kOnlyK;
+  f32x16 dk[kK ? kColumns : 1], dv[kV ? kColumns : 1];
+#pragma unroll
+  for (int d = 0; d < (kK ? kColumns : 1); ++d) dk[d] = zeros();
+#pragma unroll
+  for (int d = 0; d < (kV ? kColumns : 1); ++d) dv[d] = zeros();
+  Staged<T, DP, BQ> qs, os;
+  float stat_lse = 0.0f, stat_delta = 0.0f;
+  int stat_begin = 0, stat_end = 0;
+  auto fetch = [&](int r0) {
+    auto row = [&](const Heads& h, int r) -> const T* {
+      if (r0 + r >= r_end) return nullptr;
+      const int i = a.by_group.divide(r0 + r);
+      return at<T>(h, b, i, kv * a.group + r0 + r - i * a.group);
+    };
+    qs.load(a.D, [&](int r) { return row(a.q, r); });
+    os.load(a.D, [&](int r) { return row(a.dout, r); });
+    const int r = r0 + static_cast<int>(threadIdx.x);
+    if (threadIdx.x < BQ) {
+      stat_end = 0;
+      if (r < r_end) {
+        const int i = a.by_group.divide(r);
+        const int64_t stat = (static_cast<int64_t>(b) * a.heads + kv * a.group + r - i * a.group) * a.Sq + i;
+        stat_lse = a.lse[stat] * kLog2e;
+        stat_delta = a.delta[stat];
+        stat_begin = s.begin(i);
+        stat_end = s.end(i);
+      }
+    }
+  };
+  auto put = [&](int to) {
+    qs.store(lds[to][0]);
+    os.store(lds[to][1]);
+    if (threadIdx.x < BQ) {
+      stats[to][0][threadIdx.x] = stat_lse;
+      stats[to][1][threadIdx.x] = stat_delta;
+      sight[to][0][threadIdx.x] = stat_begin;
+      sight[to][1][threadIdx.x] = stat_end;
+    }
+  };
+  if (r_first < r_end) {
+    fetch(r_first);
+    put(0);
+    lds_barrier();
+  }
+  int now = 0;
+  for (int r0 = r_first; r0 < r_end; r0 += BQ, now ^= 1) {
+    if (r0 + BQ < r_end) fetch(r0 + BQ);
+#pragma unroll
+    for (int rb = 0; rb < BQ; rb += 32) {
+      const int r1 = r0 + rb, r2 = min(r1 + 32, r_end) - 1;  // the block's first and last row
+      if (r1 > r2) continue;
+      const int i1 = a.by_group.divide(r1), i2 = a.by_group.divide(r2);
+      if (s.end(i2) <= wave_key || (s.begin(i1) > wave_key + 31 && wave_key >= s.sinks)) continue;
+      const bool all = r2 == r1 + 31 && s.end(i1) >= wave_key + 32 && (s.begin(i2) <= wave_key || wave_key + 32 <= s.sinks);
+      f32x16 p = zeros(), dp = zeros();
+#pragma unroll
+      for (int t = 0; t < R::kSteps; ++t) {
+        p = multiply<T>(R::rows(lds[now][0], rb, t), k[t], p);
+        if (kK) dp = multiply<T>(R::rows(lds[now][1], rb, t), v[t], dp);
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {  // rows 8 n + 4 half .. + 3
+        const int r = rb + 8 * n + 4 * half;
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(&stats[now][0][r]), delta = *reinterpret_cast<const f32x4*>(&stats[now][1][r]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool seen = all || (key < sight[now][1][r + e] && (key >= sight[now][0][r + e] || key < s.sinks));
+          const float x = __builtin_amdgcn_exp2f(fmaf(p[4 * n + e], a.c, -lse[e]));
+          p[4 * n + e] = seen ? x : 0.0f;
+          if (kK) dp[4 * n + e] = seen ? x * (dp[4 * n + e] - delta[e]) : 0.0f;
+        }
+      }
+      if constexpr (kV) {
+        const Weights<T> weights(p);
+#pragma unroll
+        for (int d = 0; d < kColumns; ++d) dv[d] = multiply_columns<T, DP>(lds[now][1], rb, d, weights, dv[d]);
+      }
+      if constexpr (kK) {
+        const Weights<T> weights(dp);
+#pragma unroll
+        for (int d = 0; d < kColumns; ++d) dk[d] = multiply_columns<T, DP>(lds[now][0], rb, d, weights, dk[d]);
+      }
+    }
+    if (r0 + BQ < r_end) put(now ^ 1);
+    lds_barrier();
+  }
+  if (parts > 1) {
+    float* const to = (of_sinks ? jobs.sink_partial : jobs.partial) +
+                      (job * 2 * kRows + wave * 32 + lane % 32) * static_cast<int64_t>(a.D);
+    if constexpr (kK) {
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d) store_sums(to, a.D, d, dk[d], a.scale);
+    }
+    if constexpr (kV) {
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d) store_sums(to + static_cast<int64_t>(kRows) * a.D, a.D, d, dv[d], 1.0f);
+    }
+  } else if (key < a.Sk) {
+    if constexpr (kK) {
+      T* const to = const_cast<T*>(at<T>(a.dk, b, key, kv));
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d) store_sums(to, a.D, d, dk[d], a.scale);
+    }
+    if constexpr (kV) {
+      T* const to = const_cast<T*>(at<T>(a.dv, b, key, kv));
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d) store_sums(to, a.D, d, dv[d], 1.0f);
+    }
+  }
+}
+
+// The parts of dk and dv of a key, in their order: a wave a key and gradient.  tiles0: the first tile of these.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, const float* partial, int parts, int tiles0, int tiles, int64_t all) {
+  const int64_t n = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.x / kWave;  // (bk, tile, gradient, key)
+  if (n >= all) return;
+  const int lane = threadIdx.x % kWave, in_tile = static_cast<int>(n % kRows), of_v = static_cast<int>(n / kRows % 2);
+  const int64_t of_tile = n / (2 * kRows);
+  const int tile = static_cast<int>(of_tile % tiles), bk = static_cast<int>(of_tile / tiles), b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
+  const int key = (tiles0 + tile) * kRows + in_tile;
+  if (key >= a.Sk) return;
+  const Heads& h = of_v ? a.dv : a.dk;
+  T* const to = const_cast<T*>(at<T>(h, b, key, kv));
+  for (int d = lane; d < a.D; d += kWave) {
+    float sum = 0.0f;
+    for (int p = 0; p < parts; ++p) sum += partial[(((of_tile * parts + p) * 2 + of_v) * kRows + in_tile) * a.D + d];
+    Store<T>::store1(to + d, sum);
+  }
+}
+
+// ---- plans ----------------------------------------------------------------------------------------------------------------
+int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
+
+// Parts of the keys of a forward: enough workgroups for the chip where there are few rows, of at least two tiles of keys each.
+int forward_splits(const WindowCall& c) {
+  const int64_t rows = c.Sq * (c.heads / c.kv_heads), blocks = up(rows, kRows) * c.B * c.kv_heads;
+  const int64_t span = std::min(c.Sk, c.window + c.Sq) + std::min(c.sinks, c.Sk), most = std::max<int64_t>(up(span, 128), 1);
+  if (blocks == 0 || blocks >= compute_units()) return 1;
+  return static_cast<int>(std::min<int64_t>(std::min<int64_t>(most, 64), up(2 * compute_units(), blocks)));
+}
+struct KeyPlan {
+  KeyJobs jobs;
+  int64_t blocks, partial_floats, sink_floats;
+};
+KeyPlan key_plan(const WindowCall& c) {
+  KeyPlan p{};
+  const int64_t group = c.heads / c.kv_heads, bk = c.B * c.kv_heads, tiles = up(c.Sk, kRows);
+  const int64_t sink_tiles = std::min(tiles, up(c.sinks, kRows)), others = tiles - sink_tiles;
+  const int64_t span = std::min(c.Sq, c.window + kRows) * group, all = c.Sq * group, cus = compute_units();
+  const int64_t want = up(2 * cus, std::max<int64_t>(bk * tiles, 1));
+  p.jobs.tiles = static_cast<int>(tiles);
+  p.jobs.sink_tiles = static_cast<int>(sink_tiles);
+  p.jobs.parts = static_cast<int>(std::max<int64_t>(1, std::min({want, up(span, 128), int64_t{64}})));
+  p.jobs.part_rows = static_cast<int>(std::max<int64_t>(up(up(span, p.jobs.parts), 32), 1) * 32);
+  const int64_t sink_want = std::min(up(all, p.jobs.part_rows), up(4 * cus, std::max<int64_t>(bk * sink_tiles, 1)));
+  p.jobs.sink_parts = static_cast<int>(std::max<int64_t>(1, sink_want));
+  p.jobs.sink_part_rows = static_cast<int>(std::min<int64_t>(up(up(all, p.jobs.sink_parts), 32) * 32, INT32_MAX));
+  p.jobs.sink_jobs = bk * sink_tiles * p.jobs.sink_parts;
+  const int64_t other_jobs = bk * others * p.jobs.parts;
+  p.blocks = p.jobs.sink_jobs + other_jobs;
+  p.sink_floats = p.jobs.sink_parts > 1 ? p.jobs.sink_jobs * 2 * kRows * c.D : 0;
+  p.partial_floats = p.jobs.parts > 1 ? other_jobs * 2 * kRows * c.D : 0;
+  return p;
+}
+
+Heads heads_of(const tempo_attn_heads* h) { return h ? Heads{h->p, h->batch, h->token, h->head} : Heads{}; }
+Attn attn_of(const WindowCall& c) {
+  Attn a{};
+  a.q = heads_of(c.q), a.k = heads_of(c.k), a.v = heads_of(c.v), a.out = heads_of(c.out);
+  a.dout = heads_of(c.dout), a.dq = heads_of(c.dq), a.dk = heads_of(c.dk), a.dv = heads_of(c.dv);
+  a.lse = c.lse;
+  a.key_len = c.key_len, a.query_start = c.query_start;
+  a.Sq = static_cast<int>(c.Sq), a.Sk = static_cast<int>(c.Sk), a.heads = static_cast<int>(c.heads), a.kv_heads = static_cast<int>(c.kv_heads);
+  a.group = a.heads / a.kv_heads;
+  a.rows = a.Sq * a.group;
+  a.D = static_cast<int>(c.D);
+  a.by_group = FastDiv(static_cast<uint32_t>(a.group));
+  a.window = static_cast<int>(std::min<int64_t>(c.window, INT32_MAX));
+  a.sinks = static_cast<int>(std::min<int64_t>(c.sinks, c.Sk));
+  a.scale = c.scale;
+  a.c = c.scale * kLog2e;
+  a.tiles = static_cast<int>(up(a.rows, kRows));
+  a.splits = 1;
+  return a;
+}
+
+template <typename F>
+tempo_status with_width(int64_t D, F&& f) {
+  if (D <= 64) return f(std::integral_constant<int, 64>{});
+  if (D <= 128) return f(std::integral_constant<int, 128>{});
+  return f(std::integral_constant<int, 256>{});
+}
+template <typename F>
+tempo_status with_type(tempo_dtype dt, F&& f) {
+  return dt == TEMPO_F32 ? f(float{}) : f(bf16_t{});
+}
+template <typename K, typename... Args>
+tempo_status launch(K kernel, int64_t blocks, hipStream_t st, const Args&... args) {
+  if (blocks == 0) return TEMPO_OK;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, st, args...);
+  return launch_status();
+}
+
+}  // namespace
+
+// Launches of less than 2^32 lanes, and numbers of jobs that an int holds.
+bool window_attn_takes(const WindowCall& c) {
+  constexpr int64_t most = int64_t{1} << 23;
+  const int64_t bk = c.B * c.kv_heads, rows = c.Sq * (c.heads / c.kv_heads);
+  if (c.D > 256 || rows > INT32_MAX - kRows || up(rows, kRows) * bk > most || up(c.Sk, kRows) * bk > most / 2 || bk * rows > int64_t{1} << 32)
+    return false;
+  return key_plan(c).blocks <= most;
+}
+
+size_t window_attn_workspace_bytes(const WindowCall& c, bool back) {
+  const int64_t rows = c.B * c.heads * c.Sq;
+  if (!back) {
+    const int splits = forward_splits(c);
+    return splits > 1 ? static_cast<size_t>(splits) * rows * (c.D + 1) * sizeof(float) : 0;
+  }
+  const KeyPlan p = key_plan(c);
+  return static_cast<size_t>(up(rows, 4) * 4 + p.sink_floats + p.partial_floats) * sizeof(float);
+}
+
+tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStream_t st) {
+  if (c.workspace_bytes < window_attn_workspace_bytes(c, false)) return TEMPO_ERR_WORKSPACE;
+  Attn a = attn_of(c);
+  a.splits = forward_splits(c);
+  const int64_t all = c.B * c.heads * c.Sq;
+  if (a.splits > 1) {
+    a.partial = static_cast<float*>(c.workspace);
+    a.partial_lse = a.partial + a.splits * all * c.D;
+  }
+  const int64_t blocks = c.B * c.kv_heads * a.tiles * a.splits;
+  return with_type(dt, [&](auto type) {
+    using T = decltype(type);
+    const tempo_status s = with_width(c.D, [&](auto width) {
+      constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 ? 64 : 32;
+      return launch(forward_kernel<T, DP, BK>, blocks, st, a);
+    });
+    if (s != TEMPO_OK || a.splits == 1) return s;
+    return launch(join_kernel<T>, up(all, kWaves), st, a, all);
+  });
+}
+
+tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStream_t st) {
+  if (c.workspace_bytes < window_attn_workspace_bytes(c, true)) return TEMPO_ERR_WORKSPACE;
+  Attn a = attn_of(c);
+  a.delta = static_cast<float*>(c.workspace);
+  KeyPlan p = key_plan(c);
+  p.jobs.sink_partial = a.delta + up(c.B * c.heads * c.Sq, 4) * 4;
+  p.jobs.partial = p.jobs.sink_partial + p.sink_floats;
+  return with_type(dt, [&](auto type) {
+    using T = decltype(type);
+    tempo_status s = with_width(c.D, [&](auto width) {
+      constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 ? 64 : 32;
+      tempo_status r = a.rows > 0 ? launch(rows_kernel<T, DP, BK>, c.B * c.kv_heads * a.tiles, st, a) : TEMPO_OK;
+      if (r != TEMPO_OK) return r;
+      if constexpr (sizeof(T) * DP > 512) {  // both gradients' sums of 256 float32 elements do not fit into a wave's registers
+        r = launch(keys_kernel<T, DP, kOnlyV>, p.blocks, st, a, p.jobs);
+        return r != TEMPO_OK ? r : launch(keys_kernel<T, DP, kOnlyK>, p.blocks, st, a, p.jobs);
+      } else {
+        return launch(keys_kernel<T, DP, kBoth>, p.blocks, st, a, p.jobs);
+      }
+    });
+    const int64_t each = c.B * c.kv_heads * 2 * kRows;
+    auto join = [&](const float* partial, int parts, int tiles0, int tiles) {
+      if (s != TEMPO_OK || parts <= 1 || tiles == 0) return;
+      s = launch(join_keys_kernel<T>, up(each * tiles, kWaves), st, a, partial, parts, tiles0, tiles, each * tiles);
+    };
+    join(p.jobs.sink_partial, p.jobs.sink_parts, 0, p.jobs.sink_tiles);
+    join(p.jobs.partial, p.jobs.parts, p.jobs.sink_tiles, p.jobs.tiles - p.jobs.sink_tiles);
+    return s;
+  });
+}
+
+}  // namespace tempo
