@@ -258,6 +258,62 @@ TEMPO_API tempo_status tempo_rotary_bwd(const tempo_rotary_heads* dq, const temp
                               tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream);
 
 /*
+ * Rotary positions with several axes (of images and video: time, height, width): as above, but pair i turns by the position on axis axes[i],
+ *   theta[b,s,i] = (start + positions[axes[i],b,s]) freqs[i].
+ *   axes [R/2] in, device, one byte a pair; an axis beyond the last is taken as the last.  n_axes: 1 to TEMPO_ROTARY_MOST_AXES.
+ *   positions: element (a, b, s) at a axis_stride + b batch_stride + s token_stride (axis_stride >= 0); not NULL.
+ */
+#define TEMPO_ROTARY_MOST_AXES 4
+TEMPO_API tempo_status tempo_rotary_axes_fwd(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
+                                   const uint8_t* axes, int n_axes, const tempo_rotary_positions* positions, int64_t axis_stride,
+                                   int64_t B, int64_t S, int64_t D, int64_t R, tempo_rotary_layout layout, float scale, tempo_dtype dt,
+                                   void* hip_stream);
+TEMPO_API tempo_status tempo_rotary_axes_bwd(const tempo_rotary_heads* dq, const tempo_rotary_heads* dk, const double* freqs,
+                                   const uint8_t* axes, int n_axes, const tempo_rotary_positions* positions, int64_t axis_stride,
+                                   int64_t B, int64_t S, int64_t D, int64_t R, tempo_rotary_layout layout, float scale, tempo_dtype dt,
+                                   void* hip_stream);
+
+/*
+ * Residual norm, forward: a norm of a block's output, its gate, the residual and the norm before the next block
+ *   n = post(f),  y = alpha x + beta gate n,  h = pre(y)
+ *   a norm: (t - mean) rstd weight + bias over the M columns; LAYER: mean and the biased variance, rstd = 1/sqrt(variance + eps); RMS: mean 0.
+ *   x, f [N,M] in (dt); y [N,M] out (dt), may alias x; h [N,M] out (dt), the norm of y as it is stored.
+ *   post NULL: n = f; pre NULL: h is neither made nor looked at.  weight, bias [M] in (f32): NULL for ones and zeros.
+ *   gate [groups,M] in (f32), for N / groups rows each (a sequence; 1: for all); NULL: ones (groups is 1 then, whatever it says).
+ *   stats [N,2] (f32) mean and rstd of each row: out of the forward, where it may be NULL, and in to the backward.
+ *   Parameters need only the alignment of a float, stats that of two.
+ *   INVALID_ARG also: groups < 1 or no divisor of N, eps < 0.  UNSUPPORTED also: more than 2^22 groups beside rows to match.
+ */
+typedef enum { TEMPO_NORM_RMS = 0, TEMPO_NORM_LAYER = 1 } tempo_norm_kind;
+typedef struct {
+  tempo_norm_kind kind;
+  const float* weight;
+  const float* bias;
+  float eps;
+  float* stats;
+} tempo_norm;
+TEMPO_API tempo_status tempo_residual_norm_fwd(const void* x, const void* f, const float* gate, int64_t groups, const tempo_norm* post,
+                                     const tempo_norm* pre, void* y, void* h, float alpha, float beta, int64_t N, int64_t M,
+                                     tempo_dtype dt, void* hip_stream);
+
+/*
+ * Residual norm, backward from f, y, and the norms' statistics: f^ = (f - mean) rstd, y^ likewise
+ *   g = dh pre.weight,  d = dy + pre.rstd (g - y^ mean(g y^) - mean(g)),  dx = alpha d      (mean(g): LAYER only)
+ *   e = beta gate post.weight d,  df = post.rstd (e - f^ mean(e f^) - mean(e))                (mean(e): LAYER only; no post: df = e)
+ *   dgate = beta sum n d over its rows,  dpost_weight = sum beta gate d f^,  dpost_bias = sum beta gate d,  dpre_weight = sum dh y^,
+ *   dpre_bias = sum dh.
+ *   dy (NULL: 0, where there is a pre), dh, f, y [N,M] in (dt); dx [N,M] out (dt), may alias dy; df [N,M] out (dt); the others out (f32), each
+ *   may be NULL, summed in a fixed order.  Without pre, dh and y are not read.
+ *   workspace: at least tempo_residual_norm_bwd_workspace_bytes(N, M, groups, dt) bytes, 16-byte aligned (not needed where all of dgate ..
+ *   dpre_bias are NULL); groups is that of the call, 1 without a gate.  Calls that may run at the same time need one each.
+ */
+TEMPO_API size_t tempo_residual_norm_bwd_workspace_bytes(int64_t N, int64_t M, int64_t groups, tempo_dtype dt);
+TEMPO_API tempo_status tempo_residual_norm_bwd(const void* dy, const void* dh, const void* f, const void* y, const float* gate, int64_t groups,
+                                     const tempo_norm* post, const tempo_norm* pre, void* dx, void* df, float* dgate,
+                                     float* dpost_weight, float* dpost_bias, float* dpre_weight, float* dpre_bias, float alpha, float beta,
+                                     void* workspace, size_t workspace_bytes, int64_t N, int64_t M, tempo_dtype dt, void* hip_stream);
+
+/*
  * Gated feed-forward unit, forward: both projections, the activation and their product
  *   [g | u] = x w^T + bias,  h = act(g) u;  act: SiLU or GELU (erf, tanh), of sums in float32.
  *   x [T,H], w [2F,H] (rows of the gate, then of u) in (dt); bias [2F] in (dt), may be NULL;

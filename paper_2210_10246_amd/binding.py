@@ -27,6 +27,7 @@ TEMPO_GELU_ERF, TEMPO_GELU_TANH = 0, 1
 _DT = {torch.float32: TEMPO_F32, torch.bfloat16: TEMPO_BF16}
 _KIND = {"erf": TEMPO_GELU_ERF, "tanh": TEMPO_GELU_TANH}
 _LAYOUT = {"half": 0, "interleaved": 1}
+_NORM_KIND = {"rms": 0, "layer": 1}
 _GLU_KIND = {"silu": 0, "gelu_erf": 1, "gelu_tanh": 2}
 
 _vp, _i64, _u64 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_uint64
@@ -45,9 +46,14 @@ class _AttnHeads(ctypes.Structure):
     _fields_ = [("p", _vp), ("strides", _i64 * 3)]
 
 
-_heads = ctypes.POINTER(_AttnHeads)
+class _Norm(ctypes.Structure):
+    _fields_ = [("kind", _int), ("weight", _vp), ("bias", _vp), ("eps", _f32), ("stats", _vp)]
+
+
+_heads, _norm = ctypes.POINTER(_AttnHeads), ctypes.POINTER(_Norm)
 _rotary_args = [ctypes.POINTER(_RotaryHeads), ctypes.POINTER(_RotaryHeads), _vp, ctypes.POINTER(_RotaryPositions), _i64, _i64,
                 _i64, _i64, _int, _f32, _int, _vp]
+_rotary_axes_args = _rotary_args[:3] + [_vp, _int, _rotary_args[3], _i64] + _rotary_args[4:]
 
 _SIGNATURES = {
     "tempo_status_string": (ctypes.c_char_p, [_int]),
@@ -76,6 +82,11 @@ _SIGNATURES = {
                                                     _f32, _u64, _u64, _int, _vp]),
     "tempo_rotary_fwd": (_int, _rotary_args),
     "tempo_rotary_bwd": (_int, _rotary_args),
+    "tempo_rotary_axes_fwd": (_int, _rotary_axes_args),
+    "tempo_rotary_axes_bwd": (_int, _rotary_axes_args),
+    "tempo_residual_norm_fwd": (_int, [_vp, _vp, _vp, _i64, _norm, _norm, _vp, _vp, _f32, _f32, _i64, _i64, _int, _vp]),
+    "tempo_residual_norm_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
+    "tempo_residual_norm_bwd": (_int, [_vp] * 5 + [_i64, _norm, _norm] + [_vp] * 7 + [_f32, _f32, _vp, _sz, _i64, _i64, _int, _vp]),
     "tempo_glu_fwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
     "tempo_glu_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
     "tempo_glu_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _sz, _i64, _i64, _i64, _int, _int, _vp]),
@@ -425,9 +436,10 @@ def _rotary_heads(name, x, y, like=None):
     return s, ctypes.byref(s)
 
 
-def _rotary(where, q, k, freqs, positions, q_out, k_out, layout, scale, start, stream):
+def _rotary(where, q, k, freqs, positions, q_out, k_out, layout, scale, start, stream, axes=None):
     if stream is None and _native is not None:
-        status = getattr(_native, where)(q, k, freqs, positions, q_out, k_out, layout, scale, start)
+        of_axes = () if axes is None else (axes,)
+        status = getattr(_native, where)(q, k, freqs, *of_axes, positions, q_out, k_out, layout, scale, start)
         if status is not None:
             return _check(status, where)
     dt = _act_dtype("q", q)
@@ -442,18 +454,31 @@ def _rotary(where, q, k, freqs, positions, q_out, k_out, layout, scale, start, s
     if abs(start) > 2 ** 53:
         raise ValueError(f"start must lie within 2^53, got {start}")
     at = _RotaryPositions(None, 64, (_i64 * 2)(0, 0), start)
-    if positions is not None:
-        if positions.dtype not in (torch.int32, torch.int64):
-            raise ValueError(f"positions must be int32 or int64, got {positions.dtype}")
+    if positions is not None and positions.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"positions must be int32 or int64, got {positions.dtype}")
+    of_axes = ()
+    if axes is not None:
+        if axes.dtype != torch.uint8 or axes.shape != freqs.shape or not axes.is_contiguous():
+            raise ValueError(f"axes must be uint8 of shape {tuple(freqs.shape)}, got {axes.dtype} of {tuple(axes.shape)}")
+        if positions.dim() < 2 or not 1 <= positions.shape[0] <= 4 or positions.shape[1:] not in ((S,), (1, S), (B, S)):
+            raise ValueError(f"positions must be [1 to 4 axes, {S}] or [axes, {B}, {S}], got {tuple(positions.shape)}")
+        shared = positions.dim() == 2 or positions.shape[1] == 1
+        at = _RotaryPositions(positions.data_ptr(), 8 * positions.element_size(),
+                              (_i64 * 2)(0 if shared else positions.stride(1), positions.stride(-1)), start)
+        of_axes = axes.data_ptr(), positions.shape[0]
+    elif positions is not None:
         if positions.shape not in ((S,), (1, S), (B, S)):
             raise ValueError(f"positions must be [{S}] or [{B}, {S}], got {tuple(positions.shape)}")
         shared = positions.dim() == 1 or positions.shape[0] == 1
         at = _RotaryPositions(positions.data_ptr(), 8 * positions.element_size(),
                               (_i64 * 2)(0 if shared else positions.stride(0), positions.stride(-1)), start)
-    _same_device(q, k, freqs, positions, q_out, k_out)
+    _same_device(q, k, freqs, positions, q_out, k_out, axes)
     f = _ptr(freqs)
-    _check(getattr(load(), where)(q_ref, k_ref, f, ctypes.byref(at), B, S, D, 2 * freqs.numel(), _LAYOUT[layout], scale, dt,
-                                  _stream(stream)), where)
+    if of_axes:
+        head = q_ref, k_ref, f, *of_axes, ctypes.byref(at), positions.stride(0)
+    else:
+        head = q_ref, k_ref, f, ctypes.byref(at)
+    _check(getattr(load(), where)(*head, B, S, D, 2 * freqs.numel(), _LAYOUT[layout], scale, dt, _stream(stream)), where)
 
 
 def tempo_rotary_fwd(q, k, freqs, positions, q_out, k_out, layout="half", scale=1.0, start=0, stream=None):
@@ -466,6 +491,117 @@ def tempo_rotary_fwd(q, k, freqs, positions, q_out, k_out, layout="half", scale=
 def tempo_rotary_bwd(dq, dk, freqs, positions, dq_out, dk_out, layout="half", scale=1.0, start=0, stream=None):
     """The gradients of tempo_rotary_fwd's q and k from those of its outputs; arguments as there."""
     _rotary("tempo_rotary_bwd", dq, dk, freqs, positions, dq_out, dk_out, layout, scale, start, stream)
+
+
+def tempo_rotary_axes_fwd(q, k, freqs, axes, positions, q_out, k_out, layout="half", scale=1.0, start=0, stream=None):
+    """Rotary positions with several axes: pair i turns by the position on axis axes[i] (uint8, like freqs; an axis beyond the last is
+    taken as the last).  positions: [axes, tokens] or [axes, batch, tokens], up to 4 axes.  Else as tempo_rotary_fwd."""
+    if axes is None or positions is None:
+        raise ValueError("axes and positions are needed")
+    _rotary("tempo_rotary_axes_fwd", q, k, freqs, positions, q_out, k_out, layout, scale, start, stream, axes)
+
+
+def tempo_rotary_axes_bwd(dq, dk, freqs, axes, positions, dq_out, dk_out, layout="half", scale=1.0, start=0, stream=None):
+    """The gradients of tempo_rotary_axes_fwd's q and k from those of its outputs; arguments as there."""
+    if axes is None or positions is None:
+        raise ValueError("axes and positions are needed")
+    _rotary("tempo_rotary_axes_bwd", dq, dk, freqs, positions, dq_out, dk_out, layout, scale, start, stream, axes)
+
+
+def tempo_residual_norm_bwd_workspace_bytes(N: int, M: int, groups: int, dtype) -> int:
+    return load().tempo_residual_norm_bwd_workspace_bytes(N, M, groups, _DT[dtype])
+
+
+def _norm_of(name, kind, weight, bias, eps, stats, N, M):
+    if kind is None:
+        if weight is not None or bias is not None or stats is not None:
+            raise ValueError(f"{name} is None: there is no {name}_weight, {name}_bias or {name}_stats")
+        return None, None
+    if kind not in _NORM_KIND:
+        raise ValueError(f'{name} must be None, "rms" or "layer", got {kind!r}')
+    _want(name + "_weight", weight, torch.float32, M)
+    _want(name + "_bias", bias, torch.float32, M)
+    _want(name + "_stats", stats, torch.float32, 2 * N)
+    n = _Norm(_NORM_KIND[kind], _ptr(weight), _ptr(bias), eps, _ptr(stats))
+    return n, ctypes.byref(n)
+
+
+def _residual_sizes(like, gate):
+    M = like.shape[-1] if like.dim() > 0 else 0
+    N = like.numel() // M if M else 0
+    _want("gate", gate, torch.float32)
+    groups = 1
+    if gate is not None:
+        if gate.dim() < 1 or gate.shape[-1] != M:
+            raise ValueError(f"gate must be [..., {M}], got {tuple(gate.shape)}")
+        groups = gate.shape[:-1].numel()
+        if groups < 1 or N % groups != 0:
+            raise ValueError(f"gate is of {groups} groups of rows, which do not divide {N}")
+    return N, M, groups
+
+
+def tempo_residual_norm_fwd(x, f, gate, y, h, post, post_weight, post_bias, post_stats, pre, pre_weight, pre_bias, pre_stats, alpha=1.0,
+                            beta=1.0, post_eps=1e-5, pre_eps=1e-5, stream=None):
+    """y = alpha x + beta gate post(f), h = pre(y); y may be x.  post, pre: "rms", "layer" or None (no norm of f; no h).  gate: [M] or
+    [groups, M] float32, for as many rows each, or None.  Weights and biases: [M] float32, or None; stats: [rows, 2] float32, for the
+    backward, or None."""
+    if stream is None and _native is not None:
+        status = _native.tempo_residual_norm_fwd(x, f, gate, y, h, post, post_weight, post_bias, post_stats, pre, pre_weight, pre_bias,
+                                                 pre_stats, alpha, beta, post_eps, pre_eps)
+        if status is not None:
+            return _check(status, "tempo_residual_norm_fwd")
+    dt = _act_dtype("x", x)
+    N, M, groups = _residual_sizes(x, gate)
+    if pre is not None and h is None:
+        raise ValueError("h is needed, which pre makes")
+    for name, t in (("f", f), ("y", y), ("h", h if pre is not None else None)):
+        _want(name, t, x.dtype, x.numel())
+    a, post_ref = _norm_of("post", post, post_weight, post_bias, post_eps, post_stats, N, M)
+    b, pre_ref = _norm_of("pre", pre, pre_weight, pre_bias, pre_eps, pre_stats, N, M)
+    pointers = [_ptr(t) for t in (x, f, gate, y, h if pre is not None else None)]
+    _same_device(x, f, gate, y, h, post_weight, post_bias, post_stats, pre_weight, pre_bias, pre_stats)
+    _check(load().tempo_residual_norm_fwd(*pointers[:3], groups, post_ref, pre_ref, *pointers[3:], alpha, beta, N, M, dt, _stream(stream)),
+           "tempo_residual_norm_fwd")
+
+
+def tempo_residual_norm_bwd(dy, dh, f, y, gate, dx, df, dgate, post, post_weight, post_bias, post_stats, dpost_weight, dpost_bias, pre,
+                            pre_weight, pre_stats, dpre_weight, dpre_bias, alpha=1.0, beta=1.0, workspace=None, stream=None):
+    """The gradients of x, f, the gate and the norms' parameters (each of these None: not wanted) from those of y (dy; None: 0) and h and
+    what the forward kept; dx may be dy.  workspace: tempo_residual_norm_bwd_workspace_bytes() bytes, or None: allocated for the call."""
+    if stream is None and _native is not None:
+        status = _native.tempo_residual_norm_bwd(dy, dh, f, y, gate, dx, df, dgate, post, post_weight, post_bias, post_stats,
+                                                 dpost_weight, dpost_bias, pre, pre_weight, pre_stats, dpre_weight, dpre_bias, alpha,
+                                                 beta, workspace)
+        if status is not None:
+            return _check(status, "tempo_residual_norm_bwd")
+    dt = _act_dtype("f", f)
+    N, M, groups = _residual_sizes(f, gate)
+    if dx is None or df is None or (dy is None and pre is None) or (pre is not None and (dh is None or y is None)):
+        raise ValueError("dx, df, the gradients of y or h, and with pre y and the gradient of h are needed")
+    if (post is not None and post_stats is None) or (pre is not None and pre_stats is None):
+        raise ValueError("the stats that the forward keeps are needed")
+    if dgate is not None and gate is None:
+        raise ValueError("dgate is the gradient of a gate, which is None")
+    with_pre = (dh, y) if pre is not None else (None, None)
+    for name, t in (("dy", dy), ("dh", with_pre[0]), ("y", with_pre[1]), ("dx", dx), ("df", df)):
+        _want(name, t, f.dtype, f.numel())
+    _want("dgate", dgate, torch.float32, groups * M)
+    for name, t, kind in (("dpost_weight", dpost_weight, post), ("dpost_bias", dpost_bias, post), ("dpre_weight", dpre_weight, pre),
+                          ("dpre_bias", dpre_bias, pre)):
+        if t is not None and kind is None:
+            raise ValueError(f"{name} is the gradient of a norm that is None")
+        _want(name, t, torch.float32, M)
+    a, post_ref = _norm_of("post", post, post_weight, post_bias, 0.0, post_stats, N, M)
+    b, pre_ref = _norm_of("pre", pre, pre_weight, None, 0.0, pre_stats, N, M)
+    ins = [_ptr(t) for t in (dy, with_pre[0], f, with_pre[1], gate)]
+    outs = [_ptr(t) for t in (dx, df, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias)]
+    _same_device(dy, dh, f, y, gate, dx, df, dgate, post_weight, post_bias, post_stats, dpost_weight, dpost_bias, pre_weight, pre_stats,
+                 dpre_weight, dpre_bias, workspace)
+    columns = any(t is not None for t in (dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias))
+    need = load().tempo_residual_norm_bwd_workspace_bytes(N, M, groups, dt) if columns else 0
+    ws = _workspace(workspace, need, f.device, stream)
+    _check(load().tempo_residual_norm_bwd(*ins, groups, post_ref, pre_ref, *outs, alpha, beta, _ptr(ws), ws.numel() * ws.element_size(),
+                                          N, M, dt, _stream(stream)), "tempo_residual_norm_bwd")
 
 
 def tempo_glu_fwd_workspace_bytes(T: int, H: int, F: int, dtype) -> int:

@@ -45,6 +45,7 @@ int compute_units() {
 
 static bool dtype_ok(tempo_dtype dt) { return dt == TEMPO_F32 || dt == TEMPO_BF16; }
 static bool kind_ok(tempo_gelu_kind k) { return k == TEMPO_GELU_ERF || k == TEMPO_GELU_TANH; }
+static bool aligned_to(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 static bool prob_ok(float p) { return p >= 0.0f && p < 1.0f; }  // false for NaN
 
 // A tensor has at most 2^40 elements (terabytes: far beyond device memory), so that no product
@@ -352,7 +353,7 @@ static bool rotary_side_ok(const tempo_rotary_heads* h, int64_t B, int64_t S, in
   return last_in <= kMaxElements && last_out <= kMaxElements;
 }
 static tempo_status rotary(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
-                           const tempo_rotary_positions* at, int64_t B, int64_t S, int64_t D, int64_t R,
+                           const tempo_rotary_positions* at, const RotaryAxes* axes, int64_t B, int64_t S, int64_t D, int64_t R,
                            tempo_rotary_layout layout, float scale, bool back, tempo_dtype dt, void* hip_stream) {
   constexpr int64_t most = int64_t{1} << 24;  // elements of a token
   if (!q || !at || B < 0 || S < 0 || D < 0 || q->heads < 0 || (k && k->heads < 0) || !dtype_ok(dt) ||
@@ -366,28 +367,44 @@ static tempo_status rotary(const tempo_rotary_heads* q, const tempo_rotary_heads
   if (at->positions && ((at->bits != 32 && at->bits != 64) || at->batch_stride < 0 || at->token_stride < 0 ||
                         !count_ok(B, at->batch_stride) || !count_ok(S, at->token_stride)))
     return TEMPO_ERR_INVALID_ARG;
+  if (axes && (axes->count < 1 || axes->count > TEMPO_ROTARY_MOST_AXES || axes->stride < 0 || !count_ok(axes->count, axes->stride)))
+    return TEMPO_ERR_INVALID_ARG;
   if (k && k->heads == 0) k = nullptr;
   if (k && q->heads == 0) q = k, k = nullptr;
   if (B == 0 || S == 0 || q->heads == 0) return TEMPO_OK;
   if (!q->x || !q->y || !freqs || (k && (!k->x || !k->y))) return TEMPO_ERR_INVALID_ARG;
+  if (axes && (!axes->of_pairs || !at->positions)) return TEMPO_ERR_INVALID_ARG;
   const uintptr_t element = dt == TEMPO_F32 ? 4 : 2;
-  auto aligned = [](const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; };
-  if (!aligned(q->x, element) || !aligned(q->y, element) || (k && (!aligned(k->x, element) || !aligned(k->y, element))) ||
-      !aligned(freqs, 8) || (at->positions && !aligned(at->positions, at->bits / 8)))
+  if (!aligned_to(q->x, element) || !aligned_to(q->y, element) || (k && (!aligned_to(k->x, element) || !aligned_to(k->y, element))) ||
+      !aligned_to(freqs, 8) || (at->positions && !aligned_to(at->positions, at->bits / 8)))
     return TEMPO_ERR_UNSUPPORTED;
-  return launch_rotary(q, k, freqs, at, B, S, D, R, layout, scale, back, dt, static_cast<hipStream_t>(hip_stream));
+  return launch_rotary(q, k, freqs, at, axes, B, S, D, R, layout, scale, back, dt, static_cast<hipStream_t>(hip_stream));
 }
 
 tempo_status tempo_rotary_fwd(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
                               const tempo_rotary_positions* positions, int64_t B, int64_t S, int64_t D, int64_t R,
                               tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream) {
-  return rotary(q, k, freqs, positions, B, S, D, R, layout, scale, false, dt, hip_stream);
+  return rotary(q, k, freqs, positions, nullptr, B, S, D, R, layout, scale, false, dt, hip_stream);
 }
 
 tempo_status tempo_rotary_bwd(const tempo_rotary_heads* dq, const tempo_rotary_heads* dk, const double* freqs,
                               const tempo_rotary_positions* positions, int64_t B, int64_t S, int64_t D, int64_t R,
                               tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream) {
-  return rotary(dq, dk, freqs, positions, B, S, D, R, layout, scale, true, dt, hip_stream);
+  return rotary(dq, dk, freqs, positions, nullptr, B, S, D, R, layout, scale, true, dt, hip_stream);
+}
+
+tempo_status tempo_rotary_axes_fwd(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs, const uint8_t* axes,
+                                   int n_axes, const tempo_rotary_positions* positions, int64_t axis_stride, int64_t B, int64_t S,
+                                   int64_t D, int64_t R, tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream) {
+  const RotaryAxes a{axes, n_axes, axis_stride};
+  return rotary(q, k, freqs, positions, &a, B, S, D, R, layout, scale, false, dt, hip_stream);
+}
+
+tempo_status tempo_rotary_axes_bwd(const tempo_rotary_heads* dq, const tempo_rotary_heads* dk, const double* freqs, const uint8_t* axes,
+                                   int n_axes, const tempo_rotary_positions* positions, int64_t axis_stride, int64_t B, int64_t S,
+                                   int64_t D, int64_t R, tempo_rotary_layout layout, float scale, tempo_dtype dt, void* hip_stream) {
+  const RotaryAxes a{axes, n_axes, axis_stride};
+  return rotary(dq, dk, freqs, positions, &a, B, S, D, R, layout, scale, true, dt, hip_stream);
 }
 
 static bool glu_ok(int64_t T, int64_t H, int64_t F, tempo_glu_kind kind, tempo_dtype dt) {
@@ -435,6 +452,62 @@ tempo_status tempo_glu_bwd(const void* dh, const void* gu, const void* x, const 
   return launch_glu_bwd(c, dt, static_cast<hipStream_t>(hip_stream));
 }
 
+static bool norm_ok(const tempo_norm* n) {
+  return !n || ((n->kind == TEMPO_NORM_RMS || n->kind == TEMPO_NORM_LAYER) && n->eps >= 0.0f);  // false for NaN
+}
+static bool residual_norm_ok(int64_t N, int64_t M, int64_t groups, tempo_dtype dt) {
+  return N >= 0 && M >= 0 && M <= INT32_MAX && groups >= 1 && N % groups == 0 && dtype_ok(dt) && count_ok(N, M) && count_ok(groups, M);
+}
+static bool norm_aligned(const tempo_norm* n) {
+  return !n || (aligned_to(n->weight, 4) && aligned_to(n->bias, 4) && aligned_to(n->stats, 8));
+}
+
+size_t tempo_residual_norm_bwd_workspace_bytes(int64_t N, int64_t M, int64_t groups, tempo_dtype dt) {
+  if (!residual_norm_ok(N, M, groups, dt) || M == 0) return 0;
+  ResidualCall c{};
+  const float one = 1.0f;
+  c.gate = &one;  // there is one
+  c.N = N, c.M = M, c.groups = groups;
+  return residual_norm_takes(c, dt) ? residual_norm_workspace_bytes(c, dt) : 0;
+}
+
+tempo_status tempo_residual_norm_fwd(const void* x, const void* f, const float* gate, int64_t groups, const tempo_norm* post,
+                                     const tempo_norm* pre, void* y, void* h, float alpha, float beta, int64_t N, int64_t M,
+                                     tempo_dtype dt, void* hip_stream) {
+  if (!residual_norm_ok(N, M, groups, dt) || !norm_ok(post) || !norm_ok(pre)) return TEMPO_ERR_INVALID_ARG;
+  if (N == 0 || M == 0) return TEMPO_OK;
+  if (!x || !f || !y || (pre && !h)) return TEMPO_ERR_INVALID_ARG;
+  ResidualCall c{};
+  c.x = x, c.f = f, c.gate = gate, c.groups = gate ? groups : 1, c.post = post, c.pre = pre, c.to_y = y, c.h = h;
+  c.alpha = alpha, c.beta = beta, c.N = N, c.M = M;
+  if (!aligned16(x) || !aligned16(f) || !aligned16(y) || !aligned16(h) || !aligned_to(gate, 4) || !norm_aligned(post) ||
+      !norm_aligned(pre) || !residual_norm_takes(c, dt))
+    return TEMPO_ERR_UNSUPPORTED;
+  return launch_residual_norm_fwd(c, dt, static_cast<hipStream_t>(hip_stream));
+}
+
+tempo_status tempo_residual_norm_bwd(const void* dy, const void* dh, const void* f, const void* y, const float* gate, int64_t groups,
+                                     const tempo_norm* post, const tempo_norm* pre, void* dx, void* df, float* dgate, float* dpost_weight,
+                                     float* dpost_bias, float* dpre_weight, float* dpre_bias, float alpha, float beta, void* workspace,
+                                     size_t workspace_bytes, int64_t N, int64_t M, tempo_dtype dt, void* hip_stream) {
+  if (!residual_norm_ok(N, M, groups, dt) || !norm_ok(post) || !norm_ok(pre)) return TEMPO_ERR_INVALID_ARG;
+  if ((dgate && !gate) || ((dpost_weight || dpost_bias) && !post) || ((dpre_weight || dpre_bias) && !pre)) return TEMPO_ERR_INVALID_ARG;
+  if (M == 0) return TEMPO_OK;
+  // Sums of no rows are written too.
+  if (N > 0 && (!f || !dx || !df || (!dy && !pre) || (post && !post->stats) || (pre && (!dh || !y || !pre->stats)))) return TEMPO_ERR_INVALID_ARG;
+  ResidualCall c{};
+  c.dy = dy, c.dh = dh, c.f = f, c.y = y, c.gate = gate, c.groups = gate ? groups : 1, c.post = post, c.pre = pre, c.dx = dx, c.df = df;
+  c.dgate = dgate, c.dpost_weight = dpost_weight, c.dpost_bias = dpost_bias, c.dpre_weight = dpre_weight, c.dpre_bias = dpre_bias;
+  c.alpha = alpha, c.beta = beta, c.workspace = workspace, c.workspace_bytes = workspace ? workspace_bytes : 0, c.N = N, c.M = M;
+  for (const void* t : {dy, dh, f, y, static_cast<const void*>(dx), static_cast<const void*>(df), static_cast<const void*>(workspace)})
+    if (!aligned16(t)) return TEMPO_ERR_UNSUPPORTED;
+  for (const float* t : {gate, static_cast<const float*>(dgate), static_cast<const float*>(dpost_weight), static_cast<const float*>(dpost_bias),
+                         static_cast<const float*>(dpre_weight), static_cast<const float*>(dpre_bias)})
+    if (!aligned_to(t, 4)) return TEMPO_ERR_UNSUPPORTED;
+  if (!norm_aligned(post) || !norm_aligned(pre) || !residual_norm_takes(c, dt)) return TEMPO_ERR_UNSUPPORTED;
+  return launch_residual_norm_bwd(c, dt, static_cast<hipStream_t>(hip_stream));
+}
+
 static bool window_attn_ok(const WindowCall& c) {
   return c.B >= 0 && c.Sq >= 0 && c.Sk >= 0 && c.heads >= 0 && c.kv_heads >= 0 && c.D >= 1 && c.window >= 1 && c.sinks >= 0 &&
          (c.heads == 0 || (c.kv_heads >= 1 && c.heads % c.kv_heads == 0)) && c.Sq <= INT32_MAX && c.Sk <= INT32_MAX &&
@@ -478,7 +551,6 @@ size_t tempo_window_attn_bwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, 
 }
 
 static bool scale_ok(float scale) { return scale > 0.0f && scale <= 3.402823466e+38f; }  // false for NaN
-static bool aligned_to(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 tempo_status tempo_window_attn_fwd(const tempo_attn_heads* q, const tempo_attn_heads* k, const tempo_attn_heads* v,
                                    const tempo_attn_heads* out, float* lse, const int32_t* key_len, const int32_t* query_start,

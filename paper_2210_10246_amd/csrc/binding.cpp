@@ -251,6 +251,20 @@ tempo_rotary_heads rotary_heads(const at::Tensor& like, PyObject* in, PyObject* 
     throw NotPlain{};
   return {x.data_ptr(), y.data_ptr(), x.size(2), x.stride(0), x.stride(1), x.stride(2), y.stride(0), y.stride(1), y.stride(2)};
 }
+// The [tokens] or [batch, tokens] of positions behind their first dimensions.
+tempo_rotary_positions rotary_positions(const at::Tensor& p, int first, int64_t B, int64_t S, int64_t start) {
+  const bool batched = p.dim() == first + 2;
+  if ((p.scalar_type() != at::kInt && p.scalar_type() != at::kLong) || (p.dim() != first + 1 && !batched) || p.size(-1) != S ||
+      (batched && p.size(first) != B && p.size(first) != 1))
+    throw NotPlain{};
+  return {p.data_ptr(), p.scalar_type() == at::kInt ? 32 : 64, batched && p.size(first) != 1 ? p.stride(first) : 0, p.stride(-1), start};
+}
+tempo_rotary_layout rotary_layout(PyObject* o) {
+  if (!PyUnicode_CheckExact(o)) throw NotPlain{};
+  if (PyUnicode_CompareWithASCIIString(o, "half") == 0) return TEMPO_ROTARY_HALF;
+  if (PyUnicode_CompareWithASCIIString(o, "interleaved") == 0) return TEMPO_ROTARY_INTERLEAVED;
+  throw NotPlain{};
+}
 // q, k, freqs, positions, q_out, k_out, layout, scale, start
 PyObject* rotary(PyObject* const* a, Py_ssize_t nargs, decltype(&tempo_rotary_fwd) entry) {
   return plain_call<9>(nargs, [&] {
@@ -263,22 +277,8 @@ PyObject* rotary(PyObject* const* a, Py_ssize_t nargs, decltype(&tempo_rotary_fw
     const tempo_rotary_heads kh = both ? rotary_heads(q, a[1], a[5]) : tempo_rotary_heads{};
     if (f.scalar_type() != at::kDouble || !f.is_contiguous() || R < 2 || R > D) throw NotPlain{};
     tempo_rotary_positions at{nullptr, 64, 0, 0, integer(a[8])};
-    if (a[3] != Py_None) {
-      const at::Tensor& p = here(a[3]);
-      const bool batched = p.dim() == 2;
-      if ((p.scalar_type() != at::kInt && p.scalar_type() != at::kLong) || (p.dim() != 1 && !batched) || p.size(-1) != S ||
-          (batched && p.size(0) != B && p.size(0) != 1))
-        throw NotPlain{};
-      at.positions = p.data_ptr();
-      at.bits = p.scalar_type() == at::kInt ? 32 : 64;
-      at.batch_stride = batched && p.size(0) != 1 ? p.stride(0) : 0;
-      at.token_stride = p.stride(-1);
-    }
-    tempo_rotary_layout layout;
-    if (!PyUnicode_CheckExact(a[6])) throw NotPlain{};
-    if (PyUnicode_CompareWithASCIIString(a[6], "half") == 0) layout = TEMPO_ROTARY_HALF;
-    else if (PyUnicode_CompareWithASCIIString(a[6], "interleaved") == 0) layout = TEMPO_ROTARY_INTERLEAVED;
-    else throw NotPlain{};
+    if (a[3] != Py_None) at = rotary_positions(here(a[3]), 0, B, S, at.start);
+    const tempo_rotary_layout layout = rotary_layout(a[6]);
     return [=, freqs = static_cast<const double*>(f.data_ptr()), scale = real(a[7]),
             dt = q.scalar_type() == at::kFloat ? TEMPO_F32 : TEMPO_BF16, st = stream()] {
       return entry(&qh, both ? &kh : nullptr, freqs, &at, B, S, D, R, layout, scale, dt, st);
@@ -287,6 +287,29 @@ PyObject* rotary(PyObject* const* a, Py_ssize_t nargs, decltype(&tempo_rotary_fw
 }
 TEMPO_METHOD(rotary_fwd) { return rotary(a, nargs, tempo_rotary_fwd); }
 TEMPO_METHOD(rotary_bwd) { return rotary(a, nargs, tempo_rotary_bwd); }
+// q, k, freqs, axes, positions, q_out, k_out, layout, scale, start
+PyObject* rotary_axes(PyObject* const* a, Py_ssize_t nargs, decltype(&tempo_rotary_axes_fwd) entry) {
+  return plain_call<10>(nargs, [&] {
+    const at::Tensor &q = here(a[0]), &f = here(a[2]), &x = here(a[3]), &p = here(a[4]);
+    if (q.dim() != 4 || (q.scalar_type() != at::kFloat && q.scalar_type() != at::kBFloat16)) throw NotPlain{};
+    const int64_t B = q.size(0), S = q.size(1), D = q.size(3), R = 2 * f.numel();
+    const tempo_rotary_heads qh = rotary_heads(q, a[0], a[5]);
+    const bool both = a[1] != Py_None;
+    if (both != (a[6] != Py_None)) throw NotPlain{};
+    const tempo_rotary_heads kh = both ? rotary_heads(q, a[1], a[6]) : tempo_rotary_heads{};
+    if (f.scalar_type() != at::kDouble || !f.is_contiguous() || R < 2 || R > D || x.scalar_type() != at::kByte || x.sizes() != f.sizes() ||
+        !x.is_contiguous() || p.dim() < 2 || p.size(0) < 1 || p.size(0) > TEMPO_ROTARY_MOST_AXES)
+      throw NotPlain{};
+    const tempo_rotary_positions at = rotary_positions(p, 1, B, S, integer(a[9]));
+    return [=, freqs = static_cast<const double*>(f.data_ptr()), axes = static_cast<const uint8_t*>(x.data_ptr()),
+            n = static_cast<int>(p.size(0)), stride = p.stride(0), layout = rotary_layout(a[7]), scale = real(a[8]),
+            dt = q.scalar_type() == at::kFloat ? TEMPO_F32 : TEMPO_BF16, st = stream()] {
+      return entry(&qh, both ? &kh : nullptr, freqs, axes, n, &at, stride, B, S, D, R, layout, scale, dt, st);
+    };
+  });
+}
+TEMPO_METHOD(rotary_axes_fwd) { return rotary_axes(a, nargs, tempo_rotary_axes_fwd); }
+TEMPO_METHOD(rotary_axes_bwd) { return rotary_axes(a, nargs, tempo_rotary_axes_bwd); }
 
 // ---- the gated unit --------------------------------------------------------------------------------------------------
 struct Glu {
@@ -424,6 +447,81 @@ TEMPO_METHOD(window_attn_bwd) {
             st = stream()] {
       return tempo_window_attn_bwd(&dout, &q, &k, &v, &out, lse, &dq, &dk, &dv, len, start, ws.p, ws.bytes, w.B, w.Sq, w.Sk, w.heads,
                                    w.kv_heads, w.D, w.window, w.sinks, w.scale, w.dt, st);
+    };
+  });
+}
+
+// ---- residual norms --------------------------------------------------------------------------------------------------
+struct ResidualRows {
+  int64_t N, M, groups = 1;
+  at::ScalarType scalar;
+  tempo_dtype dt;
+  const float* gate = nullptr;
+  ResidualRows(const at::Tensor& like, PyObject* g) : scalar(like.scalar_type()) {
+    if ((scalar != at::kFloat && scalar != at::kBFloat16) || like.dim() < 1) throw NotPlain{};
+    dt = scalar == at::kFloat ? TEMPO_F32 : TEMPO_BF16;
+    M = like.size(-1);
+    N = M ? like.numel() / M : 0;
+    if (g == Py_None) return;
+    const at::Tensor& t = here(g);
+    if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.dim() < 1 || t.size(-1) != M || M == 0) throw NotPlain{};
+    groups = t.numel() / M;
+    if (groups < 1 || N % groups != 0) throw NotPlain{};
+    gate = static_cast<const float*>(t.data_ptr());
+  }
+  void* of(PyObject* o) const {
+    const at::Tensor& t = here(o);
+    if (t.scalar_type() != scalar || t.numel() != N * M || !t.is_contiguous()) throw NotPlain{};
+    return t.data_ptr();
+  }
+  void* of_or_none(PyObject* o) const { return o == Py_None ? nullptr : of(o); }
+  float* columns(PyObject* o, int64_t rows = 1) const { return small_or_none<float>(o, at::kFloat, rows * M); }
+  // No norm: kind is None, and so are the others.
+  bool norm(tempo_norm& n, PyObject* kind, PyObject* weight, PyObject* bias, float eps, PyObject* stats) const {
+    if (kind == Py_None) {
+      if (weight != Py_None || bias != Py_None || stats != Py_None) throw NotPlain{};
+      return false;
+    }
+    if (!PyUnicode_CheckExact(kind)) throw NotPlain{};
+    if (PyUnicode_CompareWithASCIIString(kind, "rms") == 0) n.kind = TEMPO_NORM_RMS;
+    else if (PyUnicode_CompareWithASCIIString(kind, "layer") == 0) n.kind = TEMPO_NORM_LAYER;
+    else throw NotPlain{};
+    n.weight = columns(weight);
+    n.bias = columns(bias);
+    n.eps = eps;
+    n.stats = small_or_none<float>(stats, at::kFloat, 2 * N);
+    return true;
+  }
+};
+// x, f, gate, y, h, post, post_weight, post_bias, post_stats, pre, pre_weight, pre_bias, pre_stats, alpha, beta, post_eps, pre_eps
+TEMPO_METHOD(residual_norm_fwd) {
+  return plain_call<17>(nargs, [&] {
+    const ResidualRows r(here(a[0]), a[2]);
+    tempo_norm post{}, pre{};
+    const bool has_post = r.norm(post, a[5], a[6], a[7], real(a[15]), a[8]), has_pre = r.norm(pre, a[9], a[10], a[11], real(a[16]), a[12]);
+    return [=, x = r.of(a[0]), f = r.of(a[1]), y = r.of(a[3]), h = has_pre ? r.of(a[4]) : nullptr, alpha = real(a[13]), beta = real(a[14]),
+            st = stream()] {
+      return tempo_residual_norm_fwd(x, f, r.gate, r.groups, has_post ? &post : nullptr, has_pre ? &pre : nullptr, y, h, alpha, beta, r.N, r.M,
+                                     r.dt, st);
+    };
+  });
+}
+// dy, dh, f, y, gate, dx, df, dgate, post, post_weight, post_bias, post_stats, dpost_weight, dpost_bias, pre, pre_weight, pre_stats,
+// dpre_weight, dpre_bias, alpha, beta, workspace
+TEMPO_METHOD(residual_norm_bwd) {
+  return plain_call<22>(nargs, [&] {
+    const at::Tensor& tf = here(a[2]);
+    const ResidualRows r(tf, a[4]);
+    tempo_norm post{}, pre{};
+    const bool has_post = r.norm(post, a[8], a[9], a[10], 0.0f, a[11]), has_pre = r.norm(pre, a[14], a[15], Py_None, 0.0f, a[16]);
+    if ((has_post && !post.stats) || (has_pre && !pre.stats) || (!has_pre && a[0] == Py_None) || (a[7] != Py_None && !r.gate)) throw NotPlain{};
+    float *dgate = r.columns(a[7], r.groups), *pw = r.columns(a[12]), *pb = r.columns(a[13]), *qw = r.columns(a[17]), *qb = r.columns(a[18]);
+    if ((!has_post && (pw || pb)) || (!has_pre && (qw || qb))) throw NotPlain{};
+    const size_t need = dgate || pw || pb || qw || qb ? tempo_residual_norm_bwd_workspace_bytes(r.N, r.M, r.groups, r.dt) : 0;
+    return [=, dy = r.of_or_none(a[0]), dh = has_pre ? r.of(a[1]) : nullptr, f = r.of(a[2]), y = has_pre ? r.of(a[3]) : nullptr,
+            dx = r.of(a[5]), df = r.of(a[6]), alpha = real(a[19]), beta = real(a[20]), ws = Workspace(a[21], tf, need), st = stream()] {
+      return tempo_residual_norm_bwd(dy, dh, f, y, r.gate, r.groups, has_post ? &post : nullptr, has_pre ? &pre : nullptr, dx, df, dgate, pw, pb,
+                                     qw, qb, alpha, beta, ws.p, ws.bytes, r.N, r.M, r.dt, st);
     };
   });
 }
@@ -690,6 +788,10 @@ PyMethodDef methods[] = {TEMPO_ENTRY(gelu_fwd),
                          TEMPO_ENTRY(rotary_bwd),
                          TEMPO_ENTRY(glu_fwd),
                          TEMPO_ENTRY(glu_bwd),
+                         TEMPO_ENTRY(rotary_axes_fwd),
+                         TEMPO_ENTRY(rotary_axes_bwd),
+                         TEMPO_ENTRY(residual_norm_fwd),
+                         TEMPO_ENTRY(residual_norm_bwd),
                          TEMPO_ENTRY(window_attn_fwd),
                          TEMPO_ENTRY(window_attn_bwd),
                          TEMPO_ENTRY(encoder_fwd),

@@ -1,7 +1,7 @@
 // Rotary positions of the attention heads of q and k:
 //   theta = position f_i, i < R/2;   y1 = scale (x1 cos theta - x2 sin theta), y2 = scale (x2 cos theta + x1 sin theta)
 // for the pairs (x1, x2) = (x[i], x[i + R/2]) or (x[2i], x[2i + 1]); elements from R on are copied.  The backward turns the
-// other way: the transposed map.
+// other way: the transposed map.  With several axes a position is one for each, and a pair turns by that of its own axis.
 //
 // Bound by the bytes of q and k, read once and written once.  Angles are made where they are used: in two numbers of 64 bits, which
 // this chip multiplies at the rate of 32, so that a position of any size keeps its place within the turn; no table is read, kept or
@@ -17,6 +17,7 @@ namespace tempo {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMostAxes = TEMPO_ROTARY_MOST_AXES;
 // Heads that share the angles of a lane, each in two pieces (half) or one: 128 bytes of a lane on their way.  One each where that leaves
 // the chip short of waves and the angles, made for every head then, are few.
 constexpr int heads_per_lane(bool half) { return half ? 4 : 8; }
@@ -56,6 +57,9 @@ struct Rotary {
   const void* positions;  // null: start, start + 1, ...
   bool wide;              // 64-bit positions
   int64_t pos_batch, pos_token, start;
+  const uint8_t* axes;  // several axes: that of each pair; an axis beyond the last is taken as the last
+  int last_axis;
+  int64_t pos_axis;
   uint32_t seq, tokens;
   int R2, D;
   float scale;
@@ -69,7 +73,7 @@ struct Rotary {
 // A lane owns one piece of HEADS heads of a token: V pairs (half) or V / 2 (interleaved), or V elements
 // behind the rotated ones; V elements are 16 bytes.
 // STREAM: what is written will not be in a cache when it is read.
-template <typename T, bool HALF, bool BACK, int HEADS, bool STREAM>
+template <typename T, bool HALF, bool BACK, int HEADS, bool STREAM, bool AXES>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r) {
   constexpr int V = Store<T>::kVec, kPairs = HALF ? V : V / 2;
   // Workgroups of the same tokens follow one another; each takes heads side by side of tokens side by side, whichever of the
@@ -135,15 +139,30 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary r) {
   float c[kPairs], sn[kPairs];
   if (turns) {
     const int64_t p = b * r.pos_batch + s * r.pos_token;
-    int64_t position = r.start;
-    if (!r.positions) position += s;
-    else if (r.wide) position += static_cast<const int64_t*>(r.positions)[p];
-    else position += static_cast<const int32_t*>(r.positions)[p];
-    const double pos = static_cast<double>(position);
+    auto position_at = [&](int64_t n) {
+      int64_t position = r.start;
+      if (!AXES && !r.positions) position += s;
+      else if (r.wide) position += static_cast<const int64_t*>(r.positions)[n];
+      else position += static_cast<const int32_t*>(r.positions)[n];
+      return static_cast<double>(position);
+    };
+    double pos[AXES ? kMostAxes : 1];
+    pos[0] = position_at(p);
+    if constexpr (AXES) {
+#pragma unroll
+      for (int a = 1; a < kMostAxes; ++a) pos[a] = a <= r.last_axis ? position_at(p + a * r.pos_axis) : pos[a - 1];
+    }
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-      const double f = r.freqs[first + min(i, count - 1)];
-      cos_sin(pos, f, r.scale, &c[i], &sn[i]);
+      const int pair = first + min(i, count - 1);
+      const double f = r.freqs[pair];
+      double at_pair = pos[0];
+      if constexpr (AXES) {
+        const int axis = r.axes[pair];
+#pragma unroll
+        for (int a = 1; a < kMostAxes; ++a) at_pair = axis >= a ? pos[a] : at_pair;
+      }
+      cos_sin(at_pair, f, r.scale, &c[i], &sn[i]);
       if (BACK) sn[i] = -sn[i];
     }
   }
@@ -185,7 +204,7 @@ Side side(const tempo_rotary_heads* h) {
 }  // namespace
 
 tempo_status launch_rotary(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
-                           const tempo_rotary_positions* at, int64_t B, int64_t S, int64_t D, int64_t R,
+                           const tempo_rotary_positions* at, const RotaryAxes* axes, int64_t B, int64_t S, int64_t D, int64_t R,
                            tempo_rotary_layout layout, float scale, bool back, tempo_dtype dt, hipStream_t st) {
   Rotary r{};
   r.q = side(q);
@@ -198,6 +217,7 @@ tempo_status launch_rotary(const tempo_rotary_heads* q, const tempo_rotary_heads
   r.pos_batch = at->batch_stride;
   r.pos_token = at->token_stride;
   r.start = at->start;
+  if (axes) r.axes = axes->of_pairs, r.last_axis = axes->count - 1, r.pos_axis = axes->stride;
   r.seq = static_cast<uint32_t>(S);
   r.tokens = static_cast<uint32_t>(B * S);
   r.R2 = static_cast<int>(R / 2);
@@ -244,16 +264,19 @@ tempo_status launch_rotary(const tempo_rotary_heads* q, const tempo_rotary_heads
     });
     return ok ? TEMPO_OK : TEMPO_ERR_LAUNCH;
   };
-  auto by_way = [&](auto type, auto halves) {
+  auto by_way = [&](auto type, auto halves, auto several) {
     using T = decltype(type);
-    constexpr bool HALF = decltype(halves)::value;
+    constexpr bool HALF = decltype(halves)::value, AXES = decltype(several)::value;
     constexpr int HEADS = heads_per_lane(HALF);
-    if (few) return back ? go(rotary_kernel<T, HALF, true, 1, false>) : go(rotary_kernel<T, HALF, false, 1, false>);
-    if (stream) return back ? go(rotary_kernel<T, HALF, true, HEADS, true>) : go(rotary_kernel<T, HALF, false, HEADS, true>);
-    return back ? go(rotary_kernel<T, HALF, true, HEADS, false>) : go(rotary_kernel<T, HALF, false, HEADS, false>);
+    if (few) return back ? go(rotary_kernel<T, HALF, true, 1, false, AXES>) : go(rotary_kernel<T, HALF, false, 1, false, AXES>);
+    if (stream) return back ? go(rotary_kernel<T, HALF, true, HEADS, true, AXES>) : go(rotary_kernel<T, HALF, false, HEADS, true, AXES>);
+    return back ? go(rotary_kernel<T, HALF, true, HEADS, false, AXES>) : go(rotary_kernel<T, HALF, false, HEADS, false, AXES>);
   };
-  if (half) return dt == TEMPO_F32 ? by_way(float{}, std::true_type{}) : by_way(bf16_t{}, std::true_type{});
-  return dt == TEMPO_F32 ? by_way(float{}, std::false_type{}) : by_way(bf16_t{}, std::false_type{});
+  auto by_type = [&](auto halves, auto several) {
+    return dt == TEMPO_F32 ? by_way(float{}, halves, several) : by_way(bf16_t{}, halves, several);
+  };
+  if (axes) return half ? by_type(std::true_type{}, std::true_type{}) : by_type(std::false_type{}, std::true_type{});
+  return half ? by_type(std::true_type{}, std::false_type{}) : by_type(std::false_type{}, std::false_type{});
 }
 
 }  // namespace tempo

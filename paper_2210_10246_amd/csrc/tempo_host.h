@@ -69,9 +69,14 @@ tempo_status launch_attn_bwd_regen(const void* dout, const void* probs, void* ds
                                    void* out_re, int64_t B, int64_t A, int64_t Sq, int64_t Sk,
                                    float p, uint64_t seed, uint64_t offset, tempo_dtype dt,
                                    hipStream_t st);
-// back: the other way round.
+// axes: null, or which axis each pair turns by; back: the other way round.
+struct RotaryAxes {
+  const uint8_t* of_pairs;
+  int count;
+  int64_t stride;  // of positions
+};
 tempo_status launch_rotary(const tempo_rotary_heads* q, const tempo_rotary_heads* k, const double* freqs,
-                           const tempo_rotary_positions* at, int64_t B, int64_t S, int64_t D, int64_t R,
+                           const tempo_rotary_positions* at, const RotaryAxes* axes, int64_t B, int64_t S, int64_t D, int64_t R,
                            tempo_rotary_layout layout, float scale, bool back, tempo_dtype dt, hipStream_t st);
 // What the two entry points of the gated unit take; each looks at its own.
 struct GluCall {
@@ -88,6 +93,23 @@ bool glu_takes(int64_t T, int64_t H, int64_t F);
 size_t glu_workspace_bytes(int64_t T, int64_t H, int64_t F, tempo_dtype dt, bool back);
 tempo_status launch_glu_fwd(const GluCall& c, tempo_dtype dt, hipStream_t st);
 tempo_status launch_glu_bwd(const GluCall& c, tempo_dtype dt, hipStream_t st);
+// What the two entry points of the residual norm take; each looks at its own.
+struct ResidualCall {
+  const void *x, *f, *y, *dy, *dh;
+  void *to_y, *h, *dx, *df;
+  const float* gate;
+  int64_t groups;
+  const tempo_norm *post, *pre;
+  float *dgate, *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
+  float alpha, beta;
+  void* workspace;
+  size_t workspace_bytes;
+  int64_t N, M;
+};
+bool residual_norm_takes(const ResidualCall& c, tempo_dtype dt);
+size_t residual_norm_workspace_bytes(const ResidualCall& c, tempo_dtype dt);
+tempo_status launch_residual_norm_fwd(const ResidualCall& c, tempo_dtype dt, hipStream_t st);
+tempo_status launch_residual_norm_bwd(const ResidualCall& c, tempo_dtype dt, hipStream_t st);
 // What the two entry points of window attention take; each looks at its own.
 struct WindowCall {
   const tempo_attn_heads *q, *k, *v, *out, *dout, *dq, *dk, *dv;
