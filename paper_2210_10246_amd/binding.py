@@ -512,18 +512,20 @@ def tempo_residual_norm_bwd_workspace_bytes(N: int, M: int, groups: int, dtype) 
     return load().tempo_residual_norm_bwd_workspace_bytes(N, M, groups, _DT[dtype])
 
 
-def _norm_of(name, kind, weight, bias, eps, stats, N, M):
+def _norm_checks(name, kind, weight, bias, stats, N, M):
     if kind is None:
         if weight is not None or bias is not None or stats is not None:
             raise ValueError(f"{name} is None: there is no {name}_weight, {name}_bias or {name}_stats")
-        return None, None
+        return
     if kind not in _NORM_KIND:
         raise ValueError(f'{name} must be None, "rms" or "layer", got {kind!r}')
     _want(name + "_weight", weight, torch.float32, M)
     _want(name + "_bias", bias, torch.float32, M)
     _want(name + "_stats", stats, torch.float32, 2 * N)
-    n = _Norm(_NORM_KIND[kind], _ptr(weight), _ptr(bias), eps, _ptr(stats))
-    return n, ctypes.byref(n)
+
+
+def _norm_of(kind, weight, bias, eps, stats):
+    return None if kind is None else _Norm(_NORM_KIND[kind], _ptr(weight), _ptr(bias), eps, _ptr(stats))
 
 
 def _residual_sizes(like, gate):
@@ -556,11 +558,12 @@ def tempo_residual_norm_fwd(x, f, gate, y, h, post, post_weight, post_bias, post
         raise ValueError("h is needed, which pre makes")
     for name, t in (("f", f), ("y", y), ("h", h if pre is not None else None)):
         _want(name, t, x.dtype, x.numel())
-    a, post_ref = _norm_of("post", post, post_weight, post_bias, post_eps, post_stats, N, M)
-    b, pre_ref = _norm_of("pre", pre, pre_weight, pre_bias, pre_eps, pre_stats, N, M)
+    _norm_checks("post", post, post_weight, post_bias, post_stats, N, M)
+    _norm_checks("pre", pre, pre_weight, pre_bias, pre_stats, N, M)
     pointers = [_ptr(t) for t in (x, f, gate, y, h if pre is not None else None)]
+    norms = _norm_of(post, post_weight, post_bias, post_eps, post_stats), _norm_of(pre, pre_weight, pre_bias, pre_eps, pre_stats)
     _same_device(x, f, gate, y, h, post_weight, post_bias, post_stats, pre_weight, pre_bias, pre_stats)
-    _check(load().tempo_residual_norm_fwd(*pointers[:3], groups, post_ref, pre_ref, *pointers[3:], alpha, beta, N, M, dt, _stream(stream)),
+    _check(load().tempo_residual_norm_fwd(*pointers[:3], groups, *norms, *pointers[3:], alpha, beta, N, M, dt, _stream(stream)),
            "tempo_residual_norm_fwd")
 
 
@@ -591,8 +594,9 @@ def tempo_residual_norm_bwd(dy, dh, f, y, gate, dx, df, dgate, post, post_weight
         if t is not None and kind is None:
             raise ValueError(f"{name} is the gradient of a norm that is None")
         _want(name, t, torch.float32, M)
-    a, post_ref = _norm_of("post", post, post_weight, post_bias, 0.0, post_stats, N, M)
-    b, pre_ref = _norm_of("pre", pre, pre_weight, None, 0.0, pre_stats, N, M)
+    _norm_checks("post", post, post_weight, post_bias, post_stats, N, M)
+    _norm_checks("pre", pre, pre_weight, None, pre_stats, N, M)
+    norms = _norm_of(post, post_weight, post_bias, 0.0, post_stats), _norm_of(pre, pre_weight, None, 0.0, pre_stats)
     ins = [_ptr(t) for t in (dy, with_pre[0], f, with_pre[1], gate)]
     outs = [_ptr(t) for t in (dx, df, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias)]
     _same_device(dy, dh, f, y, gate, dx, df, dgate, post_weight, post_bias, post_stats, dpost_weight, dpost_bias, pre_weight, pre_stats,
@@ -600,7 +604,7 @@ def tempo_residual_norm_bwd(dy, dh, f, y, gate, dx, df, dgate, post, post_weight
     columns = any(t is not None for t in (dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias))
     need = load().tempo_residual_norm_bwd_workspace_bytes(N, M, groups, dt) if columns else 0
     ws = _workspace(workspace, need, f.device, stream)
-    _check(load().tempo_residual_norm_bwd(*ins, groups, post_ref, pre_ref, *outs, alpha, beta, _ptr(ws), ws.numel() * ws.element_size(),
+    _check(load().tempo_residual_norm_bwd(*ins, groups, *norms, *outs, alpha, beta, _ptr(ws), ws.numel() * ws.element_size(),
                                           N, M, dt, _stream(stream)), "tempo_residual_norm_bwd")
 
 

@@ -7,7 +7,11 @@ Only what is stashed for backward differs from the stock layers:
   TempoAttentionCore softmax -> dropout -> (. @ V) keeping the softmax output P and a 1-bit
                      mask; the dropout output is a transient in forward and is recomputed by
                      the backward kernel for the gradient of V (Sec. 3.3).
-  RotaryPositions    turns the heads of q and k by their positions; keeps nothing but those
+  RotaryPositions    turns the heads of q and k by their positions, on one axis or several; keeps nothing but those
+  TempoWindowAttention  attention with a sliding window and first tokens that stay visible, over no matrix of scores: keeps q, k, v,
+                     its output and one float per row
+  TempoResidualNorm  the place between two blocks: a norm of the block's output, its gate, the residual and the next block's norm, from
+                     the block's output, the residual and two floats per norm and row
   TempoGatedFFN      a gated feed-forward block keeping its input and the two projections; their
                      activated product, which the second Linear would keep, is made once more by
                      the backward kernel
@@ -116,16 +120,7 @@ class _InplaceLayerNormFn(torch.autograd.Function):
         return dx, dgamma, dbeta, None, None
 
 
-class InplaceLayerNorm(nn.Module):
-    """LayerNorm over the last dimension whose backward needs the output and rstd (Sec. 3.2).
-    Parameters are float32 whatever the activation dtype; gamma must stay non-zero."""
-
-    def __init__(self, hidden: int, eps: float = 1e-5):
-        super().__init__()
-        self.weight = nn.Parameter(torch.ones(hidden, dtype=torch.float32))
-        self.bias = nn.Parameter(torch.zeros(hidden, dtype=torch.float32))
-        self.eps = eps
-
+class _Float32Parameters(nn.Module):
     def _apply(self, fn, recurse=True):
         # .bfloat16() / .half() / .to(dtype) on a model must not narrow gamma and beta: the
         # kernels read them as float32.  Follow the device of the cast, keep the values.
@@ -135,6 +130,17 @@ class InplaceLayerNorm(nn.Module):
                 out = t.to(device=out.device)
             return out
         return super()._apply(keep_float32, recurse)
+
+
+class InplaceLayerNorm(_Float32Parameters):
+    """LayerNorm over the last dimension whose backward needs the output and rstd (Sec. 3.2).
+    Parameters are float32 whatever the activation dtype; gamma must stay non-zero."""
+
+    def __init__(self, hidden: int, eps: float = 1e-5):
+        super().__init__()
+        self.weight = nn.Parameter(torch.ones(hidden, dtype=torch.float32))
+        self.bias = nn.Parameter(torch.zeros(hidden, dtype=torch.float32))
+        self.eps = eps
 
     def forward(self, x):
         w, b = self.weight, self.bias
@@ -227,53 +233,216 @@ class _RotaryFn(torch.autograd.Function):
     other way, which is differentiable in turn."""
 
     @staticmethod
-    def forward(ctx, q, k, freqs, positions, start, layout, scale, back):
+    def forward(ctx, q, k, freqs, positions, start, layout, scale, back, axes=None):
         ctx.set_materialize_grads(False)
-        ctx.save_for_backward(freqs, positions)
+        ctx.save_for_backward(freqs, positions, axes)
         ctx.setting = start, layout, scale, back
         sides = [None if t is None else t if t.stride(-1) == 1 else t.contiguous() for t in (q, k)]
         out = [None if t is None else t.new_empty(t.shape[0], t.shape[2], t.shape[1], t.shape[3]).transpose(1, 2) for t in sides]
-        call = B.tempo_rotary_bwd if back else B.tempo_rotary_fwd
         first, second = (0, 1) if q is not None else (1, 0)
-        call(sides[first], sides[second], freqs, positions, out[first], out[second], layout, scale, start)
+        if axes is None:
+            call, where = B.tempo_rotary_bwd if back else B.tempo_rotary_fwd, (positions,)
+        else:
+            call, where = B.tempo_rotary_axes_bwd if back else B.tempo_rotary_axes_fwd, (axes, positions)
+        call(sides[first], sides[second], freqs, *where, out[first], out[second], layout, scale, start)
         return tuple(out)
 
     @staticmethod
     def backward(ctx, dq, dk):
         start, layout, scale, back = ctx.setting
-        freqs, positions = ctx.saved_tensors
+        freqs, positions, axes = ctx.saved_tensors
         dq, dk = (g if n else None for g, n in zip((dq, dk), ctx.needs_input_grad))
         if dq is not None or dk is not None:
-            dq, dk = _RotaryFn.apply(dq, dk, freqs, positions, start, layout, scale, not back)
-        return dq, dk, None, None, None, None, None, None
+            dq, dk = _RotaryFn.apply(dq, dk, freqs, positions, start, layout, scale, not back, axes)
+        return dq, dk, None, None, None, None, None, None, None
+
+
+def rotary_axes(sections: Tuple[int, ...], order: str = "blocks") -> torch.Tensor:
+    """Which axis each pair turns by (uint8), sections[a] of them by axis a: "blocks" of pairs, or "cyclic", dealt out in turn to the axes
+    that have not got theirs."""
+    if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) < 1:
+        raise ValueError(f"sections are of 1 to 4 axes and not all empty, got {sections}")
+    if order == "blocks":
+        of_pairs = [a for a, n in enumerate(sections) for _ in range(n)]
+    elif order == "cyclic":
+        of_pairs = [a for turn in range(max(sections)) for a, n in enumerate(sections) if turn < n]
+    else:
+        raise ValueError(f'order must be "blocks" or "cyclic", got {order!r}')
+    return torch.tensor(of_pairs, dtype=torch.uint8)
 
 
 class RotaryPositions(nn.Module):
     """Rotary positions of q and k [B, heads, S, D], of any strides, whose numbers of heads may differ; k may be None.  positions:
     [S] or [B, S], int32 or int64 (0, 1, ... if None); start is added to them.  Turns the first `dim` elements of a head; layout:
-    "half" pairs element i with i + dim / 2, "interleaved" 2 i with 2 i + 1.  The other arguments are rotary_frequencies()'s."""
+    "half" pairs element i with i + dim / 2, "interleaved" 2 i with 2 i + 1.  sections, order: rotary_axes()'s, for several axes (time,
+    height and width); positions are [axes, S] or [axes, B, S] then.  own: each axis has all frequencies of its own pairs' number, not its
+    part of one row of them.  The other arguments are rotary_frequencies()'s."""
 
     def __init__(self, dim: int, base: float = 10000.0, layout: str = "half", scaling: Optional[str] = None, factor: float = 1.0,
-                 trained: int = 0, turns: Tuple[float, float] = (1.0, 32.0)):
+                 trained: int = 0, turns: Tuple[float, float] = (1.0, 32.0), sections: Optional[Tuple[int, ...]] = None,
+                 order: str = "blocks", own: bool = False):
         super().__init__()
         if layout not in ("half", "interleaved"):
             raise ValueError(f'layout must be "half" or "interleaved", got {layout!r}')
         freqs, self.scale = rotary_frequencies(dim, base, scaling, factor, trained, turns)
-        self.layout = layout
+        self.layout, axes = layout, None
+        if sections is not None:
+            axes = rotary_axes(sections, order)
+            if axes.numel() != dim // 2:
+                raise ValueError(f"sections must make {dim // 2} pairs, got {sections}")
+            if own:
+                for a, n in enumerate(sections):
+                    if n > 0:
+                        freqs[axes == a] = rotary_frequencies(2 * n, base, scaling, factor, trained, turns)[0]
+        elif own:
+            raise ValueError("own frequencies are those of sections' axes")
         self.register_buffer("freqs", freqs, persistent=False)
+        self.register_buffer("axes", axes, persistent=False)
 
     def _apply(self, fn, recurse=True):
         # a cast of the model follows the device and leaves the frequencies in float64
-        freqs = self.freqs
+        freqs, axes = self.freqs, self.axes
         super()._apply(fn, recurse)
         if self.freqs.dtype != torch.float64:
             self.freqs = freqs.to(device=self.freqs.device)
+        if axes is not None and self.axes.dtype != torch.uint8:
+            self.axes = axes.to(device=self.axes.device)
         return self
 
     def forward(self, q, k=None, positions=None, start: int = 0):
+        if self.axes is not None and positions is None:
+            raise ValueError("several axes have positions, [axes, S] or [axes, B, S]")
         k_in = None if k is None else k.transpose(1, 2)
-        q, k = _RotaryFn.apply(q.transpose(1, 2), k_in, self.freqs, positions, start, self.layout, self.scale, False)
+        q, k = _RotaryFn.apply(q.transpose(1, 2), k_in, self.freqs, positions, start, self.layout, self.scale, False, self.axes)
         return q.transpose(1, 2), None if k is None else k.transpose(1, 2)
+
+
+class _WindowAttentionFn(torch.autograd.Function):
+    """q [B, Sq, heads, D], k and v [B, Sk, kv_heads, D] to an output that lies by token."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, window, sinks, scale, key_len, query_start, keep):
+        q, k, v = (t if t.stride(-1) == 1 else t.contiguous() for t in (q, k, v))
+        out = q.new_empty(q.shape)
+        lse = q.new_empty(q.shape[0], q.shape[2], q.shape[1], dtype=torch.float32) if keep else None
+        B.tempo_window_attn_fwd(q, k, v, out, lse, window, sinks, scale, key_len, query_start)
+        ctx.setting = window, sinks, scale
+        if keep:
+            ctx.save_for_backward(q, k, v, out, lse, key_len, query_start)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        if torch.is_grad_enabled():      # the kernels' gradients would be constants to a second derivative
+            raise RuntimeError("TempoWindowAttention has no second derivative: its gradients cannot be taken with create_graph=True")
+        q, k, v, out, lse, key_len, query_start = ctx.saved_tensors
+        dout = dout if dout.stride(-1) == 1 else dout.contiguous()
+        dq, dk, dv = (t.new_empty(t.shape) for t in (q, k, v))
+        B.tempo_window_attn_bwd(dout, q, k, v, out, lse, dq, dk, dv, *ctx.setting[:2], ctx.setting[2], key_len, query_start)
+        return tuple(g if n else None for g, n in zip((dq, dk, dv), ctx.needs_input_grad)) + (None,) * 6
+
+
+class TempoWindowAttention(nn.Module):
+    """Attention of q [B, heads, Sq, D] over k and v [B, kv_heads, Sk, D], of any strides: a query at position P sees the keys up to P that
+    are among the last `window` or the first `sinks`.  Heads of q share those of k and v where there are more of them.  key_len [B]
+    int32: keys from there on do not exist; query_start [B] int32: positions of the first queries (Sk - Sq if None), as for new tokens
+    of sequences in a cache.  scale: D^-0.5 if None.  No dropout, no second derivative."""
+
+    def __init__(self, window: int, sinks: int = 0, scale: Optional[float] = None):
+        super().__init__()
+        if window < 1 or sinks < 0:
+            raise ValueError(f"window must be at least 1 and sinks at least 0, got {window} and {sinks}")
+        if scale is not None and not 0.0 < scale < math.inf:
+            raise ValueError(f"scale must be positive and finite, got {scale}")
+        self.window, self.sinks, self.scale = window, sinks, scale
+
+    def forward(self, q, k, v, key_len=None, query_start=None):
+        if torch.is_autocast_enabled("cuda"):    # as a product would take them
+            q, k, v = (t.to(torch.get_autocast_dtype("cuda")) for t in (q, k, v))
+        keep = torch.is_grad_enabled() and any(t.requires_grad for t in (q, k, v))
+        q, k, v = (t.transpose(1, 2) for t in (q, k, v))
+        return _WindowAttentionFn.apply(q, k, v, self.window, self.sinks, self.scale, key_len, query_start, keep).transpose(1, 2)
+
+
+class _ResidualNormFn(torch.autograd.Function):
+    """y = alpha x + beta gate post(f) and h = pre(y), or y alone."""
+
+    @staticmethod
+    def forward(ctx, x, f, gate, pw, pb, qw, qb, post, pre, alpha, beta, eps):
+        x, f = _aligned(x), _aligned(f)
+        M = x.shape[-1]
+        rows = x.numel() // M if M else 0
+        y, h = torch.empty_like(x), torch.empty_like(x) if pre else None
+        stats = [x.new_empty(rows, 2, dtype=torch.float32) if kind else None for kind in (post, pre)]
+        B.tempo_residual_norm_fwd(x, f, gate, y, h, post, pw, pb, stats[0], pre, qw, qb, stats[1], alpha, beta, eps, eps)
+        ctx.setting = post, pre, alpha, beta
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(f, y if pre else None, gate, pw, pb, qw, *stats)
+        return (y, h) if pre else y
+
+    @staticmethod
+    def backward(ctx, dy, dh=None):
+        if torch.is_grad_enabled():      # the kernels' gradients would be constants to a second derivative
+            raise RuntimeError("TempoResidualNorm has no second derivative: its gradients cannot be taken with create_graph=True")
+        post, pre, alpha, beta = ctx.setting
+        f, y, gate, pw, pb, qw, post_stats, pre_stats = ctx.saved_tensors
+        if dy is None and dh is None:
+            return (None,) * 12
+        if pre and dh is None:
+            dh = torch.zeros_like(f)
+        dx, df = torch.empty_like(f), torch.empty_like(f)
+        need = ctx.needs_input_grad
+        like = [torch.empty_like(t) if n else None for t, n in zip((gate, pw, pb, qw), need[2:6])]
+        dqb = f.new_empty(f.shape[-1], dtype=torch.float32) if need[6] else None
+        B.tempo_residual_norm_bwd(_aligned(dy), _aligned(dh), f, y, gate, dx, df, like[0], post, pw, pb, post_stats, like[1], like[2], pre, qw,
+                                  pre_stats, like[3], dqb, alpha, beta)
+        return (dx if need[0] else None, df if need[1] else None, *like, dqb) + (None,) * 5
+
+
+class TempoResidualNorm(_Float32Parameters):
+    """The place between two blocks of a pre-norm model, for the residual x and a block's output f: y = alpha x + beta gate post(f), the next
+    residual, and h = pre(y), the next block's input (None without a pre).  post, pre: "rms", "layer" or None.  gate: a learned one of
+    `hidden` elements that begins at that value; or None, and forward takes one, [hidden] or one for each of equally many rows (as
+    [B, 1, hidden] beside [B, S, hidden]), or none.  affine: the norms have weights, and with "layer" biases.  Parameters and gates
+    are float32 whatever the activation dtype.  No second derivative."""
+
+    def __init__(self, hidden: int, post: Optional[str] = None, pre: Optional[str] = "rms", gate: Optional[float] = None, alpha: float = 1.0,
+                 beta: float = 1.0, eps: float = 1e-5, affine: bool = True):
+        super().__init__()
+        for name, kind in (("post", post), ("pre", pre)):
+            if kind not in (None, "rms", "layer"):
+                raise ValueError(f'{name} must be "rms", "layer" or None, got {kind!r}')
+            weight = nn.Parameter(torch.ones(hidden)) if kind and affine else None
+            self.register_parameter(name + "_weight", weight)
+            self.register_parameter(name + "_bias", nn.Parameter(torch.zeros(hidden)) if kind == "layer" and affine else None)
+        self.register_parameter("gate", None if gate is None else nn.Parameter(torch.full((hidden,), float(gate))))
+        self.hidden, self.post, self.pre, self.alpha, self.beta, self.eps = hidden, post, pre, alpha, beta, eps
+
+    def _gate_of_groups(self, gate, x):
+        """[hidden] or [groups, hidden]; with as many dimensions as x it has x's sizes first, then ones."""
+        if gate.dim() == x.dim() > 2:
+            first = 0
+            while first < x.dim() - 1 and gate.shape[first] == x.shape[first]:
+                first += 1
+            if all(n == 1 for n in gate.shape[first:-1]):
+                return gate.reshape(-1, gate.shape[-1])
+        elif gate.dim() in (1, 2):
+            return gate
+        raise ValueError(f"gate must be [{self.hidden}], [groups, {self.hidden}] or like x with ones behind its groups, got {tuple(gate.shape)}")
+
+    def forward(self, x, f, gate=None):
+        if torch.is_autocast_enabled("cuda"):
+            f = f.to(x.dtype)       # a block's output beside a residual in float32
+        if x.shape[-1:] != (self.hidden,) or f.shape != x.shape:
+            raise ValueError(f"x and f must be [..., {self.hidden}], got {tuple(x.shape)} and {tuple(f.shape)}")
+        if gate is not None and self.gate is not None:
+            raise ValueError("this place has a gate of its own")
+        gate = self.gate if gate is None else gate
+        if gate is not None:
+            gate = self._gate_of_groups(gate, x).float().contiguous()
+        params = [None if p is None else p.float() for p in (self.post_weight, self.post_bias, self.pre_weight, self.pre_bias)]
+        out = _ResidualNormFn.apply(x, f, gate, *params, self.post, self.pre, self.alpha, self.beta, self.eps)
+        return out if self.pre else (out, None)
 
 
 def _aligned(t):
