@@ -40,7 +40,9 @@ struct Heads {
 };
 struct Attn {
   Heads q, k, v, out, dout, dq, dk, dv;
-  float *lse, *delta;  // [B, heads, Sq]
+  float* lse;          // [B, heads, Sq]
+  float* stats;        // backward: lse of base 2, then delta, [2, B, heads, Sq]
+  int64_t stat_rows;   // B heads Sq
   const int32_t *key_len, *query_start;
   int Sq, Sk, heads, kv_heads, group, rows, D;  // rows: Sq * group
   FastDiv by_group;
@@ -73,19 +75,22 @@ struct Sight {
 // ---- matrices in LDS ----------------------------------------------------------------------------------------------------
 // Rows of DP elements in pieces of 16 bytes.  A matrix instruction takes 32 rows by two pieces (lane n: row n % 32, piece 2 s + n / 32)
 // or, transposed, 32 columns by the rows that a lane's sums of the other product lie in (4 (n / 32) + 0 .. 3 of each eight).
-// Pieces are stored in another order in each row so that the lanes of a read meet different banks.
+// Pieces are stored in another order in each row, in bfloat16 rows of 16 pieces and more with a gap behind every fourth row, so that the
+// lanes of a read meet different banks.
 template <typename T, int DP>
 struct Rows {
-  static constexpr int V = Store<T>::kVec, P = DP / V, kPitch = P * 16, kSteps = P / 2;
+  static constexpr int V = Store<T>::kVec, P = DP / V, kPitch = P * 16, kSteps = P / 2, kGap = sizeof(T) == 2 && P >= 16 ? 16 : 0;
   static_assert(P >= 8, "");
+  static constexpr int bytes(int rows) { return rows * kPitch + rows / 4 * kGap; }
   __device__ static __forceinline__ int swizzle(int row) {
     if constexpr (sizeof(T) == 4) return (row >> 2 & 1) << 3 | (row & 3) | (row >> 3 & 1) << 2;
     else if constexpr (P == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
-    else return (row & 3) << 2 | (row >> 2 & 3);
+    else return (row & 3) << 2;
   }
+  __device__ static __forceinline__ int place(int row) { return row * kPitch + row / 4 * kGap; }
   __device__ static __forceinline__ u32x4 rows(const char* lds, int row0, int step) {
-    const int lane = threadIdx.x % kWave, row = row0 + lane % 32, piece = 2 * step + lane / 32;
-    return *reinterpret_cast<const u32x4*>(lds + row * kPitch + ((piece ^ swizzle(row)) << 4));
+    const int lane = threadIdx.x % kWave, row = lane % 32, piece = 2 * step + lane / 32;
+    return *reinterpret_cast<const u32x4*>(lds + bytes(row0) + place(row) + ((piece ^ swizzle(row)) << 4));
   }
 };
 
@@ -126,7 +131,7 @@ __device__ __forceinline__ f32x16 multiply_columns(const char* lds, int row0, in
   const int lane = threadIdx.x % kWave;
   if constexpr (sizeof(T) == 2) {
     // 16 lanes read 4 rows of 16 columns, 4 columns each, and get 4 rows of a column each
-    const int j = lane % 16, line = row0 + 4 * (lane / 32) + j / 4, piece = block * 4 + (lane / 16 & 1) * 2 + (j % 4) / 2;
+    const int j = lane % 16, line = 4 * (lane / 32) + j / 4, piece = block * 4 + (lane / 16 & 1) * 2 + (j % 4) / 2;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       union {
@@ -135,8 +140,9 @@ __device__ __forceinline__ f32x16 multiply_columns(const char* lds, int row0, in
       } a;
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        const int r = line + 16 * u + 8 * n;
-        a.h[n] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + r * R::kPitch + ((piece ^ R::swizzle(r)) << 4) + (j & 1) * 8));
+        const int r = 16 * u + 8 * n;  // rows beyond `line`, whose order of pieces is that of line but for rows of 8 pieces
+        a.h[n] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + R::bytes(row0 + r) + R::place(line) +
+                                                                      ((piece ^ R::swizzle(R::kGap ? line : line + r)) << 4) + (j & 1) * 8));
       }
       c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.all, __builtin_bit_cast(bf16x8, w.w[u]), c, 0, 0, 0);
     }
@@ -145,7 +151,7 @@ __device__ __forceinline__ f32x16 multiply_columns(const char* lds, int row0, in
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int r = row0 + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
-      const float a = *reinterpret_cast<const float*>(lds + r * R::kPitch + ((column / 4 ^ R::swizzle(r)) << 4) + column % 4 * 4);
+      const float a = *reinterpret_cast<const float*>(lds + R::place(r) + ((column / 4 ^ R::swizzle(r)) << 4) + column % 4 * 4);
       c = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[i], c, 0, 0, 0);
     }
   }
@@ -171,21 +177,71 @@ struct Staged {
   static constexpr int kPieces = N * R::P / kThreads;
   static_assert(N * R::P % kThreads == 0, "whole pieces a lane");
   u32x4 v[kPieces];
-  // row_at: row -> its elements, or null for zeros
+  __device__ __forceinline__ explicit Staged(const Heads&) {}
+  // of: row -> its elements
   template <typename F>
-  __device__ __forceinline__ void load(int D, F&& row_at) {
+  __device__ __forceinline__ void load(int D, F&& of) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int at = i * kThreads + static_cast<int>(threadIdx.x), row = at / R::P, piece = at % R::P ^ R::swizzle(row);
-      const T* p = row_at(row);
-      v[i] = p ? load_of_row<T>(p, piece, D) : u32x4{0, 0, 0, 0};
+      v[i] = load_of_row<T>(of(row), piece, D);
     }
   }
   __device__ __forceinline__ void store(char* lds) const {
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) *reinterpret_cast<u32x4*>(lds + (i * kThreads + static_cast<int>(threadIdx.x)) * 16) = v[i];
+    for (int i = 0; i < kPieces; ++i) {
+      const int at = i * kThreads + static_cast<int>(threadIdx.x);
+      *reinterpret_cast<u32x4*>(lds + R::place(at / R::P) + at % R::P * 16) = v[i];
+    }
   }
 };
+
+// Waits until all of the wave's loads have come (and for nothing else).
+__device__ __forceinline__ void landed() { __builtin_amdgcn_s_waitcnt(0xF70); }
+// N rows of a matrix from memory to LDS without registers: rows that begin at multiples of 16 bytes, D a multiple of a piece.  In assembly
+// because the compiler waits for all such loads before any read of LDS; whoever calls this waits for them.  It has no output, and nothing else
+// here uses m0.  Lanes of pieces behind D load nothing, and what LDS holds there stays.
+template <typename T, int DP, int N>
+struct Direct {
+  using R = Rows<T, DP>;
+  static constexpr int kPieces = N * R::P / kThreads;
+  static_assert(R::kGap == 0 || R::P * 4 % kWave == 0 || kWave % (R::P * 4) == 0, "no gap within what a wave loads");
+  uint32_t offset[kPieces];  // bytes from the first row
+  __device__ __forceinline__ Direct(const Heads& h) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      offset[i] = static_cast<uint32_t>(row(i)) * static_cast<uint32_t>(h.token * sizeof(T)) + static_cast<uint32_t>(piece(i)) * 16;
+  }
+  __device__ static __forceinline__ int row(int i) { return (i * kThreads + static_cast<int>(threadIdx.x)) / R::P; }
+  __device__ static __forceinline__ int piece(int i) {
+    return (i * kThreads + static_cast<int>(threadIdx.x)) % R::P ^ R::swizzle(row(i));
+  }
+  __device__ static __forceinline__ uint32_t to(char* lds, int i) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds)) +
+           R::place((i * kThreads + wave * kWave) / R::P) + (i * kThreads + wave * kWave) % R::P * 16;
+  }
+  // first: the first row (uniform)
+  __device__ __forceinline__ void load(const T* first, int D, char* lds) const {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (DP == D || piece(i) * R::V < D)
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(offset[i]), "s"(to(lds, i)), "s"(first) : "m0", "memory");
+  }
+  // of: row -> its elements
+  template <typename F>
+  __device__ __forceinline__ void load_each(int D, char* lds, F&& of) const {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const T* const p = of(row(i)) + piece(i) * R::V;
+      if (DP == D || piece(i) * R::V < D)
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(to(lds, i)) : "m0", "memory");
+    }
+  }
+};
+__device__ __forceinline__ void clear_lds(char* lds, int bytes) {
+  for (int i = threadIdx.x * 16; i < bytes; i += kThreads * 16) *reinterpret_cast<u32x4*>(lds + i) = u32x4{0, 0, 0, 0};
+}
 
 template <typename T>
 __device__ __forceinline__ const T* at(const Heads& h, int b, int token, int head) {
@@ -221,15 +277,79 @@ __device__ __forceinline__ int in_order(int block, int total) {
 // The key tiles that the rows of a workgroup see: those of the first keys, then those of the window.
 struct KeyTiles {
   int of_sinks, first, count;
-  int low, high;  // of the window; keys from high on are seen by none
+  int low, high, sinks;  // seen by some row: [low, high) and those below sinks
   __device__ __forceinline__ KeyTiles(const Sight& s, int i0, int i1, int keys) {
     low = s.begin(i0);
     high = s.end(i1);
-    of_sinks = (min(s.sinks, high) + keys - 1) / keys;
+    sinks = min(s.sinks, high);
+    of_sinks = (sinks + keys - 1) / keys;
     first = max(low / keys, of_sinks);
-    count = of_sinks + max((high + keys - 1) / keys - first, 0);
+    count = of_sinks + (low < high ? max((high + keys - 1) / keys - first, 0) : 0);
   }
   __device__ __forceinline__ int key(int n, int keys) const { return (n < of_sinks ? n : first + n - of_sinks) * keys; }
+  // Whether some row sees key j of a tile; if none does, one beside it that is seen, whose elements are then in its place: of a key that
+  // is not looked at nothing is known, and 0 times it need not be 0.
+  __device__ __forceinline__ bool all(int j0, int keys) const { return j0 + keys <= high && (j0 >= low || j0 + keys <= sinks); }
+  __device__ __forceinline__ int seen(int j) const {
+    if (j < sinks || (j >= low && j < high)) return j;
+    return low < high ? min(max(j, low), high - 1) : sinks - 1;
+  }
+};
+
+// The tiles of k and v that the rows of a workgroup see, one after the other through two buffers: while one is worked on, the next is on
+// its way.  DIRECT: without registers.
+template <typename T, int DP, int BK, bool DIRECT>
+struct KeyStream {
+  static constexpr int kBytes = Rows<T, DP>::bytes(BK);
+  const Attn& a;
+  const Sight& s;
+  const KeyTiles& keys;
+  const T *k, *v;  // of key 0
+  char (*lds)[2][kBytes];
+  std::conditional_t<DIRECT, Direct<T, DP, BK>, Staged<T, DP, BK>> ks, vs;
+  __device__ __forceinline__ KeyStream(const Attn& a_, const Sight& s_, const KeyTiles& keys_, int b, int kv, char (*lds_)[2][kBytes])
+      : a(a_), s(s_), keys(keys_), k(at<T>(a_.k, b, 0, kv)), v(at<T>(a_.v, b, 0, kv)), lds(lds_), ks(a_.k), vs(a_.v) {
+    if (DIRECT && a.D < DP) {
+      clear_lds(lds[0][0], 4 * kBytes);
+      lds_barrier();
+    }
+  }
+  __device__ __forceinline__ void fetch(int n, int to) {
+    const int j0 = keys.key(n, BK);
+    if constexpr (DIRECT) {
+      if (keys.all(j0, BK)) {
+        ks.load(k + j0 * a.k.token, a.D, lds[to][0]);
+        vs.load(v + j0 * a.v.token, a.D, lds[to][1]);
+      } else {
+        ks.load_each(a.D, lds[to][0], [&](int r) { return k + keys.seen(j0 + r) * a.k.token; });
+        vs.load_each(a.D, lds[to][1], [&](int r) { return v + keys.seen(j0 + r) * a.v.token; });
+      }
+    } else {
+      ks.load(a.D, [&](int r) { return k + keys.seen(j0 + r) * a.k.token; });
+      vs.load(a.D, [&](int r) { return v + keys.seen(j0 + r) * a.v.token; });
+    }
+  }
+  __device__ __forceinline__ void put(int to) {
+    if constexpr (!DIRECT) {
+      ks.store(lds[to][0]);
+      vs.store(lds[to][1]);
+    }
+  }
+  // work(tile's first key, its k, its v) for tiles [n0, n1)
+  template <typename F>
+  __device__ __forceinline__ void each(int n0, int n1, F&& work) {
+    if (n0 >= n1) return;
+    fetch(n0, 0);
+    put(0);
+    for (int n = n0; n < n1; ++n) {
+      const int now = (n - n0) & 1;
+      if constexpr (DIRECT) landed();
+      lds_barrier();  // the tile is there, and the other buffer has been read
+      if (n + 1 < n1) fetch(n + 1, now ^ 1);
+      work(keys.key(n, BK), lds[now][0], lds[now][1]);
+      if (n + 1 < n1) put(now ^ 1);
+    }
+  }
 };
 
 // What a wave's 32 rows see of keys [j0, j0 + n).
@@ -259,11 +379,16 @@ struct WaveRows {
 __device__ __forceinline__ int key_of(int i) { return 8 * (i / 4) + 4 * (static_cast<int>(threadIdx.x) % kWave / 32) + i % 4; }
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
-template <typename T, int DP, int BK>
-__global__ __launch_bounds__(kThreads) void forward_kernel(Attn a) {
+// Waves on a SIMD: two where their registers allow it, one at its matrix instructions while the other is at its exponentials.
+template <typename T, int DP, bool DIRECT>
+constexpr int kAtOnce = DIRECT && sizeof(T) * DP <= 256 ? 2 : 1;
+
+template <typename T, int DP, int BK, bool DIRECT>
+__global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_kernel(Attn a) {
   using R = Rows<T, DP>;
-  constexpr int kBytes = BK * R::kPitch, kBlocks = BK / 32, kColumns = DP / 32;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][kBytes];
+  using Stream = KeyStream<T, DP, BK, DIRECT>;
+  constexpr int kBlocks = BK / 32, kColumns = DP / 32;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][Stream::kBytes];
   const int job = in_order(blockIdx.x, gridDim.x), split = job % a.splits, tile = job / a.splits % a.tiles;
   const int bk = job / a.splits / a.tiles, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
   const Sight s(a, b);
@@ -282,69 +407,49 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(Attn a) {
 #pragma unroll
   for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
   float m = kMinusInf, sum = 0.0f;  // maximum, of base 2, and the lane's part of the sum
-  Staged<T, DP, BK> ks, vs;
-  auto fetch = [&](int n) {
-    const int j0 = keys.key(n, BK);
-    auto there = [&](int r) { return j0 + r < keys.high && (j0 + r >= keys.low || j0 + r < s.sinks); };
-    ks.load(a.D, [&](int r) { return there(r) ? at<T>(a.k, b, j0 + r, kv) : nullptr; });
-    vs.load(a.D, [&](int r) { return there(r) ? at<T>(a.v, b, j0 + r, kv) : nullptr; });
-  };
-  if (n0 < n1) {
-    fetch(n0);
-    ks.store(lds[0][0]);
-    vs.store(lds[0][1]);
-    lds_barrier();
-  }
-  for (int n = n0; n < n1; ++n) {
-    const int j0 = keys.key(n, BK), now = (n - n0) & 1;
-    if (n + 1 < n1) fetch(n + 1);
-    if (w.any && !w.none(s, j0, BK)) {
-      f32x16 p[kBlocks];
+  Stream stream(a, s, keys, b, kv, lds);
+  stream.each(n0, n1, [&](int j0, const char* k_tile, const char* v_tile) {
+    if (!w.any || w.none(s, j0, BK)) return;
+    f32x16 p[kBlocks];
 #pragma unroll
-      for (int kb = 0; kb < kBlocks; ++kb) {
-        p[kb] = zeros();
+    for (int kb = 0; kb < kBlocks; ++kb) {
+      p[kb] = zeros();
 #pragma unroll
-        for (int t = 0; t < R::kSteps; ++t) p[kb] = multiply<T>(R::rows(lds[now][0], kb * 32, t), q[t], p[kb]);
-      }
-      if (!w.all(s, j0, BK)) {
-#pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) p[kb][i] = w.sees(s, j0 + kb * 32 + key_of(i)) ? p[kb][i] : kMinusInf;
-      }
-      float top = p[0][0];
+      for (int t = 0; t < R::kSteps; ++t) p[kb] = multiply<T>(R::rows(k_tile, kb * 32, t), q[t], p[kb]);
+    }
+    if (!w.all(s, j0, BK)) {
 #pragma unroll
       for (int kb = 0; kb < kBlocks; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, p[kb][i]);
-      top = a.c * across_rows<32>(top, [](float x, float y) { return fmaxf(x, y); });
-      // What the exponentials are relative to follows the maximum only where they would pass 2^8: nothing is lost below that.
-      if (__any(top > m + 8.0f)) {
-        const float next = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (next == kMinusInf ? 0.0f : next));
-        m = next;
-        sum *= by;
-#pragma unroll
-        for (int d = 0; d < kColumns; ++d) acc[d] *= by;
-      }
-      const float from = m == kMinusInf ? 0.0f : m;
-#pragma unroll
-      for (int kb = 0; kb < kBlocks; ++kb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          p[kb][i] = __builtin_amdgcn_exp2f(fmaf(p[kb][i], a.c, -from));
-          sum += p[kb][i];
-        }
-        const Weights<T> weights(p[kb]);
-#pragma unroll
-        for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(lds[now][1], kb * 32, d, weights, acc[d]);
-      }
+        for (int i = 0; i < 16; ++i) p[kb][i] = w.sees(s, j0 + kb * 32 + key_of(i)) ? p[kb][i] : kMinusInf;
     }
-    if (n + 1 < n1) {
-      ks.store(lds[now ^ 1][0]);
-      vs.store(lds[now ^ 1][1]);
+    float top = p[0][0];
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, p[kb][i]);
+    top = a.c * across_rows<32>(top, [](float x, float y) { return fmaxf(x, y); });
+    // What the exponentials are relative to follows the maximum only where they would pass 2^8: nothing is lost below that.
+    if (__any(top > m + 8.0f)) {
+      const float next = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (next == kMinusInf ? 0.0f : next));
+      m = next;
+      sum *= by;
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d) acc[d] *= by;
     }
-    lds_barrier();
-  }
+    const float from = m == kMinusInf ? 0.0f : m;
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[kb][i] = __builtin_amdgcn_exp2f(fmaf(p[kb][i], a.c, -from));
+        sum += p[kb][i];
+      }
+      const Weights<T> weights(p[kb]);
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(v_tile, kb * 32, d, weights, acc[d]);
+    }
+  });
   if (w.r0 + static_cast<int>(threadIdx.x) % 32 >= a.rows) return;
   sum = across_rows<32>(sum, [](float x, float y) { return x + y; });
   const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -394,11 +499,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Attn a, int64_t all) {
 }
 
 // ---- backward by rows: delta and dq ---------------------------------------------------------------------------------------
-template <typename T, int DP, int BK>
-__global__ __launch_bounds__(kThreads) void rows_kernel(Attn a) {
+template <typename T, int DP, int BK, bool DIRECT>
+__global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void rows_kernel(Attn a) {
   using R = Rows<T, DP>;
-  constexpr int kBytes = BK * R::kPitch, kBlocks = BK / 32, kColumns = DP / 32;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][kBytes];
+  using Stream = KeyStream<T, DP, BK, DIRECT>;
+  constexpr int kBlocks = BK / 32, kColumns = DP / 32;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][Stream::kBytes];
   const int job = in_order(blockIdx.x, gridDim.x), tile = job % a.tiles;
   const int bk = job / a.tiles, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
   const Sight s(a, b);
@@ -425,53 +531,36 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Attn a) {
     delta = across_rows<32>(delta, [](float x, float y) { return x + y; });
   }
   const bool exists = w.r0 + static_cast<int>(threadIdx.x) % 32 < a.rows;
-  if (exists && half == 0) a.delta[stat] = delta;
   const float lse = a.lse[stat] * kLog2e;
+  if (exists && half == 0) {
+    a.stats[stat] = lse;
+    a.stats[a.stat_rows + stat] = delta;
+  }
   f32x16 acc[kColumns];
 #pragma unroll
   for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
-  Staged<T, DP, BK> ks, vs;
-  auto fetch = [&](int n) {
-    const int j0 = keys.key(n, BK);
-    auto there = [&](int r) { return j0 + r < keys.high && (j0 + r >= keys.low || j0 + r < s.sinks); };
-    ks.load(a.D, [&](int r) { return there(r) ? at<T>(a.k, b, j0 + r, kv) : nullptr; });
-    vs.load(a.D, [&](int r) { return there(r) ? at<T>(a.v, b, j0 + r, kv) : nullptr; });
-  };
-  if (keys.count > 0) {
-    fetch(0);
-    ks.store(lds[0][0]);
-    vs.store(lds[0][1]);
-    lds_barrier();
-  }
-  for (int n = 0; n < keys.count; ++n) {
-    const int j0 = keys.key(n, BK), now = n & 1;
-    if (n + 1 < keys.count) fetch(n + 1);
-    if (w.any && !w.none(s, j0, BK)) {
-      const bool all = w.all(s, j0, BK);
+  Stream stream(a, s, keys, b, kv, lds);
+  stream.each(0, keys.count, [&](int j0, const char* k_tile, const char* v_tile) {
+    if (!w.any || w.none(s, j0, BK)) return;
+    const bool all = w.all(s, j0, BK);
 #pragma unroll
-      for (int kb = 0; kb < kBlocks; ++kb) {
-        f32x16 p = zeros(), dp = zeros();
+    for (int kb = 0; kb < kBlocks; ++kb) {
+      f32x16 p = zeros(), dp = zeros();
 #pragma unroll
-        for (int t = 0; t < R::kSteps; ++t) {
-          p = multiply<T>(R::rows(lds[now][0], kb * 32, t), q[t], p);
-          dp = multiply<T>(R::rows(lds[now][1], kb * 32, t), dout[t], dp);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float ds = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - delta);
-          p[i] = all || w.sees(s, j0 + kb * 32 + key_of(i)) ? ds : 0.0f;
-        }
-        const Weights<T> weights(p);
-#pragma unroll
-        for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(lds[now][0], kb * 32, d, weights, acc[d]);
+      for (int t = 0; t < R::kSteps; ++t) {
+        p = multiply<T>(R::rows(k_tile, kb * 32, t), q[t], p);
+        dp = multiply<T>(R::rows(v_tile, kb * 32, t), dout[t], dp);
       }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float ds = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - delta);
+        p[i] = all || w.sees(s, j0 + kb * 32 + key_of(i)) ? ds : 0.0f;
+      }
+      const Weights<T> weights(p);
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(k_tile, kb * 32, d, weights, acc[d]);
     }
-    if (n + 1 < keys.count) {
-      ks.store(lds[now ^ 1][0]);
-      vs.store(lds[now ^ 1][1]);
-    }
-    lds_barrier();
-  }
+  });
   if (!exists) return;
   T* const to = const_cast<T*>(at<T>(a.dq, b, w.i, head));
 #pragma unroll
@@ -479,28 +568,37 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(Attn a) {
 }
 
 // ---- backward by keys: dk and dv ------------------------------------------------------------------------------------------
-// The rows that see a tile of keys are those of its window, or all behind it where one of its keys is one of the first.  A tile's rows
-// may be taken in several parts, whose sums are joined in their order.
+// The queries that see a tile of keys are those of its window, or all behind it where one of its keys is one of the first; they are taken
+// in blocks of BQ of one head after the other, in several parts where that is many, whose sums are joined in their order.
 struct KeyJobs {
   int tiles, sink_tiles;            // of kRows keys; the first sink_tiles have first keys
-  int parts, sink_parts;            // of a tile's rows
-  int part_rows, sink_part_rows;
+  int parts, sink_parts;            // of a tile's blocks of queries
   int64_t sink_jobs;
   float *partial, *sink_partial;    // [job][2][kRows][D], where there is more than one part
 };
+#ifndef TEMPO_KEYS
+#define TEMPO_KEYS kAtOnce<T, DP, DIRECT>
+#endif
 enum Wanted { kBoth, kOnlyV, kOnlyK };
+// v of the workgroup's keys in LDS, not in registers: with it there a wave needs more than the 256 registers that let two run on a SIMD
+// (rows of 128), or than there are (of 256).
+template <typename T, int DP>
+constexpr bool kValuesInLds = sizeof(T) == 2 && DP >= 128;
+template <typename T, int DP>
+constexpr int kQueries = sizeof(T) == 2 && DP == 64 ? 64 : 32;  // of a block
 
-template <typename T, int DP, Wanted WANTED>
-__global__ __launch_bounds__(kThreads) void keys_kernel(Attn a, KeyJobs jobs) {
+template <typename T, int DP, Wanted WANTED, bool DIRECT>
+__global__ __launch_bounds__(kThreads, (TEMPO_KEYS)) void keys_kernel(Attn a, KeyJobs jobs) {
   using R = Rows<T, DP>;
-  constexpr int BQ = sizeof(T) == 2 && DP == 64 ? 64 : 32, kBytes = BQ * R::kPitch, kColumns = DP / 32;
+  constexpr int BQ = kQueries<T, DP>, kBytes = R::bytes(BQ), kColumns = DP / 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][kBytes];
   __shared__ __attribute__((aligned(16))) float stats[2][2][BQ];  // lse of base 2, delta
-  __shared__ __attribute__((aligned(16))) int sight[2][2][BQ];    // begin, end
+  constexpr bool kK = WANTED != kOnlyV, kV = WANTED != kOnlyK, kInLds = kK && kValuesInLds<T, DP>;
+  __shared__ __attribute__((aligned(16))) char values[kInLds ? R::bytes(kRows) : 16];
   int64_t job = blockIdx.x;
   const bool of_sinks = job < jobs.sink_jobs;
   if (!of_sinks) job -= jobs.sink_jobs;
-  const int parts = of_sinks ? jobs.sink_parts : jobs.parts, part_rows = of_sinks ? jobs.sink_part_rows : jobs.part_rows;
+  const int parts = of_sinks ? jobs.sink_parts : jobs.parts;
   const int tiles = of_sinks ? jobs.sink_tiles : jobs.tiles - jobs.sink_tiles;
   if (!of_sinks) job = in_order(static_cast<int>(job), static_cast<int>(gridDim.x - jobs.sink_jobs));
   const int part = static_cast<int>(job % parts), tile = static_cast<int>(job / parts % tiles) + (of_sinks ? 0 : jobs.sink_tiles);
@@ -508,98 +606,129 @@ __global__ __launch_bounds__(kThreads) void keys_kernel(Attn a, KeyJobs jobs) {
   const Sight s(a, b);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
   const int key0 = tile * kRows, wave_key = key0 + wave * 32, key = wave_key + lane % 32;
-  // rows [r, end) of this part
-  int r_first, r_end;
-  {
-    const int64_t i0 = key0 - s.start, last = min(key0 + kRows, s.keys) - 1;
-    const int64_t i1 = key0 < s.sinks ? int64_t{a.Sq} : last + s.window - s.start;
-    const int64_t from = (i0 > 0 ? i0 : 0) * a.group, to = (i1 < a.Sq ? i1 : int64_t{a.Sq}) * a.group;
-    const int64_t first = from + static_cast<int64_t>(part) * part_rows, end = first + part_rows < to ? first + part_rows : to;
-    const bool none = key0 >= s.keys || first >= end;
-    r_first = none ? 0 : static_cast<int>(first);
-    r_end = none ? 0 : static_cast<int>(end);
-  }
-  u32x4 k[R::kSteps], v[R::kSteps];
+  // Queries [from, to) see key j.
+  auto from = [&](int j) {
+    const int64_t i = j - s.start;
+    return j >= s.keys || i >= a.Sq ? a.Sq : i > 0 ? static_cast<int>(i) : 0;
+  };
+  auto to = [&](int j) {
+    if (j >= s.keys) return 0;
+    const int64_t i = j < s.sinks ? int64_t{a.Sq} : j + int64_t{s.window} - s.start;
+    return i >= a.Sq ? a.Sq : i > 0 ? static_cast<int>(i) : 0;
+  };
+  const int tile_last = min(key0 + kRows, s.keys) - 1;
+  const int first = from(key0), end = key0 >= s.keys ? 0 : key0 < s.sinks ? a.Sq : to(tile_last);
+  const int blocks = first < end ? (end - first + BQ - 1) / BQ : 0;  // of a head
+  const int each = static_cast<int>((static_cast<int64_t>(blocks) * a.group + parts - 1) / parts);
+  const int u0 = min(part * each, blocks * a.group), u1 = min(u0 + each, blocks * a.group);
+  // The wave's keys: all of a block of queries see them, or none does, or each is looked at.
+  const int wave_last = wave_key + 31;
+  const int any_from = from(wave_key), any_to = wave_key < s.sinks ? (wave_key < s.keys ? a.Sq : 0) : to(min(wave_last, s.keys - 1));
+  const int all_from = from(wave_last), all_to = wave_last < s.keys ? to(wave_last < s.sinks ? wave_key : max(wave_key, s.sinks)) : 0;
+  const int key_from = from(key);
+  const uint32_t key_span = static_cast<uint32_t>(max(to(key) - key_from, 0));
+  u32x4 k[R::kSteps], v[kInLds ? 1 : R::kSteps];
   {
     const int there = min(key, a.Sk - 1);
     const T *kr = at<T>(a.k, b, there, kv), *vr = at<T>(a.v, b, there, kv);
 #pragma unroll
     for (int p = 0; p < R::kSteps; ++p) {
       k[p] = load_of_row<T>(kr, 2 * p + half, a.D);
-      if (WANTED != kOnlyV) v[p] = load_of_row<T>(vr, 2 * p + half, a.D);
+      if (kK && !kInLds) v[p] = load_of_row<T>(vr, 2 * p + half, a.D);
+    }
+    if constexpr (kInLds) {  // a wave's own rows
+#pragma unroll
+      for (int p = 0; p < R::kSteps; ++p) {
+        const int row = wave * 32 + lane % 32, piece = 2 * p + half;
+        *reinterpret_cast<u32x4*>(values + R::place(row) + ((piece ^ R::swizzle(row)) << 4)) = load_of_row<T>(vr, piece, a.D);
+      }
     }
   }
-  constexpr bool kK = WANTED != kOnlyV, kV = WANTED != kOnlyK;
+  auto value = [&](int step) {
+    if constexpr (kInLds) return R::rows(values, wave * 32, step);
+    else return v[step];
+  };
   f32x16 dk[kK ? kColumns : 1], dv[kV ? kColumns : 1];
 #pragma unroll
   for (int d = 0; d < (kK ? kColumns : 1); ++d) dk[d] = zeros();
 #pragma unroll
   for (int d = 0; d < (kV ? kColumns : 1); ++d) dv[d] = zeros();
-  Staged<T, DP, BQ> qs, os;
-  float stat_lse = 0.0f, stat_delta = 0.0f;
-  int stat_begin = 0, stat_end = 0;
-  auto fetch = [&](int r0) {
-    auto row = [&](const Heads& h, int r) -> const T* {
-      if (r0 + r >= r_end) return nullptr;
-      const int i = a.by_group.divide(r0 + r);
-      return at<T>(h, b, i, kv * a.group + r0 + r - i * a.group);
-    };
-    qs.load(a.D, [&](int r) { return row(a.q, r); });
-    os.load(a.D, [&](int r) { return row(a.dout, r); });
-    const int r = r0 + static_cast<int>(threadIdx.x);
-    if (threadIdx.x < BQ) {
-      stat_end = 0;
-      if (r < r_end) {
-        const int i = a.by_group.divide(r);
-        const int64_t stat = (static_cast<int64_t>(b) * a.heads + kv * a.group + r - i * a.group) * a.Sq + i;
-        stat_lse = a.lse[stat] * kLog2e;
-        stat_delta = a.delta[stat];
-        stat_begin = s.begin(i);
-        stat_end = s.end(i);
-      }
-    }
-  };
-  auto put = [&](int to) {
-    qs.store(lds[to][0]);
-    os.store(lds[to][1]);
-    if (threadIdx.x < BQ) {
-      stats[to][0][threadIdx.x] = stat_lse;
-      stats[to][1][threadIdx.x] = stat_delta;
-      sight[to][0][threadIdx.x] = stat_begin;
-      sight[to][1][threadIdx.x] = stat_end;
-    }
-  };
-  if (r_first < r_end) {
-    fetch(r_first);
-    put(0);
+  std::conditional_t<DIRECT, Direct<T, DP, BQ>, Staged<T, DP, BQ>> qs(a.q), os(a.dout);
+  float stat = 0.0f;  // of lane BQ n + i: lse (n 0) or delta (n 1) of query i of the block
+  if (DIRECT && a.D < DP) {
+    clear_lds(lds[0][0], 4 * kBytes);
     lds_barrier();
   }
-  int now = 0;
-  for (int r0 = r_first; r0 < r_end; r0 += BQ, now ^= 1) {
-    if (r0 + BQ < r_end) fetch(r0 + BQ);
+  // Where a block is: head `g` of the group, queries from `i`.
+  struct Place {
+    int g, i;
+  };
+  auto following = [&](Place at) { return at.i + BQ < end ? Place{at.g, at.i + BQ} : Place{at.g + 1, first}; };
+  auto fetch = [&](Place at_block, int into) {
+    const int i0 = at_block.i, head = kv * a.group + at_block.g, last = end - 1;
+    const T *q = at<T>(a.q, b, 0, head), *dout = at<T>(a.dout, b, 0, head);
+    if constexpr (DIRECT) {
+      if (i0 + BQ <= end) {
+        qs.load(q + i0 * a.q.token, a.D, lds[into][0]);
+        os.load(dout + i0 * a.dout.token, a.D, lds[into][1]);
+      } else {
+        qs.load_each(a.D, lds[into][0], [&](int r) { return q + min(i0 + r, last) * a.q.token; });
+        os.load_each(a.D, lds[into][1], [&](int r) { return dout + min(i0 + r, last) * a.dout.token; });
+      }
+    } else {
+      qs.load(a.D, [&](int r) { return q + min(i0 + r, last) * a.q.token; });
+      os.load(a.D, [&](int r) { return dout + min(i0 + r, last) * a.dout.token; });
+    }
+    const int t = threadIdx.x;
+    if (t < 2 * BQ) stat = a.stats[t / BQ * a.stat_rows + (static_cast<int64_t>(b) * a.heads + head) * a.Sq + min(i0 + t % BQ, last)];
+  };
+  auto put = [&](int into) {
+    if constexpr (!DIRECT) {
+      qs.store(lds[into][0]);
+      os.store(lds[into][1]);
+    }
+    if (threadIdx.x < 2 * BQ) (&stats[into][0][0])[threadIdx.x] = stat;
+  };
+  Place block{0, 0};
+  if (u0 < u1) {
+    block = Place{u0 / blocks, first + u0 % blocks * BQ};
+    fetch(block, 0);
+    put(0);
+  }
+  for (int u = u0; u < u1; ++u) {
+    const int now = (u - u0) & 1, i0 = block.i;
+    if constexpr (DIRECT) landed();
+    lds_barrier();  // the block is there, and the other buffer has been read
+    block = following(block);
+    if (u + 1 < u1) fetch(block, now ^ 1);
 #pragma unroll
     for (int rb = 0; rb < BQ; rb += 32) {
-      const int r1 = r0 + rb, r2 = min(r1 + 32, r_end) - 1;  // the block's first and last row
-      if (r1 > r2) continue;
-      const int i1 = a.by_group.divide(r1), i2 = a.by_group.divide(r2);
-      if (s.end(i2) <= wave_key || (s.begin(i1) > wave_key + 31 && wave_key >= s.sinks)) continue;
-      const bool all = r2 == r1 + 31 && s.end(i1) >= wave_key + 32 && (s.begin(i2) <= wave_key || wave_key + 32 <= s.sinks);
+      const int i1 = i0 + rb;
+      if (i1 >= any_to || i1 + 32 <= any_from) continue;
+      const bool all = i1 >= all_from && i1 + 32 <= all_to;
       f32x16 p = zeros(), dp = zeros();
 #pragma unroll
       for (int t = 0; t < R::kSteps; ++t) {
         p = multiply<T>(R::rows(lds[now][0], rb, t), k[t], p);
-        if (kK) dp = multiply<T>(R::rows(lds[now][1], rb, t), v[t], dp);
+        if (kK) dp = multiply<T>(R::rows(lds[now][1], rb, t), value(t), dp);
       }
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {  // rows 8 n + 4 half .. + 3
+      for (int n = 0; n < 4; ++n) {  // queries 8 n + 4 half .. + 3
         const int r = rb + 8 * n + 4 * half;
         const f32x4 lse = *reinterpret_cast<const f32x4*>(&stats[now][0][r]), delta = *reinterpret_cast<const f32x4*>(&stats[now][1][r]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const bool seen = all || (key < sight[now][1][r + e] && (key >= sight[now][0][r + e] || key < s.sinks));
           const float x = __builtin_amdgcn_exp2f(fmaf(p[4 * n + e], a.c, -lse[e]));
-          p[4 * n + e] = seen ? x : 0.0f;
-          if (kK) dp[4 * n + e] = seen ? x * (dp[4 * n + e] - delta[e]) : 0.0f;
+          p[4 * n + e] = x;
+          if (kK) dp[4 * n + e] = x * (dp[4 * n + e] - delta[e]);
+        }
+      }
+      if (!all) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool seen = static_cast<uint32_t>(i1 + key_of(i) - key_from) < key_span;
+          p[i] = seen ? p[i] : 0.0f;
+          if (kK) dp[i] = seen ? dp[i] : 0.0f;
         }
       }
       if constexpr (kV) {
@@ -613,30 +742,29 @@ __global__ __launch_bounds__(kThreads) void keys_kernel(Attn a, KeyJobs jobs) {
         for (int d = 0; d < kColumns; ++d) dk[d] = multiply_columns<T, DP>(lds[now][0], rb, d, weights, dk[d]);
       }
     }
-    if (r0 + BQ < r_end) put(now ^ 1);
-    lds_barrier();
+    if (u + 1 < u1) put(now ^ 1);
   }
   if (parts > 1) {
-    float* const to = (of_sinks ? jobs.sink_partial : jobs.partial) +
-                      (job * 2 * kRows + wave * 32 + lane % 32) * static_cast<int64_t>(a.D);
+    float* const into = (of_sinks ? jobs.sink_partial : jobs.partial) +
+                        (job * 2 * kRows + wave * 32 + lane % 32) * static_cast<int64_t>(a.D);
     if constexpr (kK) {
 #pragma unroll
-      for (int d = 0; d < kColumns; ++d) store_sums(to, a.D, d, dk[d], a.scale);
+      for (int d = 0; d < kColumns; ++d) store_sums(into, a.D, d, dk[d], a.scale);
     }
     if constexpr (kV) {
 #pragma unroll
-      for (int d = 0; d < kColumns; ++d) store_sums(to + static_cast<int64_t>(kRows) * a.D, a.D, d, dv[d], 1.0f);
+      for (int d = 0; d < kColumns; ++d) store_sums(into + static_cast<int64_t>(kRows) * a.D, a.D, d, dv[d], 1.0f);
     }
   } else if (key < a.Sk) {
     if constexpr (kK) {
-      T* const to = const_cast<T*>(at<T>(a.dk, b, key, kv));
+      T* const into = const_cast<T*>(at<T>(a.dk, b, key, kv));
 #pragma unroll
-      for (int d = 0; d < kColumns; ++d) store_sums(to, a.D, d, dk[d], a.scale);
+      for (int d = 0; d < kColumns; ++d) store_sums(into, a.D, d, dk[d], a.scale);
     }
     if constexpr (kV) {
-      T* const to = const_cast<T*>(at<T>(a.dv, b, key, kv));
+      T* const into = const_cast<T*>(at<T>(a.dv, b, key, kv));
 #pragma unroll
-      for (int d = 0; d < kColumns; ++d) store_sums(to, a.D, d, dv[d], 1.0f);
+      for (int d = 0; d < kColumns; ++d) store_sums(into, a.D, d, dv[d], 1.0f);
     }
   }
 }
@@ -678,15 +806,13 @@ KeyPlan key_plan(const WindowCall& c) {
   KeyPlan p{};
   const int64_t group = c.heads / c.kv_heads, bk = c.B * c.kv_heads, tiles = up(c.Sk, kRows);
   const int64_t sink_tiles = std::min(tiles, up(c.sinks, kRows)), others = tiles - sink_tiles;
-  const int64_t span = std::min(c.Sq, c.window + kRows) * group, all = c.Sq * group, cus = compute_units();
+  const int64_t span = up(std::min(c.Sq, c.window + kRows), 32) * group, all = up(c.Sq, 32) * group, cus = compute_units();
   const int64_t want = up(2 * cus, std::max<int64_t>(bk * tiles, 1));
   p.jobs.tiles = static_cast<int>(tiles);
   p.jobs.sink_tiles = static_cast<int>(sink_tiles);
-  p.jobs.parts = static_cast<int>(std::max<int64_t>(1, std::min({want, up(span, 128), int64_t{64}})));
-  p.jobs.part_rows = static_cast<int>(std::max<int64_t>(up(up(span, p.jobs.parts), 32), 1) * 32);
-  const int64_t sink_want = std::min(up(all, p.jobs.part_rows), up(4 * cus, std::max<int64_t>(bk * sink_tiles, 1)));
+  p.jobs.parts = static_cast<int>(std::max<int64_t>(1, std::min({want, up(span, 4), int64_t{64}})));
+  const int64_t sink_want = std::min(up(all, std::max<int64_t>(up(span, p.jobs.parts), 1)), up(4 * cus, std::max<int64_t>(bk * sink_tiles, 1)));
   p.jobs.sink_parts = static_cast<int>(std::max<int64_t>(1, sink_want));
-  p.jobs.sink_part_rows = static_cast<int>(std::min<int64_t>(up(up(all, p.jobs.sink_parts), 32) * 32, INT32_MAX));
   p.jobs.sink_jobs = bk * sink_tiles * p.jobs.sink_parts;
   const int64_t other_jobs = bk * others * p.jobs.parts;
   p.blocks = p.jobs.sink_jobs + other_jobs;
@@ -726,6 +852,20 @@ template <typename F>
 tempo_status with_type(tempo_dtype dt, F&& f) {
   return dt == TEMPO_F32 ? f(float{}) : f(bf16_t{});
 }
+// Whether rows of all of these can go to LDS without registers.
+bool direct(const WindowCall& c, tempo_dtype dt, std::initializer_list<const tempo_attn_heads*> of) {
+  const int64_t size = dt == TEMPO_F32 ? 4 : 2, piece = 16 / size;
+  if (c.D % piece != 0) return false;
+  for (const tempo_attn_heads* h : of)
+    if (reinterpret_cast<uintptr_t>(h->p) % 16 != 0 || h->batch % piece != 0 || h->token % piece != 0 || h->head % piece != 0 ||
+        h->token * size > INT32_MAX / 64)
+      return false;
+  return true;
+}
+template <typename F>
+tempo_status either(bool which, F&& f) {
+  return which ? f(std::true_type{}) : f(std::false_type{});
+}
 template <typename K, typename... Args>
 tempo_status launch(K kernel, int64_t blocks, hipStream_t st, const Args&... args) {
   if (blocks == 0) return TEMPO_OK;
@@ -751,7 +891,7 @@ size_t window_attn_workspace_bytes(const WindowCall& c, bool back) {
     return splits > 1 ? static_cast<size_t>(splits) * rows * (c.D + 1) * sizeof(float) : 0;
   }
   const KeyPlan p = key_plan(c);
-  return static_cast<size_t>(up(rows, 4) * 4 + p.sink_floats + p.partial_floats) * sizeof(float);
+  return static_cast<size_t>(up(2 * rows, 4) * 4 + p.sink_floats + p.partial_floats) * sizeof(float);
 }
 
 tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStream_t st) {
@@ -768,7 +908,9 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
     using T = decltype(type);
     const tempo_status s = with_width(c.D, [&](auto width) {
       constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 ? 64 : 32;
-      return launch(forward_kernel<T, DP, BK>, blocks, st, a);
+      return either(direct(c, dt, {c.k, c.v}), [&](auto straight) {
+        return launch(forward_kernel<T, DP, BK, decltype(straight)::value>, blocks, st, a);
+      });
     });
     if (s != TEMPO_OK || a.splits == 1) return s;
     return launch(join_kernel<T>, up(all, kWaves), st, a, all);
@@ -778,22 +920,28 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
 tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStream_t st) {
   if (c.workspace_bytes < window_attn_workspace_bytes(c, true)) return TEMPO_ERR_WORKSPACE;
   Attn a = attn_of(c);
-  a.delta = static_cast<float*>(c.workspace);
+  a.stats = static_cast<float*>(c.workspace);
+  a.stat_rows = c.B * c.heads * c.Sq;
   KeyPlan p = key_plan(c);
-  p.jobs.sink_partial = a.delta + up(c.B * c.heads * c.Sq, 4) * 4;
+  p.jobs.sink_partial = a.stats + up(2 * a.stat_rows, 4) * 4;
   p.jobs.partial = p.jobs.sink_partial + p.sink_floats;
   return with_type(dt, [&](auto type) {
     using T = decltype(type);
     tempo_status s = with_width(c.D, [&](auto width) {
       constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 ? 64 : 32;
-      tempo_status r = a.rows > 0 ? launch(rows_kernel<T, DP, BK>, c.B * c.kv_heads * a.tiles, st, a) : TEMPO_OK;
+      const tempo_status r = either(direct(c, dt, {c.k, c.v}), [&](auto straight) {
+        return launch(rows_kernel<T, DP, BK, decltype(straight)::value>, c.B * c.kv_heads * a.tiles, st, a);
+      });
       if (r != TEMPO_OK) return r;
-      if constexpr (sizeof(T) * DP > 512) {  // both gradients' sums of 256 float32 elements do not fit into a wave's registers
-        r = launch(keys_kernel<T, DP, kOnlyV>, p.blocks, st, a, p.jobs);
-        return r != TEMPO_OK ? r : launch(keys_kernel<T, DP, kOnlyK>, p.blocks, st, a, p.jobs);
-      } else {
-        return launch(keys_kernel<T, DP, kBoth>, p.blocks, st, a, p.jobs);
-      }
+      return either(direct(c, dt, {c.q, c.dout}), [&](auto straight) {
+        constexpr bool DIRECT = decltype(straight)::value;
+        if constexpr (sizeof(T) * DP > 512) {  // both gradients' sums of 256 float32 elements do not fit into a wave's registers
+          const tempo_status of_v = launch(keys_kernel<T, DP, kOnlyV, DIRECT>, p.blocks, st, a, p.jobs);
+          return of_v != TEMPO_OK ? of_v : launch(keys_kernel<T, DP, kOnlyK, DIRECT>, p.blocks, st, a, p.jobs);
+        } else {
+          return launch(keys_kernel<T, DP, kBoth, DIRECT>, p.blocks, st, a, p.jobs);
+        }
+      });
     });
     const int64_t each = c.B * c.kv_heads * 2 * kRows;
     auto join = [&](const float* partial, int parts, int tiles0, int tiles) {
