@@ -34,7 +34,6 @@ struct Residual {
   int M;
   float inv;              // 1 / M
   int parts;              // workgroups of a gate's rows
-  int64_t part_rows;
   float* partial;         // backward: [groups * parts][sums][M]
 };
 
@@ -73,17 +72,36 @@ struct Columns {
     return s;
   }
 };
-// The rows [first, end) of this workgroup, all of one gate.
+// The rows of this workgroup, all of one gate: every parts-th, so that what the workgroups read and write at a time lies together
+// (65536 x 4096 bfloat16 backward 568 us; 612 where each has rows side by side).
 struct Walk {
-  int64_t group, first, end;
+  int64_t group, first, end, step;
   __device__ __forceinline__ explicit Walk(const Residual& r) {
     group = blockIdx.x / r.parts;
-    const int64_t base = group * r.group_rows, from = static_cast<int64_t>(blockIdx.x - group * r.parts) * r.part_rows;
-    first = base + (from < r.group_rows ? from : r.group_rows);
-    const int64_t to = from + r.part_rows;
-    end = base + (to < r.group_rows ? to : r.group_rows);
+    step = r.parts;
+    first = group * r.group_rows + (blockIdx.x - group * r.parts);
+    end = (group + 1) * r.group_rows;
   }
 };
+
+// Rows that are on their way while one is worked on: 65536 x 4096 bfloat16 backward 568 us with two, 654 with one.
+template <int CH>
+constexpr int kAhead = CH == 1 ? 2 : 1;
+// work(row, its turn, that modulo AHEAD as a constant)
+template <int AHEAD, int I = 0, typename F>
+__device__ __forceinline__ bool turns(const Walk& w, int64_t row, int turn, F&& work) {
+  if constexpr (I < AHEAD) {
+    if (row >= w.end) return false;
+    work(row, turn, std::integral_constant<int, I>{});
+    return turns<AHEAD, I + 1>(w, row + w.step, turn + 1, work);
+  }
+  return true;
+}
+template <int AHEAD, typename F>
+__device__ __forceinline__ void each_row(const Walk& w, F&& work) {
+  int turn = 0;
+  for (int64_t row = w.first; turns<AHEAD>(w, row, turn, work); row += AHEAD * w.step) turn += AHEAD;
+}
 
 // Mean and 1 / sqrt(variance + eps) of a row; a sum at a time.
 template <int LANES, typename C, typename F>
@@ -105,12 +123,15 @@ __global__ __launch_bounds__(WAVES* kWave) void forward_kernel(Residual r) {
   const Columns<T, CH, LANES, RAG> at(r.M);
   const Walk walk(r);
   const int64_t M = r.M;
-  u32x4 x[CH], f[CH], next_x[CH], next_f[CH];
-  auto fetch = [&](int64_t row) {
-    at.load(static_cast<const T*>(r.x) + row * M, next_x);
-    at.load(static_cast<const T*>(r.f) + row * M, next_f);
+  constexpr int AHEAD = kAhead<CH>;
+  u32x4 x[AHEAD][CH], f[AHEAD][CH];
+  auto fetch = [&](int64_t row, int to) {
+    at.load(static_cast<const T*>(r.x) + row * M, x[to]);
+    at.load(static_cast<const T*>(r.f) + row * M, f[to]);
   };
-  if (walk.first < walk.end) fetch(walk.first);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (walk.first + i * walk.step < walk.end) fetch(walk.first + i * walk.step, i);
   float by[CH][V], more[BIAS ? CH : 1][V], weight[CH][V], bias[BIAS ? CH : 1][V];  // of f^ and of y^
   {
     float gate[CH][V];
@@ -129,22 +150,24 @@ __global__ __launch_bounds__(WAVES* kWave) void forward_kernel(Residual r) {
         if constexpr (BIAS) more[c][i] *= r.beta * gate[c][i];
       }
   }
-  for (int64_t row = walk.first; row < walk.end; ++row) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) x[c] = next_x[c], f[c] = next_f[c];
-    if (row + 1 < walk.end) fetch(row + 1);
+  each_row<AHEAD>(walk, [&](int64_t row, int turn, auto slot) {
+    u32x4 xs[CH];
     float v[CH][V], y[CH][V];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) Store<T>::unpack(f[c], v[c]);
+    for (int c = 0; c < CH; ++c) {
+      xs[c] = x[slot][c];
+      Store<T>::unpack(f[slot][c], v[c]);
+    }
+    if (row + AHEAD * walk.step < walk.end) fetch(row + AHEAD * walk.step, slot);
     float2 st = make_float2(0.0f, 1.0f);
     if (r.post.there) {
-      st = statistics<LANES>(at, r.post, r.inv, slots[row & 1], [&](int c, int i) { return v[c][i]; });
+      st = statistics<LANES>(at, r.post, r.inv, slots[turn & 1], [&](int c, int i) { return v[c][i]; });
       if (r.post.stats && threadIdx.x == 0) r.post.stats[row] = st;
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float xv[V];
-      Store<T>::unpack(x[c], xv);
+      Store<T>::unpack(xs[c], xv);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float n = (v[c][i] - st.x) * st.y * by[c][i];
@@ -156,8 +179,8 @@ __global__ __launch_bounds__(WAVES* kWave) void forward_kernel(Residual r) {
       if (at.has(c)) stg_piece<RAG>(static_cast<T*>(r.to_y) + row * M + at.at(c), w);
       Store<T>::unpack(w, y[c]);
     }
-    if (!r.pre.there) continue;
-    st = statistics<LANES>(at, r.pre, r.inv, slots[row & 1] + 2 * WAVES, [&](int c, int i) { return y[c][i]; });
+    if (!r.pre.there) return;
+    st = statistics<LANES>(at, r.pre, r.inv, slots[turn & 1] + 2 * WAVES, [&](int c, int i) { return y[c][i]; });
     if (r.pre.stats && threadIdx.x == 0) r.pre.stats[row] = st;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -168,7 +191,7 @@ __global__ __launch_bounds__(WAVES* kWave) void forward_kernel(Residual r) {
       }
       if (at.has(c)) stg_piece<RAG>(static_cast<T*>(r.h) + row * M + at.at(c), Store<T>::pack(y[c]));
     }
-  }
+  });
 }
 
 // SUMS: 2 (C, D) or 4 (C, D, F, E).
@@ -179,21 +202,26 @@ __global__ __launch_bounds__(WAVES* kWave) void backward_kernel(Residual r) {
   const Columns<T, CH, LANES, RAG> at(r.M);
   const Walk walk(r);
   const int64_t M = r.M;
-  u32x4 dy[CH], dh[CH], f[CH], y[CH], next_dy[CH], next_dh[CH], next_f[CH], next_y[CH];
-  float2 pre, post, next_pre = make_float2(0.0f, 0.0f), next_post = make_float2(0.0f, 1.0f);
-  auto fetch = [&](int64_t row) {
-    if (r.dy) at.load(static_cast<const T*>(r.dy) + row * M, next_dy);
+  constexpr int AHEAD = kAhead<CH>;
+  u32x4 dys[AHEAD][CH], dhs[AHEAD][CH], fs[AHEAD][CH], ys[AHEAD][CH];
+  float2 pres[AHEAD], posts[AHEAD];
+  auto fetch = [&](int64_t row, int to) {
+    if (r.dy) at.load(static_cast<const T*>(r.dy) + row * M, dys[to]);
     if (r.pre.there) {
-      at.load(static_cast<const T*>(r.dh) + row * M, next_dh);
-      at.load(static_cast<const T*>(r.y) + row * M, next_y);
-      next_pre = r.pre.stats[row];
+      at.load(static_cast<const T*>(r.dh) + row * M, dhs[to]);
+      at.load(static_cast<const T*>(r.y) + row * M, ys[to]);
+      pres[to] = r.pre.stats[row];
     }
-    at.load(static_cast<const T*>(r.f) + row * M, next_f);
-    if (r.post.there) next_post = r.post.stats[row];
+    at.load(static_cast<const T*>(r.f) + row * M, fs[to]);
+    if (r.post.there) posts[to] = r.post.stats[row];
   };
 #pragma unroll
-  for (int c = 0; c < CH; ++c) next_dy[c] = next_dh[c] = next_f[c] = next_y[c] = u32x4{0, 0, 0, 0};
-  if (walk.first < walk.end) fetch(walk.first);
+  for (int i = 0; i < AHEAD; ++i) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) dys[i][c] = dhs[i][c] = fs[i][c] = ys[i][c] = u32x4{0, 0, 0, 0};
+    pres[i] = make_float2(0.0f, 0.0f), posts[i] = make_float2(0.0f, 1.0f);
+    if (walk.first + i * walk.step < walk.end) fetch(walk.first + i * walk.step, i);
+  }
   float by[CH][V], weight[CH][V], sums[SUMS][CH][V];
   {
     float gate[CH][V];
@@ -209,11 +237,12 @@ __global__ __launch_bounds__(WAVES* kWave) void backward_kernel(Residual r) {
         for (int s = 0; s < SUMS; ++s) sums[s][c][i] = 0.0f;
       }
   }
-  for (int64_t row = walk.first; row < walk.end; ++row) {
+  each_row<AHEAD>(walk, [&](int64_t row, int turn, auto slot) {
+    u32x4 dy[CH], dh[CH], f[CH], y[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) dy[c] = next_dy[c], dh[c] = next_dh[c], f[c] = next_f[c], y[c] = next_y[c];
-    pre = next_pre, post = next_post;
-    if (row + 1 < walk.end) fetch(row + 1);
+    for (int c = 0; c < CH; ++c) dy[c] = dys[slot][c], dh[c] = dhs[slot][c], f[c] = fs[slot][c], y[c] = ys[slot][c];
+    const float2 pre = pres[slot], post = posts[slot];
+    if (row + AHEAD * walk.step < walk.end) fetch(row + AHEAD * walk.step, slot);
     float d[CH][V], v[CH][V], g[CH][V];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -231,7 +260,7 @@ __global__ __launch_bounds__(WAVES* kWave) void backward_kernel(Residual r) {
     if (r.pre.there) {
       s1 = at.sum([&](int c, int i) { return g[c][i] * v[c][i]; });
       if (r.pre.layer) s2 = at.sum([&](int c, int i) { return g[c][i]; });
-      row_sum2<LANES>(s1, s2, slots[row & 1][0]);
+      row_sum2<LANES>(s1, s2, slots[turn & 1][0]);
     }
     s1 *= r.inv, s2 *= r.inv;
 #pragma unroll
@@ -257,7 +286,7 @@ __global__ __launch_bounds__(WAVES* kWave) void backward_kernel(Residual r) {
     if (r.post.there) {
       s1 = at.sum([&](int c, int i) { return g[c][i] * v[c][i]; });
       if (r.post.layer) s2 = at.sum([&](int c, int i) { return g[c][i]; });
-      row_sum2<LANES>(s1, s2, slots[row & 1][1]);
+      row_sum2<LANES>(s1, s2, slots[turn & 1][1]);
     }
     s1 *= r.inv, s2 *= r.inv;
 #pragma unroll
@@ -266,7 +295,7 @@ __global__ __launch_bounds__(WAVES* kWave) void backward_kernel(Residual r) {
       for (int i = 0; i < V; ++i) g[c][i] = post.y * (g[c][i] - v[c][i] * s1 - s2);
       if (at.has(c)) stg_piece<RAG>(static_cast<T*>(r.df) + row * M + at.at(c), Store<T>::pack(g[c]));
     }
-  }
+  });
   if (!r.partial) return;
 #pragma unroll
   for (int s = 0; s < SUMS; ++s) {
@@ -305,7 +334,7 @@ __global__ __launch_bounds__(kAnyThreads) void forward_any_kernel(Residual r) {
   const Walk walk(r);
   const int64_t M = r.M;
   const float* gate = r.gate ? r.gate + walk.group * M : nullptr;
-  for (int64_t row = walk.first; row < walk.end; ++row) {
+  for (int64_t row = walk.first; row < walk.end; row += walk.step) {
     const T *x = static_cast<const T*>(r.x) + row * M, *f = static_cast<const T*>(r.f) + row * M;
     T* const y = static_cast<T*>(r.to_y) + row * M;
     float2 st = make_float2(0.0f, 1.0f);
@@ -337,7 +366,7 @@ __global__ __launch_bounds__(kAnyThreads) void backward_any_kernel(Residual r) {
   if (sums)
     for (int c = threadIdx.x; c < r.M; c += kAnyThreads)
       for (int s = 0; s < SUMS; ++s) sums[s * M + c] = 0.0f;
-  for (int64_t row = walk.first; row < walk.end; ++row) {
+  for (int64_t row = walk.first; row < walk.end; row += walk.step) {
     auto element = [&](const void* t, int c) { return t ? Store<T>::load1(static_cast<const T*>(t) + row * M + c) : 0.0f; };
     const float2 pre = r.pre.there ? r.pre.stats[row] : make_float2(0.0f, 0.0f), post = r.post.there ? r.post.stats[row] : make_float2(0.0f, 1.0f);
     auto y_hat = [&](int c) { return r.pre.there ? (element(r.y, c) - pre.x) * pre.y : 0.0f; };
@@ -371,49 +400,73 @@ __global__ __launch_bounds__(kAnyThreads) void backward_any_kernel(Residual r) {
   }
 }
 
-// The sums of all workgroups: 16 columns by 16 lanes that take every 16th part, whose sums are added in their order.
+// The sums of all workgroups: 16 columns by 64 lanes, of which `share` take the parts of a gate's rows in turn (all of them where there is
+// one gate), those of other gates at the same time; added up in a fixed order.
 struct Sums {
   const float* partial;
   int64_t groups;
-  int parts, sums, M;
+  int parts, sums, M, share;
   const float *gate, *post_weight, *post_bias;
   float beta;
   float *dgate, *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
 };
-__global__ __launch_bounds__(256) void columns_kernel(Sums s) {
-  __shared__ float of_lanes[4][16][17];
-  const int column = blockIdx.x * 16 + threadIdx.x % 16, lane = threadIdx.x / 16;
-  const bool exists = column < s.M;
-  float total[4] = {0, 0, 0, 0};  // of lane 0: dpost.weight, D, dpost.bias, E
-  for (int64_t group = 0; group < s.groups; ++group) {
-    float v[4] = {0, 0, 0, 0};
-    if (exists) {
-      const float* p = s.partial + group * s.parts * s.sums * s.M + column;
-      for (int part = lane; part < s.parts; part += 16)
-        for (int n = 0; n < s.sums; ++n) v[n] += p[(static_cast<int64_t>(part) * s.sums + n) * s.M];
-    }
-    for (int n = 0; n < s.sums; ++n) of_lanes[n][lane][threadIdx.x % 16] = v[n];
-    lds_barrier();
-    if (lane == 0 && exists) {
-      for (int n = 0; n < s.sums; ++n) {
-        v[n] = 0.0f;
-        for (int l = 0; l < 16; ++l) v[n] += of_lanes[n][l][threadIdx.x];
+constexpr int kSumLanes = 64, kSumColumns = 16;
+template <int SUMS>
+__global__ __launch_bounds__(kSumColumns* kSumLanes) void columns_kernel(Sums s) {
+  __shared__ float of_lanes[SUMS][kSumLanes][kSumColumns];
+  const int x = threadIdx.x % kSumColumns, lane = threadIdx.x / kSumColumns, column = blockIdx.x * kSumColumns + x, in_share = lane % s.share;
+  const bool exists = column < s.M, leads = in_share == 0 && exists;
+  const int at_once = kSumLanes / s.share;
+  const int64_t M = s.M;
+  float total[SUMS] = {};  // of a leader: dpost.weight, D, dpost.bias, E
+  for (int64_t first = 0; first < s.groups; first += at_once) {
+    const int64_t group = first + lane / s.share;
+    float v[SUMS] = {};
+    if (exists && group < s.groups) {
+      const float* p = s.partial + group * s.parts * SUMS * M + column;
+#pragma unroll 4
+      for (int part = in_share; part < s.parts; part += s.share) {
+#pragma unroll
+        for (int n = 0; n < SUMS; ++n) v[n] += p[(static_cast<int64_t>(part) * SUMS + n) * M];
       }
-      const float by = s.beta * param(s.gate ? s.gate + group * s.M : nullptr, column, 1.0f);
-      if (s.dgate)
-        s.dgate[group * s.M + column] = s.beta * (param(s.post_weight, column, 1.0f) * v[0] + param(s.post_bias, column, 0.0f) * v[2]);
+    }
+    if (s.share > 1) {
+#pragma unroll
+      for (int n = 0; n < SUMS; ++n) of_lanes[n][lane][x] = v[n];
+      lds_barrier();
+      if (leads) {
+        for (int l = 1; l < s.share; ++l)
+#pragma unroll
+          for (int n = 0; n < SUMS; ++n) v[n] += of_lanes[n][lane + l][x];
+      }
+      lds_barrier();
+    }
+    if (leads && group < s.groups) {
+      const float by = s.beta * param(s.gate ? s.gate + group * M : nullptr, column, 1.0f);
+      float d = param(s.post_weight, column, 1.0f) * v[0];
+      if constexpr (SUMS == 4) d += param(s.post_bias, column, 0.0f) * v[2];
+      if (s.dgate) s.dgate[group * M + column] = s.beta * d;
       total[0] = fmaf(by, v[0], total[0]);
       total[1] += v[1];
-      total[2] = fmaf(by, v[2], total[2]);
-      total[3] += v[3];
+      if constexpr (SUMS == 4) {
+        total[2] = fmaf(by, v[2], total[2]);
+        total[3] += v[3];
+      }
     }
-    lds_barrier();
   }
+#pragma unroll
+  for (int n = 0; n < SUMS; ++n) of_lanes[n][lane][x] = total[n];
+  lds_barrier();
   if (lane != 0 || !exists) return;
+  for (int l = s.share; l < kSumLanes; l += s.share)
+#pragma unroll
+    for (int n = 0; n < SUMS; ++n) total[n] += of_lanes[n][l][x];
   if (s.dpost_weight) s.dpost_weight[column] = total[0];
   if (s.dpre_weight) s.dpre_weight[column] = total[1];
-  if (s.dpost_bias) s.dpost_bias[column] = total[2];
-  if (s.dpre_bias) s.dpre_bias[column] = total[3];
+  if constexpr (SUMS == 4) {
+    if (s.dpost_bias) s.dpost_bias[column] = total[2];
+    if (s.dpre_bias) s.dpre_bias[column] = total[3];
+  }
 }
 
 // ---- plans ----------------------------------------------------------------------------------------------------------------
@@ -425,10 +478,10 @@ Shape shape_of(int64_t M, tempo_dtype dt) {
   const int64_t pieces = (M + V - 1) / V;
   if (M < V || pieces > 2048) return {0, 0};
   if (pieces <= 64) return {1, 1};
-  if (pieces <= 128) return {1, 2};
-  if (pieces <= 256) return {2, 2};
-  if (pieces <= 512) return {4, 2};
-  if (pieces <= 1024) return {8, 2};
+  if (pieces <= 128) return {2, 1};
+  if (pieces <= 256) return {4, 1};
+  if (pieces <= 512) return {8, 1};
+  if (pieces <= 1024) return {16, 1};
   return {16, 2};
 }
 // Workgroups: rows that a gate is for are cut into parts.
@@ -436,15 +489,17 @@ struct Plan {
   Shape shape;
   int64_t groups, group_rows, part_rows, parts;
 };
-Plan plan_of(const ResidualCall& c, tempo_dtype dt) {
+Plan plan_of(const ResidualCall& c, tempo_dtype dt, bool back) {
   Plan p{};
   p.shape = shape_of(c.M, dt);
   p.groups = c.gate ? c.groups : 1;
   p.group_rows = c.N / p.groups;
-  const int64_t blocks = int64_t{compute_units()} * 16 / std::max(p.shape.waves, 1);
+  // 32 waves for each compute unit, and backward 8 rows each where there are as many for all of them, so that the sums are a small part of what
+  // is read and written.  us with 2, 4, 8 and 12: 3063 x 1001 float32 54.5, 38.4, 32.0, 30.4, 4096 x 1024 bfloat16 31.8, 24.5, 22.0, 24.7.
+  const int64_t cus = compute_units(), blocks = cus * 32 / std::max(p.shape.waves, 1);
   p.part_rows = std::max<int64_t>((c.N + blocks - 1) / blocks, 1);
+  if (back) p.part_rows = std::max(p.part_rows, std::min<int64_t>(8, (c.N + cus - 1) / cus));
   p.parts = std::max<int64_t>((p.group_rows + p.part_rows - 1) / p.part_rows, 1);
-  p.part_rows = std::max<int64_t>((p.group_rows + p.parts - 1) / p.parts, 1);
   return p;
 }
 int sums_of(const ResidualCall& c) { return c.dpost_bias || c.dpre_bias || (c.dgate && c.post && c.post->bias) ? 4 : 2; }
@@ -463,7 +518,6 @@ Residual residual_of(const ResidualCall& c, const Plan& p) {
   r.group_rows = p.group_rows;
   r.inv = 1.0f / static_cast<float>(c.M);
   r.parts = static_cast<int>(p.parts);
-  r.part_rows = p.part_rows;
   return r;
 }
 template <typename T, typename F>
@@ -473,15 +527,13 @@ bool with_shape(const Shape& s, int64_t M, F&& f) {
     else f(waves, pieces, std::true_type{});
     return true;
   };
-  const std::integral_constant<int, 2> two;
+  const std::integral_constant<int, 1> one;
   switch (s.waves) {
-    case 1:
-      return s.pieces == 1 ? by_row(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{})
-                           : by_row(std::integral_constant<int, 1>{}, two);
-    case 2: return by_row(two, two);
-    case 4: return by_row(std::integral_constant<int, 4>{}, two);
-    case 8: return by_row(std::integral_constant<int, 8>{}, two);
-    case 16: return by_row(std::integral_constant<int, 16>{}, two);
+    case 1: return by_row(one, one);
+    case 2: return by_row(std::integral_constant<int, 2>{}, one);
+    case 4: return by_row(std::integral_constant<int, 4>{}, one);
+    case 8: return by_row(std::integral_constant<int, 8>{}, one);
+    case 16: return s.pieces == 1 ? by_row(std::integral_constant<int, 16>{}, one) : by_row(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
     default: return false;
   }
 }
@@ -489,17 +541,17 @@ bool with_shape(const Shape& s, int64_t M, F&& f) {
 }  // namespace
 
 bool residual_norm_takes(const ResidualCall& c, tempo_dtype dt) {
-  const Plan p = plan_of(c, dt);
+  const Plan p = plan_of(c, dt, false);  // more parts than backward
   return p.groups * p.parts <= int64_t{1} << 22;  // launches of less than 2^32 lanes
 }
 
 size_t residual_norm_workspace_bytes(const ResidualCall& c, tempo_dtype dt) {
-  const Plan p = plan_of(c, dt);
+  const Plan p = plan_of(c, dt, true);
   return static_cast<size_t>(p.groups) * p.parts * 4 * c.M * sizeof(float);
 }
 
 tempo_status launch_residual_norm_fwd(const ResidualCall& c, tempo_dtype dt, hipStream_t st) {
-  const Plan p = plan_of(c, dt);
+  const Plan p = plan_of(c, dt, false);
   const Residual r = residual_of(c, p);
   const dim3 grid(static_cast<uint32_t>(p.groups * p.parts));
   const bool bias = (c.post && c.post->bias) || (c.pre && c.pre->bias);
@@ -518,7 +570,7 @@ tempo_status launch_residual_norm_fwd(const ResidualCall& c, tempo_dtype dt, hip
 }
 
 tempo_status launch_residual_norm_bwd(const ResidualCall& c, tempo_dtype dt, hipStream_t st) {
-  const Plan p = plan_of(c, dt);
+  const Plan p = plan_of(c, dt, true);
   Residual r = residual_of(c, p);
   const int sums = sums_of(c);
   if (wants_columns(c)) {
@@ -540,9 +592,13 @@ tempo_status launch_residual_norm_bwd(const ResidualCall& c, tempo_dtype dt, hip
   };
   const tempo_status s = dt == TEMPO_F32 ? of_type(float{}) : of_type(bf16_t{});
   if (s != TEMPO_OK || !r.partial) return s;
-  const Sums all{r.partial, p.groups, r.parts, sums, r.M, c.gate, c.post ? c.post->weight : nullptr, c.post ? c.post->bias : nullptr, c.beta,
+  int share = kSumLanes;
+  while (share > 1 && kSumLanes / share < p.groups) share /= 2;
+  const Sums all{r.partial, p.groups, r.parts, sums, r.M, share, c.gate, c.post ? c.post->weight : nullptr, c.post ? c.post->bias : nullptr, c.beta,
                  c.dgate, c.dpost_weight, c.dpost_bias, c.dpre_weight, c.dpre_bias};
-  hipLaunchKernelGGL(columns_kernel, dim3(static_cast<uint32_t>((c.M + 15) / 16)), dim3(256), 0, st, all);
+  const dim3 columns(static_cast<uint32_t>((c.M + kSumColumns - 1) / kSumColumns)), lanes(kSumColumns * kSumLanes);
+  if (sums == 4) hipLaunchKernelGGL(columns_kernel<4>, columns, lanes, 0, st, all);
+  else hipLaunchKernelGGL(columns_kernel<2>, columns, lanes, 0, st, all);
   return launch_status();
 }
 

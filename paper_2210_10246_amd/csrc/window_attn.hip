@@ -196,8 +196,12 @@ struct Staged {
   }
 };
 
-// Waits until all of the wave's loads have come (and for nothing else).
-__device__ __forceinline__ void landed() { __builtin_amdgcn_s_waitcnt(0xF70); }
+// Waits until all but the last N loads of the wave have come (and for nothing else).
+template <int N>
+__device__ __forceinline__ void landed() {
+  static_assert(N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xF70);
+}
 // N rows of a matrix from memory to LDS without registers: rows that begin at multiples of 16 bytes, D a multiple of a piece.  In assembly
 // because the compiler waits for all such loads before any read of LDS; whoever calls this waits for them.  It has no output, and nothing else
 // here uses m0.  Lanes of pieces behind D load nothing, and what LDS holds there stays.
@@ -296,23 +300,27 @@ struct KeyTiles {
   }
 };
 
-// The tiles of k and v that the rows of a workgroup see, one after the other through two buffers: while one is worked on, the next is on
-// its way.  DIRECT: without registers.
-template <typename T, int DP, int BK, bool DIRECT>
+// The tiles of k and v that the rows of a workgroup see, one after the other through BUFS buffers: while one is worked on, the next ones are on
+// their way.  DIRECT: without registers; else there are two buffers.
+template <typename T, int DP, int BK, bool DIRECT, int MOST>
 struct KeyStream {
-  static constexpr int kBytes = Rows<T, DP>::bytes(BK);
+  static constexpr int kBytes = Rows<T, DP>::bytes(BK), BUFS = DIRECT ? MOST : 2;
   const Attn& a;
-  const Sight& s;
   const KeyTiles& keys;
   const T *k, *v;  // of key 0
   char (*lds)[2][kBytes];
+  int n0, n1;
   std::conditional_t<DIRECT, Direct<T, DP, BK>, Staged<T, DP, BK>> ks, vs;
-  __device__ __forceinline__ KeyStream(const Attn& a_, const Sight& s_, const KeyTiles& keys_, int b, int kv, char (*lds_)[2][kBytes])
-      : a(a_), s(s_), keys(keys_), k(at<T>(a_.k, b, 0, kv)), v(at<T>(a_.v, b, 0, kv)), lds(lds_), ks(a_.k), vs(a_.v) {
+  // Tiles [n0, n1); the first ones are on their way from here on.
+  __device__ __forceinline__ KeyStream(const Attn& a_, const KeyTiles& keys_, int b, int kv, char (*lds_)[2][kBytes], int n0_, int n1_)
+      : a(a_), keys(keys_), k(at<T>(a_.k, b, 0, kv)), v(at<T>(a_.v, b, 0, kv)), lds(lds_), n0(n0_), n1(n1_), ks(a_.k), vs(a_.v) {
     if (DIRECT && a.D < DP) {
-      clear_lds(lds[0][0], 4 * kBytes);
+      clear_lds(lds[0][0], 2 * BUFS * kBytes);
       lds_barrier();
     }
+#pragma unroll
+    for (int i = 0; i < BUFS - 1; ++i)
+      if (n0 + i < n1) fetch(n0 + i, i);
   }
   __device__ __forceinline__ void fetch(int n, int to) {
     const int j0 = keys.key(n, BK);
@@ -335,19 +343,21 @@ struct KeyStream {
       vs.store(lds[to][1]);
     }
   }
-  // work(tile's first key, its k, its v) for tiles [n0, n1)
+  // work(tile's first key, its k, its v)
   template <typename F>
-  __device__ __forceinline__ void each(int n0, int n1, F&& work) {
-    if (n0 >= n1) return;
-    fetch(n0, 0);
-    put(0);
+  __device__ __forceinline__ void each(F&& work) {
+    if (n0 < n1) put(0);
+    int now = 0;
     for (int n = n0; n < n1; ++n) {
-      const int now = (n - n0) & 1;
-      if constexpr (DIRECT) landed();
-      lds_barrier();  // the tile is there, and the other buffer has been read
-      if (n + 1 < n1) fetch(n + 1, now ^ 1);
+      if constexpr (DIRECT) {  // the tiles behind this one may still be on their way
+        if (BUFS == 2 || n + BUFS - 1 > n1) landed<0>();
+        else landed<(BUFS - 2) * 2 * decltype(ks)::kPieces>();
+      }
+      lds_barrier();  // the tile is there, and the buffer before it has been read
+      if (n + BUFS - 1 < n1) fetch(n + BUFS - 1, now == 0 ? BUFS - 1 : now - 1);
       work(keys.key(n, BK), lds[now][0], lds[now][1]);
       if (n + 1 < n1) put(now ^ 1);
+      now = now + 1 == BUFS ? 0 : now + 1;
     }
   }
 };
@@ -383,12 +393,12 @@ __device__ __forceinline__ int key_of(int i) { return 8 * (i / 4) + 4 * (static_
 template <typename T, int DP, bool DIRECT>
 constexpr int kAtOnce = DIRECT && sizeof(T) * DP <= 256 ? 2 : 1;
 
-template <typename T, int DP, int BK, bool DIRECT>
+template <typename T, int DP, int BK, bool DIRECT, int MOST>
 __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_kernel(Attn a) {
   using R = Rows<T, DP>;
-  using Stream = KeyStream<T, DP, BK, DIRECT>;
+  using Stream = KeyStream<T, DP, BK, DIRECT, MOST>;
   constexpr int kBlocks = BK / 32, kColumns = DP / 32;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][Stream::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds[Stream::BUFS][2][Stream::kBytes];
   const int job = in_order(blockIdx.x, gridDim.x), split = job % a.splits, tile = job / a.splits % a.tiles;
   const int bk = job / a.splits / a.tiles, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
   const Sight s(a, b);
@@ -396,6 +406,7 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_ke
   const int first_row = tile * kRows, last_row = min(first_row + kRows, a.rows) - 1;
   const KeyTiles keys(s, a.by_group.divide(first_row), a.by_group.divide(last_row), BK);
   const int each = (keys.count + a.splits - 1) / a.splits, n0 = split * each, n1 = min(n0 + each, keys.count);
+  Stream stream(a, keys, b, kv, lds, n0, n1);
   const WaveRows w(a, s, first_row + wave * 32);
   u32x4 q[R::kSteps];
   {
@@ -407,8 +418,7 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_ke
 #pragma unroll
   for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
   float m = kMinusInf, sum = 0.0f;  // maximum, of base 2, and the lane's part of the sum
-  Stream stream(a, s, keys, b, kv, lds);
-  stream.each(n0, n1, [&](int j0, const char* k_tile, const char* v_tile) {
+  stream.each([&](int j0, const char* k_tile, const char* v_tile) {
     if (!w.any || w.none(s, j0, BK)) return;
     f32x16 p[kBlocks];
 #pragma unroll
@@ -499,18 +509,19 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Attn a, int64_t all) {
 }
 
 // ---- backward by rows: delta and dq ---------------------------------------------------------------------------------------
-template <typename T, int DP, int BK, bool DIRECT>
+template <typename T, int DP, int BK, bool DIRECT, int MOST>
 __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void rows_kernel(Attn a) {
   using R = Rows<T, DP>;
-  using Stream = KeyStream<T, DP, BK, DIRECT>;
+  using Stream = KeyStream<T, DP, BK, DIRECT, MOST>;
   constexpr int kBlocks = BK / 32, kColumns = DP / 32;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][Stream::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds[Stream::BUFS][2][Stream::kBytes];
   const int job = in_order(blockIdx.x, gridDim.x), tile = job % a.tiles;
   const int bk = job / a.tiles, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
   const Sight s(a, b);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int first_row = tile * kRows, last_row = min(first_row + kRows, a.rows) - 1;
   const KeyTiles keys(s, a.by_group.divide(first_row), a.by_group.divide(last_row), BK);
+  Stream stream(a, keys, b, kv, lds, 0, keys.count);
   const WaveRows w(a, s, first_row + wave * 32);
   const int head = kv * a.group + w.g, half = threadIdx.x % kWave / 32;
   const int64_t stat = (static_cast<int64_t>(b) * a.heads + head) * a.Sq + w.i;
@@ -539,8 +550,7 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void rows_kerne
   f32x16 acc[kColumns];
 #pragma unroll
   for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
-  Stream stream(a, s, keys, b, kv, lds);
-  stream.each(0, keys.count, [&](int j0, const char* k_tile, const char* v_tile) {
+  stream.each([&](int j0, const char* k_tile, const char* v_tile) {
     if (!w.any || w.none(s, j0, BK)) return;
     const bool all = w.all(s, j0, BK);
 #pragma unroll
@@ -697,7 +707,7 @@ __global__ __launch_bounds__(kThreads, (TEMPO_KEYS)) void keys_kernel(Attn a, Ke
   }
   for (int u = u0; u < u1; ++u) {
     const int now = (u - u0) & 1, i0 = block.i;
-    if constexpr (DIRECT) landed();
+    if constexpr (DIRECT) landed<0>();
     lds_barrier();  // the block is there, and the other buffer has been read
     block = following(block);
     if (u + 1 < u1) fetch(block, now ^ 1);
@@ -787,6 +797,17 @@ __global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, const float
     Store<T>::store1(to + d, sum);
   }
 }
+
+#ifndef KT
+#define KT 64
+#define KB 3
+#define KT2 64
+#define KB2 2
+#endif
+template <typename T, int DP>
+constexpr int key_tile = sizeof(T) * DP == 128 ? KT : sizeof(T) * DP <= 256 ? KT2 : 32;
+template <typename T, int DP>
+constexpr int key_buffers = sizeof(T) * DP == 128 ? KB : sizeof(T) == 2 && DP == 128 ? KB2 : 2;
 
 // ---- plans ----------------------------------------------------------------------------------------------------------------
 int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
@@ -907,9 +928,9 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
   return with_type(dt, [&](auto type) {
     using T = decltype(type);
     const tempo_status s = with_width(c.D, [&](auto width) {
-      constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 ? 64 : 32;
+      constexpr int DP = decltype(width)::value, BK = key_tile<T, DP>, BUFS = key_buffers<T, DP>;
       return either(direct(c, dt, {c.k, c.v}), [&](auto straight) {
-        return launch(forward_kernel<T, DP, BK, decltype(straight)::value>, blocks, st, a);
+        return launch(forward_kernel<T, DP, BK, decltype(straight)::value, BUFS>, blocks, st, a);
       });
     });
     if (s != TEMPO_OK || a.splits == 1) return s;
@@ -928,9 +949,9 @@ tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStre
   return with_type(dt, [&](auto type) {
     using T = decltype(type);
     tempo_status s = with_width(c.D, [&](auto width) {
-      constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 ? 64 : 32;
+      constexpr int DP = decltype(width)::value, BK = key_tile<T, DP>, BUFS = key_buffers<T, DP>;
       const tempo_status r = either(direct(c, dt, {c.k, c.v}), [&](auto straight) {
-        return launch(rows_kernel<T, DP, BK, decltype(straight)::value>, c.B * c.kv_heads * a.tiles, st, a);
+        return launch(rows_kernel<T, DP, BK, decltype(straight)::value, BUFS>, c.B * c.kv_heads * a.tiles, st, a);
       });
       if (r != TEMPO_OK) return r;
       return either(direct(c, dt, {c.q, c.dout}), [&](auto straight) {
