@@ -374,14 +374,14 @@ typedef struct {
   int64_t batch, token, head; /* strides in elements */
 } tempo_attn_heads;
 TEMPO_API size_t tempo_window_attn_fwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D,
-                                             int64_t window, int64_t sinks);
+                                             int64_t window, int64_t sinks, tempo_dtype dt);
 TEMPO_API tempo_status tempo_window_attn_fwd(const tempo_attn_heads* q, const tempo_attn_heads* k, const tempo_attn_heads* v,
                                    const tempo_attn_heads* out, float* lse, const int32_t* key_len, const int32_t* query_start,
                                    void* workspace, size_t workspace_bytes, int64_t B, int64_t Sq, int64_t Sk, int64_t heads,
                                    int64_t kv_heads, int64_t D, int64_t window, int64_t sinks, float scale, tempo_dtype dt,
                                    void* hip_stream);
 TEMPO_API size_t tempo_window_attn_bwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D,
-                                             int64_t window, int64_t sinks);
+                                             int64_t window, int64_t sinks, tempo_dtype dt);
 TEMPO_API tempo_status tempo_window_attn_bwd(const tempo_attn_heads* dout, const tempo_attn_heads* q, const tempo_attn_heads* k,
                                    const tempo_attn_heads* v, const tempo_attn_heads* out, const float* lse, const tempo_attn_heads* dq,
                                    const tempo_attn_heads* dk, const tempo_attn_heads* dv, const int32_t* key_len,

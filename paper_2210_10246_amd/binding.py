@@ -91,8 +91,8 @@ _SIGNATURES = {
     "tempo_glu_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
     "tempo_glu_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _sz, _i64, _i64, _i64, _int, _int, _vp]),
     "tempo_glu_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _i64, _i64, _i64, _int, _int, _vp]),
-    "tempo_window_attn_fwd_workspace_bytes": (_sz, [_i64] * 8),
-    "tempo_window_attn_bwd_workspace_bytes": (_sz, [_i64] * 8),
+    "tempo_window_attn_fwd_workspace_bytes": (_sz, [_i64] * 8 + [_int]),
+    "tempo_window_attn_bwd_workspace_bytes": (_sz, [_i64] * 8 + [_int]),
     "tempo_window_attn_fwd": (_int, [_heads] * 4 + [_vp] * 4 + [_sz] + [_i64] * 8 + [_f32, _int, _vp]),
     "tempo_window_attn_bwd": (_int, [_heads] * 5 + [_vp] + [_heads] * 3 + [_vp] * 3 + [_sz] + [_i64] * 8 + [_f32, _int, _vp]),
     "tempo_mask_bits_to_bytes": (_int, [_vp, _vp, _i64, _vp]),
@@ -680,12 +680,12 @@ def tempo_glu_bwd(dh, gu, x, w, dgu, h, dx, dw, dbias, kind="silu", workspace=No
            "tempo_glu_bwd")
 
 
-def tempo_window_attn_fwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks) -> int:
-    return load().tempo_window_attn_fwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks)
+def tempo_window_attn_fwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks, dtype) -> int:
+    return load().tempo_window_attn_fwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks, _DT[dtype])
 
 
-def tempo_window_attn_bwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks) -> int:
-    return load().tempo_window_attn_bwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks)
+def tempo_window_attn_bwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks, dtype) -> int:
+    return load().tempo_window_attn_bwd_workspace_bytes(B, Sq, Sk, heads, kv_heads, D, window, sinks, _DT[dtype])
 
 
 def _window_attn(where, like_q, like_k, lse, window, sinks, scale, key_len, query_start, workspace, stream):
@@ -717,7 +717,7 @@ def _window_attn(where, like_q, like_k, lse, window, sinks, scale, key_len, quer
     _same_device(*tensors, lse, key_len, query_start, workspace)
     structs = {n: _AttnHeads(t.data_ptr(), (_i64 * 3)(*t.stride()[:3])) for n, t in like_q + like_k}
     sizes = B, Sq, Sk, heads, kv_heads, D, window, sinks
-    ws = _workspace(workspace, getattr(load(), where + "_workspace_bytes")(*sizes), q.device, stream)
+    ws = _workspace(workspace, getattr(load(), where + "_workspace_bytes")(*sizes, dt), q.device, stream)
     return structs, pointers, [_ptr(ws), ws.numel() * ws.element_size(), *sizes, scale, dt, _stream(stream)]
 
 

@@ -534,20 +534,20 @@ static WindowCall window_sizes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads,
   c.sinks = sinks < most ? sinks : most;
   return c;
 }
-static size_t window_attn_bytes(const WindowCall& c, bool back) {
-  return window_attn_ok(c) && c.B > 0 && c.heads > 0 && window_attn_takes(c) ? window_attn_workspace_bytes(c, back) : 0;
+static size_t window_attn_bytes(const WindowCall& c, tempo_dtype dt, bool back) {
+  return window_attn_ok(c) && dtype_ok(dt) && c.B > 0 && c.heads > 0 && window_attn_takes(c) ? window_attn_workspace_bytes(c, dt, back) : 0;
 }
 
 size_t tempo_window_attn_fwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D,
-                                             int64_t window, int64_t sinks) {
+                                             int64_t window, int64_t sinks, tempo_dtype dt) {
   const WindowCall c = window_sizes(B, Sq, Sk, heads, kv_heads, D, window, sinks);
-  return window_attn_bytes(c, false);
+  return window_attn_bytes(c, dt, false);
 }
 
 size_t tempo_window_attn_bwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D,
-                                             int64_t window, int64_t sinks) {
+                                             int64_t window, int64_t sinks, tempo_dtype dt) {
   const WindowCall c = window_sizes(B, Sq, Sk, heads, kv_heads, D, window, sinks);
-  return window_attn_bytes(c, true);
+  return window_attn_bytes(c, dt, true);
 }
 
 static bool scale_ok(float scale) { return scale > 0.0f && scale <= 3.402823466e+38f; }  // false for NaN

@@ -426,7 +426,7 @@ TEMPO_METHOD(window_attn_fwd) {  // q, k, v, out, lse, window, sinks, scale, key
     const tempo_attn_heads q = attn_heads(a[0], tq), k = attn_heads(a[1], tk), v = attn_heads(a[2], tk), out = attn_heads(a[3], tq);
     float* lse = small_or_none<float>(a[4], at::kFloat, w.B * w.heads * w.Sq);
     const auto *len = small_or_none<int32_t>(a[8], at::kInt, w.B), *start = small_or_none<int32_t>(a[9], at::kInt, w.B);
-    return [=, ws = Workspace(a[10], tq, tempo_window_attn_fwd_workspace_bytes(w.B, w.Sq, w.Sk, w.heads, w.kv_heads, w.D, w.window, w.sinks)),
+    return [=, ws = Workspace(a[10], tq, tempo_window_attn_fwd_workspace_bytes(w.B, w.Sq, w.Sk, w.heads, w.kv_heads, w.D, w.window, w.sinks, w.dt)),
             st = stream()] {
       return tempo_window_attn_fwd(&q, &k, &v, &out, lse, len, start, ws.p, ws.bytes, w.B, w.Sq, w.Sk, w.heads, w.kv_heads, w.D, w.window,
                                    w.sinks, w.scale, w.dt, st);
@@ -443,7 +443,7 @@ TEMPO_METHOD(window_attn_bwd) {
     if (a[5] == Py_None) throw NotPlain{};
     const float* lse = small_or_none<float>(a[5], at::kFloat, w.B * w.heads * w.Sq);
     const auto *len = small_or_none<int32_t>(a[12], at::kInt, w.B), *start = small_or_none<int32_t>(a[13], at::kInt, w.B);
-    return [=, ws = Workspace(a[14], tq, tempo_window_attn_bwd_workspace_bytes(w.B, w.Sq, w.Sk, w.heads, w.kv_heads, w.D, w.window, w.sinks)),
+    return [=, ws = Workspace(a[14], tq, tempo_window_attn_bwd_workspace_bytes(w.B, w.Sq, w.Sk, w.heads, w.kv_heads, w.D, w.window, w.sinks, w.dt)),
             st = stream()] {
       return tempo_window_attn_bwd(&dout, &q, &k, &v, &out, lse, &dq, &dk, &dv, len, start, ws.p, ws.bytes, w.B, w.Sq, w.Sk, w.heads,
                                    w.kv_heads, w.D, w.window, w.sinks, w.scale, w.dt, st);

@@ -121,7 +121,7 @@ struct WindowCall {
   float scale;
 };
 bool window_attn_takes(const WindowCall& c);
-size_t window_attn_workspace_bytes(const WindowCall& c, bool back);
+size_t window_attn_workspace_bytes(const WindowCall& c, tempo_dtype dt, bool back);
 tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStream_t st);
 tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStream_t st);
 tempo_status launch_mask_bits_to_bytes(const uint32_t* bits, uint8_t* bytes, int64_t n,

@@ -362,6 +362,9 @@ struct KeyStream {
   }
 };
 
+// The key (or query) of a lane's sum i.
+__device__ __forceinline__ int key_of(int i) { return 8 * (i / 4) + 4 * (static_cast<int>(threadIdx.x) % kWave / 32) + i % 4; }
+
 // What a wave's 32 rows see of keys [j0, j0 + n).
 struct WaveRows {
   int r0, row, i, g;        // the wave's first row, the lane's, its query and head
@@ -384,11 +387,86 @@ struct WaveRows {
   __device__ __forceinline__ bool all(const Sight& s, int j0, int n) const {
     return j0 + n <= first_end && (j0 >= last_begin || j0 + n <= s.sinks);
   }
-  __device__ __forceinline__ bool sees(const Sight& s, int j) const { return j < end && (j >= begin || j < s.sinks); }
+  // Of the sums of keys from j0 on, those of keys that the row does not see become `otherwise`.
+  template <int BLOCKS>
+  __device__ __forceinline__ void hide(const Sight& s, int j0, f32x16 (&p)[BLOCKS], float otherwise) const {
+    if (j0 >= s.sinks) {  // one stretch of keys
+      const uint32_t from = j0 + key_of(0) - begin, span = max(end - begin, 0);
+#pragma unroll
+      for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[kb][i] = from + (kb * 32 + 8 * (i / 4) + i % 4) < span ? p[kb][i] : otherwise;
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = j0 + kb * 32 + key_of(i);
+          p[kb][i] = j < end && (j >= begin || j < s.sinks) ? p[kb][i] : otherwise;
+        }
+    }
+  }
 };
-__device__ __forceinline__ int key_of(int i) { return 8 * (i / 4) + 4 * (static_cast<int>(threadIdx.x) % kWave / 32) + i % 4; }
 
 // ---- forward ------------------------------------------------------------------------------------------------------------
+// A lane's running maximum (of base 2) and its part of the sum of exponentials, of the row that the lane has.
+struct Running {
+  float top = kMinusInf, sum = 0.0f;
+  // Scores of BLOCKS x 32 keys to exponentials; c: scale log2(e).  What they are relative to follows the maximum only where they would pass
+  // 2^8: nothing is lost below that.
+  template <int BLOCKS, int COLUMNS>
+  __device__ __forceinline__ void exponentials(f32x16 (&p)[BLOCKS], float c, f32x16 (&acc)[COLUMNS]) {
+    float most = p[0][0];
+#pragma unroll
+    for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, p[kb][i]);
+    most = c * across_rows<32>(most, [](float x, float y) { return fmaxf(x, y); });
+    if (__any(most > top + 8.0f)) {
+      const float next = fmaxf(top, most);
+      rescale(next, __builtin_amdgcn_exp2f(top - finite(next)), acc);
+    }
+    const float from = finite(top);
+#pragma unroll
+    for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[kb][i] = __builtin_amdgcn_exp2f(fmaf(p[kb][i], c, -from));
+        sum += p[kb][i];
+      }
+  }
+  __device__ static __forceinline__ float finite(float x) { return x == kMinusInf ? 0.0f : x; }
+  template <int COLUMNS>
+  __device__ __forceinline__ void rescale(float next, float by, f32x16 (&acc)[COLUMNS]) {
+    top = next;
+    sum *= by;
+#pragma unroll
+    for (int d = 0; d < COLUMNS; ++d) acc[d] *= by;
+  }
+};
+
+// What a row has in the end, to the output or as part `part` of it, of a.splits.
+template <typename T, int COLUMNS>
+__device__ __forceinline__ void finish(const Attn& a, const Running& run, const f32x16 (&acc)[COLUMNS], int b, int kv, const WaveRows& w, int part,
+                                       int64_t all_rows) {
+  const float sum = across_rows<32>(run.sum, [](float x, float y) { return x + y; });
+  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float lse = sum == 0.0f ? kMinusInf : run.top + __builtin_amdgcn_logf(sum);
+  const bool first_half = threadIdx.x % kWave < 32;
+  if (a.splits > 1) {
+    const int64_t at_row = part * all_rows + (static_cast<int64_t>(b) * a.kv_heads + kv) * a.rows + w.row;
+    if (first_half) a.partial_lse[at_row] = lse;
+#pragma unroll
+    for (int d = 0; d < COLUMNS; ++d) store_sums(a.partial + at_row * a.D, a.D, d, acc[d], by);
+  } else {
+    const int head = kv * a.group + w.g;
+    if (a.lse && first_half) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + w.i] = lse * kLn2;
+    T* const to = const_cast<T*>(at<T>(a.out, b, w.i, head));
+#pragma unroll
+    for (int d = 0; d < COLUMNS; ++d) store_sums(to, a.D, d, acc[d], by);
+  }
+}
+
 // Waves on a SIMD: two where their registers allow it, one at its matrix instructions while the other is at its exponentials.
 template <typename T, int DP, bool DIRECT>
 constexpr int kAtOnce = DIRECT && sizeof(T) * DP <= 256 ? 2 : 1;
@@ -417,7 +495,7 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_ke
   f32x16 acc[kColumns];
 #pragma unroll
   for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
-  float m = kMinusInf, sum = 0.0f;  // maximum, of base 2, and the lane's part of the sum
+  Running run;
   stream.each([&](int j0, const char* k_tile, const char* v_tile) {
     if (!w.any || w.none(s, j0, BK)) return;
     f32x16 p[kBlocks];
@@ -427,56 +505,105 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_ke
 #pragma unroll
       for (int t = 0; t < R::kSteps; ++t) p[kb] = multiply<T>(R::rows(k_tile, kb * 32, t), q[t], p[kb]);
     }
-    if (!w.all(s, j0, BK)) {
-#pragma unroll
-      for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[kb][i] = w.sees(s, j0 + kb * 32 + key_of(i)) ? p[kb][i] : kMinusInf;
-    }
-    float top = p[0][0];
-#pragma unroll
-    for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, p[kb][i]);
-    top = a.c * across_rows<32>(top, [](float x, float y) { return fmaxf(x, y); });
-    // What the exponentials are relative to follows the maximum only where they would pass 2^8: nothing is lost below that.
-    if (__any(top > m + 8.0f)) {
-      const float next = fmaxf(m, top), by = __builtin_amdgcn_exp2f(m - (next == kMinusInf ? 0.0f : next));
-      m = next;
-      sum *= by;
-#pragma unroll
-      for (int d = 0; d < kColumns; ++d) acc[d] *= by;
-    }
-    const float from = m == kMinusInf ? 0.0f : m;
+    if (!w.all(s, j0, BK)) w.hide(s, j0, p, kMinusInf);
+    run.exponentials(p, a.c, acc);
 #pragma unroll
     for (int kb = 0; kb < kBlocks; ++kb) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[kb][i] = __builtin_amdgcn_exp2f(fmaf(p[kb][i], a.c, -from));
-        sum += p[kb][i];
-      }
       const Weights<T> weights(p[kb]);
 #pragma unroll
       for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(v_tile, kb * 32, d, weights, acc[d]);
     }
   });
   if (w.r0 + static_cast<int>(threadIdx.x) % 32 >= a.rows) return;
-  sum = across_rows<32>(sum, [](float x, float y) { return x + y; });
-  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const float lse = sum == 0.0f ? kMinusInf : m + __builtin_amdgcn_logf(sum);
-  const bool first_half = threadIdx.x % kWave < 32;
-  if (a.splits > 1) {
-    const int64_t at_row = (static_cast<int64_t>(split) * (gridDim.x / (a.splits * a.tiles)) + bk) * a.rows + w.row;
-    if (first_half) a.partial_lse[at_row] = lse;
+  finish<T>(a, run, acc, b, kv, w, split, static_cast<int64_t>(gridDim.x / (a.splits * a.tiles)) * a.rows);
+}
+
+// Up to 32 rows for a key head, as for a token each of the sequences of a cache: bound by the bytes of k and v.  Each wave takes its own blocks of 32
+// keys, without barriers: k from memory as a matrix instruction takes it, v by way of the wave's own LDS; both registers are filled with
+// the next block's as soon as they are free.  The waves' sums are joined in LDS, those of the workgroups that share a head by join_kernel.
+template <typename T, int DP>
+constexpr int kFewWaves = sizeof(T) * DP <= 256 ? 8 : 4;
+template <typename T, int DP>
+__global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4)) void few_kernel(Attn a) {
+  using R = Rows<T, DP>;
+  constexpr int W = kFewWaves<T, DP>, kColumns = DP / 32, kBytes = R::bytes(32), kSums = kColumns * 16 * kWave * 4;
+  constexpr int kAll = W * kBytes > kSums * (W / 2) ? W * kBytes : kSums * (W / 2);
+  __shared__ __attribute__((aligned(16))) char lds[kAll];
+  __shared__ float2 tops[W][kWave];
+  const int job = in_order(blockIdx.x, gridDim.x), split = job % a.splits, bk = job / a.splits, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
+  const Sight s(a, b);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
+  const KeyTiles keys(s, 0, a.by_group.divide(a.rows - 1), 32);
+  const WaveRows w(a, s, 0);
+  char* const own = lds + wave * kBytes;
+  const int step = a.splits * W;
+  int n = split * W + wave;
+  u32x4 k[R::kSteps], v[R::kSteps], q[R::kSteps];
+  auto fetch = [&](int j0) {
+    const T* row = at<T>(a.k, b, keys.seen(j0 + lane % 32), kv);
 #pragma unroll
-    for (int d = 0; d < kColumns; ++d) store_sums(a.partial + at_row * a.D, a.D, d, acc[d], by);
-  } else {
-    const int head = kv * a.group + w.g;
-    if (a.lse && first_half) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + w.i] = lse * kLn2;
-    T* const row = const_cast<T*>(at<T>(a.out, b, w.i, head));
+    for (int p = 0; p < R::kSteps; ++p) k[p] = load_of_row<T>(row, 2 * p + half, a.D);
 #pragma unroll
-    for (int d = 0; d < kColumns; ++d) store_sums(row, a.D, d, acc[d], by);
+    for (int p = 0; p < R::kSteps; ++p)  // lanes side by side have pieces side by side
+      v[p] = load_of_row<T>(at<T>(a.v, b, keys.seen(j0 + (p * kWave + lane) / R::P), kv), (p * kWave + lane) % R::P, a.D);
+  };
+  if (n < keys.count) fetch(keys.key(n, 32));
+  {
+    const T* row = at<T>(a.q, b, w.i, kv * a.group + w.g);
+#pragma unroll
+    for (int p = 0; p < R::kSteps; ++p) q[p] = load_of_row<T>(row, 2 * p + half, a.D);
   }
+  f32x16 acc[kColumns];
+#pragma unroll
+  for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
+  Running run;
+  for (; n < keys.count; n += step) {
+    const int j0 = keys.key(n, 32);
+    f32x16 p[1] = {zeros()};
+#pragma unroll
+    for (int t = 0; t < R::kSteps; ++t) p[0] = multiply<T>(k[t], q[t], p[0]);
+#pragma unroll
+    for (int t = 0; t < R::kSteps; ++t) {
+      const int row = (t * kWave + lane) / R::P, piece = (t * kWave + lane) % R::P;
+      *reinterpret_cast<u32x4*>(own + R::place(row) + ((piece ^ R::swizzle(row)) << 4)) = v[t];
+    }
+    if (n + step < keys.count) fetch(keys.key(n + step, 32));
+    if (!w.all(s, j0, 32)) w.hide(s, j0, p, kMinusInf);
+    run.exponentials(p, a.c, acc);
+    const Weights<T> weights(p[0]);
+    wave_lds_fence();
+#pragma unroll
+    for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(own, 0, d, weights, acc[d]);
+    wave_lds_fence();
+  }
+  const bool exists = lane % 32 < a.rows;
+  lds_barrier();
+#pragma unroll
+  for (int others = W / 2; others > 0; others /= 2) {
+    float* const sums = reinterpret_cast<float*>(lds) + (wave % others) * (kSums / 4) + lane;
+    if (wave >= others && wave < 2 * others && exists) {
+      tops[wave][lane] = make_float2(run.top, run.sum);
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[(d * 16 + i) * kWave] = acc[d][i];
+    }
+    lds_barrier();
+    if (wave < others && exists) {
+      const float2 other = tops[wave + others][lane];
+      const float next = fmaxf(run.top, other.x), from = Running::finite(next);
+      run.rescale(next, __builtin_amdgcn_exp2f(run.top - from), acc);
+      const float by = __builtin_amdgcn_exp2f(other.x - from);
+      run.sum = fmaf(other.y, by, run.sum);
+#pragma unroll
+      for (int d = 0; d < kColumns; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = fmaf(sums[(d * 16 + i) * kWave], by, acc[d][i]);
+    }
+    lds_barrier();
+  }
+  if (wave > 0 || !exists) return;
+  finish<T>(a, run, acc, b, kv, w, split, static_cast<int64_t>(gridDim.x / a.splits) * a.rows);
 }
 
 // The parts of a row, each weighted by its sum of exponentials: a wave a row.
@@ -555,18 +682,16 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void rows_kerne
     const bool all = w.all(s, j0, BK);
 #pragma unroll
     for (int kb = 0; kb < kBlocks; ++kb) {
-      f32x16 p = zeros(), dp = zeros();
+      f32x16 p[1] = {zeros()}, dp = zeros();
 #pragma unroll
       for (int t = 0; t < R::kSteps; ++t) {
-        p = multiply<T>(R::rows(k_tile, kb * 32, t), q[t], p);
+        p[0] = multiply<T>(R::rows(k_tile, kb * 32, t), q[t], p[0]);
         dp = multiply<T>(R::rows(v_tile, kb * 32, t), dout[t], dp);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float ds = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - delta);
-        p[i] = all || w.sees(s, j0 + kb * 32 + key_of(i)) ? ds : 0.0f;
-      }
-      const Weights<T> weights(p);
+      for (int i = 0; i < 16; ++i) p[0][i] = __builtin_amdgcn_exp2f(fmaf(p[0][i], a.c, -lse)) * (dp[i] - delta);
+      if (!all) w.hide(s, j0 + kb * 32, p, 0.0f);
+      const Weights<T> weights(p[0]);
 #pragma unroll
       for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(k_tile, kb * 32, d, weights, acc[d]);
     }
@@ -798,6 +923,12 @@ __global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, const float
   }
 }
 
+#ifndef FEWB
+#define FEWB 4
+#endif
+#ifndef FEWC
+#define FEWC 12
+#endif
 #ifndef KT
 #define KT 64
 #define KB 3
@@ -812,10 +943,18 @@ constexpr int key_buffers = sizeof(T) * DP == 128 ? KB : sizeof(T) == 2 && DP ==
 // ---- plans ----------------------------------------------------------------------------------------------------------------
 int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
+// Up to 32 rows for a key head: the kernel for few, where a wave's registers hold what it needs.
+bool few(const WindowCall& c, tempo_dtype dt) {
+  return c.Sq * (c.heads / c.kv_heads) <= 32 && c.D <= (dt == TEMPO_F32 ? 128 : 256);
+}
 // Parts of the keys of a forward: enough workgroups for the chip where there are few rows, of at least two tiles of keys each.
-int forward_splits(const WindowCall& c) {
+int forward_splits(const WindowCall& c, tempo_dtype dt) {
   const int64_t rows = c.Sq * (c.heads / c.kv_heads), blocks = up(rows, kRows) * c.B * c.kv_heads;
   const int64_t span = std::min(c.Sk, c.window + c.Sq) + std::min(c.sinks, c.Sk), most = std::max<int64_t>(up(span, 128), 1);
+  if (blocks > 0 && few(c, dt)) {
+    const int64_t waves = c.D * (dt == TEMPO_F32 ? 4 : 2) <= 256 ? 8 : 4;
+    return static_cast<int>(std::max<int64_t>(1, std::min({up(span, 32 * waves * FEWB), up(FEWC * compute_units() / 4, blocks), int64_t{64}})));
+  }
   if (blocks == 0 || blocks >= compute_units()) return 1;
   return static_cast<int>(std::min<int64_t>(std::min<int64_t>(most, 64), up(2 * compute_units(), blocks)));
 }
@@ -905,10 +1044,10 @@ bool window_attn_takes(const WindowCall& c) {
   return key_plan(c).blocks <= most;
 }
 
-size_t window_attn_workspace_bytes(const WindowCall& c, bool back) {
+size_t window_attn_workspace_bytes(const WindowCall& c, tempo_dtype dt, bool back) {
   const int64_t rows = c.B * c.heads * c.Sq;
   if (!back) {
-    const int splits = forward_splits(c);
+    const int splits = forward_splits(c, dt);
     return splits > 1 ? static_cast<size_t>(splits) * rows * (c.D + 1) * sizeof(float) : 0;
   }
   const KeyPlan p = key_plan(c);
@@ -916,9 +1055,9 @@ size_t window_attn_workspace_bytes(const WindowCall& c, bool back) {
 }
 
 tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStream_t st) {
-  if (c.workspace_bytes < window_attn_workspace_bytes(c, false)) return TEMPO_ERR_WORKSPACE;
+  if (c.workspace_bytes < window_attn_workspace_bytes(c, dt, false)) return TEMPO_ERR_WORKSPACE;
   Attn a = attn_of(c);
-  a.splits = forward_splits(c);
+  a.splits = forward_splits(c, dt);
   const int64_t all = c.B * c.heads * c.Sq;
   if (a.splits > 1) {
     a.partial = static_cast<float*>(c.workspace);
@@ -929,6 +1068,12 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
     using T = decltype(type);
     const tempo_status s = with_width(c.D, [&](auto width) {
       constexpr int DP = decltype(width)::value, BK = key_tile<T, DP>, BUFS = key_buffers<T, DP>;
+      if constexpr (sizeof(T) * DP <= 512) {
+        if (few(c, dt)) {
+          hipLaunchKernelGGL((few_kernel<T, DP>), dim3(static_cast<uint32_t>(c.B * c.kv_heads * a.splits)), dim3(kFewWaves<T, DP> * kWave), 0, st, a);
+          return launch_status();
+        }
+      }
       return either(direct(c, dt, {c.k, c.v}), [&](auto straight) {
         return launch(forward_kernel<T, DP, BK, decltype(straight)::value, BUFS>, blocks, st, a);
       });
@@ -939,7 +1084,7 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
 }
 
 tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStream_t st) {
-  if (c.workspace_bytes < window_attn_workspace_bytes(c, true)) return TEMPO_ERR_WORKSPACE;
+  if (c.workspace_bytes < window_attn_workspace_bytes(c, dt, true)) return TEMPO_ERR_WORKSPACE;
   Attn a = attn_of(c);
   a.stats = static_cast<float*>(c.workspace);
   a.stat_rows = c.B * c.heads * c.Sq;

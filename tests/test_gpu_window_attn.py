@@ -328,7 +328,7 @@ def test_given_workspaces_side_by_side_on_two_streams_and_replays():
         q, k, v = (t + seed for t in inputs(*size, "f32"))
         state = dict(q=q, k=k, v=v, out=torch.empty_like(q), lse=torch.empty(2, 4, 260, device="cuda"), dout=torch.ones_like(q),
                      grads=[torch.empty_like(t) for t in (q, k, v)])
-        state["ws"] = [torch.empty(n(*args), dtype=torch.uint8, device="cuda")
+        state["ws"] = [torch.empty(n(*args, torch.float32), dtype=torch.uint8, device="cuda")
                        for n in (B.tempo_window_attn_fwd_workspace_bytes, B.tempo_window_attn_bwd_workspace_bytes)]
         sides.append(state)
 

@@ -54,7 +54,7 @@ def test_window_attention_arguments_are_checked_before_any_launch():
     assert window_bwd(lse=None) == INVALID
     # a workspace that is too small, or none where one is needed
     sizes = dict(B_=1, S=1, Sk=4000, A=1, K=1, D=64, window=4000)
-    assert B.tempo_window_attn_fwd_workspace_bytes(1, 1, 4000, 1, 1, 64, 4000, 1) > 16
+    assert B.tempo_window_attn_fwd_workspace_bytes(1, 1, 4000, 1, 1, 64, 4000, 1, torch.float32) > 16
     assert window_fwd(**sizes) == WORKSPACE and window_fwd(ws=16, size=16, **sizes) == WORKSPACE
     assert window_bwd(**sizes) == WORKSPACE and window_bwd(ws=None, size=1 << 30, **sizes) == WORKSPACE
 
@@ -66,8 +66,8 @@ def test_window_attention_workspaces_of_any_sizes():
             for value in (-1, 0, 1, (1 << 31) - 1, 1 << 31, 1 << 40, (1 << 63) - 1):
                 sizes = [2, 100, 300, 4, 2, 64, 50, 3]
                 sizes[n] = value
-                assert way(*sizes) >= 0
-        assert way(2, 100, 300, 4, 0, 64, 50, 3) == 0 and way(2, 100, 300, 4, 3, 64, 50, 3) == 0
+                assert way(*sizes, torch.bfloat16) >= 0 and way(*sizes, torch.float32) >= 0
+        assert way(2, 100, 300, 4, 0, 64, 50, 3, torch.float32) == 0 and way(2, 100, 300, 4, 3, 64, 50, 3, torch.float32) == 0
 
 
 def norm(kind=0, weight=32, bias=None, eps=1e-5, stats=32):
