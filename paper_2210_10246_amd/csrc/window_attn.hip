@@ -159,10 +159,11 @@ __device__ __forceinline__ f32x16 multiply_columns(const char* lds, int row0, in
 }
 
 // Piece `piece` of a row of D elements at any address; zeros behind its end.
-template <typename T>
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ u32x4 load_of_row(const T* row, int piece, int D) {
   constexpr int V = Store<T>::kVec;
   const int left = D - piece * V;
+  if (STREAM && left >= V) return ldg_stream_any(row + piece * V);
   if (left >= V) return *reinterpret_cast<const u32x4_any*>(row + piece * V);
   float e[V];
 #pragma unroll
@@ -252,23 +253,25 @@ __device__ __forceinline__ const T* at(const Heads& h, int b, int token, int hea
   return static_cast<const T*>(h.p) + b * h.batch + token * h.token + head * h.head;
 }
 
-// A lane's sums of column block `block` to a row of D elements: 8 (i / 4) + 4 (lane / 32) + i % 4 are four neighbours each.
+// Four neighbouring elements of a row of D.
+template <typename T>
+__device__ __forceinline__ void store_four(T* row, int D, int d, f32x4 v) {
+  const int left = D - d;
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_any*>(row + d) = v;
+    else *reinterpret_cast<u32x2_any*>(row + d) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) Store<T>::store1(row + d + e, v[e]);
+  }
+}
+// A lane's sums of column block `block`: 8 (i / 4) + 4 (lane / 32) + i % 4 are four neighbours each.
 template <typename T>
 __device__ __forceinline__ void store_sums(T* row, int D, int block, const f32x16& s, float by) {
-  const int lane = threadIdx.x % kWave;
+  const int d = block * 32 + 4 * (static_cast<int>(threadIdx.x) % kWave / 32);
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int d = block * 32 + 8 * n + 4 * (lane / 32), left = D - d;
-    const float v[4] = {s[4 * n] * by, s[4 * n + 1] * by, s[4 * n + 2] * by, s[4 * n + 3] * by};
-    if (left >= 4) {
-      if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_any*>(row + d) = f32x4{v[0], v[1], v[2], v[3]};
-      else *reinterpret_cast<u32x2_any*>(row + d) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-    } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (e < left) Store<T>::store1(row + d + e, v[e]);
-    }
-  }
+  for (int n = 0; n < 4; ++n) store_four(row, D, d + 8 * n, f32x4{s[4 * n], s[4 * n + 1], s[4 * n + 2], s[4 * n + 3]} * by);
 }
 __device__ __forceinline__ f32x16 zeros() { return f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}; }
 
@@ -519,33 +522,34 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_ke
 }
 
 // Up to 32 rows for a key head, as for a token each of the sequences of a cache: bound by the bytes of k and v.  Each wave takes its own blocks of 32
-// keys, without barriers: k from memory as a matrix instruction takes it, v by way of the wave's own LDS; both registers are filled with
-// the next block's as soon as they are free.  The waves' sums are joined in LDS, those of the workgroups that share a head by join_kernel.
+// keys, without barriers, by way of registers, which the next block is on its way to while one is worked on, and the wave's own LDS.  Lanes side
+// by side load pieces side by side, past the caches: 48 tokens of 32 / 8 heads of 128, window 4096 XX us, 160 through them, 181 with k as a matrix
+// instruction takes it, two pieces of each row at a time.  The waves' sums are joined in LDS, those of the workgroups that share a head by join_kernel.
 template <typename T, int DP>
 constexpr int kFewWaves = sizeof(T) * DP <= 256 ? 8 : 4;
 template <typename T, int DP>
 __global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4)) void few_kernel(Attn a) {
   using R = Rows<T, DP>;
-  constexpr int W = kFewWaves<T, DP>, kColumns = DP / 32, kBytes = R::bytes(32), kSums = kColumns * 16 * kWave * 4;
-  constexpr int kAll = W * kBytes > kSums * (W / 2) ? W * kBytes : kSums * (W / 2);
-  __shared__ __attribute__((aligned(16))) char lds[kAll];
-  __shared__ float2 tops[W][kWave];
+  constexpr int W = kFewWaves<T, DP>, kColumns = DP / 32, kBytes = R::bytes(32);
+  constexpr int kRow = DP + 4;  // floats of a row of a wave's sums, 16 bytes further in the banks than the row before
+  __shared__ __attribute__((aligned(16))) char lds[W * (2 * kBytes > 32 * kRow * 4 ? 2 * kBytes : 32 * kRow * 4)];
+  __shared__ float2 tops[W][32];
   const int job = in_order(blockIdx.x, gridDim.x), split = job % a.splits, bk = job / a.splits, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
   const Sight s(a, b);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
   const KeyTiles keys(s, 0, a.by_group.divide(a.rows - 1), 32);
   const WaveRows w(a, s, 0);
-  char* const own = lds + wave * kBytes;
+  char *const own_k = lds + 2 * wave * kBytes, *const own_v = own_k + kBytes;
   const int step = a.splits * W;
   int n = split * W + wave;
   u32x4 k[R::kSteps], v[R::kSteps], q[R::kSteps];
   auto fetch = [&](int j0) {
-    const T* row = at<T>(a.k, b, keys.seen(j0 + lane % 32), kv);
 #pragma unroll
-    for (int p = 0; p < R::kSteps; ++p) k[p] = load_of_row<T>(row, 2 * p + half, a.D);
-#pragma unroll
-    for (int p = 0; p < R::kSteps; ++p)  // lanes side by side have pieces side by side
-      v[p] = load_of_row<T>(at<T>(a.v, b, keys.seen(j0 + (p * kWave + lane) / R::P), kv), (p * kWave + lane) % R::P, a.D);
+    for (int p = 0; p < R::kSteps; ++p) {
+      const int row = (p * kWave + lane) / R::P, piece = (p * kWave + lane) % R::P, key = keys.seen(j0 + row);
+      k[p] = load_of_row<T, true>(at<T>(a.k, b, key, kv), piece, a.D);
+      v[p] = load_of_row<T, true>(at<T>(a.v, b, key, kv), piece, a.D);
+    }
   };
   if (n < keys.count) fetch(keys.key(n, 32));
   {
@@ -559,51 +563,64 @@ __global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4))
   Running run;
   for (; n < keys.count; n += step) {
     const int j0 = keys.key(n, 32);
-    f32x16 p[1] = {zeros()};
-#pragma unroll
-    for (int t = 0; t < R::kSteps; ++t) p[0] = multiply<T>(k[t], q[t], p[0]);
 #pragma unroll
     for (int t = 0; t < R::kSteps; ++t) {
-      const int row = (t * kWave + lane) / R::P, piece = (t * kWave + lane) % R::P;
-      *reinterpret_cast<u32x4*>(own + R::place(row) + ((piece ^ R::swizzle(row)) << 4)) = v[t];
+      const int row = (t * kWave + lane) / R::P, to = R::place(row) + (((t * kWave + lane) % R::P ^ R::swizzle(row)) << 4);
+      *reinterpret_cast<u32x4*>(own_k + to) = k[t];
+      *reinterpret_cast<u32x4*>(own_v + to) = v[t];
     }
     if (n + step < keys.count) fetch(keys.key(n + step, 32));
+    wave_lds_fence();
+    f32x16 p[1] = {zeros()};
+#pragma unroll
+    for (int t = 0; t < R::kSteps; ++t) p[0] = multiply<T>(R::rows(own_k, 0, t), q[t], p[0]);
     if (!w.all(s, j0, 32)) w.hide(s, j0, p, kMinusInf);
     run.exponentials(p, a.c, acc);
     const Weights<T> weights(p[0]);
-    wave_lds_fence();
 #pragma unroll
-    for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(own, 0, d, weights, acc[d]);
+    for (int d = 0; d < kColumns; ++d) acc[d] = multiply_columns<T, DP>(own_v, 0, d, weights, acc[d]);
     wave_lds_fence();
   }
-  const bool exists = lane % 32 < a.rows;
   lds_barrier();
+  float* const all_sums = reinterpret_cast<float*>(lds);
+  if (lane % 32 < a.rows) {
+    const float sum = across_rows<32>(run.sum, [](float x, float y) { return x + y; });
+    if (half == 0) tops[wave][lane] = make_float2(run.top, sum);
+    float* const to = all_sums + (wave * 32 + lane) * kRow - half * 32 * kRow + 4 * half;
 #pragma unroll
-  for (int others = W / 2; others > 0; others /= 2) {
-    float* const sums = reinterpret_cast<float*>(lds) + (wave % others) * (kSums / 4) + lane;
-    if (wave >= others && wave < 2 * others && exists) {
-      tops[wave][lane] = make_float2(run.top, run.sum);
+    for (int d = 0; d < kColumns; ++d)
 #pragma unroll
-      for (int d = 0; d < kColumns; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sums[(d * 16 + i) * kWave] = acc[d][i];
-    }
-    lds_barrier();
-    if (wave < others && exists) {
-      const float2 other = tops[wave + others][lane];
-      const float next = fmaxf(run.top, other.x), from = Running::finite(next);
-      run.rescale(next, __builtin_amdgcn_exp2f(run.top - from), acc);
-      const float by = __builtin_amdgcn_exp2f(other.x - from);
-      run.sum = fmaf(other.y, by, run.sum);
-#pragma unroll
-      for (int d = 0; d < kColumns; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[d][i] = fmaf(sums[(d * 16 + i) * kWave], by, acc[d][i]);
-    }
-    lds_barrier();
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(to + d * 32 + 8 * e) = f32x4{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
   }
-  if (wave > 0 || !exists) return;
-  finish<T>(a, run, acc, b, kv, w, split, static_cast<int64_t>(gridDim.x / a.splits) * a.rows);
+  lds_barrier();
+  // four elements of a row a lane
+  const int64_t all_rows = static_cast<int64_t>(gridDim.x / a.splits) * a.rows;
+  for (int at_sum = threadIdx.x; at_sum < a.rows * (DP / 4); at_sum += W * kWave) {
+    const int row = at_sum / (DP / 4), d = at_sum % (DP / 4) * 4;
+    float top = kMinusInf, sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) top = fmaxf(top, tops[i][row].x);
+    const float from = Running::finite(top);
+    f32x4 out = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float by = __builtin_amdgcn_exp2f(tops[i][row].x - from);
+      sum = fmaf(tops[i][row].y, by, sum);
+      out += by * *reinterpret_cast<const f32x4*>(all_sums + (i * 32 + row) * kRow + d);
+    }
+    out *= sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float lse = sum == 0.0f ? kMinusInf : top + __builtin_amdgcn_logf(sum);
+    if (a.splits > 1) {
+      const int64_t at_row = split * all_rows + static_cast<int64_t>(bk) * a.rows + row;
+      if (d == 0) a.partial_lse[at_row] = lse;
+      store_four(a.partial + at_row * a.D, a.D, d, out);
+    } else {
+      const int i = a.by_group.divide(row), head = kv * a.group + row - i * a.group;
+      if (a.lse && d == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + i] = lse * kLn2;
+      store_four(const_cast<T*>(at<T>(a.out, b, i, head)), a.D, d, out);
+    }
+  }
 }
 
 // The parts of a row, each weighted by its sum of exponentials: a wave a row.
