@@ -79,12 +79,13 @@ struct Sight {
 // lanes of a read meet different banks.
 template <typename T, int DP>
 struct Rows {
-  static constexpr int V = Store<T>::kVec, P = DP / V, kPitch = P * 16, kSteps = P / 2, kGap = sizeof(T) == 2 && P >= 16 ? 16 : 0;
-  static_assert(P >= 8, "");
+  // pieces of a row, room for them, a power of two, and matrix instructions that take two of them each
+  static constexpr int V = Store<T>::kVec, P = DP / V, kRoom = P <= 8 ? 8 : P <= 16 ? 16 : P <= 32 ? 32 : 64, kSteps = P / 2;
+  static constexpr int kPitch = kRoom * 16, kGap = sizeof(T) == 2 && kRoom >= 16 ? 16 : 0;
   static constexpr int bytes(int rows) { return rows * kPitch + rows / 4 * kGap; }
   __device__ static __forceinline__ int swizzle(int row) {
     if constexpr (sizeof(T) == 4) return (row >> 2 & 1) << 3 | (row & 3) | (row >> 3 & 1) << 2;
-    else if constexpr (P == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    else if constexpr (kRoom == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
     else return (row & 3) << 2;
   }
   __device__ static __forceinline__ int place(int row) { return row * kPitch + row / 4 * kGap; }
@@ -175,8 +176,8 @@ __device__ __forceinline__ u32x4 load_of_row(const T* row, int piece, int D) {
 template <typename T, int DP, int N>
 struct Staged {
   using R = Rows<T, DP>;
-  static constexpr int kPieces = N * R::P / kThreads;
-  static_assert(N * R::P % kThreads == 0, "whole pieces a lane");
+  static constexpr int kPieces = N * R::kRoom / kThreads;
+  static_assert(N * R::kRoom % kThreads == 0, "whole pieces a lane");
   u32x4 v[kPieces];
   __device__ __forceinline__ explicit Staged(const Heads&) {}
   // of: row -> its elements
@@ -184,7 +185,7 @@ struct Staged {
   __device__ __forceinline__ void load(int D, F&& of) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = i * kThreads + static_cast<int>(threadIdx.x), row = at / R::P, piece = at % R::P ^ R::swizzle(row);
+      const int at = i * kThreads + static_cast<int>(threadIdx.x), row = at / R::kRoom, piece = at % R::kRoom ^ R::swizzle(row);
       v[i] = load_of_row<T>(of(row), piece, D);
     }
   }
@@ -192,45 +193,41 @@ struct Staged {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int at = i * kThreads + static_cast<int>(threadIdx.x);
-      *reinterpret_cast<u32x4*>(lds + R::place(at / R::P) + at % R::P * 16) = v[i];
+      *reinterpret_cast<u32x4*>(lds + R::place(at / R::kRoom) + at % R::kRoom * 16) = v[i];
     }
   }
 };
 
-// Waits until all but the last N loads of the wave have come (and for nothing else).
-template <int N>
-__device__ __forceinline__ void landed() {
-  static_assert(N < 64, "six bits");
-  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xF70);
-}
+// Waits until all of the wave's loads have come (and for nothing else).
+__device__ __forceinline__ void landed() { __builtin_amdgcn_s_waitcnt(0xF70); }
 // N rows of a matrix from memory to LDS without registers: rows that begin at multiples of 16 bytes, D a multiple of a piece.  In assembly
 // because the compiler waits for all such loads before any read of LDS; whoever calls this waits for them.  It has no output, and nothing else
 // here uses m0.  Lanes of pieces behind D load nothing, and what LDS holds there stays.
 template <typename T, int DP, int N>
 struct Direct {
   using R = Rows<T, DP>;
-  static constexpr int kPieces = N * R::P / kThreads;
-  static_assert(R::kGap == 0 || R::P * 4 % kWave == 0 || kWave % (R::P * 4) == 0, "no gap within what a wave loads");
+  static constexpr int kPieces = N * R::kRoom / kThreads;
+  static_assert(R::kGap == 0 || R::kRoom * 4 % kWave == 0 || kWave % (R::kRoom * 4) == 0, "no gap within what a wave loads");
   uint32_t offset[kPieces];  // bytes from the first row
   __device__ __forceinline__ Direct(const Heads& h) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
       offset[i] = static_cast<uint32_t>(row(i)) * static_cast<uint32_t>(h.token * sizeof(T)) + static_cast<uint32_t>(piece(i)) * 16;
   }
-  __device__ static __forceinline__ int row(int i) { return (i * kThreads + static_cast<int>(threadIdx.x)) / R::P; }
+  __device__ static __forceinline__ int row(int i) { return (i * kThreads + static_cast<int>(threadIdx.x)) / R::kRoom; }
   __device__ static __forceinline__ int piece(int i) {
-    return (i * kThreads + static_cast<int>(threadIdx.x)) % R::P ^ R::swizzle(row(i));
+    return (i * kThreads + static_cast<int>(threadIdx.x)) % R::kRoom ^ R::swizzle(row(i));
   }
   __device__ static __forceinline__ uint32_t to(char* lds, int i) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds)) +
-           R::place((i * kThreads + wave * kWave) / R::P) + (i * kThreads + wave * kWave) % R::P * 16;
+           R::place((i * kThreads + wave * kWave) / R::kRoom) + (i * kThreads + wave * kWave) % R::kRoom * 16;
   }
   // first: the first row (uniform)
   __device__ __forceinline__ void load(const T* first, int D, char* lds) const {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
-      if (DP == D || piece(i) * R::V < D)
+      if (R::kRoom * R::V == D || piece(i) * R::V < D)
         asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(offset[i]), "s"(to(lds, i)), "s"(first) : "m0", "memory");
   }
   // of: row -> its elements
@@ -239,7 +236,7 @@ struct Direct {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const T* const p = of(row(i)) + piece(i) * R::V;
-      if (DP == D || piece(i) * R::V < D)
+      if (R::kRoom * R::V == D || piece(i) * R::V < D)
         asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(to(lds, i)) : "m0", "memory");
     }
   }
@@ -303,27 +300,25 @@ struct KeyTiles {
   }
 };
 
-// The tiles of k and v that the rows of a workgroup see, one after the other through BUFS buffers: while one is worked on, the next ones are on
-// their way.  DIRECT: without registers; else there are two buffers.
-template <typename T, int DP, int BK, bool DIRECT, int MOST>
+// The tiles of k and v that the rows of a workgroup see, one after the other through two buffers: while one is worked on, the next is on
+// its way.  DIRECT: without registers.
+template <typename T, int DP, int BK, bool DIRECT>
 struct KeyStream {
-  static constexpr int kBytes = Rows<T, DP>::bytes(BK), BUFS = DIRECT ? MOST : 2;
+  static constexpr int kBytes = Rows<T, DP>::bytes(BK);
   const Attn& a;
   const KeyTiles& keys;
   const T *k, *v;  // of key 0
   char (*lds)[2][kBytes];
   int n0, n1;
   std::conditional_t<DIRECT, Direct<T, DP, BK>, Staged<T, DP, BK>> ks, vs;
-  // Tiles [n0, n1); the first ones are on their way from here on.
+  // Tiles [n0, n1); the first one is on its way from here on.
   __device__ __forceinline__ KeyStream(const Attn& a_, const KeyTiles& keys_, int b, int kv, char (*lds_)[2][kBytes], int n0_, int n1_)
       : a(a_), keys(keys_), k(at<T>(a_.k, b, 0, kv)), v(at<T>(a_.v, b, 0, kv)), lds(lds_), n0(n0_), n1(n1_), ks(a_.k), vs(a_.v) {
     if (DIRECT && a.D < DP) {
-      clear_lds(lds[0][0], 2 * BUFS * kBytes);
+      clear_lds(lds[0][0], 4 * kBytes);
       lds_barrier();
     }
-#pragma unroll
-    for (int i = 0; i < BUFS - 1; ++i)
-      if (n0 + i < n1) fetch(n0 + i, i);
+    if (n0 < n1) fetch(n0, 0);
   }
   __device__ __forceinline__ void fetch(int n, int to) {
     const int j0 = keys.key(n, BK);
@@ -350,17 +345,13 @@ struct KeyStream {
   template <typename F>
   __device__ __forceinline__ void each(F&& work) {
     if (n0 < n1) put(0);
-    int now = 0;
     for (int n = n0; n < n1; ++n) {
-      if constexpr (DIRECT) {  // the tiles behind this one may still be on their way
-        if (BUFS == 2 || n + BUFS - 1 > n1) landed<0>();
-        else landed<(BUFS - 2) * 2 * decltype(ks)::kPieces>();
-      }
-      lds_barrier();  // the tile is there, and the buffer before it has been read
-      if (n + BUFS - 1 < n1) fetch(n + BUFS - 1, now == 0 ? BUFS - 1 : now - 1);
+      const int now = (n - n0) & 1;
+      if constexpr (DIRECT) landed();
+      lds_barrier();  // the tile is there, and the other buffer has been read
+      if (n + 1 < n1) fetch(n + 1, now ^ 1);
       work(keys.key(n, BK), lds[now][0], lds[now][1]);
       if (n + 1 < n1) put(now ^ 1);
-      now = now + 1 == BUFS ? 0 : now + 1;
     }
   }
 };
@@ -470,16 +461,21 @@ __device__ __forceinline__ void finish(const Attn& a, const Running& run, const 
   }
 }
 
-// Waves on a SIMD: two where their registers allow it, one at its matrix instructions while the other is at its exponentials.
+// Waves on a SIMD: two where their registers allow it, one at its matrix instructions while the other is at its exponentials.  The forward of
+// rows of up to 128 bfloat16 with tiles of 32 keys allows three: 8192 tokens of 32 / 8 heads of 128, window 1024 164 us, 178 with tiles of 64
+// and two, 172 with tiles of 32 and two; 16384 with a window of 4096 994, 1000 and 1050 us (968 TFLOP/s).  Two groups of waves held
+// apart by barriers, one at the exponentials while the other is at its products, take 204 and 1148 us.
 template <typename T, int DP, bool DIRECT>
 constexpr int kAtOnce = DIRECT && sizeof(T) * DP <= 256 ? 2 : 1;
+template <typename T, int DP, bool DIRECT>
+constexpr int kForward = DIRECT && sizeof(T) == 2 && DP <= 128 ? 3 : kAtOnce<T, DP, DIRECT>;
 
-template <typename T, int DP, int BK, bool DIRECT, int MOST>
-__global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_kernel(Attn a) {
+template <typename T, int DP, int BK, bool DIRECT>
+__global__ __launch_bounds__(kThreads, (kForward<T, DP, DIRECT>)) void forward_kernel(Attn a) {
   using R = Rows<T, DP>;
-  using Stream = KeyStream<T, DP, BK, DIRECT, MOST>;
+  using Stream = KeyStream<T, DP, BK, DIRECT>;
   constexpr int kBlocks = BK / 32, kColumns = DP / 32;
-  __shared__ __attribute__((aligned(16))) char lds[Stream::BUFS][2][Stream::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds[2][2][Stream::kBytes];
   const int job = in_order(blockIdx.x, gridDim.x), split = job % a.splits, tile = job / a.splits % a.tiles;
   const int bk = job / a.splits / a.tiles, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
   const Sight s(a, b);
@@ -523,7 +519,7 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void forward_ke
 
 // Up to 32 rows for a key head, as for a token each of the sequences of a cache: bound by the bytes of k and v.  Each wave takes its own blocks of 32
 // keys, without barriers, by way of registers, which the next block is on its way to while one is worked on, and the wave's own LDS.  Lanes side
-// by side load pieces side by side, past the caches: 48 tokens of 32 / 8 heads of 128, window 4096 XX us, 160 through them, 181 with k as a matrix
+// by side load pieces side by side, past the caches: 48 tokens of 32 / 8 heads of 128, window 4096 134 us, 160 through them, 181 with k as a matrix
 // instruction takes it, two pieces of each row at a time.  The waves' sums are joined in LDS, those of the workgroups that share a head by join_kernel.
 template <typename T, int DP>
 constexpr int kFewWaves = sizeof(T) * DP <= 256 ? 8 : 4;
@@ -653,12 +649,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Attn a, int64_t all) {
 }
 
 // ---- backward by rows: delta and dq ---------------------------------------------------------------------------------------
-template <typename T, int DP, int BK, bool DIRECT, int MOST>
+template <typename T, int DP, int BK, bool DIRECT>
 __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void rows_kernel(Attn a) {
   using R = Rows<T, DP>;
-  using Stream = KeyStream<T, DP, BK, DIRECT, MOST>;
+  using Stream = KeyStream<T, DP, BK, DIRECT>;
   constexpr int kBlocks = BK / 32, kColumns = DP / 32;
-  __shared__ __attribute__((aligned(16))) char lds[Stream::BUFS][2][Stream::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds[2][2][Stream::kBytes];
   const int job = in_order(blockIdx.x, gridDim.x), tile = job % a.tiles;
   const int bk = job / a.tiles, b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
   const Sight s(a, b);
@@ -728,9 +724,6 @@ struct KeyJobs {
   int64_t sink_jobs;
   float *partial, *sink_partial;    // [job][2][kRows][D], where there is more than one part
 };
-#ifndef TEMPO_KEYS
-#define TEMPO_KEYS kAtOnce<T, DP, DIRECT>
-#endif
 enum Wanted { kBoth, kOnlyV, kOnlyK };
 // v of the workgroup's keys in LDS, not in registers: with it there a wave needs more than the 256 registers that let two run on a SIMD
 // (rows of 128), or than there are (of 256).
@@ -740,7 +733,7 @@ template <typename T, int DP>
 constexpr int kQueries = sizeof(T) == 2 && DP == 64 ? 64 : 32;  // of a block
 
 template <typename T, int DP, Wanted WANTED, bool DIRECT>
-__global__ __launch_bounds__(kThreads, (TEMPO_KEYS)) void keys_kernel(Attn a, KeyJobs jobs) {
+__global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void keys_kernel(Attn a, KeyJobs jobs) {
   using R = Rows<T, DP>;
   constexpr int BQ = kQueries<T, DP>, kBytes = R::bytes(BQ), kColumns = DP / 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][kBytes];
@@ -849,7 +842,7 @@ __global__ __launch_bounds__(kThreads, (TEMPO_KEYS)) void keys_kernel(Attn a, Ke
   }
   for (int u = u0; u < u1; ++u) {
     const int now = (u - u0) & 1, i0 = block.i;
-    if constexpr (DIRECT) landed<0>();
+    if constexpr (DIRECT) landed();
     lds_barrier();  // the block is there, and the other buffer has been read
     block = following(block);
     if (u + 1 < u1) fetch(block, now ^ 1);
@@ -935,27 +928,11 @@ __global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, const float
   T* const to = const_cast<T*>(at<T>(h, b, key, kv));
   for (int d = lane; d < a.D; d += kWave) {
     float sum = 0.0f;
+#pragma unroll 8
     for (int p = 0; p < parts; ++p) sum += partial[(((of_tile * parts + p) * 2 + of_v) * kRows + in_tile) * a.D + d];
     Store<T>::store1(to + d, sum);
   }
 }
-
-#ifndef FEWB
-#define FEWB 4
-#endif
-#ifndef FEWC
-#define FEWC 12
-#endif
-#ifndef KT
-#define KT 64
-#define KB 3
-#define KT2 64
-#define KB2 2
-#endif
-template <typename T, int DP>
-constexpr int key_tile = sizeof(T) * DP == 128 ? KT : sizeof(T) * DP <= 256 ? KT2 : 32;
-template <typename T, int DP>
-constexpr int key_buffers = sizeof(T) * DP == 128 ? KB : sizeof(T) == 2 && DP == 128 ? KB2 : 2;
 
 // ---- plans ----------------------------------------------------------------------------------------------------------------
 int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
@@ -970,7 +947,7 @@ int forward_splits(const WindowCall& c, tempo_dtype dt) {
   const int64_t span = std::min(c.Sk, c.window + c.Sq) + std::min(c.sinks, c.Sk), most = std::max<int64_t>(up(span, 128), 1);
   if (blocks > 0 && few(c, dt)) {
     const int64_t waves = c.D * (dt == TEMPO_F32 ? 4 : 2) <= 256 ? 8 : 4;
-    return static_cast<int>(std::max<int64_t>(1, std::min({up(span, 32 * waves * FEWB), up(FEWC * compute_units() / 4, blocks), int64_t{64}})));
+    return static_cast<int>(std::max<int64_t>(1, std::min({up(span, 32 * waves * 4), up(3 * compute_units(), blocks), int64_t{64}})));
   }
   if (blocks == 0 || blocks >= compute_units()) return 1;
   return static_cast<int>(std::min<int64_t>(std::min<int64_t>(most, 64), up(2 * compute_units(), blocks)));
@@ -984,7 +961,8 @@ KeyPlan key_plan(const WindowCall& c) {
   const int64_t group = c.heads / c.kv_heads, bk = c.B * c.kv_heads, tiles = up(c.Sk, kRows);
   const int64_t sink_tiles = std::min(tiles, up(c.sinks, kRows)), others = tiles - sink_tiles;
   const int64_t span = up(std::min(c.Sq, c.window + kRows), 32) * group, all = up(c.Sq, 32) * group, cus = compute_units();
-  const int64_t want = up(2 * cus, std::max<int64_t>(bk * tiles, 1));
+  // Workgroups for each compute unit: 1.5, so that the parts' sums cost less than an even end is worth.
+  const int64_t want = up(3 * cus / 2, std::max<int64_t>(bk * tiles, 1));
   p.jobs.tiles = static_cast<int>(tiles);
   p.jobs.sink_tiles = static_cast<int>(sink_tiles);
   p.jobs.parts = static_cast<int>(std::max<int64_t>(1, std::min({want, up(span, 4), int64_t{64}})));
@@ -1022,6 +1000,7 @@ Attn attn_of(const WindowCall& c) {
 template <typename F>
 tempo_status with_width(int64_t D, F&& f) {
   if (D <= 64) return f(std::integral_constant<int, 64>{});
+  if (D <= 96) return f(std::integral_constant<int, 96>{});
   if (D <= 128) return f(std::integral_constant<int, 128>{});
   return f(std::integral_constant<int, 256>{});
 }
@@ -1084,7 +1063,7 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
   return with_type(dt, [&](auto type) {
     using T = decltype(type);
     const tempo_status s = with_width(c.D, [&](auto width) {
-      constexpr int DP = decltype(width)::value, BK = key_tile<T, DP>, BUFS = key_buffers<T, DP>;
+      constexpr int DP = decltype(width)::value, BK = sizeof(T) == 4 && DP == 64 ? 64 : 32;
       if constexpr (sizeof(T) * DP <= 512) {
         if (few(c, dt)) {
           hipLaunchKernelGGL((few_kernel<T, DP>), dim3(static_cast<uint32_t>(c.B * c.kv_heads * a.splits)), dim3(kFewWaves<T, DP> * kWave), 0, st, a);
@@ -1092,7 +1071,7 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
         }
       }
       return either(direct(c, dt, {c.k, c.v}), [&](auto straight) {
-        return launch(forward_kernel<T, DP, BK, decltype(straight)::value, BUFS>, blocks, st, a);
+        return launch(forward_kernel<T, DP, BK, decltype(straight)::value>, blocks, st, a);
       });
     });
     if (s != TEMPO_OK || a.splits == 1) return s;
@@ -1111,9 +1090,9 @@ tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStre
   return with_type(dt, [&](auto type) {
     using T = decltype(type);
     tempo_status s = with_width(c.D, [&](auto width) {
-      constexpr int DP = decltype(width)::value, BK = key_tile<T, DP>, BUFS = key_buffers<T, DP>;
+      constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 ? 64 : 32;
       const tempo_status r = either(direct(c, dt, {c.k, c.v}), [&](auto straight) {
-        return launch(rows_kernel<T, DP, BK, decltype(straight)::value, BUFS>, c.B * c.kv_heads * a.tiles, st, a);
+        return launch(rows_kernel<T, DP, BK, decltype(straight)::value>, c.B * c.kv_heads * a.tiles, st, a);
       });
       if (r != TEMPO_OK) return r;
       return either(direct(c, dt, {c.q, c.dout}), [&](auto straight) {
