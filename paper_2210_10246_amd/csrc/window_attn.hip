@@ -263,6 +263,11 @@ __device__ __forceinline__ void store_four(T* row, int D, int d, f32x4 v) {
       if (e < left) Store<T>::store1(row + d + e, v[e]);
   }
 }
+// Four neighbouring floats of a row of D; zeros behind its end.
+__device__ __forceinline__ f32x4 load_four(const float* row, int D, int d) {
+  if (D - d >= 4) return *reinterpret_cast<const f32x4_any*>(row + d);
+  return f32x4{row[d], d + 1 < D ? row[d + 1] : 0.0f, d + 2 < D ? row[d + 2] : 0.0f, 0.0f};
+}
 // A lane's sums of column block `block`: 8 (i / 4) + 4 (lane / 32) + i % 4 are four neighbours each.
 template <typename T>
 __device__ __forceinline__ void store_sums(T* row, int D, int block, const f32x16& s, float by) {
@@ -619,33 +624,28 @@ __global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4))
   }
 }
 
-// The parts of a row, each weighted by its sum of exponentials: a wave a row.
+// The parts of a row, each weighted by its sum of exponentials: 16 lanes a row.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void join_kernel(Attn a, int64_t all) {
-  const int64_t at_row = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.x / kWave;
+  const int64_t at_row = static_cast<int64_t>(blockIdx.x) * (kThreads / 16) + threadIdx.x / 16;
   if (at_row >= all) return;
-  const int lane = threadIdx.x % kWave;
-  float top = kMinusInf;
+  float top = kMinusInf, sum = 0.0f;
   for (int p = 0; p < a.splits; ++p) top = fmaxf(top, a.partial_lse[p * all + at_row]);
-  const float from = top == kMinusInf ? 0.0f : top;
-  float sum = 0.0f, out[4] = {0, 0, 0, 0};
-  for (int p = 0; p < a.splits; ++p) {
-    const float by = __builtin_amdgcn_exp2f(a.partial_lse[p * all + at_row] - from);
-    sum += by;
-    const float* o = a.partial + (p * all + at_row) * a.D;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (lane + e * kWave < a.D) out[e] = fmaf(by, o[lane + e * kWave], out[e]);
-  }
+  const float from = Running::finite(top);
+  for (int p = 0; p < a.splits; ++p) sum += __builtin_amdgcn_exp2f(a.partial_lse[p * all + at_row] - from);
+  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
   const int bk = static_cast<int>(at_row / a.rows), row = static_cast<int>(at_row - static_cast<int64_t>(bk) * a.rows);
   const int b = bk / a.kv_heads, i = a.by_group.divide(row), head = (bk - b * a.kv_heads) * a.group + row - i * a.group;
-  if (a.lse && lane == 0)
+  if (a.lse && threadIdx.x % 16 == 0)
     a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + i] = sum == 0.0f ? kMinusInf : (from + __builtin_amdgcn_logf(sum)) * kLn2;
-  const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
   T* const to = const_cast<T*>(at<T>(a.out, b, i, head));
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (lane + e * kWave < a.D) Store<T>::store1(to + lane + e * kWave, out[e] * by);
+  for (int d = threadIdx.x % 16 * 4; d < a.D; d += 64) {
+    f32x4 out = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int p = 0; p < a.splits; ++p)
+      out += __builtin_amdgcn_exp2f(a.partial_lse[p * all + at_row] - from) * load_four(a.partial + (p * all + at_row) * a.D, a.D, d);
+    store_four(to, a.D, d, out * by);
+  }
 }
 
 // ---- backward by rows: delta and dq ---------------------------------------------------------------------------------------
@@ -716,62 +716,70 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void rows_kerne
 }
 
 // ---- backward by keys: dk and dv ------------------------------------------------------------------------------------------
-// The queries that see a tile of keys are those of its window, or all behind it where one of its keys is one of the first; they are taken
-// in blocks of BQ of one head after the other, in several parts where that is many, whose sums are joined in their order.
+// The queries that see a tile of keys in their window, taken in blocks of BQ of one head after the other.  Those further on see only the first
+// keys: jobs of their own take them for 32 of these keys at a time, the blocks dealt out to the four waves.  Where there is more than one sum for
+// a key (parts of a tile's blocks, what is further on), the sums are joined in their order.
 struct KeyJobs {
-  int tiles, sink_tiles;            // of kRows keys; the first sink_tiles have first keys
-  int parts, sink_parts;            // of a tile's blocks of queries
-  int64_t sink_jobs;
-  float *partial, *sink_partial;    // [job][2][kRows][D], where there is more than one part
+  int tiles, parts;                // of kRows keys; parts of a tile's blocks of queries
+  int sink_tiles;                  // tiles that have first keys whose sums go on
+  int strips, further_parts;       // of 32 first keys
+  int64_t further_jobs;
+  float *partial, *further;        // [job][2][kRows][D] (one part: of the sink tiles alone), [job][4][2][32][D]
 };
 enum Wanted { kBoth, kOnlyV, kOnlyK };
-// v of the workgroup's keys in LDS, not in registers: with it there a wave needs more than the 256 registers that let two run on a SIMD
-// (rows of 128), or than there are (of 256).
-template <typename T, int DP>
-constexpr bool kValuesInLds = sizeof(T) == 2 && DP >= 128;
+// bfloat16: v of the workgroup's keys in LDS, not in registers.  There a wave of rows of 128 would need more than the 256 that let two run on a
+// SIMD (32768 tokens, window 4096 7.0 ms, and 4.2 in LDS), one of 64 more than the 168 that let three.
+template <typename T>
+constexpr bool kValuesInLds = sizeof(T) == 2;
+template <typename T, int DP, bool DIRECT>
+constexpr int kKeysAtOnce = DIRECT && sizeof(T) == 2 && DP == 64 ? 3 : kAtOnce<T, DP, DIRECT>;
 template <typename T, int DP>
 constexpr int kQueries = sizeof(T) == 2 && DP == 64 ? 64 : 32;  // of a block
 
 template <typename T, int DP, Wanted WANTED, bool DIRECT>
-__global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void keys_kernel(Attn a, KeyJobs jobs) {
+__global__ __launch_bounds__(kThreads, (kKeysAtOnce<T, DP, DIRECT>)) void keys_kernel(Attn a, KeyJobs jobs) {
   using R = Rows<T, DP>;
   constexpr int BQ = kQueries<T, DP>, kBytes = R::bytes(BQ), kColumns = DP / 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][kBytes];
   __shared__ __attribute__((aligned(16))) float stats[2][2][BQ];  // lse of base 2, delta
-  constexpr bool kK = WANTED != kOnlyV, kV = WANTED != kOnlyK, kInLds = kK && kValuesInLds<T, DP>;
+  constexpr bool kK = WANTED != kOnlyV, kV = WANTED != kOnlyK, kInLds = kK && kValuesInLds<T>;
   __shared__ __attribute__((aligned(16))) char values[kInLds ? R::bytes(kRows) : 16];
   int64_t job = blockIdx.x;
-  const bool of_sinks = job < jobs.sink_jobs;
-  if (!of_sinks) job -= jobs.sink_jobs;
-  const int parts = of_sinks ? jobs.sink_parts : jobs.parts;
-  const int tiles = of_sinks ? jobs.sink_tiles : jobs.tiles - jobs.sink_tiles;
-  if (!of_sinks) job = in_order(static_cast<int>(job), static_cast<int>(gridDim.x - jobs.sink_jobs));
-  const int part = static_cast<int>(job % parts), tile = static_cast<int>(job / parts % tiles) + (of_sinks ? 0 : jobs.sink_tiles);
+  const bool further = job < jobs.further_jobs;
+  if (!further) job = in_order(static_cast<int>(job - jobs.further_jobs), static_cast<int>(gridDim.x - jobs.further_jobs));
+  const int parts = further ? jobs.further_parts : jobs.parts, tiles = further ? jobs.strips : jobs.tiles;
+  const int part = static_cast<int>(job % parts), tile = static_cast<int>(job / parts % tiles);
   const int bk = static_cast<int>(job / parts / tiles), b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
   const Sight s(a, b);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
-  const int key0 = tile * kRows, wave_key = key0 + wave * 32, key = wave_key + lane % 32;
-  // Queries [from, to) see key j.
+  const int key0 = tile * (further ? 32 : kRows), wave_key = key0 + (further ? 0 : wave * 32), key = wave_key + lane % 32;
+  const int wave_last = wave_key + 31;
+  // Queries [from, to) see key j in their window; those of [to, Sq) see it if it is one of the first.
   auto from = [&](int j) {
     const int64_t i = j - s.start;
     return j >= s.keys || i >= a.Sq ? a.Sq : i > 0 ? static_cast<int>(i) : 0;
   };
   auto to = [&](int j) {
-    if (j >= s.keys) return 0;
-    const int64_t i = j < s.sinks ? int64_t{a.Sq} : j + int64_t{s.window} - s.start;
-    return i >= a.Sq ? a.Sq : i > 0 ? static_cast<int>(i) : 0;
+    const int64_t i = j + int64_t{s.window} - s.start;
+    return j >= s.keys || i <= 0 ? 0 : i < a.Sq ? static_cast<int>(i) : a.Sq;
   };
-  const int tile_last = min(key0 + kRows, s.keys) - 1;
-  const int first = from(key0), end = key0 >= s.keys ? 0 : key0 < s.sinks ? a.Sq : to(tile_last);
+  auto beyond = [&](int j) { return j < s.sinks ? max(from(j), to(j)) : a.Sq; };
+  // The job's queries, those that see some key of the wave, those that see all, and the lane's.
+  int first, end, any_from, any_to, all_from, all_to, key_from, key_to;
+  if (further) {
+    first = any_from = beyond(key0), all_from = beyond(wave_last), key_from = beyond(key);
+    end = any_to = all_to = key_to = a.Sq;
+  } else {
+    const int tile_last = min(key0 + kRows, s.keys) - 1;
+    first = from(key0), end = key0 < s.keys ? to(tile_last) : 0;
+    any_from = from(wave_key), any_to = wave_key < s.keys ? to(min(wave_last, s.keys - 1)) : 0;
+    all_from = from(wave_last), all_to = wave_last < s.keys ? to(wave_key) : 0;
+    key_from = from(key), key_to = to(key);
+  }
+  const uint32_t key_span = static_cast<uint32_t>(max(key_to - key_from, 0));
   const int blocks = first < end ? (end - first + BQ - 1) / BQ : 0;  // of a head
   const int each = static_cast<int>((static_cast<int64_t>(blocks) * a.group + parts - 1) / parts);
   const int u0 = min(part * each, blocks * a.group), u1 = min(u0 + each, blocks * a.group);
-  // The wave's keys: all of a block of queries see them, or none does, or each is looked at.
-  const int wave_last = wave_key + 31;
-  const int any_from = from(wave_key), any_to = wave_key < s.sinks ? (wave_key < s.keys ? a.Sq : 0) : to(min(wave_last, s.keys - 1));
-  const int all_from = from(wave_last), all_to = wave_last < s.keys ? to(wave_last < s.sinks ? wave_key : max(wave_key, s.sinks)) : 0;
-  const int key_from = from(key);
-  const uint32_t key_span = static_cast<uint32_t>(max(to(key) - key_from, 0));
   u32x4 k[R::kSteps], v[kInLds ? 1 : R::kSteps];
   {
     const int there = min(key, a.Sk - 1);
@@ -849,7 +857,7 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void keys_kerne
 #pragma unroll
     for (int rb = 0; rb < BQ; rb += 32) {
       const int i1 = i0 + rb;
-      if (i1 >= any_to || i1 + 32 <= any_from) continue;
+      if (i1 >= any_to || i1 + 32 <= any_from || (further && (u * (BQ / 32) + rb / 32) % kWaves != wave)) continue;
       const bool all = i1 >= all_from && i1 + 32 <= all_to;
       f32x16 p = zeros(), dp = zeros();
 #pragma unroll
@@ -889,16 +897,18 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void keys_kerne
     }
     if (u + 1 < u1) put(now ^ 1);
   }
-  if (parts > 1) {
-    float* const into = (of_sinks ? jobs.sink_partial : jobs.partial) +
-                        (job * 2 * kRows + wave * 32 + lane % 32) * static_cast<int64_t>(a.D);
+  if (further || parts > 1 || tile < jobs.sink_tiles) {
+    const int64_t slot = parts > 1 ? job : static_cast<int64_t>(bk) * jobs.sink_tiles + tile;
+    const int rows = further ? 32 : kRows;  // keys of a sum
+    float* const into = (further ? jobs.further + (job * kWaves + wave) * 2 * 32 * a.D : jobs.partial + (slot * 2 * kRows + wave * 32) * a.D) +
+                        lane % 32 * a.D;
     if constexpr (kK) {
 #pragma unroll
       for (int d = 0; d < kColumns; ++d) store_sums(into, a.D, d, dk[d], a.scale);
     }
     if constexpr (kV) {
 #pragma unroll
-      for (int d = 0; d < kColumns; ++d) store_sums(into + static_cast<int64_t>(kRows) * a.D, a.D, d, dv[d], 1.0f);
+      for (int d = 0; d < kColumns; ++d) store_sums(into + static_cast<int64_t>(rows) * a.D, a.D, d, dv[d], 1.0f);
     }
   } else if (key < a.Sk) {
     if constexpr (kK) {
@@ -914,23 +924,38 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void keys_kerne
   }
 }
 
-// The parts of dk and dv of a key, in their order: a wave a key and gradient.  tiles0: the first tile of these.
+// sum += four floats of each of `count` rows, N of them on their way at a time.
+template <int N>
+__device__ __forceinline__ void add_parts(f32x4& sum, const float* p, int64_t step, int count, int left) {
+  for (int i = 0; i < count; i += N) {
+    f32x4 v[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = load_four(p + min(i + n, count - 1) * step, left, 0);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (i + n < count) sum += v[n];
+  }
+}
+// The sums for a key, in their order: 32 lanes a key and gradient.  tiles: all where they have parts, else those with first keys.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, const float* partial, int parts, int tiles0, int tiles, int64_t all) {
-  const int64_t n = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.x / kWave;  // (bk, tile, gradient, key)
+__global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, KeyJobs jobs, int tiles, int64_t all) {
+  const int64_t n = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32;  // (bk, tile, gradient, key)
   if (n >= all) return;
-  const int lane = threadIdx.x % kWave, in_tile = static_cast<int>(n % kRows), of_v = static_cast<int>(n / kRows % 2);
+  const int in_tile = static_cast<int>(n % kRows), of_v = static_cast<int>(n / kRows % 2);
   const int64_t of_tile = n / (2 * kRows);
   const int tile = static_cast<int>(of_tile % tiles), bk = static_cast<int>(of_tile / tiles), b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
-  const int key = (tiles0 + tile) * kRows + in_tile;
+  const int key = tile * kRows + in_tile, strip = key / 32;
   if (key >= a.Sk) return;
   const Heads& h = of_v ? a.dv : a.dk;
   T* const to = const_cast<T*>(at<T>(h, b, key, kv));
-  for (int d = lane; d < a.D; d += kWave) {
-    float sum = 0.0f;
-#pragma unroll 8
-    for (int p = 0; p < parts; ++p) sum += partial[(((of_tile * parts + p) * 2 + of_v) * kRows + in_tile) * a.D + d];
-    Store<T>::store1(to + d, sum);
+  const float* const parts = jobs.partial + ((of_tile * jobs.parts * 2 + of_v) * kRows + in_tile) * a.D;
+  const float* const further = jobs.further + (((static_cast<int64_t>(bk) * jobs.strips + strip) * jobs.further_parts * kWaves * 2 + of_v) * 32 + key % 32) * a.D;
+  const int further_sums = strip < jobs.strips ? jobs.further_parts * kWaves : 0;
+  for (int d = threadIdx.x % 32 * 4; d < a.D; d += 128) {
+    f32x4 sum = {0, 0, 0, 0};
+    add_parts<4>(sum, parts + d, int64_t{2} * kRows * a.D, jobs.parts, a.D - d);
+    add_parts<8>(sum, further + d, int64_t{2} * 32 * a.D, further_sums, a.D - d);
+    store_four(to, a.D, d, sum);
   }
 }
 
@@ -954,25 +979,27 @@ int forward_splits(const WindowCall& c, tempo_dtype dt) {
 }
 struct KeyPlan {
   KeyJobs jobs;
-  int64_t blocks, partial_floats, sink_floats;
+  int64_t blocks, partial_floats, further_floats;
 };
 KeyPlan key_plan(const WindowCall& c) {
   KeyPlan p{};
-  const int64_t group = c.heads / c.kv_heads, bk = c.B * c.kv_heads, tiles = up(c.Sk, kRows);
-  const int64_t sink_tiles = std::min(tiles, up(c.sinks, kRows)), others = tiles - sink_tiles;
-  const int64_t span = up(std::min(c.Sq, c.window + kRows), 32) * group, all = up(c.Sq, 32) * group, cus = compute_units();
+  const int64_t group = c.heads / c.kv_heads, bk = c.B * c.kv_heads, tiles = up(c.Sk, kRows), cus = compute_units();
+  const int64_t span = up(std::min(c.Sq, c.window + kRows), 32) * group, all = up(c.Sq, 32) * group;  // blocks of queries
   // Workgroups for each compute unit: 1.5, so that the parts' sums cost less than an even end is worth.
   const int64_t want = up(3 * cus / 2, std::max<int64_t>(bk * tiles, 1));
   p.jobs.tiles = static_cast<int>(tiles);
-  p.jobs.sink_tiles = static_cast<int>(sink_tiles);
   p.jobs.parts = static_cast<int>(std::max<int64_t>(1, std::min({want, up(span, 4), int64_t{64}})));
-  const int64_t sink_want = std::min(up(all, std::max<int64_t>(up(span, p.jobs.parts), 1)), up(4 * cus, std::max<int64_t>(bk * sink_tiles, 1)));
-  p.jobs.sink_parts = static_cast<int>(std::max<int64_t>(1, sink_want));
-  p.jobs.sink_jobs = bk * sink_tiles * p.jobs.sink_parts;
-  const int64_t other_jobs = bk * others * p.jobs.parts;
-  p.blocks = p.jobs.sink_jobs + other_jobs;
-  p.sink_floats = p.jobs.sink_parts > 1 ? p.jobs.sink_jobs * 2 * kRows * c.D : 0;
-  p.partial_floats = p.jobs.parts > 1 ? other_jobs * 2 * kRows * c.D : 0;
+  // Without positions of the caller's the last query stands at the last key: none is further on than a window that holds all keys.
+  if (c.sinks > 0 && c.Sq > 0 && (c.query_start || c.window < c.Sk)) {
+    p.jobs.strips = static_cast<int>(up(std::min(c.sinks, c.Sk), 32));
+    p.jobs.sink_tiles = static_cast<int>(up(p.jobs.strips, kWaves));
+    const int64_t part = 2 * std::max<int64_t>(up(span, p.jobs.parts), 1);  // two of a wave's blocks for one of the others'
+    p.jobs.further_parts = static_cast<int>(std::max<int64_t>(1, std::min(up(all, part), up(4 * cus, std::max<int64_t>(bk * p.jobs.strips, 1)))));
+  }
+  p.jobs.further_jobs = bk * p.jobs.strips * p.jobs.further_parts;
+  p.blocks = p.jobs.further_jobs + bk * tiles * p.jobs.parts;
+  p.partial_floats = bk * (p.jobs.parts > 1 ? tiles * p.jobs.parts : p.jobs.sink_tiles) * 2 * kRows * c.D;
+  p.further_floats = p.jobs.further_jobs * kWaves * 2 * 32 * c.D;
   return p;
 }
 
@@ -1046,8 +1073,11 @@ size_t window_attn_workspace_bytes(const WindowCall& c, tempo_dtype dt, bool bac
     const int splits = forward_splits(c, dt);
     return splits > 1 ? static_cast<size_t>(splits) * rows * (c.D + 1) * sizeof(float) : 0;
   }
-  const KeyPlan p = key_plan(c);
-  return static_cast<size_t>(up(2 * rows, 4) * 4 + p.sink_floats + p.partial_floats) * sizeof(float);
+  WindowCall any = c;  // with positions of the caller's there may be more to do
+  const int32_t position = 0;
+  any.query_start = &position;
+  const KeyPlan p = key_plan(any);
+  return static_cast<size_t>(up(2 * rows, 4) * 4 + p.partial_floats + p.further_floats) * sizeof(float);
 }
 
 tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStream_t st) {
@@ -1075,7 +1105,7 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
       });
     });
     if (s != TEMPO_OK || a.splits == 1) return s;
-    return launch(join_kernel<T>, up(all, kWaves), st, a, all);
+    return launch(join_kernel<T>, up(all, kThreads / 16), st, a, all);
   });
 }
 
@@ -1085,12 +1115,12 @@ tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStre
   a.stats = static_cast<float*>(c.workspace);
   a.stat_rows = c.B * c.heads * c.Sq;
   KeyPlan p = key_plan(c);
-  p.jobs.sink_partial = a.stats + up(2 * a.stat_rows, 4) * 4;
-  p.jobs.partial = p.jobs.sink_partial + p.sink_floats;
+  p.jobs.partial = a.stats + up(2 * a.stat_rows, 4) * 4;
+  p.jobs.further = p.jobs.partial + p.partial_floats;
   return with_type(dt, [&](auto type) {
     using T = decltype(type);
     tempo_status s = with_width(c.D, [&](auto width) {
-      constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 ? 64 : 32;
+      constexpr int DP = decltype(width)::value, BK = sizeof(T) * DP <= 256 && sizeof(T) * DP > 128 ? 64 : 32;
       const tempo_status r = either(direct(c, dt, {c.k, c.v}), [&](auto straight) {
         return launch(rows_kernel<T, DP, BK, decltype(straight)::value>, c.B * c.kv_heads * a.tiles, st, a);
       });
@@ -1105,13 +1135,9 @@ tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStre
         }
       });
     });
-    const int64_t each = c.B * c.kv_heads * 2 * kRows;
-    auto join = [&](const float* partial, int parts, int tiles0, int tiles) {
-      if (s != TEMPO_OK || parts <= 1 || tiles == 0) return;
-      s = launch(join_keys_kernel<T>, up(each * tiles, kWaves), st, a, partial, parts, tiles0, tiles, each * tiles);
-    };
-    join(p.jobs.sink_partial, p.jobs.sink_parts, 0, p.jobs.sink_tiles);
-    join(p.jobs.partial, p.jobs.parts, p.jobs.sink_tiles, p.jobs.tiles - p.jobs.sink_tiles);
+    const int tiles = p.jobs.parts > 1 ? p.jobs.tiles : p.jobs.sink_tiles;
+    const int64_t keys = c.B * c.kv_heads * 2 * kRows * tiles;
+    if (s == TEMPO_OK && keys > 0) s = launch(join_keys_kernel<T>, up(keys, kThreads / 32), st, a, p.jobs, tiles, keys);
     return s;
   });
 }
