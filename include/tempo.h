@@ -282,7 +282,7 @@ TEMPO_API tempo_status tempo_rotary_axes_bwd(const tempo_rotary_heads* dq, const
  *   gate [groups,M] in (f32), for N / groups rows each (a sequence; 1: for all); NULL: ones (groups is 1 then, whatever it says).
  *   stats [N,2] (f32) mean and rstd of each row: out of the forward, where it may be NULL, and in to the backward.
  *   Parameters need only the alignment of a float, stats that of two.
- *   INVALID_ARG also: groups < 1 or no divisor of N, eps < 0.  UNSUPPORTED also: more than 2^22 groups beside rows to match.
+ *   INVALID_ARG also: groups < 1 or no divisor of N, eps < 0.  UNSUPPORTED also: 2^22 groups and more.
  */
 typedef enum { TEMPO_NORM_RMS = 0, TEMPO_NORM_LAYER = 1 } tempo_norm_kind;
 typedef struct {
@@ -364,10 +364,10 @@ TEMPO_API tempo_status tempo_glu_bwd(const void* dh, const void* gu, const void*
  *   fixed order: the same call gives the same bits.
  *   workspace: device memory of at least tempo_window_attn_fwd/bwd_workspace_bytes() bytes, 16-byte aligned (NULL if that is 0); calls that
  *   may run at the same time need one each.
- *   INVALID_ARG also: kv_heads < 1 (with heads > 0), heads no multiple of it, D < 1, window < 1, sinks < 0, a scale that is not positive
- *   and finite, a negative stride, a stride of an output that is 0 where there are two elements along it.
- *   UNSUPPORTED also: D > 256; more than 2^31 - 129 rows of a key head (Sq heads / kv_heads) or 2^32 queries of all heads; more than 2^23 tiles of 128 rows,
- *   or 2^22 of 128 keys, in all.
+ *   INVALID_ARG also: kv_heads < 1 (with heads > 0), heads no multiple of it, D < 1, window < 1, sinks < 0, a scale outside
+ *   [2^-126, 2^127], a negative stride, a stride of an output that is 0 where there are two elements along it.
+ *   UNSUPPORTED also: D > 256; more than 2^32 queries of all heads; more than 2^22 tiles of 128 rows (Sq heads / kv_heads of a key
+ *   head) or of 128 keys in all, or 2^19 of 128 keys that hold some of the first `sinks`.
  */
 typedef struct {
   const void* p; /* written through if it is an output */

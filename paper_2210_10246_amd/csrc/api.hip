@@ -550,7 +550,8 @@ size_t tempo_window_attn_bwd_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, 
   return window_attn_bytes(c, dt, true);
 }
 
-static bool scale_ok(float scale) { return scale > 0.0f && scale <= 3.402823466e+38f; }  // false for NaN
+// Normal, as scale log2(e) is too (false for NaN).
+static bool scale_ok(float scale) { return scale >= 1.17549435e-38f && scale <= 1.70141183e+38f; }
 
 tempo_status tempo_window_attn_fwd(const tempo_attn_heads* q, const tempo_attn_heads* k, const tempo_attn_heads* v,
                                    const tempo_attn_heads* out, float* lse, const int32_t* key_len, const int32_t* query_start,

@@ -542,7 +542,7 @@ bool with_shape(const Shape& s, int64_t M, F&& f) {
 
 bool residual_norm_takes(const ResidualCall& c, tempo_dtype dt) {
   const Plan p = plan_of(c, dt, false);  // more parts than backward
-  return p.groups * p.parts <= int64_t{1} << 22;  // launches of less than 2^32 lanes
+  return p.groups * p.parts < int64_t{1} << 22;  // launches of less than 2^32 lanes
 }
 
 size_t residual_norm_workspace_bytes(const ResidualCall& c, tempo_dtype dt) {

@@ -1058,13 +1058,21 @@ tempo_status launch(K kernel, int64_t blocks, hipStream_t st, const Args&... arg
 
 }  // namespace
 
+// The call as if it gave positions: there may be more to do then.
+static WindowCall with_positions(WindowCall c) {
+  static const int32_t any = 0;
+  c.query_start = &any;
+  return c;
+}
+
 // Launches of less than 2^32 lanes, and numbers of jobs that an int holds.
 bool window_attn_takes(const WindowCall& c) {
-  constexpr int64_t most = int64_t{1} << 23;
+  constexpr int64_t most = int64_t{1} << 22;
   const int64_t bk = c.B * c.kv_heads, rows = c.Sq * (c.heads / c.kv_heads);
-  if (c.D > 256 || rows > INT32_MAX - kRows || up(rows, kRows) * bk > most || up(c.Sk, kRows) * bk > most / 2 || bk * rows > int64_t{1} << 32)
+  if (c.D > 256 || rows > INT32_MAX - kRows || up(rows, kRows) * bk > most || up(c.Sk, kRows) * bk > most || bk * rows > int64_t{1} << 32)
     return false;
-  return key_plan(c).blocks <= most;
+  const KeyPlan p = key_plan(with_positions(c));
+  return p.blocks <= 2 * most && bk * p.jobs.sink_tiles <= most / 8;
 }
 
 size_t window_attn_workspace_bytes(const WindowCall& c, tempo_dtype dt, bool back) {
@@ -1073,10 +1081,7 @@ size_t window_attn_workspace_bytes(const WindowCall& c, tempo_dtype dt, bool bac
     const int splits = forward_splits(c, dt);
     return splits > 1 ? static_cast<size_t>(splits) * rows * (c.D + 1) * sizeof(float) : 0;
   }
-  WindowCall any = c;  // with positions of the caller's there may be more to do
-  const int32_t position = 0;
-  any.query_start = &position;
-  const KeyPlan p = key_plan(any);
+  const KeyPlan p = key_plan(with_positions(c));
   return static_cast<size_t>(up(2 * rows, 4) * 4 + p.partial_floats + p.further_floats) * sizeof(float);
 }
 

@@ -175,6 +175,9 @@ def test_sizes_both_ways(size, dtype):
     ((2, 40, 60, 2, 2, 48, 9, 2), None, [-25, 100]),                          # before the first key, behind the last
     ((2, 40, 60, 2, 2, 48, 9, 2), [1000, -3], [2 ** 31 - 1, -2 ** 31]),       # lengths beyond the keys and below none
     ((1, 200, 300, 2, 1, 128, 2 ** 31, 0), [211], [5]),
+    ((2, 40, 60, 2, 2, 48, 100, 5), None, [200, 10]),                         # beyond a window that holds all keys: the first ones alone
+    ((1, 600, 600, 4, 2, 64, 50, 300), [577], None),                          # first keys in several tiles
+    ((2, 300, 300, 2, 1, 96, 33, 40), None, [0, 45]),
 ], ids=str)
 def test_lengths_and_places(size, key_len, start, dtype):
     both_ways(*size, dtype, key_len, start)

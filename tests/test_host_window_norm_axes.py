@@ -32,7 +32,7 @@ def test_window_attention_arguments_are_checked_before_any_launch():
     for call in (window_fwd, window_bwd):
         for args in (dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(B_=-1), dict(S=-1), dict(Sk=-1), dict(A=-1), dict(K=-1), dict(K=0),
                      dict(A=3), dict(D=0), dict(D=-1), dict(window=0), dict(window=-1), dict(sinks=-1), dict(scale=0.0), dict(scale=-1.0),
-                     dict(scale=math.nan), dict(scale=math.inf), dict(dt=2), dict(dt=-1), dict(S=1 << 31), dict(Sk=1 << 31), dict(B_=big), dict(D=big),
+                     dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-39), dict(scale=3e38), dict(dt=2), dict(dt=-1), dict(S=1 << 31), dict(Sk=1 << 31), dict(B_=big), dict(D=big),
                      dict(A=big, K=big), dict(q=heads(strides=(-1, 1, 1))), dict(k=heads(strides=(64, -1, 1))), dict(v=heads(strides=(1 << 50, 1, 1))),
                      dict(q=heads(None)), dict(k=heads(None)), dict(v=heads(None)), dict(out=heads(None))):
             assert call(**args) == INVALID, args
