@@ -724,7 +724,7 @@ struct KeyJobs {
   int sink_tiles;                  // tiles that have first keys whose sums go on
   int strips, further_parts;       // of 32 first keys
   int64_t further_jobs;
-  float *partial, *further;        // [job][2][kRows][D] (one part: of the sink tiles alone), [job][4][2][32][D]
+  float *partial, *further;        // [job][2][kRows][D] (one part: of the sink tiles, for the strips' keys), [job][4][2][32][D]
 };
 enum Wanted { kBoth, kOnlyV, kOnlyK };
 // bfloat16: v of the workgroup's keys in LDS, not in registers.  There a wave of rows of 128 would need more than the 256 that let two run on a
@@ -897,7 +897,7 @@ __global__ __launch_bounds__(kThreads, (kKeysAtOnce<T, DP, DIRECT>)) void keys_k
     }
     if (u + 1 < u1) put(now ^ 1);
   }
-  if (further || parts > 1 || tile < jobs.sink_tiles) {
+  if (further || parts > 1 || wave_key / 32 < jobs.strips) {
     const int64_t slot = parts > 1 ? job : static_cast<int64_t>(bk) * jobs.sink_tiles + tile;
     const int rows = further ? 32 : kRows;  // keys of a sum
     float* const into = (further ? jobs.further + (job * kWaves + wave) * 2 * 32 * a.D : jobs.partial + (slot * 2 * kRows + wave * 32) * a.D) +
@@ -936,16 +936,17 @@ __device__ __forceinline__ void add_parts(f32x4& sum, const float* p, int64_t st
       if (i + n < count) sum += v[n];
   }
 }
-// The sums for a key, in their order: 32 lanes a key and gradient.  tiles: all where they have parts, else those with first keys.
+// The sums for a key, in their order: 32 lanes a key and gradient.  units: of 32 keys, all where tiles have parts, else the strips.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, KeyJobs jobs, int tiles, int64_t all) {
-  const int64_t n = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32;  // (bk, tile, gradient, key)
+__global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, KeyJobs jobs, int units, int64_t all) {
+  const int64_t n = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32;  // (bk, unit, gradient, key)
   if (n >= all) return;
-  const int in_tile = static_cast<int>(n % kRows), of_v = static_cast<int>(n / kRows % 2);
-  const int64_t of_tile = n / (2 * kRows);
-  const int tile = static_cast<int>(of_tile % tiles), bk = static_cast<int>(of_tile / tiles), b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
-  const int key = tile * kRows + in_tile, strip = key / 32;
+  const int of_v = static_cast<int>(n / 32 % 2);
+  const int64_t of_unit = n / 64;
+  const int strip = static_cast<int>(of_unit % units), bk = static_cast<int>(of_unit / units), b = bk / a.kv_heads, kv = bk - b * a.kv_heads;
+  const int key = strip * 32 + static_cast<int>(n % 32), tile = key / kRows, in_tile = key % kRows;
   if (key >= a.Sk) return;
+  const int64_t of_tile = static_cast<int64_t>(bk) * (jobs.parts > 1 ? jobs.tiles : jobs.sink_tiles) + tile;
   const Heads& h = of_v ? a.dv : a.dk;
   T* const to = const_cast<T*>(at<T>(h, b, key, kv));
   const float* const parts = jobs.partial + ((of_tile * jobs.parts * 2 + of_v) * kRows + in_tile) * a.D;
@@ -1140,9 +1141,9 @@ tempo_status launch_window_attn_bwd(const WindowCall& c, tempo_dtype dt, hipStre
         }
       });
     });
-    const int tiles = p.jobs.parts > 1 ? p.jobs.tiles : p.jobs.sink_tiles;
-    const int64_t keys = c.B * c.kv_heads * 2 * kRows * tiles;
-    if (s == TEMPO_OK && keys > 0) s = launch(join_keys_kernel<T>, up(keys, kThreads / 32), st, a, p.jobs, tiles, keys);
+    const int units = p.jobs.parts > 1 ? p.jobs.tiles * kWaves : p.jobs.strips;
+    const int64_t keys = c.B * c.kv_heads * units * 2 * 32;
+    if (s == TEMPO_OK && keys > 0) s = launch(join_keys_kernel<T>, up(keys, kThreads / 32), st, a, p.jobs, units, keys);
     return s;
   });
 }
