@@ -358,16 +358,17 @@ TEMPO_API tempo_status tempo_glu_bwd(const void* dh, const void* gu, const void*
  *   with any strides >= 0; they need only the alignment of an element.  out, dq, dk and dv overlap nothing.
  *   lse [B, heads, Sq] (f32) out of the forward, where it may be NULL, and in to the backward.
  *   key_len, query_start [B] int32 in, device, may be NULL; key_len is taken as 0 below 0 and as Sk above it, query_start may be negative.
- *   Keys that none of 128 neighbouring rows sees (a row: a query of one of the heads that share a key head) are not looked at, whatever they hold; an element of k, v, q or dout that is not finite
- *   makes NaN of the sums that it takes part in, and may of those of the rows and keys beside it that do not see it.  dk and dv of keys that no query sees are 0.
+ *   Keys that none of 128 neighbouring rows sees (a row: a query of one of the heads that share a key head) are not looked at, whatever they
+ *   hold; an element of k, v, q or dout that is not finite makes NaN of the sums that it takes part in, and may of those of the rows and keys
+ *   beside it that do not see it.  dk and dv of keys that no query sees are 0.
  *   bfloat16: the weights exp(s - max) and ds are rounded to bfloat16 for the second product, sums are in float32.  Sums are made in a
  *   fixed order: the same call gives the same bits.
  *   workspace: device memory of at least tempo_window_attn_fwd/bwd_workspace_bytes() bytes, 16-byte aligned (NULL if that is 0); calls that
  *   may run at the same time need one each.
  *   INVALID_ARG also: kv_heads < 1 (with heads > 0), heads no multiple of it, D < 1, window < 1, sinks < 0, a scale outside
  *   [2^-126, 2^127], a negative stride, a stride of an output that is 0 where there are two elements along it.
- *   UNSUPPORTED also: D > 256; more than 2^32 queries of all heads; more than 2^22 tiles of 128 rows (Sq heads / kv_heads of a key
- *   head) or of 128 keys in all, or 2^19 of 128 keys that hold some of the first `sinks`.
+ *   UNSUPPORTED also: D > 256; more than 2^22 tiles of 128 rows (Sq heads / kv_heads of a key head) or of 128 keys in all, or 2^19 and more
+ *   of 128 keys that hold some of the first `sinks`.
  */
 typedef struct {
   const void* p; /* written through if it is an output */

@@ -159,17 +159,57 @@ __device__ __forceinline__ f32x16 multiply_columns(const char* lds, int row0, in
   return c;
 }
 
-// Piece `piece` of a row of D elements at any address; zeros behind its end.
-template <typename T, bool STREAM = false>
-__device__ __forceinline__ u32x4 load_of_row(const T* row, int piece, int D) {
+// Piece `piece` of a row of D elements at any address: what is loaded, by all lanes at once, and what the piece then is.  A piece that the row ends
+// in is loaded from earlier on, and its elements are moved to their places once they have come, those behind the row become 0.  With a branch for
+// such pieces beside the load, the wave waits for each load there: one token of 16 sequences, 4096 keys of 32 / 8 heads of 83 float32 181 us,
+// 275 with it; 2 x 1000 tokens of 8 / 2 heads of 125 bfloat16 backward 114 us, 159 with it.
+template <typename T, bool STREAM = false, bool WHOLE = false>
+__device__ __forceinline__ u32x4 load_piece(const T* row, int piece, int D) {
   constexpr int V = Store<T>::kVec;
-  const int left = D - piece * V;
-  if (STREAM && left >= V) return ldg_stream_any(row + piece * V);
-  if (left >= V) return *reinterpret_cast<const u32x4_any*>(row + piece * V);
-  float e[V];
+  if (!WHOLE && D < V) {
+    float e[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) e[j] = j < left ? Store<T>::load1(row + piece * V + j) : 0.0f;
-  return Store<T>::pack(e);
+    for (int j = 0; j < V; ++j) {
+      const float x = Store<T>::load1(row + min(j, D - 1));
+      e[j] = j < D ? x : 0.0f;
+    }
+    return Store<T>::pack(e);
+  }
+  const T* const p = row + (WHOLE ? piece * V : min(piece * V, D - V));
+  return STREAM ? ldg_stream_any(p) : *reinterpret_cast<const u32x4_any*>(p);
+}
+template <typename T>
+__device__ __forceinline__ u32x4 fitted(u32x4 v, int piece, int D, int DP) {
+  constexpr int V = Store<T>::kVec;
+  if (D == DP) return v;
+  const int left = D - piece * V;
+  if (D % V != 0 && D > V) {
+    const int by = left > 0 && left < V ? V - left : 0;  // elements
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) v[n] = by & 1 ? v[n] >> 16 | (n < 3 ? v[n + 1] << 16 : 0) : v[n];
+    }
+#pragma unroll
+    for (int words = 1; words < 4; words *= 2) {
+      const bool moves = by * static_cast<int>(sizeof(T)) / 4 & words;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) v[n] = moves ? (n + words < 4 ? v[n + words] : 0) : v[n];
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < 4; ++n) v[n] = left > 0 ? v[n] : 0;
+  return v;
+}
+// Every second piece of a row, from `first` on.
+template <typename T, int DP>
+__device__ __forceinline__ void load_half_row(const T* row, int first, int D, u32x4 (&to)[Rows<T, DP>::kSteps]) {
+#pragma unroll
+  for (int p = 0; p < Rows<T, DP>::kSteps; ++p) to[p] = load_piece<T>(row, 2 * p + first, D);
+}
+template <typename T, int DP>
+__device__ __forceinline__ void fit_half_row(int first, int D, u32x4 (&v)[Rows<T, DP>::kSteps]) {
+#pragma unroll
+  for (int p = 0; p < Rows<T, DP>::kSteps; ++p) v[p] = fitted<T>(v[p], 2 * p + first, D, DP);
 }
 
 // N rows of a matrix on their way to LDS by way of registers.
@@ -186,14 +226,14 @@ struct Staged {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int at = i * kThreads + static_cast<int>(threadIdx.x), row = at / R::kRoom, piece = at % R::kRoom ^ R::swizzle(row);
-      v[i] = load_of_row<T>(of(row), piece, D);
+      v[i] = load_piece<T>(of(row), piece, D);
     }
   }
-  __device__ __forceinline__ void store(char* lds) const {
+  __device__ __forceinline__ void store(int D, char* lds) const {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int at = i * kThreads + static_cast<int>(threadIdx.x);
-      *reinterpret_cast<u32x4*>(lds + R::place(at / R::kRoom) + at % R::kRoom * 16) = v[i];
+      const int at = i * kThreads + static_cast<int>(threadIdx.x), row = at / R::kRoom, piece = at % R::kRoom ^ R::swizzle(row);
+      *reinterpret_cast<u32x4*>(lds + R::place(row) + at % R::kRoom * 16) = fitted<T>(v[i], piece, D, DP);
     }
   }
 };
@@ -342,8 +382,8 @@ struct KeyStream {
   }
   __device__ __forceinline__ void put(int to) {
     if constexpr (!DIRECT) {
-      ks.store(lds[to][0]);
-      vs.store(lds[to][1]);
+      ks.store(a.D, lds[to][0]);
+      vs.store(a.D, lds[to][1]);
     }
   }
   // work(tile's first key, its k, its v)
@@ -491,11 +531,9 @@ __global__ __launch_bounds__(kThreads, (kForward<T, DP, DIRECT>)) void forward_k
   Stream stream(a, keys, b, kv, lds, n0, n1);
   const WaveRows w(a, s, first_row + wave * 32);
   u32x4 q[R::kSteps];
-  {
-    const T* row = at<T>(a.q, b, w.i, kv * a.group + w.g);
-#pragma unroll
-    for (int p = 0; p < R::kSteps; ++p) q[p] = load_of_row<T>(row, 2 * p + threadIdx.x % kWave / 32, a.D);
-  }
+  const int half = threadIdx.x % kWave / 32;
+  load_half_row<T, DP>(at<T>(a.q, b, w.i, kv * a.group + w.g), half, a.D, q);
+  fit_half_row<T, DP>(half, a.D, q);
   f32x16 acc[kColumns];
 #pragma unroll
   for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
@@ -528,8 +566,10 @@ __global__ __launch_bounds__(kThreads, (kForward<T, DP, DIRECT>)) void forward_k
 // instruction takes it, two pieces of each row at a time.  The waves' sums are joined in LDS, those of the workgroups that share a head by join_kernel.
 template <typename T, int DP>
 constexpr int kFewWaves = sizeof(T) * DP <= 256 ? 8 : 4;
-template <typename T, int DP>
+// WHOLE: rows of DP elements.
+template <typename T, int DP, bool WHOLE>
 __global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4)) void few_kernel(Attn a) {
+  const int D = WHOLE ? DP : a.D;
   using R = Rows<T, DP>;
   constexpr int W = kFewWaves<T, DP>, kColumns = DP / 32, kBytes = R::bytes(32);
   constexpr int kRow = DP + 4;  // floats of a row of a wave's sums, 16 bytes further in the banks than the row before
@@ -548,16 +588,13 @@ __global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4))
 #pragma unroll
     for (int p = 0; p < R::kSteps; ++p) {
       const int row = (p * kWave + lane) / R::P, piece = (p * kWave + lane) % R::P, key = keys.seen(j0 + row);
-      k[p] = load_of_row<T, true>(at<T>(a.k, b, key, kv), piece, a.D);
-      v[p] = load_of_row<T, true>(at<T>(a.v, b, key, kv), piece, a.D);
+      k[p] = load_piece<T, true, WHOLE>(at<T>(a.k, b, key, kv), piece, D);
+      v[p] = load_piece<T, true, WHOLE>(at<T>(a.v, b, key, kv), piece, D);
     }
   };
   if (n < keys.count) fetch(keys.key(n, 32));
-  {
-    const T* row = at<T>(a.q, b, w.i, kv * a.group + w.g);
-#pragma unroll
-    for (int p = 0; p < R::kSteps; ++p) q[p] = load_of_row<T>(row, 2 * p + half, a.D);
-  }
+  load_half_row<T, DP>(at<T>(a.q, b, w.i, kv * a.group + w.g), half, D, q);
+  fit_half_row<T, DP>(half, D, q);
   f32x16 acc[kColumns];
 #pragma unroll
   for (int d = 0; d < kColumns; ++d) acc[d] = zeros();
@@ -566,9 +603,9 @@ __global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4))
     const int j0 = keys.key(n, 32);
 #pragma unroll
     for (int t = 0; t < R::kSteps; ++t) {
-      const int row = (t * kWave + lane) / R::P, to = R::place(row) + (((t * kWave + lane) % R::P ^ R::swizzle(row)) << 4);
-      *reinterpret_cast<u32x4*>(own_k + to) = k[t];
-      *reinterpret_cast<u32x4*>(own_v + to) = v[t];
+      const int row = (t * kWave + lane) / R::P, piece = (t * kWave + lane) % R::P, to = R::place(row) + ((piece ^ R::swizzle(row)) << 4);
+      *reinterpret_cast<u32x4*>(own_k + to) = fitted<T>(k[t], piece, D, DP);
+      *reinterpret_cast<u32x4*>(own_v + to) = fitted<T>(v[t], piece, D, DP);
     }
     if (n + step < keys.count) fetch(keys.key(n + step, 32));
     wave_lds_fence();
@@ -615,11 +652,11 @@ __global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4))
     if (a.splits > 1) {
       const int64_t at_row = split * all_rows + static_cast<int64_t>(bk) * a.rows + row;
       if (d == 0) a.partial_lse[at_row] = lse;
-      store_four(a.partial + at_row * a.D, a.D, d, out);
+      store_four(a.partial + at_row * D, D, d, out);
     } else {
       const int i = a.by_group.divide(row), head = kv * a.group + row - i * a.group;
       if (a.lse && d == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + i] = lse * kLn2;
-      store_four(const_cast<T*>(at<T>(a.out, b, i, head)), a.D, d, out);
+      store_four(const_cast<T*>(at<T>(a.out, b, i, head)), D, d, out);
     }
   }
 }
@@ -668,14 +705,18 @@ __global__ __launch_bounds__(kThreads, (kAtOnce<T, DP, DIRECT>)) void rows_kerne
   u32x4 q[R::kSteps], dout[R::kSteps];
   float delta = 0.0f;
   {
-    const T *qr = at<T>(a.q, b, w.i, head), *dr = at<T>(a.dout, b, w.i, head), *orow = at<T>(a.out, b, w.i, head);
+    u32x4 out[R::kSteps];
+    load_half_row<T, DP>(at<T>(a.dout, b, w.i, head), half, a.D, dout);
+    load_half_row<T, DP>(at<T>(a.out, b, w.i, head), half, a.D, out);
+    load_half_row<T, DP>(at<T>(a.q, b, w.i, head), half, a.D, q);
+    fit_half_row<T, DP>(half, a.D, dout);
+    fit_half_row<T, DP>(half, a.D, out);
+    fit_half_row<T, DP>(half, a.D, q);
 #pragma unroll
     for (int p = 0; p < R::kSteps; ++p) {
-      q[p] = load_of_row<T>(qr, 2 * p + half, a.D);
-      dout[p] = load_of_row<T>(dr, 2 * p + half, a.D);
       float x[R::V], y[R::V];
       Store<T>::unpack(dout[p], x);
-      Store<T>::unpack(load_of_row<T>(orow, 2 * p + half, a.D), y);
+      Store<T>::unpack(out[p], y);
 #pragma unroll
       for (int e = 0; e < R::V; ++e) delta = fmaf(x[e], y[e], delta);
     }
@@ -780,20 +821,18 @@ __global__ __launch_bounds__(kThreads, (kKeysAtOnce<T, DP, DIRECT>)) void keys_k
   const int blocks = first < end ? (end - first + BQ - 1) / BQ : 0;  // of a head
   const int each = static_cast<int>((static_cast<int64_t>(blocks) * a.group + parts - 1) / parts);
   const int u0 = min(part * each, blocks * a.group), u1 = min(u0 + each, blocks * a.group);
-  u32x4 k[R::kSteps], v[kInLds ? 1 : R::kSteps];
+  u32x4 k[R::kSteps], v[R::kSteps];
   {
     const int there = min(key, a.Sk - 1);
-    const T *kr = at<T>(a.k, b, there, kv), *vr = at<T>(a.v, b, there, kv);
-#pragma unroll
-    for (int p = 0; p < R::kSteps; ++p) {
-      k[p] = load_of_row<T>(kr, 2 * p + half, a.D);
-      if (kK && !kInLds) v[p] = load_of_row<T>(vr, 2 * p + half, a.D);
-    }
+    load_half_row<T, DP>(at<T>(a.k, b, there, kv), half, a.D, k);
+    if constexpr (kK) load_half_row<T, DP>(at<T>(a.v, b, there, kv), half, a.D, v);
+    fit_half_row<T, DP>(half, a.D, k);
+    if constexpr (kK) fit_half_row<T, DP>(half, a.D, v);
     if constexpr (kInLds) {  // a wave's own rows
 #pragma unroll
       for (int p = 0; p < R::kSteps; ++p) {
         const int row = wave * 32 + lane % 32, piece = 2 * p + half;
-        *reinterpret_cast<u32x4*>(values + R::place(row) + ((piece ^ R::swizzle(row)) << 4)) = load_of_row<T>(vr, piece, a.D);
+        *reinterpret_cast<u32x4*>(values + R::place(row) + ((piece ^ R::swizzle(row)) << 4)) = v[p];
       }
     }
   }
@@ -837,8 +876,8 @@ __global__ __launch_bounds__(kThreads, (kKeysAtOnce<T, DP, DIRECT>)) void keys_k
   };
   auto put = [&](int into) {
     if constexpr (!DIRECT) {
-      qs.store(lds[into][0]);
-      os.store(lds[into][1]);
+      qs.store(a.D, lds[into][0]);
+      os.store(a.D, lds[into][1]);
     }
     if (threadIdx.x < 2 * BQ) (&stats[into][0][0])[threadIdx.x] = stat;
   };
@@ -1070,10 +1109,9 @@ static WindowCall with_positions(WindowCall c) {
 bool window_attn_takes(const WindowCall& c) {
   constexpr int64_t most = int64_t{1} << 22;
   const int64_t bk = c.B * c.kv_heads, rows = c.Sq * (c.heads / c.kv_heads);
-  if (c.D > 256 || rows > INT32_MAX - kRows || up(rows, kRows) * bk > most || up(c.Sk, kRows) * bk > most || bk * rows > int64_t{1} << 32)
-    return false;
+  if (c.D > 256 || rows > INT32_MAX - kRows || up(rows, kRows) * bk > most || up(c.Sk, kRows) * bk > most) return false;
   const KeyPlan p = key_plan(with_positions(c));
-  return p.blocks <= 2 * most && bk * p.jobs.sink_tiles <= most / 8;
+  return p.blocks <= 2 * most && bk * p.jobs.sink_tiles < most / 8;
 }
 
 size_t window_attn_workspace_bytes(const WindowCall& c, tempo_dtype dt, bool back) {
@@ -1102,8 +1140,11 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
       constexpr int DP = decltype(width)::value, BK = sizeof(T) == 4 && DP == 64 ? 64 : 32;
       if constexpr (sizeof(T) * DP <= 512) {
         if (few(c, dt)) {
-          hipLaunchKernelGGL((few_kernel<T, DP>), dim3(static_cast<uint32_t>(c.B * c.kv_heads * a.splits)), dim3(kFewWaves<T, DP> * kWave), 0, st, a);
-          return launch_status();
+          return either(a.D == DP, [&](auto whole) {
+            hipLaunchKernelGGL((few_kernel<T, DP, decltype(whole)::value>), dim3(static_cast<uint32_t>(c.B * c.kv_heads * a.splits)),
+                               dim3(kFewWaves<T, DP> * kWave), 0, st, a);
+            return launch_status();
+          });
         }
       }
       return either(direct(c, dt, {c.k, c.v}), [&](auto straight) {

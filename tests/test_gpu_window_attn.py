@@ -167,6 +167,14 @@ def test_sizes_both_ways(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [*range(1, 18), *range(57, 64), *range(121, 128)])
+def test_rows_that_end_in_a_piece(D, dtype):
+    """Every number of elements in a row's last piece of 16 bytes, with few rows and with many."""
+    both_ways(2, 3, 70, 4, 2, D, 40, 1, dtype)
+    both_ways(1, 70, 70, 2, 1, D, 40, 1, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("size,key_len,start", [
     ((4, 90, 90, 4, 2, 64, 20, 0), [90, 1, 0, 47], None),                     # padded; rows behind a sequence see nothing
     ((4, 90, 90, 4, 2, 64, 20, 3), [90, 1, 0, 47], None),
