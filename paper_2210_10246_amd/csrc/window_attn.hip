@@ -49,7 +49,8 @@ struct Attn {
   int window, sinks;
   float scale, c;  // c: scale log2(e)
   int tiles, splits;
-  float *partial, *partial_lse;  // splits > 1: [splits, B kv_heads, rows, D] and [splits, B kv_heads, rows], of base 2
+  int pitch;                     // floats of a row of sums in the workspace: D up to whole pieces
+  float *partial, *partial_lse;  // splits > 1: [splits, B kv_heads, rows, pitch] and [splits, B kv_heads, rows], of base 2
 };
 
 // Which keys the queries of a sequence see.
@@ -304,10 +305,6 @@ __device__ __forceinline__ void store_four(T* row, int D, int d, f32x4 v) {
   }
 }
 // Four neighbouring floats of a row of D; zeros behind its end.
-__device__ __forceinline__ f32x4 load_four(const float* row, int D, int d) {
-  if (D - d >= 4) return *reinterpret_cast<const f32x4_any*>(row + d);
-  return f32x4{row[d], d + 1 < D ? row[d + 1] : 0.0f, d + 2 < D ? row[d + 2] : 0.0f, 0.0f};
-}
 // A lane's sums of column block `block`: 8 (i / 4) + 4 (lane / 32) + i % 4 are four neighbours each.
 template <typename T>
 __device__ __forceinline__ void store_sums(T* row, int D, int block, const f32x16& s, float by) {
@@ -496,7 +493,7 @@ __device__ __forceinline__ void finish(const Attn& a, const Running& run, const 
     const int64_t at_row = part * all_rows + (static_cast<int64_t>(b) * a.kv_heads + kv) * a.rows + w.row;
     if (first_half) a.partial_lse[at_row] = lse;
 #pragma unroll
-    for (int d = 0; d < COLUMNS; ++d) store_sums(a.partial + at_row * a.D, a.D, d, acc[d], by);
+    for (int d = 0; d < COLUMNS; ++d) store_sums(a.partial + at_row * a.pitch, a.pitch, d, acc[d], by);
   } else {
     const int head = kv * a.group + w.g;
     if (a.lse && first_half) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + w.i] = lse * kLn2;
@@ -652,7 +649,7 @@ __global__ __launch_bounds__((kFewWaves<T, DP> * kWave), (kFewWaves<T, DP> / 4))
     if (a.splits > 1) {
       const int64_t at_row = split * all_rows + static_cast<int64_t>(bk) * a.rows + row;
       if (d == 0) a.partial_lse[at_row] = lse;
-      store_four(a.partial + at_row * D, D, d, out);
+      store_four(a.partial + at_row * a.pitch, a.pitch, d, out);
     } else {
       const int i = a.by_group.divide(row), head = kv * a.group + row - i * a.group;
       if (a.lse && d == 0) a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.Sq + i] = lse * kLn2;
@@ -680,7 +677,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Attn a, int64_t all) {
     f32x4 out = {0, 0, 0, 0};
 #pragma unroll 4
     for (int p = 0; p < a.splits; ++p)
-      out += __builtin_amdgcn_exp2f(a.partial_lse[p * all + at_row] - from) * load_four(a.partial + (p * all + at_row) * a.D, a.D, d);
+      out += __builtin_amdgcn_exp2f(a.partial_lse[p * all + at_row] - from) * *reinterpret_cast<const f32x4*>(a.partial + (p * all + at_row) * a.pitch + d);
     store_four(to, a.D, d, out * by);
   }
 }
@@ -765,7 +762,7 @@ struct KeyJobs {
   int sink_tiles;                  // tiles that have first keys whose sums go on
   int strips, further_parts;       // of 32 first keys
   int64_t further_jobs;
-  float *partial, *further;        // [job][2][kRows][D] (one part: of the sink tiles, for the strips' keys), [job][4][2][32][D]
+  float *partial, *further;        // [job][2][kRows][pitch] (one part: of the sink tiles, for the strips' keys), [job][4][2][32][pitch]
 };
 enum Wanted { kBoth, kOnlyV, kOnlyK };
 // bfloat16: v of the workgroup's keys in LDS, not in registers.  There a wave of rows of 128 would need more than the 256 that let two run on a
@@ -939,15 +936,15 @@ __global__ __launch_bounds__(kThreads, (kKeysAtOnce<T, DP, DIRECT>)) void keys_k
   if (further || parts > 1 || wave_key / 32 < jobs.strips) {
     const int64_t slot = parts > 1 ? job : static_cast<int64_t>(bk) * jobs.sink_tiles + tile;
     const int rows = further ? 32 : kRows;  // keys of a sum
-    float* const into = (further ? jobs.further + (job * kWaves + wave) * 2 * 32 * a.D : jobs.partial + (slot * 2 * kRows + wave * 32) * a.D) +
-                        lane % 32 * a.D;
+    float* const into = (further ? jobs.further + (job * kWaves + wave) * 2 * 32 * a.pitch : jobs.partial + (slot * 2 * kRows + wave * 32) * a.pitch) +
+                        lane % 32 * a.pitch;
     if constexpr (kK) {
 #pragma unroll
-      for (int d = 0; d < kColumns; ++d) store_sums(into, a.D, d, dk[d], a.scale);
+      for (int d = 0; d < kColumns; ++d) store_sums(into, a.pitch, d, dk[d], a.scale);
     }
     if constexpr (kV) {
 #pragma unroll
-      for (int d = 0; d < kColumns; ++d) store_sums(into + static_cast<int64_t>(rows) * a.D, a.D, d, dv[d], 1.0f);
+      for (int d = 0; d < kColumns; ++d) store_sums(into + static_cast<int64_t>(rows) * a.pitch, a.pitch, d, dv[d], 1.0f);
     }
   } else if (key < a.Sk) {
     if constexpr (kK) {
@@ -965,11 +962,11 @@ __global__ __launch_bounds__(kThreads, (kKeysAtOnce<T, DP, DIRECT>)) void keys_k
 
 // sum += four floats of each of `count` rows, N of them on their way at a time.
 template <int N>
-__device__ __forceinline__ void add_parts(f32x4& sum, const float* p, int64_t step, int count, int left) {
+__device__ __forceinline__ void add_parts(f32x4& sum, const float* p, int64_t step, int count) {
   for (int i = 0; i < count; i += N) {
     f32x4 v[N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = load_four(p + min(i + n, count - 1) * step, left, 0);
+    for (int n = 0; n < N; ++n) v[n] = *reinterpret_cast<const f32x4*>(p + min(i + n, count - 1) * step);
 #pragma unroll
     for (int n = 0; n < N; ++n)
       if (i + n < count) sum += v[n];
@@ -988,19 +985,20 @@ __global__ __launch_bounds__(kThreads) void join_keys_kernel(Attn a, KeyJobs job
   const int64_t of_tile = static_cast<int64_t>(bk) * (jobs.parts > 1 ? jobs.tiles : jobs.sink_tiles) + tile;
   const Heads& h = of_v ? a.dv : a.dk;
   T* const to = const_cast<T*>(at<T>(h, b, key, kv));
-  const float* const parts = jobs.partial + ((of_tile * jobs.parts * 2 + of_v) * kRows + in_tile) * a.D;
-  const float* const further = jobs.further + (((static_cast<int64_t>(bk) * jobs.strips + strip) * jobs.further_parts * kWaves * 2 + of_v) * 32 + key % 32) * a.D;
+  const float* const parts = jobs.partial + ((of_tile * jobs.parts * 2 + of_v) * kRows + in_tile) * a.pitch;
+  const float* const further = jobs.further + (((static_cast<int64_t>(bk) * jobs.strips + strip) * jobs.further_parts * kWaves * 2 + of_v) * 32 + key % 32) * a.pitch;
   const int further_sums = strip < jobs.strips ? jobs.further_parts * kWaves : 0;
   for (int d = threadIdx.x % 32 * 4; d < a.D; d += 128) {
     f32x4 sum = {0, 0, 0, 0};
-    add_parts<4>(sum, parts + d, int64_t{2} * kRows * a.D, jobs.parts, a.D - d);
-    add_parts<8>(sum, further + d, int64_t{2} * 32 * a.D, further_sums, a.D - d);
+    add_parts<4>(sum, parts + d, int64_t{2} * kRows * a.pitch, jobs.parts);
+    add_parts<8>(sum, further + d, int64_t{2} * 32 * a.pitch, further_sums);
     store_four(to, a.D, d, sum);
   }
 }
 
 // ---- plans ----------------------------------------------------------------------------------------------------------------
 int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
+int64_t pitch_of(const WindowCall& c) { return up(c.D, 4) * 4; }
 
 // Up to 32 rows for a key head: the kernel for few, where a wave's registers hold what it needs.
 bool few(const WindowCall& c, tempo_dtype dt) {
@@ -1038,8 +1036,8 @@ KeyPlan key_plan(const WindowCall& c) {
   }
   p.jobs.further_jobs = bk * p.jobs.strips * p.jobs.further_parts;
   p.blocks = p.jobs.further_jobs + bk * tiles * p.jobs.parts;
-  p.partial_floats = bk * (p.jobs.parts > 1 ? tiles * p.jobs.parts : p.jobs.sink_tiles) * 2 * kRows * c.D;
-  p.further_floats = p.jobs.further_jobs * kWaves * 2 * 32 * c.D;
+  p.partial_floats = bk * (p.jobs.parts > 1 ? tiles * p.jobs.parts : p.jobs.sink_tiles) * 2 * kRows * pitch_of(c);
+  p.further_floats = p.jobs.further_jobs * kWaves * 2 * 32 * pitch_of(c);
   return p;
 }
 
@@ -1054,6 +1052,7 @@ Attn attn_of(const WindowCall& c) {
   a.group = a.heads / a.kv_heads;
   a.rows = a.Sq * a.group;
   a.D = static_cast<int>(c.D);
+  a.pitch = static_cast<int>(pitch_of(c));
   a.by_group = FastDiv(static_cast<uint32_t>(a.group));
   a.window = static_cast<int>(std::min<int64_t>(c.window, INT32_MAX));
   a.sinks = static_cast<int>(std::min<int64_t>(c.sinks, c.Sk));
@@ -1118,7 +1117,7 @@ size_t window_attn_workspace_bytes(const WindowCall& c, tempo_dtype dt, bool bac
   const int64_t rows = c.B * c.heads * c.Sq;
   if (!back) {
     const int splits = forward_splits(c, dt);
-    return splits > 1 ? static_cast<size_t>(splits) * rows * (c.D + 1) * sizeof(float) : 0;
+    return splits > 1 ? static_cast<size_t>(splits) * rows * (pitch_of(c) + 1) * sizeof(float) : 0;
   }
   const KeyPlan p = key_plan(with_positions(c));
   return static_cast<size_t>(up(2 * rows, 4) * 4 + p.partial_floats + p.further_floats) * sizeof(float);
@@ -1131,7 +1130,7 @@ tempo_status launch_window_attn_fwd(const WindowCall& c, tempo_dtype dt, hipStre
   const int64_t all = c.B * c.heads * c.Sq;
   if (a.splits > 1) {
     a.partial = static_cast<float*>(c.workspace);
-    a.partial_lse = a.partial + a.splits * all * c.D;
+    a.partial_lse = a.partial + a.splits * all * a.pitch;
   }
   const int64_t blocks = c.B * c.kv_heads * a.tiles * a.splits;
   return with_type(dt, [&](auto type) {
