@@ -303,7 +303,7 @@ TEMPO_API tempo_status tempo_residual_norm_fwd(const void* x, const void* f, con
  *   dgate = beta sum n d over its rows,  dpost_weight = sum beta gate d f^,  dpost_bias = sum beta gate d,  dpre_weight = sum dh y^,
  *   dpre_bias = sum dh.
  *   dy (NULL: 0, where there is a pre), dh, f, y [N,M] in (dt); dx [N,M] out (dt), may alias dy; df [N,M] out (dt); the others out (f32), each
- *   may be NULL, summed in a fixed order.  Without pre, dh and y are not read.
+ *   may be NULL, summed in a fixed order (of no rows: zeros).  Without pre, dh and y are not read.
  *   workspace: at least tempo_residual_norm_bwd_workspace_bytes(N, M, groups, dt) bytes, 16-byte aligned (not needed where all of dgate ..
  *   dpre_bias are NULL); groups is that of the call, 1 without a gate.  Calls that may run at the same time need one each.
  */

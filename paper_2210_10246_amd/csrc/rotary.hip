@@ -5,7 +5,8 @@
 //
 // Bound by the bytes of q and k, read once and written once.  Angles are made where they are used: in two numbers of 64 bits, which
 // this chip multiplies at the rate of 32, so that a position of any size keeps its place within the turn; no table is read, kept or
-// bounded by a longest sequence.
+// bounded by a longest sequence.  The positions of a token's axes are held in registers, of which a pair selects: 30784 tokens of 40 + 8 heads of 128
+// bfloat16 on three axes 144 us (5.3 TB/s).
 #include <algorithm>
 #include <type_traits>
 
