@@ -286,6 +286,7 @@ class RotaryPositions(nn.Module):
             raise ValueError(f'layout must be "half" or "interleaved", got {layout!r}')
         freqs, self.scale = rotary_frequencies(dim, base, scaling, factor, trained, turns)
         self.layout, axes = layout, None
+        self.n_axes = 0 if sections is None else len(sections)
         if sections is not None:
             axes = rotary_axes(sections, order)
             if axes.numel() != dim // 2:
@@ -310,8 +311,9 @@ class RotaryPositions(nn.Module):
         return self
 
     def forward(self, q, k=None, positions=None, start: int = 0):
-        if self.axes is not None and positions is None:
-            raise ValueError("several axes have positions, [axes, S] or [axes, B, S]")
+        if self.axes is not None and (positions is None or positions.dim() < 2 or positions.shape[0] != self.n_axes):
+            raise ValueError(f"{self.n_axes} axes have positions, [{self.n_axes}, S] or [{self.n_axes}, B, S], got "
+                             f"{None if positions is None else tuple(positions.shape)}")
         k_in = None if k is None else k.transpose(1, 2)
         q, k = _RotaryFn.apply(q.transpose(1, 2), k_in, self.freqs, positions, start, self.layout, self.scale, False, self.axes)
         return q.transpose(1, 2), None if k is None else k.transpose(1, 2)
@@ -402,8 +404,8 @@ class _ResidualNormFn(torch.autograd.Function):
 class TempoResidualNorm(_Float32Parameters):
     """The place between two blocks of a pre-norm model, for the residual x and a block's output f: y = alpha x + beta gate post(f), the next
     residual, and h = pre(y), the next block's input (None without a pre).  post, pre: "rms", "layer" or None.  gate: a learned one of
-    `hidden` elements that begins at that value; or None, and forward takes one, [hidden] or one for each of equally many rows (as
-    [B, 1, hidden] beside [B, S, hidden]), or none.  affine: the norms have weights, and with "layer" biases.  Parameters and gates
+    `hidden` elements that begins at that value; or None, and forward takes one, [hidden] or one for each of equally many rows
+    (as [B, hidden] or [B, 1, hidden] beside [B, S, hidden]), or none.  affine: the norms have weights, and with "layer" biases.  Parameters and gates
     are float32 whatever the activation dtype.  No second derivative."""
 
     def __init__(self, hidden: int, post: Optional[str] = None, pre: Optional[str] = "rms", gate: Optional[float] = None, alpha: float = 1.0,
@@ -419,16 +421,18 @@ class TempoResidualNorm(_Float32Parameters):
         self.hidden, self.post, self.pre, self.alpha, self.beta, self.eps = hidden, post, pre, alpha, beta, eps
 
     def _gate_of_groups(self, gate, x):
-        """[hidden] or [groups, hidden]; with as many dimensions as x it has x's sizes first, then ones."""
+        """[hidden] or [groups, hidden], the groups being of x's first dimensions; with as many dimensions as x it has x's sizes first, then
+        ones."""
         if gate.dim() == x.dim() > 2:
             first = 0
             while first < x.dim() - 1 and gate.shape[first] == x.shape[first]:
                 first += 1
             if all(n == 1 for n in gate.shape[first:-1]):
                 return gate.reshape(-1, gate.shape[-1])
-        elif gate.dim() in (1, 2):
+        elif gate.dim() == 1 or (gate.dim() == 2 and (x.dim() == 2 or gate.shape[0] in [x.shape[:n].numel() for n in range(x.dim())])):
             return gate
-        raise ValueError(f"gate must be [{self.hidden}], [groups, {self.hidden}] or like x with ones behind its groups, got {tuple(gate.shape)}")
+        raise ValueError(f"gate must be [{self.hidden}], [groups, {self.hidden}] for groups of x's first dimensions or like x with ones behind them, "
+                         f"got {tuple(gate.shape)} beside {tuple(x.shape)}")
 
     def forward(self, x, f, gate=None):
         if torch.is_autocast_enabled("cuda"):

@@ -187,6 +187,9 @@ def test_which_axis_a_pair_turns_by():
             RotaryPositions(12, **args)
     with pytest.raises(ValueError, match="positions"):
         r(torch.zeros(1, 1, 2, 12))
+    for shape in ((2,), (1, 2), (2, 2), (4, 2), (2, 3, 2)):      # of other numbers of axes, batches' positions on one
+        with pytest.raises(ValueError, match="3 axes"):
+            r(torch.zeros(1, 1, 2, 12), positions=torch.zeros(shape, dtype=torch.int64))
 
 
 def test_modules_refuse_other_forms_and_keep_float32():
@@ -205,6 +208,6 @@ def test_modules_refuse_other_forms_and_keep_float32():
         with pytest.raises(ValueError, match=message):
             n(*args)
     n = TempoResidualNorm(8)
-    for shape in ((1, 3, 8), (2, 3, 1), (3, 1, 8), (2, 1, 1, 8), ()):
+    for shape in ((1, 3, 8), (2, 3, 1), (3, 1, 8), (2, 1, 1, 8), (), (3, 8), (4, 8)):
         with pytest.raises(ValueError):
             n(x, x, torch.zeros(shape))
