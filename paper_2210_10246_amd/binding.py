@@ -706,7 +706,9 @@ def _window_attn(where, like_q, like_k, lse, window, sinks, scale, key_len, quer
         raise ValueError(f"the heads of q must be a multiple of those of k, got {heads} and {kv_heads}")
     if not 1 <= window < 2 ** 63 or not 0 <= sinks < 2 ** 63:
         raise ValueError(f"window must be at least 1 and sinks at least 0, got {window} and {sinks}")
-    scale = D ** -0.5 if scale is None and D > 0 else scale
+    if D < 1:
+        raise ValueError(f"q must have elements, got {tuple(q.shape)}")
+    scale = D ** -0.5 if scale is None else scale
     if not 0.0 < scale <= torch.finfo(torch.float32).max:
         raise ValueError(f"scale must be positive and finite, got {scale}")
     _want("lse", lse, torch.float32, B * heads * Sq)

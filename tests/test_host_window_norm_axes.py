@@ -133,7 +133,7 @@ def test_binding_refuses_other_forms():
             ("adjacent", dict(q=t(2, 4, 4, 16)[..., ::2])), ("adjacent", dict(k=t(2, 6, 16))), ("shape", dict(out=t(2, 4, 4, 9))),
             ("shape", dict(v=t(2, 5, 2, 8))), ("batch and elements", dict(k=t(1, 6, 2, 8), v=t(1, 6, 2, 8))), ("multiple", dict(k=t(2, 6, 3, 8), v=t(2, 6, 3, 8))),
             ("window", dict(window=0)), ("sinks", dict(sinks=-1)), ("window", dict(window=1 << 63)), ("scale", dict(scale=0.0)), ("scale", dict(scale=math.nan)),
-            ("lse", dict(lse=lse.double())), ("lse", dict(lse=t(2, 4, 3))), ("key_len", dict(key_len=t(2, dtype=torch.int64))),
+            ("elements", dict(q=t(2, 4, 4, 0), k=t(2, 6, 2, 0), v=t(2, 6, 2, 0), out=t(2, 4, 4, 0))), ("lse", dict(lse=lse.double())), ("lse", dict(lse=t(2, 4, 3))), ("key_len", dict(key_len=t(2, dtype=torch.int64))),
             ("query_start", dict(query_start=t(3, dtype=torch.int32))), ("CUDA", {})):
         with pytest.raises(ValueError, match=message):
             B.tempo_window_attn_fwd(**{**good, **args})
