@@ -167,7 +167,7 @@ def test_sizes_both_ways(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("D", [*range(1, 18), *range(57, 64), *range(121, 128)])
+@pytest.mark.parametrize("D", [*range(1, 18), *range(57, 64), *range(121, 128), 129, 160, 187, 192])
 def test_rows_that_end_in_a_piece(D, dtype):
     """Every number of elements in a row's last piece of 16 bytes, with few rows and with many."""
     both_ways(2, 3, 70, 4, 2, D, 40, 1, dtype)
