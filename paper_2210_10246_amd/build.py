@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libtempo.so")
 SOURCES = ("api.hip", "gelu.hip", "layernorm.hip", "attention.hip", "mask.hip", "matmul.hip", "encoder.hip", "rotary.hip",
-           "glu.hip", "window_attn.hip", "residual_norm.hip")
+           "glu.hip", "window_attn.hip", "window_attn_bwd.hip", "residual_norm.hip")
 NATIVE_PATH = os.path.join(HERE, "_native.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
