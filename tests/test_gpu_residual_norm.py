@@ -193,6 +193,41 @@ def test_sizes_both_ways(N, M, post, pre, biases, dtype):
     both_ways(N, M, dtype, post, pre, biases=biases, alpha=0.75, beta=0.5)
 
 
+# Rows whose last piece begins earlier, within what the wave before it has: a wave of pieces, several, and one more element each.
+ONE_BEHIND_A_WAVE = {"f32": (257, 259, 513, 1025, 4097), "bf16": (513, 519, 1025, 4097, 8193)}
+
+
+@pytest.mark.parametrize("post,pre", [(None, None), (None, "rms"), ("layer", None), ("rms", "layer")])
+@pytest.mark.parametrize("dtype,M", [(dtype, M) for dtype, widths in ONE_BEHIND_A_WAVE.items() for M in widths])
+def test_in_place_where_two_waves_share_elements(dtype, M, post, pre):
+    """y = x and dx = dy, over thousands of rows: the same bits as into tensors of their own, which are right."""
+    both_ways(9, M, dtype, post, pre, alpha=0.75, beta=0.5)
+    N, alpha, beta = 20011, 0.75, 0.5
+    x, f, dy = (normal(N, M, dtype=dtype, seed=s) for s in (1, 2, 3))
+    dh = normal(N, M, dtype=dtype, seed=4) if pre else None
+    w = [normal(M, seed=5 + n, shift=1.0) if kind else None for n, kind in enumerate((post, pre))]
+    st = [torch.empty(N, 2, device="cuda") if kind else None for kind in (post, pre)]
+    y, h, h2 = torch.empty_like(x), *(torch.empty_like(x) if pre else None for _ in range(2))
+
+    def forward(x, y, h):
+        B.tempo_residual_norm_fwd(x, f, None, y, h, post, w[0], None, st[0], pre, w[1], None, st[1], alpha, beta, EPS, EPS)
+
+    def backward(dy, dx, df):
+        grads = [torch.empty_like(t) if t is not None else None for t in w]
+        B.tempo_residual_norm_bwd(dy, dh, f, y if pre else None, None, dx, df, None, post, w[0], None, st[0], grads[0], None, pre, w[1], st[1],
+                                  grads[1], None, alpha, beta)
+        return [g for g in grads if g is not None]
+    forward(x, y, h)
+    dx, df, df2 = (torch.empty_like(x) for _ in range(3))
+    grads = backward(dy, dx, df)
+    for _ in range(3):
+        into, into_dy = x.clone(), dy.clone()
+        forward(into, into, h2)
+        assert torch.equal(into, y) and (not pre or torch.equal(h2, h))
+        again = backward(into_dy, into_dy, df2)
+        assert torch.equal(into_dy, dx) and torch.equal(df2, df) and all(torch.equal(a, b) for a, b in zip(again, grads))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N,groups", [(12, 12), (96, 4), (1000, 8), (4096, 2), (3000, 1)])
 @pytest.mark.parametrize("post,biases", [(None, False), ("rms", True), ("layer", False)])
