@@ -32,7 +32,7 @@ struct Residual {
   Norm post, pre;
   float alpha, beta;
   int64_t N, group_rows;  // rows of a gate
-  int M;
+  uint32_t M;
   float inv;              // 1 / M
   int parts;              // workgroups of a gate's rows
   float* partial;         // backward: [groups * parts][sums][M]
@@ -322,23 +322,24 @@ __global__ __launch_bounds__(WAVES* kWave) void backward_kernel(Residual r) {
   }
 }
 
-// Rows of any length, longer than a workgroup's registers or shorter than a piece: element by element, read again for each step.
+// Rows of any length, longer than a workgroup's registers or shorter than a piece: element by element, read again for each step.  Columns are
+// counted without a sign: the last turn passes 2^31 where M is next to it.
 constexpr int kAnyThreads = 1024;
 template <typename F>
-__device__ __forceinline__ float sum_of_row(int M, float* slots, F&& of) {
+__device__ __forceinline__ float sum_of_row(uint32_t M, float* slots, F&& of) {
   float s = 0.0f;
-  for (int c = threadIdx.x; c < M; c += kAnyThreads) s += of(c);
+  for (uint32_t c = threadIdx.x; c < M; c += kAnyThreads) s += of(c);
   s = row_reduce<kAnyThreads, false>(s, slots);
   lds_barrier();
   return s;
 }
 template <typename F>
-__device__ __forceinline__ float2 statistics_of_row(const Norm& n, int M, float inv, float* slots, F&& value) {
+__device__ __forceinline__ float2 statistics_of_row(const Norm& n, uint32_t M, float inv, float* slots, F&& value) {
   const float mean = n.layer ? sum_of_row(M, slots, value) * inv : 0.0f;
-  const float square = sum_of_row(M, slots, [&](int c) { return (value(c) - mean) * (value(c) - mean); });
+  const float square = sum_of_row(M, slots, [&](uint32_t c) { return (value(c) - mean) * (value(c) - mean); });
   return make_float2(mean, 1.0f / sqrtf(square * inv + n.eps));
 }
-__device__ __forceinline__ float param(const float* p, int c, float otherwise) { return p ? p[c] : otherwise; }
+__device__ __forceinline__ float param(const float* p, uint32_t c, float otherwise) { return p ? p[c] : otherwise; }
 
 template <typename T>
 __global__ __launch_bounds__(kAnyThreads) void forward_any_kernel(Residual r) {
@@ -351,18 +352,18 @@ __global__ __launch_bounds__(kAnyThreads) void forward_any_kernel(Residual r) {
     T* const y = static_cast<T*>(r.to_y) + row * M;
     float2 st = make_float2(0.0f, 1.0f);
     if (r.post.there) {
-      st = statistics_of_row(r.post, r.M, r.inv, slots, [&](int c) { return Store<T>::load1(f + c); });
+      st = statistics_of_row(r.post, r.M, r.inv, slots, [&](uint32_t c) { return Store<T>::load1(f + c); });
       if (r.post.stats && threadIdx.x == 0) r.post.stats[row] = st;
     }
-    for (int c = threadIdx.x; c < r.M; c += kAnyThreads) {
+    for (uint32_t c = threadIdx.x; c < r.M; c += kAnyThreads) {
       const float g = r.beta * param(gate, c, 1.0f);
       const float n = (Store<T>::load1(f + c) - st.x) * st.y * (g * param(r.post.weight, c, 1.0f)) + g * param(r.post.bias, c, 0.0f);
       Store<T>::store1(y + c, fmaf(r.alpha, Store<T>::load1(x + c), n));
     }
     if (!r.pre.there) continue;
-    st = statistics_of_row(r.pre, r.M, r.inv, slots, [&](int c) { return Store<T>::load1(y + c); });  // a lane's own
+    st = statistics_of_row(r.pre, r.M, r.inv, slots, [&](uint32_t c) { return Store<T>::load1(y + c); });  // a lane's own
     if (r.pre.stats && threadIdx.x == 0) r.pre.stats[row] = st;
-    for (int c = threadIdx.x; c < r.M; c += kAnyThreads)
+    for (uint32_t c = threadIdx.x; c < r.M; c += kAnyThreads)
       Store<T>::store1(static_cast<T*>(r.h) + row * M + c, (Store<T>::load1(y + c) - st.x) * st.y * param(r.pre.weight, c, 1.0f) +
                                                                param(r.pre.bias, c, 0.0f));
   }
@@ -376,27 +377,27 @@ __global__ __launch_bounds__(kAnyThreads) void backward_any_kernel(Residual r) {
   const float* gate = r.gate ? r.gate + walk.group * M : nullptr;
   float* const sums = r.partial ? r.partial + static_cast<int64_t>(blockIdx.x) * SUMS * M : nullptr;
   if (sums)
-    for (int c = threadIdx.x; c < r.M; c += kAnyThreads)
+    for (uint32_t c = threadIdx.x; c < r.M; c += kAnyThreads)
       for (int s = 0; s < SUMS; ++s) sums[s * M + c] = 0.0f;
   for (int64_t row = walk.first; row < walk.end; row += walk.step) {
-    auto element = [&](const void* t, int c) { return t ? Store<T>::load1(static_cast<const T*>(t) + row * M + c) : 0.0f; };
+    auto element = [&](const void* t, uint32_t c) { return t ? Store<T>::load1(static_cast<const T*>(t) + row * M + c) : 0.0f; };
     const float2 pre = r.pre.there ? r.pre.stats[row] : make_float2(0.0f, 0.0f), post = r.post.there ? r.post.stats[row] : make_float2(0.0f, 1.0f);
-    auto y_hat = [&](int c) { return r.pre.there ? (element(r.y, c) - pre.x) * pre.y : 0.0f; };
-    auto f_hat = [&](int c) { return (element(r.f, c) - post.x) * post.y; };
-    auto g = [&](int c) { return r.pre.there ? element(r.dh, c) * param(r.pre.weight, c, 1.0f) : 0.0f; };
+    auto y_hat = [&](uint32_t c) { return r.pre.there ? (element(r.y, c) - pre.x) * pre.y : 0.0f; };
+    auto f_hat = [&](uint32_t c) { return (element(r.f, c) - post.x) * post.y; };
+    auto g = [&](uint32_t c) { return r.pre.there ? element(r.dh, c) * param(r.pre.weight, c, 1.0f) : 0.0f; };
     float s1 = 0.0f, s2 = 0.0f;
     if (r.pre.there) {
-      s1 = sum_of_row(r.M, slots, [&](int c) { return g(c) * y_hat(c); }) * r.inv;
+      s1 = sum_of_row(r.M, slots, [&](uint32_t c) { return g(c) * y_hat(c); }) * r.inv;
       if (r.pre.layer) s2 = sum_of_row(r.M, slots, g) * r.inv;
     }
-    auto d = [&](int c) { return fmaf(pre.y, g(c) - y_hat(c) * s1 - s2, element(r.dy, c)); };
-    auto e = [&](int c) { return d(c) * (r.beta * param(gate, c, 1.0f) * param(r.post.weight, c, 1.0f)); };
+    auto d = [&](uint32_t c) { return fmaf(pre.y, g(c) - y_hat(c) * s1 - s2, element(r.dy, c)); };
+    auto e = [&](uint32_t c) { return d(c) * (r.beta * param(gate, c, 1.0f) * param(r.post.weight, c, 1.0f)); };
     float t1 = 0.0f, t2 = 0.0f;
     if (r.post.there) {
-      t1 = sum_of_row(r.M, slots, [&](int c) { return e(c) * f_hat(c); }) * r.inv;
+      t1 = sum_of_row(r.M, slots, [&](uint32_t c) { return e(c) * f_hat(c); }) * r.inv;
       if (r.post.layer) t2 = sum_of_row(r.M, slots, e) * r.inv;
     }
-    for (int c = threadIdx.x; c < r.M; c += kAnyThreads) {
+    for (uint32_t c = threadIdx.x; c < r.M; c += kAnyThreads) {
       const float dc = d(c), fc = f_hat(c), df = post.y * (e(c) - fc * t1 - t2);
       if (sums) {
         sums[c] = fmaf(fc, dc, sums[c]);
@@ -526,7 +527,7 @@ Residual residual_of(const ResidualCall& c, const Plan& p) {
   r.gate = c.gate;
   r.post = norm_of(c.post), r.pre = norm_of(c.pre);
   r.alpha = c.alpha, r.beta = c.beta;
-  r.N = c.N, r.M = static_cast<int>(c.M);
+  r.N = c.N, r.M = static_cast<uint32_t>(c.M);
   r.group_rows = p.group_rows;
   r.inv = 1.0f / static_cast<float>(c.M);
   r.parts = static_cast<int>(p.parts);
@@ -606,7 +607,7 @@ tempo_status launch_residual_norm_bwd(const ResidualCall& c, tempo_dtype dt, hip
   if (s != TEMPO_OK || !r.partial) return s;
   int share = kSumLanes;
   while (share > 1 && kSumLanes / share < p.groups) share /= 2;
-  const Sums all{r.partial, p.groups, r.parts, sums, r.M, share, c.gate, c.post ? c.post->weight : nullptr, c.post ? c.post->bias : nullptr, c.beta,
+  const Sums all{r.partial, p.groups, r.parts, sums, static_cast<int>(c.M), share, c.gate, c.post ? c.post->weight : nullptr, c.post ? c.post->bias : nullptr, c.beta,
                  c.dgate, c.dpost_weight, c.dpost_bias, c.dpre_weight, c.dpre_bias};
   const dim3 columns(static_cast<uint32_t>((c.M + kSumColumns - 1) / kSumColumns)), lanes(kSumColumns * kSumLanes);
   if (sums == 4) hipLaunchKernelGGL(columns_kernel<4>, columns, lanes, 0, st, all);

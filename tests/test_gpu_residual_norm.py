@@ -333,3 +333,19 @@ def test_beyond_2_to_32_elements():
     assert bool((y[:-2] == 0).all())
     del x, y
     torch.cuda.empty_cache()
+
+
+def test_the_longest_row():
+    """Columns up to 2^31 - 2: the turn of the last ones does not begin anew below 0, and nothing behind them is touched."""
+    M, alpha, beta = 2 ** 31 - 1, 0.75, 0.5
+    x, f = (torch.empty(1, M, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    y, end = guarded(1, M, dtype=torch.bfloat16)
+    for n, t in enumerate((x, f)):
+        t.view(-1)[:].copy_(normal(2 ** 20 + 1, dtype="bf16", seed=n).repeat(2 ** 11)[:M])
+    B.tempo_residual_norm_fwd(x, f, None, y, None, None, None, None, None, None, None, None, None, alpha, beta)
+    for a, b, got in zip(*(t[0].split(2 ** 28) for t in (x, f, y))):
+        want = alpha * a.double() + beta * b.double()
+        near(got, want, 4 * U * ((alpha * a.double()).abs() + (beta * b.double()).abs()))
+    assert bool((end == 777).all())
+    del x, f, y
+    torch.cuda.empty_cache()
