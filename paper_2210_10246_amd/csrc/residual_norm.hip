@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "launch_split.h"
 #include "tempo_device.h"
 #include "tempo_host.h"
 
@@ -418,16 +419,19 @@ __global__ __launch_bounds__(kAnyThreads) void backward_any_kernel(Residual r) {
 struct Sums {
   const float* partial;
   int64_t groups;
-  int parts, sums, M, share;
+  int parts, sums;
+  uint32_t M;
+  int share;
   const float *gate, *post_weight, *post_bias;
   float beta;
   float *dgate, *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
 };
 constexpr int kSumLanes = 64, kSumColumns = 16;
 template <int SUMS>
-__global__ __launch_bounds__(kSumColumns* kSumLanes) void columns_kernel(Sums s) {
+__global__ __launch_bounds__(kSumColumns* kSumLanes) void columns_kernel(Sums s, uint32_t first_block) {
   __shared__ float of_lanes[SUMS][kSumLanes][kSumColumns];
-  const int x = threadIdx.x % kSumColumns, lane = threadIdx.x / kSumColumns, column = blockIdx.x * kSumColumns + x, in_share = lane % s.share;
+  const int x = threadIdx.x % kSumColumns, lane = threadIdx.x / kSumColumns, in_share = lane % s.share;
+  const uint32_t column = (first_block + blockIdx.x) * kSumColumns + x;
   const bool exists = column < s.M, leads = in_share == 0 && exists;
   const int at_once = kSumLanes / s.share;
   const int64_t M = s.M;
@@ -607,12 +611,15 @@ tempo_status launch_residual_norm_bwd(const ResidualCall& c, tempo_dtype dt, hip
   if (s != TEMPO_OK || !r.partial) return s;
   int share = kSumLanes;
   while (share > 1 && kSumLanes / share < p.groups) share /= 2;
-  const Sums all{r.partial, p.groups, r.parts, sums, static_cast<int>(c.M), share, c.gate, c.post ? c.post->weight : nullptr, c.post ? c.post->bias : nullptr, c.beta,
+  const Sums all{r.partial, p.groups, r.parts, sums, r.M, share, c.gate, c.post ? c.post->weight : nullptr, c.post ? c.post->bias : nullptr, c.beta,
                  c.dgate, c.dpost_weight, c.dpost_bias, c.dpre_weight, c.dpre_bias};
-  const dim3 columns(static_cast<uint32_t>((c.M + kSumColumns - 1) / kSumColumns)), lanes(kSumColumns * kSumLanes);
-  if (sums == 4) hipLaunchKernelGGL(columns_kernel<4>, columns, lanes, 0, st, all);
-  else hipLaunchKernelGGL(columns_kernel<2>, columns, lanes, 0, st, all);
-  return launch_status();
+  const dim3 lanes(kSumColumns * kSumLanes);
+  const bool ok = split_launch((c.M + kSumColumns - 1) / kSumColumns, most_groups(INT64_MAX, lanes.x), [&](uint32_t first, uint32_t blocks) {
+    if (sums == 4) hipLaunchKernelGGL(columns_kernel<4>, dim3(blocks), lanes, 0, st, all, first);
+    else hipLaunchKernelGGL(columns_kernel<2>, dim3(blocks), lanes, 0, st, all, first);
+    return launch_status() == TEMPO_OK;
+  });
+  return ok ? TEMPO_OK : TEMPO_ERR_LAUNCH;
 }
 
 }  // namespace tempo

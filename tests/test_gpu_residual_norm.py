@@ -335,6 +335,12 @@ def test_beyond_2_to_32_elements():
     torch.cuda.empty_cache()
 
 
+def test_rows_of_2_to_26_columns():
+    """More columns than one launch of the sums' kernel has lanes for."""
+    both_ways(2, 2 ** 26 + 5, "bf16", None, "rms", biases=True, gated=False, dy=False)
+    torch.cuda.empty_cache()
+
+
 def test_the_longest_row():
     """Columns up to 2^31 - 2: the turn of the last ones does not begin anew below 0, and nothing behind them is touched."""
     M, alpha, beta = 2 ** 31 - 1, 0.75, 0.5
