@@ -530,6 +530,7 @@ static WindowCall window_sizes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads,
   constexpr int64_t most = INT32_MAX;  // beyond any position
   WindowCall c{};
   c.B = B, c.Sq = Sq, c.Sk = Sk, c.heads = heads, c.kv_heads = kv_heads, c.D = D;
+  if (heads == 0 && kv_heads > 0 && Sq >= 0) c.heads = kv_heads, c.Sq = 0;  // key heads that none reads: no queries, whose gradients are zeros
   c.window = window < most ? window : most;
   c.sinks = sinks < most ? sinks : most;
   return c;
@@ -591,9 +592,9 @@ tempo_status tempo_window_attn_bwd(const tempo_attn_heads* dout, const tempo_att
   if (!attn_heads_ok(dq, B, Sq, heads, D, true) || !attn_heads_ok(dk, B, Sk, kv_heads, D, true) ||
       !attn_heads_ok(dv, B, Sk, kv_heads, D, true))
     return TEMPO_ERR_INVALID_ARG;
-  if (B == 0 || heads == 0 || (Sq == 0 && Sk == 0)) return TEMPO_OK;
+  if (B == 0 || c.heads == 0 || (c.Sq == 0 && Sk == 0)) return TEMPO_OK;
   // Gradients of no queries are written too: zeros.
-  if (Sq > 0 && (!q->p || !out->p || !dout->p || !dq->p || !lse)) return TEMPO_ERR_INVALID_ARG;
+  if (c.Sq > 0 && (!q->p || !out->p || !dout->p || !dq->p || !lse)) return TEMPO_ERR_INVALID_ARG;
   if (Sk > 0 && (!k->p || !v->p || !dk->p || !dv->p)) return TEMPO_ERR_INVALID_ARG;
   const uintptr_t element = dt == TEMPO_F32 ? 4 : 2;
   for (const tempo_attn_heads* h : {q, k, v, out, dout, dq, dk, dv})

@@ -203,6 +203,19 @@ def test_nothing_to_do(size):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,Sq,Sk,kv,D", [(1, 3, 3, 2, 16), (2, 0, 300, 3, 83), (2, 70, 300, 1, 256)])
+def test_key_heads_that_no_head_reads(batch, Sq, Sk, kv, D, dtype):
+    """No heads of queries beside heads of keys: gradients of zeros, through both halves of the binding."""
+    q, k, v = inputs(batch, Sq, Sk, 0, kv, D, dtype)
+    out, lse = torch.empty_like(q), torch.empty(batch, 0, Sq, device="cuda")
+    for stream in (None, torch.cuda.current_stream()):
+        B.tempo_window_attn_fwd(q, k, v, out, lse, 3, 1, stream=stream)
+        (dk, e1), (dv, e2) = (guarded(*t.shape, dtype=t.dtype) for t in (k, v))
+        B.tempo_window_attn_bwd(out, q, k, v, out, lse, out, dk, dv, 3, 1, stream=stream)
+        assert bool((dk == 0).all() and (dv == 0).all() and (e1 == 777).all() and (e2 == 777).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_scales(dtype):
     both_ways(1, 70, 70, 2, 1, 64, 33, 1, dtype, scale=1.5)
     both_ways(1, 70, 70, 2, 1, 64, 33, 1, dtype, scale=1e-3)

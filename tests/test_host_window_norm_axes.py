@@ -59,6 +59,19 @@ def test_window_attention_arguments_are_checked_before_any_launch():
     assert window_bwd(**sizes) == WORKSPACE and window_bwd(ws=None, size=1 << 30, **sizes) == WORKSPACE
 
 
+def test_key_heads_that_no_head_reads_have_gradients():
+    """Where there are no heads of queries, a backward needs k, v and what it writes zeros to, and no workspace, as for no queries."""
+    none = heads(None)
+    sizes = dict(A=0, K=2, Sk=4)
+    assert window_fwd(q=none, k=none, v=none, out=none, **sizes) == OK
+    nothing = dict(q=none, out=none, dout=none, dq=none, lse=None)
+    for name in ("k", "v", "dk", "dv"):
+        assert window_bwd(**{**nothing, name: none}, **sizes) == INVALID
+    for sizes_of in ((2, 4, 4, 0, 2), (2, 0, 4, 2, 2)):
+        assert B.tempo_window_attn_bwd_workspace_bytes(*sizes_of, 8, 3, 1, torch.float32) == 0
+    assert window_bwd(**nothing, **{**sizes, "Sk": 0}) == OK
+
+
 def test_window_attention_workspaces_of_any_sizes():
     """Every size is looked at before it divides anything, and none overflows."""
     for way in (B.tempo_window_attn_fwd_workspace_bytes, B.tempo_window_attn_bwd_workspace_bytes):
