@@ -191,6 +191,26 @@ def test_lengths_and_places(size, key_len, start, dtype):
     both_ways(*size, dtype, key_len, start)
 
 
+MANY = [  # tiles enough for the whole chip, so that neither keys nor queries of a tile are in parts; key_len, start
+    ((8, 400, 400, 16, 16, 64, 150, 1), None, None),
+    ((8, 400, 400, 16, 16, 64, 150, 40), None, None),
+    ((8, 400, 400, 16, 16, 64, 1000, 0), None, None),
+    ((16, 300, 300, 16, 8, 128, 90, 3), [300, 299, 128, 129, 1, 0, 257, 256, 31, 32, 33, 200, 300, 90, 64, 5], None),
+    ((16, 300, 300, 8, 8, 83, 90, 35), [300, 299, 128, 129, 1, 0, 257, 256, 31, 32, 33, 200, 300, 90, 64, 5], None),
+    ((4, 1500, 1500, 8, 8, 96, 700, 130), None, None),                    # first keys in two tiles, then a window of many
+    ((4, 1500, 1500, 8, 8, 64, 31, 7), None, [0, 3000, -700, 40]),
+    ((16, 280, 280, 8, 8, 192, 60, 20), None, None),
+    ((8, 400, 400, 12, 12, 256, 110, 2), None, None),
+    ((2, 3300, 3300, 8, 8, 128, 2000, 4), [3300, 2999], None)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size,key_len,start", MANY, ids=str)
+def test_many_tiles(size, key_len, start, dtype):
+    both_ways(*size, dtype, key_len, start)
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("size", [(0, 3, 3, 2, 1), (1, 3, 3, 0, 0), (1, 0, 0, 2, 2)], ids=str)
 def test_nothing_to_do(size):
     batch, Sq, Sk, heads, kv = size
