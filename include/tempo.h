@@ -360,7 +360,9 @@ TEMPO_API tempo_status tempo_glu_bwd(const void* dh, const void* gu, const void*
  *   key_len, query_start [B] int32 in, device, may be NULL; key_len is taken as 0 below 0 and as Sk above it, query_start may be negative.
  *   Keys that none of 128 neighbouring rows sees (a row: a query of one of the heads that share a key head) are not looked at, whatever they
  *   hold; an element of k, v, q or dout that is not finite makes NaN of the sums that it takes part in, and may of those of the rows and keys
- *   beside it that do not see it.  dk and dv of keys that no query sees are 0.
+ *   beside it that do not see it.  dk and dv of keys that no query sees are 0.  heads may be 0: no queries then.
+ *   Scores are in float32.  From 2^24 on, where they are off by one and more, weights mean little, and beyond 2^30 they need not be finite.
+ *   The backward's weights are made from lse as it is kept: they are off by up to 2^-22 |lse| of themselves.
  *   bfloat16: the weights exp(s - max) and ds are rounded to bfloat16 for the second product, sums are in float32.  Sums are made in a
  *   fixed order: the same call gives the same bits.
  *   workspace: device memory of at least tempo_window_attn_fwd/bwd_workspace_bytes() bytes, 16-byte aligned (NULL if that is 0); calls that

@@ -8,8 +8,10 @@
 //
 // Bound by the bytes of four tensors forward and six backward, each once: a row is held in registers by the waves of one workgroup, which
 // walks rows and fetches the next while it reduces, keeps the parameters of its columns in registers and, backward, their sums, which a
-// second kernel adds up in a fixed order.  8192 x 4096 bfloat16 forward 50.5 us (5.3 TB/s), 65536 x 4096 backward 553 (5.8 TB/s) and 13 for the column
-// sums; 3063 x 1001 float32 backward, rows at any multiple of 4 bytes, 22 and 10.
+// second kernel adds up in a fixed order.  8192 x 4096 bfloat16 forward 50.7 us (5.3 TB/s), 65536 x 4096 backward 546 (5.9 TB/s) and 13 for the column
+// sums; 3063 x 1001 float32 backward, rows at any multiple of 4 bytes, 22 and 6.  A workgroup of 16 waves leaves 128 registers a lane, of which
+// the backward spills some: rows of 513 to 1024 pieces 36 to 112 bytes a lane in bfloat16 (16384 x 8192 318 us, 5.1 TB/s, 16384 x 5120 243, 4.1), longer ones 320 to
+// 576 (8192 x 16384 1168 us, 1.4 TB/s) and 40 to 220 in float32 (8192 x 8192 298 us, 5.4 TB/s); the forward only with biases, 8 to 76.
 #include <algorithm>
 #include <type_traits>
 
@@ -87,7 +89,7 @@ struct Columns {
   }
 };
 // The rows of this workgroup, all of one gate: every parts-th, so that what the workgroups read and write at a time lies together
-// (65536 x 4096 bfloat16 backward 568 us; 612 where each has rows side by side).
+// (65536 x 4096 bfloat16 backward with its column sums 558 us; 612 where each has rows side by side).
 struct Walk {
   int64_t group, first, end, step;
   __device__ __forceinline__ explicit Walk(const Residual& r) {
@@ -98,7 +100,7 @@ struct Walk {
   }
 };
 
-// Rows that are on their way while one is worked on: 65536 x 4096 bfloat16 backward 568 us with two, 654 with one.
+// Rows that are on their way while one is worked on: 65536 x 4096 bfloat16 backward with its column sums 558 us with two, 667 with one.
 template <int CH>
 constexpr int kAhead = CH == 1 ? 2 : 1;
 // work(row, its turn, that modulo AHEAD as a constant)
@@ -512,7 +514,7 @@ Plan plan_of(const ResidualCall& c, tempo_dtype dt, bool back) {
   p.groups = c.gate ? c.groups : 1;
   p.group_rows = c.N / p.groups;
   // 32 waves for each compute unit, and backward 8 rows each where there are as many for all of them, so that the sums are a small part of what
-  // is read and written.  us with 2, 4, 8 and 12: 3063 x 1001 float32 54.5, 38.4, 32.0, 30.4, 4096 x 1024 bfloat16 31.8, 24.5, 22.0, 24.7.
+  // is read and written.  us with 2, 4, 8 and 12: 3063 x 1001 float32 42.8, 33.4, 29.6, 26.2, 4096 x 1024 bfloat16 30.9, 24.0, 22.0, 24.3.
   const int64_t cus = compute_units(), blocks = cus * 32 / std::max(p.shape.waves, 1);
   p.part_rows = std::max<int64_t>((c.N + blocks - 1) / blocks, 1);
   if (back) p.part_rows = std::max(p.part_rows, std::min<int64_t>(8, (c.N + cus - 1) / cus));
