@@ -527,7 +527,7 @@ static bool attn_heads_ok(const tempo_attn_heads* h, int64_t B, int64_t S, int64
 }
 static WindowCall window_sizes(int64_t B, int64_t Sq, int64_t Sk, int64_t heads, int64_t kv_heads, int64_t D, int64_t window,
                                int64_t sinks) {
-  constexpr int64_t most = INT32_MAX;  // beyond any position
+  constexpr int64_t most = int64_t{1} << 33;  // beyond any position
   WindowCall c{};
   c.B = B, c.Sq = Sq, c.Sk = Sk, c.heads = heads, c.kv_heads = kv_heads, c.D = D;
   if (heads == 0 && kv_heads > 0 && Sq >= 0) c.heads = kv_heads, c.Sq = 0;  // key heads that none reads: no queries, whose gradients are zeros

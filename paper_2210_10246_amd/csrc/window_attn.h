@@ -48,7 +48,8 @@ struct Attn {
   const int32_t *key_len, *query_start;
   int Sq, Sk, heads, kv_heads, group, rows, D;  // rows: Sq * group
   FastDiv by_group;
-  int window, sinks;
+  int64_t window;  // positions go up to 2^32
+  int sinks;
   float scale, c;  // c: scale log2(e)
   int tiles, splits;
   int pitch;                     // floats of a row of sums in the workspace: D up to whole pieces
@@ -57,11 +58,12 @@ struct Attn {
 
 // Which keys the queries of a sequence see.
 struct Sight {
-  int64_t start;
-  int keys, window, sinks;
-  __device__ __forceinline__ Sight(const Attn& a, int b) : window(a.window) {
+  int64_t start, before;  // position of the first query, and of the last key before its window
+  int keys, sinks;
+  __device__ __forceinline__ Sight(const Attn& a, int b) {
     keys = a.key_len ? min(max(a.key_len[b], 0), a.Sk) : a.Sk;
     start = a.query_start ? a.query_start[b] : int64_t{a.Sk} - a.Sq;
+    before = start - a.window;
     sinks = min(a.sinks, keys);
   }
   // keys [begin, end) and those below min(sinks, end)
@@ -70,7 +72,7 @@ struct Sight {
     return e <= 0 ? 0 : e < keys ? static_cast<int>(e) : keys;
   }
   __device__ __forceinline__ int begin(int i) const {
-    const int64_t e = start + i + 1 - window;
+    const int64_t e = before + i + 1;
     return e <= 0 ? 0 : e < INT32_MAX ? static_cast<int>(e) : INT32_MAX;
   }
 };
@@ -517,7 +519,7 @@ Attn attn_of(const WindowCall& c) {
   a.D = static_cast<int>(c.D);
   a.pitch = static_cast<int>(pitch_of(c));
   a.by_group = FastDiv(static_cast<uint32_t>(a.group));
-  a.window = static_cast<int>(std::min<int64_t>(c.window, INT32_MAX));
+  a.window = c.window;
   a.sinks = static_cast<int>(std::min<int64_t>(c.sinks, c.Sk));
   a.scale = c.scale;
   a.c = c.scale * kLog2e;

@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kThreads, (kKeysAtOnce<T, DP, DIRECT>)) void keys_k
     return j >= s.keys || i >= a.Sq ? a.Sq : i > 0 ? static_cast<int>(i) : 0;
   };
   auto to = [&](int j) {
-    const int64_t i = j + int64_t{s.window} - s.start;
+    const int64_t i = j - s.before;
     return j >= s.keys || i <= 0 ? 0 : i < a.Sq ? static_cast<int>(i) : a.Sq;
   };
   auto beyond = [&](int j) { return j < s.sinks ? max(from(j), to(j)) : a.Sq; };

@@ -223,6 +223,15 @@ def test_nothing_to_do(size):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Sq", [3, 200])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31, 2 ** 31 + 30, 2 ** 40, 2 ** 63 - 1])
+def test_windows_and_positions_next_to_2_to_31(window, Sq, dtype):
+    """A window of more than 2^31 keys holds what it says at the furthest positions too."""
+    both_ways(3, Sq, 60, 2, 2, 48, window, 0, dtype, None, [2 ** 31 - 1, 2 ** 31 - 25, -2 ** 31])
+    both_ways(2, Sq, 60, 2, 1, 48, window, 2, dtype, [60, 41], [2 ** 31 - 1, 2 ** 31 - 200])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("batch,Sq,Sk,kv,D", [(1, 3, 3, 2, 16), (2, 0, 300, 3, 83), (2, 70, 300, 1, 256)])
 def test_key_heads_that_no_head_reads(batch, Sq, Sk, kv, D, dtype):
     """No heads of queries beside heads of keys: gradients of zeros, through both halves of the binding."""
